@@ -374,6 +374,118 @@ int gefen_newton_schulz(const uint16_t* x_in, uint16_t* x_out, int32_t batch, in
 int gefen_stream_mix(float* theta, const void* grad, int32_t grad_dtype, uint8_t* codes,
                      int64_t n, void* stream);
 
+/* ------------------------------------------------------------------------------
+ * Feed-forward operators: the half of a transformer block whose gradients the step takes,
+ * trained with one byte per saved activation. None of them needs a state, allocates or
+ * synchronises: every device operation is enqueued on `stream`, workspaces are the caller's
+ * (16-byte aligned; their contents need not be kept between calls), outputs must not overlap
+ * inputs. Matrices are dense and row-major; pointers may have any alignment that their type has.
+ * A call with no rows (tokens) writes nothing but zero weight gradients.
+ *
+ * 8-bit activation checkpoint of a rows x cols matrix: int8 codes[rows * cols] and uint8
+ * exponents[rows * ceil(cols / 64)], one per group of 64 consecutive elements of a row (the last
+ * group of a row may be shorter). With E the group's exponent an element stands for
+ * code * 2^(E - 127), |code| <= 127; E is the smallest number >= 1 for which every
+ * |element| / 2^(E - 127) rounds to at most 127, and codes are rounded to nearest, ties to
+ * even. (E ends at 248, where codes of elements from 127.5 * 2^121 on are held at 127.) Scales are powers of two so that every value is exact in bfloat16 (a scale of
+ * absmax / 127 would save about half a bit of rounding error and cost another rounding where a
+ * bfloat16 matrix product reads the values). A group that holds an infinity or NaN has E = 255
+ * and codes 0 and stands for NaN throughout.
+ * ---------------------------------------------------------------------------- */
+
+/* gefen_checkpoint_encode -- the checkpoint of x (GEFEN_F32 or GEFEN_BF16).
+ * Errors: EINVAL (NULL, rows < 0, cols < 1, more than 2^40 elements), EDTYPE, EHIP. */
+int gefen_checkpoint_encode(const void* x, int32_t dtype, int64_t rows, int64_t cols,
+                            int8_t* codes, uint8_t* exponents, void* stream);
+
+/* gefen_checkpoint_decode -- the values of a checkpoint, times gain[column] where gain (device
+ * float[cols]) is not NULL, as `dtype`. Errors as gefen_checkpoint_encode. */
+int gefen_checkpoint_decode(const int8_t* codes, const uint8_t* exponents, const float* gain,
+                            int64_t rows, int64_t cols, void* out, int32_t dtype, void* stream);
+
+/* gefen_rms_norm -- the residual's addition and the RMS norm of each row:
+ *   h = x + residual;  rstd = (mean_j h_j^2 + eps)^(-1/2);  n = h * rstd;  y = n * weight
+ * in float32, y and h rounded once to `dtype` (the norm sees h before it is rounded).
+ *  x, residual  rows x cols of dtype (GEFEN_F32 or GEFEN_BF16); residual may be NULL (h = x).
+ *  weight       device float[cols].
+ *  y            rows x cols of dtype. May be x or residual itself, as may h.
+ *  h            rows x cols of dtype, or NULL.
+ *  rstd         device float[rows].
+ *  codes, exponents  the 8-bit checkpoint of n (not of y: it serves the norm's own backward
+ *               pass, and with `weight` as the gain that of what reads y), or both NULL.
+ *  cols in [1, 16384]; eps >= 0 and finite.
+ * Errors: EINVAL, EDTYPE, EHIP. */
+int gefen_rms_norm(const void* x, const void* residual, int32_t dtype, const float* weight,
+                   int64_t rows, int64_t cols, double eps, void* y, void* h, float* rstd,
+                   int8_t* codes, uint8_t* exponents, void* stream);
+
+/* gefen_rms_norm_backward -- with dn = dy * weight and n from the forward pass:
+ *   dx = rstd * (dn - n * mean_j(dn_j n_j)) + dh;   dweight_j = sum over rows of dy_j n_j
+ * in float32; dx is the gradient of x and of the residual alike.
+ *  dy, dx       rows x cols of dtype; dh (the gradient of h from its other uses) likewise, or
+ *               NULL. dx may be dy or dh itself.
+ *  h            rows x cols of dtype (n = h * rstd), or NULL: then codes and exponents, the
+ *               checkpoint of n that the forward pass wrote. Exactly one of the two.
+ *  dweight      device float[cols], overwritten; the sum's order depends on the sizes alone.
+ *  workspace    gefen_rms_norm_backward_workspace(rows, cols) bytes.
+ * Errors: EINVAL, EDTYPE, EHIP. */
+int gefen_rms_norm_backward_workspace(int64_t rows, int64_t cols, int64_t* bytes);
+int gefen_rms_norm_backward(const void* dy, const void* dh, int32_t dtype, const void* h,
+                            const int8_t* codes, const uint8_t* exponents, const float* rstd,
+                            const float* weight, int64_t rows, int64_t cols, void* dx,
+                            float* dweight, void* workspace, int64_t workspace_bytes,
+                            void* stream);
+
+typedef enum {
+    GEFEN_SILU = 0,   /* act(g) = g / (1 + exp(-g)) */
+    GEFEN_GELU = 1    /* act(g) = g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+} gefen_activation;
+
+/* gefen_gated_ffn -- the gated feed-forward block of `tokens` rows x:
+ *   G = x w_gate^T;  U = x w_up^T;  A = act(G) * U;  y = A w_down^T
+ * bfloat16 matrices (uint16 bit patterns), float32 accumulation; G and U are not rounded, A and
+ * y once each to bfloat16. Both projections, the activation, the product and the checkpoints
+ * are one kernel.
+ *  x       tokens x width;  w_gate, w_up  inner x width;  w_down  width x inner;
+ *  y       tokens x width.
+ *  gate_codes, ... the 8-bit checkpoints of G and U (tokens x inner each) for the backward
+ *          pass, or all four NULL.
+ *  workspace  gefen_gated_ffn_workspace(...) bytes: flags 0 (forward) or GEFEN_FFN_BACKWARD,
+ *          plus GEFEN_FFN_UNALIGNED if a matrix is not 16-byte aligned. It holds A (and the
+ *          gradients of G and U) in bfloat16, a padded copy of matrices whose rows are no
+ *          multiple of 8 elements long, and float32 partial sums of products whose sum is split.
+ *  tokens in [0, 2^24], width and inner in [1, 2^20].
+ * Errors: EINVAL, EHIP. */
+#define GEFEN_FFN_BACKWARD 1
+#define GEFEN_FFN_UNALIGNED 2
+int gefen_gated_ffn_workspace(int64_t tokens, int64_t width, int64_t inner, int32_t flags,
+                              int64_t* bytes);
+int gefen_gated_ffn(const uint16_t* x, const uint16_t* w_gate, const uint16_t* w_up,
+                    const uint16_t* w_down, int64_t tokens, int64_t width, int64_t inner,
+                    int32_t activation, uint16_t* y, int8_t* gate_codes, uint8_t* gate_exponents,
+                    int8_t* up_codes, uint8_t* up_exponents, void* workspace,
+                    int64_t workspace_bytes, void* stream);
+
+/* gefen_gated_ffn_backward -- the block's gradients from the checkpoints of G and U:
+ *   dA = dy w_down;  dG = dA * U * act'(G);  dU = dA * act(G);  A = act(G) * U
+ *   dw_down = dy^T A;  dw_gate = dG^T x;  dw_up = dU^T x;  dx = dG w_gate + dU w_up
+ * with float32 accumulation; dG, dU and A are rounded to bfloat16 for the products that read
+ * them, and each output once. Sums do not depend on timing.
+ *  x        the forward pass's input, or NULL: then x_codes and x_exponents, an 8-bit
+ *           checkpoint (tokens x width), times gain[column] (device float[width], or NULL).
+ *           Exactly one of the two; no gain with x. After gefen_rms_norm with codes, those and
+ *           its weight as the gain are x without a second copy.
+ *  dx       tokens x width; dw_* like the weights.
+ * Errors: EINVAL, EHIP. */
+int gefen_gated_ffn_backward(const uint16_t* dy, const uint16_t* x, const int8_t* x_codes,
+                             const uint8_t* x_exponents, const float* gain,
+                             const int8_t* gate_codes, const uint8_t* gate_exponents,
+                             const int8_t* up_codes, const uint8_t* up_exponents,
+                             const uint16_t* w_gate, const uint16_t* w_up, const uint16_t* w_down,
+                             int64_t tokens, int64_t width, int64_t inner, int32_t activation,
+                             uint16_t* dx, uint16_t* dw_gate, uint16_t* dw_up, uint16_t* dw_down,
+                             void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Free the state and every device buffer it owns. NULL is a no-op. */
 void gefen_destroy(gefen_state* st);
 

@@ -13,6 +13,10 @@ Entry points mirror ``include/gefen.h``:
 * :func:`dp_codebook` -- ``gefen_dp_codebook`` (Alg. 3 / App. D DP on a histogram).
 * :class:`Gefen` -- a ``torch.optim.Optimizer`` front end (AdamW-compatible arguments)
   that initialises the state from the first gradients.
+* the feed-forward operators of ``feed_forward.py``, loaded on first use: 8-bit activation
+  checkpoints (:class:`Checkpoint8`, :func:`checkpoint8`), :func:`rms_norm`,
+  :func:`gated_ffn`, their backward passes, and :class:`FeedForward`, the block of both under
+  autograd.
 """
 from __future__ import annotations
 
@@ -36,7 +40,9 @@ SYMBOLS = [
     "gefen_checkpoint_bytes", "gefen_export", "gefen_import", "gefen_profile_begin",
     "gefen_profile_end", "gefen_destroy", "gefen_last_error", "gefen_muon_init",
     "gefen_muon_step", "gefen_muon_profile_end", "gefen_stream_mix", "gefen_newton_schulz",
-    "gefen_dp_codebook_static",
+    "gefen_dp_codebook_static", "gefen_checkpoint_encode", "gefen_checkpoint_decode",
+    "gefen_rms_norm", "gefen_rms_norm_backward", "gefen_rms_norm_backward_workspace",
+    "gefen_gated_ffn", "gefen_gated_ffn_backward", "gefen_gated_ffn_workspace",
 ]
 
 
@@ -99,6 +105,15 @@ def load_library(path: str = LIB_PATH):
     lib.gefen_muon_profile_end.argtypes = [vp, P(i32), P(f64), P(f64)]
     lib.gefen_stream_mix.argtypes = [vp, vp, i32, vp, i64, vp]
     lib.gefen_newton_schulz.argtypes = [vp, vp, i32, i64, i64, i32, f64, f64, f64, vp]
+    lib.gefen_checkpoint_encode.argtypes = [vp, i32, i64, i64, vp, vp, vp]
+    lib.gefen_checkpoint_decode.argtypes = [vp, vp, vp, i64, i64, vp, i32, vp]
+    lib.gefen_rms_norm.argtypes = [vp, vp, i32, vp, i64, i64, f64, vp, vp, vp, vp, vp, vp]
+    lib.gefen_rms_norm_backward.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, i64, i64, vp, vp, vp,
+                                            i64, vp]
+    lib.gefen_rms_norm_backward_workspace.argtypes = [i64, i64, P(i64)]
+    lib.gefen_gated_ffn.argtypes = [vp] * 4 + [i64] * 3 + [i32] + [vp] * 6 + [i64, vp]
+    lib.gefen_gated_ffn_backward.argtypes = [vp] * 12 + [i64] * 3 + [i32] + [vp] * 5 + [i64, vp]
+    lib.gefen_gated_ffn_workspace.argtypes = [i64, i64, i64, i32, P(i64)]
     lib.gefen_destroy.argtypes = [vp]
     lib.gefen_destroy.restype = None
     lib.gefen_last_error.argtypes = []
@@ -508,3 +523,17 @@ class GefenMuon:
             self.state.muon_init([p.shape[0] if p.dim() >= 2 else 1 for p in self.params])
         self.state.muon_step(self.params, grads, self.lr, self.momentum, self.weight_decay,
                              self.nesterov, self.ns_steps, self.ns_coefficients, self.eps)
+
+
+_FEED_FORWARD = ("Checkpoint8", "checkpoint8", "RMSNormOutput", "rms_norm", "rms_norm_backward",
+                 "gated_ffn", "gated_ffn_backward", "FeedForward")
+
+
+def __getattr__(name):
+    if name in _FEED_FORWARD:   # needs torch, which importing the binding does not
+        import importlib
+        mod = importlib.import_module(__name__ + ".feed_forward")
+        for n in _FEED_FORWARD:
+            globals()[n] = getattr(mod, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,0 +1,394 @@
+// 8-bit activation checkpoints, and the RMS norm that writes and reads them.
+//
+// All of these are bound by memory: every element is read once and written once, in vectors of
+// eight (16 bytes of bfloat16) per lane. A checkpoint's group of 64 is eight neighbouring lanes'
+// vectors, so its scale is three lane exchanges away and nothing is read twice.
+#include "act8_device.h"
+#include "ffn_internal.h"
+
+#include <algorithm>
+
+namespace gefen {
+namespace {
+
+// ---------------------------------------------------------------- encode and decode
+// A workgroup takes 256 vectors: 2^lx lanes along a row (a whole number of groups) by
+// 256 >> lx rows. Rows that are whole groups long are one long row to these kernels.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_act8_encode(const void* __restrict__ x, int64_t rows,
+                                                     int64_t cols, int64_t groups, int lx,
+                                                     int8_t* __restrict__ codes,
+                                                     uint8_t* __restrict__ exps)
+{
+    const int64_t e = ((static_cast<int64_t>(blockIdx.x) << lx) +
+                       (threadIdx.x & ((1 << lx) - 1))) * 8;
+    const int64_t step = static_cast<int64_t>(gridDim.y) << (8 - lx);
+    for (int64_t r = (static_cast<int64_t>(blockIdx.y) << (8 - lx)) + (threadIdx.x >> lx);
+         r < rows; r += step) {
+        float v[8];
+        const int64_t at = r * cols;
+        load_row8<BF16>(static_cast<const char*>(x) + at * (BF16 ? 2 : 4), e, cols, v);
+        act8_write_group(v, e, cols, codes + at, exps + r * groups);
+    }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_act8_decode(const int8_t* __restrict__ codes,
+                                                     const uint8_t* __restrict__ exps,
+                                                     const float* __restrict__ gain, int64_t rows,
+                                                     int64_t cols, int64_t groups, int lx,
+                                                     void* __restrict__ out, int64_t ldo)
+{
+    const int64_t e = ((static_cast<int64_t>(blockIdx.x) << lx) +
+                       (threadIdx.x & ((1 << lx) - 1))) * 8;
+    const int64_t step = static_cast<int64_t>(gridDim.y) << (8 - lx);
+    float g[8];
+    if (gain) load_row8<false>(gain, e, cols, g);
+    for (int64_t r = (static_cast<int64_t>(blockIdx.y) << (8 - lx)) + (threadIdx.x >> lx);
+         r < rows; r += step) {
+        float v[8];
+        act8_read8(codes + r * cols, exps + r * groups, e, cols, v);
+        if (gain) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= g[j];
+        }
+        store_row8<BF16>(static_cast<char*>(out) + r * ldo * (BF16 ? 2 : 4), e, ldo, v);
+    }
+}
+
+// lx, grid for `rows` rows of `vectors` vectors, a whole number of groups.
+struct RowGrid {
+    int lx;
+    dim3 grid;
+};
+RowGrid row_grid(int64_t rows, int64_t vectors)
+{
+    RowGrid g;
+    g.lx = 3;
+    while (g.lx < 8 && (int64_t(1) << g.lx) < vectors) ++g.lx;
+    const int64_t gx = (vectors + (int64_t(1) << g.lx) - 1) >> g.lx;
+    const int64_t gy = (rows + (256 >> g.lx) - 1) / (256 >> g.lx);
+    g.grid = dim3(static_cast<unsigned>(gx), static_cast<unsigned>(std::min<int64_t>(gy, 65535)));
+    return g;
+}
+
+// ---------------------------------------------------------------- RMS norm
+// A row is held in the registers of TPR lanes (a wave, or a whole workgroup), NV vectors each:
+// one pass over memory. Workgroups take several rows, so that the weight is read once.
+constexpr int kNormThreads(int tpr) { return tpr < 256 ? 256 : tpr; }
+
+// The sum over the row's lanes, in every lane. All threads of the workgroup call it.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float s, float* red)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    if constexpr (TPR > 64) {
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();   // the last row's sum has been read
+        if ((threadIdx.x & 63) == 0) red[wave] = s;
+        __syncthreads();
+        s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < TPR / 64; ++w) s += red[w];
+    }
+    return s;
+}
+
+template <bool BF16, int TPR, int NV>
+__global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm(const NormArgs a, int64_t groups)
+{
+    constexpr int kRows = kNormThreads(TPR) / TPR;
+    constexpr int kSize = BF16 ? 2 : 4;
+    __shared__ float red[TPR / 64];
+    const int lane = threadIdx.x & (TPR - 1);
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+    const int cols = static_cast<int>(a.cols);
+    const float inv_n = 1.0f / static_cast<float>(cols);
+    float w[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load_row8<false>(a.weight, (i * TPR + lane) * 8, cols, w[i]);
+    // rows advance together in a workgroup: every thread takes part in the row's sum
+    for (int64_t base = static_cast<int64_t>(blockIdx.x) * kRows; base < a.rows; base += step) {
+        const int64_t row = base + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+        const bool on = row < a.rows;
+        const int n = on ? cols : 0;
+        const int64_t at = on ? row * cols : 0;
+        float v[NV][8];
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            load_row8<BF16>(static_cast<const char*>(a.x) + at * kSize, (i * TPR + lane) * 8, n,
+                            v[i]);
+        if (a.r) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float q[8];
+                load_row8<BF16>(static_cast<const char*>(a.r) + at * kSize, (i * TPR + lane) * 8,
+                                n, q);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] += q[j];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s = fmaf(v[i][j], v[i][j], s);
+        s = row_sum<TPR>(s, red);
+        const float rstd = 1.0f / sqrtf(s * inv_n + a.eps);
+        if (!on) continue;
+        if (lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = (i * TPR + lane) * 8;
+            if (a.h) store_row8<BF16>(static_cast<char*>(a.h) + at * kSize, e, n, v[i]);
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[i][j] *= rstd;
+                y[j] = v[i][j] * w[i][j];
+            }
+            store_row8<BF16>(static_cast<char*>(a.y) + at * kSize, e, n, y);
+            if (a.codes) act8_write_group(v[i], e, n, a.codes + at, a.exps + row * groups);
+        }
+    }
+}
+
+// dn = dy w;  dx = rstd (dn - n mean(dn n)) + dh;  dw = the sum over rows of dy n. A workgroup
+// keeps its rows' share of dw in registers and writes it once; k_norm_dw adds the shares in
+// order, so that dw does not depend on timing.
+template <bool BF16, int TPR, int NV>
+__global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormGradArgs a,
+                                                                     int64_t groups)
+{
+    constexpr int kRows = kNormThreads(TPR) / TPR;
+    constexpr int kSize = BF16 ? 2 : 4;
+    __shared__ float red[TPR / 64];
+    __shared__ float share[kRows > 1 ? kRows - 1 : 1][kRows > 1 ? TPR * NV * 8 : 1];
+    const int lane = threadIdx.x & (TPR - 1);
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+    const int cols = static_cast<int>(a.cols);
+    const float inv_n = 1.0f / static_cast<float>(cols);
+    float w[NV][8], dw[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        load_row8<false>(a.weight, (i * TPR + lane) * 8, cols, w[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
+    }
+    for (int64_t base = static_cast<int64_t>(blockIdx.x) * kRows; base < a.rows; base += step) {
+        const int64_t row = base + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+        const bool on = row < a.rows;
+        const int n = on ? cols : 0;
+        const int64_t at = on ? row * cols : 0;
+        const float rstd = on ? a.rstd[row] : 0.0f;
+        float d[NV][8], v[NV][8];
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            load_row8<BF16>(static_cast<const char*>(a.dy) + at * kSize, (i * TPR + lane) * 8, n,
+                            d[i]);
+        if (a.h) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                load_row8<BF16>(static_cast<const char*>(a.h) + at * kSize, (i * TPR + lane) * 8,
+                                n, v[i]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] *= rstd;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                act8_read8(a.codes + at, a.exps + (on ? row : 0) * groups, (i * TPR + lane) * 8, n,
+                           v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                dw[i][j] = fmaf(d[i][j], v[i][j], dw[i][j]);
+                d[i][j] *= w[i][j];
+                s = fmaf(d[i][j], v[i][j], s);
+            }
+        s = row_sum<TPR>(s, red);
+        if (!on) continue;
+        const float c = s * inv_n;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = (i * TPR + lane) * 8;
+            float g[8];
+            if (a.dh) {
+                load_row8<BF16>(static_cast<const char*>(a.dh) + at * kSize, e, n, g);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) g[j] = 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] = fmaf(rstd, fmaf(-v[i][j], c, d[i][j]), g[j]);
+            store_row8<BF16>(static_cast<char*>(a.dx) + at * kSize, e, n, g);
+        }
+    }
+    const int sub = threadIdx.x / TPR;
+    if constexpr (kRows > 1) {
+        __syncthreads();
+        if (sub > 0) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) share[sub - 1][(j * NV + i) * TPR + lane] = dw[i][j];
+        }
+        __syncthreads();
+        if (sub > 0) return;
+#pragma unroll
+        for (int q = 0; q < kRows - 1; ++q)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dw[i][j] += share[q][(j * NV + i) * TPR + lane];
+    }
+    float* __restrict__ out = a.partial + static_cast<int64_t>(blockIdx.x) * a.cols;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) store_row8<false>(out, (i * TPR + lane) * 8, cols, dw[i]);
+}
+
+// dw[c] = the sum over p of partial[p][c]: 64 columns a workgroup, four waves of every fourth row.
+__global__ __launch_bounds__(256) void k_norm_dw(const float* __restrict__ partial, int64_t parts,
+                                                 int64_t cols, float* __restrict__ dw)
+{
+    __shared__ float t[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+    float s = 0.0f;
+    if (c < cols) {
+#pragma unroll 8
+        for (int64_t p = wave; p < parts; p += 4) s += partial[p * cols + c];
+    }
+    t[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < cols) dw[c] = (t[0][lane] + t[1][lane]) + (t[2][lane] + t[3][lane]);
+}
+
+__global__ __launch_bounds__(256) void k_fill_zero(float* __restrict__ p, int64_t n)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i < n) p[i] = 0.0f;
+}
+
+int64_t norm_rows_per_group(int64_t cols) { return cols <= 1024 ? 4 : 1; }
+
+}  // namespace
+
+hipError_t launch_act8_encode(const void* x, bool bf16, int64_t rows, int64_t cols, int8_t* codes,
+                              uint8_t* exps, hipStream_t stream)
+{
+    if (rows <= 0 || cols <= 0) return hipSuccess;
+    if (cols % kAct8Group == 0) {
+        cols *= rows;
+        rows = 1;
+    }
+    const int64_t groups = act8_groups(cols);
+    if (groups > 0x7fffffffLL) return hipErrorInvalidValue;
+    const RowGrid g = row_grid(rows, groups * 8);
+    if (bf16)
+        hipLaunchKernelGGL(k_act8_encode<true>, g.grid, dim3(256), 0, stream, x, rows, cols,
+                           groups, g.lx, codes, exps);
+    else
+        hipLaunchKernelGGL(k_act8_encode<false>, g.grid, dim3(256), 0, stream, x, rows, cols,
+                           groups, g.lx, codes, exps);
+    return hipGetLastError();
+}
+
+hipError_t launch_act8_decode(const int8_t* codes, const uint8_t* exps, const float* gain,
+                              int64_t rows, int64_t cols, void* out, bool bf16, int64_t ldo,
+                              hipStream_t stream)
+{
+    if (rows <= 0 || cols <= 0) return hipSuccess;
+    if (ldo < cols || ldo >= cols + kAct8Group) return hipErrorInvalidValue;
+    if (cols % kAct8Group == 0 && ldo == cols && !gain) {
+        cols *= rows;
+        ldo = cols;
+        rows = 1;
+    }
+    const int64_t groups = act8_groups(cols);
+    if (groups > 0x7fffffffLL) return hipErrorInvalidValue;
+    const RowGrid g = row_grid(rows, groups * 8);
+    if (bf16)
+        hipLaunchKernelGGL(k_act8_decode<true>, g.grid, dim3(256), 0, stream, codes, exps, gain,
+                           rows, cols, groups, g.lx, out, ldo);
+    else
+        hipLaunchKernelGGL(k_act8_decode<false>, g.grid, dim3(256), 0, stream, codes, exps, gain,
+                           rows, cols, groups, g.lx, out, ldo);
+    return hipGetLastError();
+}
+
+// The kernel for a row width: a wave per row while the row fits its registers, else a workgroup.
+#define GEFEN_NORM_WIDTHS(LAUNCH)                                                          \
+    do {                                                                                   \
+        if (cols <= 512) LAUNCH(64, 1);                                                    \
+        else if (cols <= 1024) LAUNCH(64, 2);                                              \
+        else if (cols <= 2048) LAUNCH(256, 1);                                             \
+        else if (cols <= 4096) LAUNCH(256, 2);                                             \
+        else if (cols <= 8192) LAUNCH(512, 2);                                             \
+        else LAUNCH(1024, 2);                                                              \
+    } while (0)
+
+hipError_t launch_rms_norm(const NormArgs& a, bool bf16, hipStream_t stream)
+{
+    const int64_t cols = a.cols;
+    if (cols < 1 || cols > kNormMaxCols) return hipErrorInvalidValue;
+    if (a.rows <= 0) return hipSuccess;
+    const int64_t per = norm_rows_per_group(cols);
+    const int64_t blocks = std::min<int64_t>((a.rows + per - 1) / per, 2048);
+    const int64_t groups = act8_groups(cols);
+    const dim3 grid(static_cast<unsigned>(blocks));
+#define LAUNCH(TPR, NV)                                                                    \
+    do {                                                                                   \
+        if (bf16)                                                                          \
+            hipLaunchKernelGGL((k_rms_norm<true, TPR, NV>), grid, dim3(kNormThreads(TPR)), \
+                               0, stream, a, groups);                                      \
+        else                                                                               \
+            hipLaunchKernelGGL((k_rms_norm<false, TPR, NV>), grid,                         \
+                               dim3(kNormThreads(TPR)), 0, stream, a, groups);             \
+    } while (0)
+    GEFEN_NORM_WIDTHS(LAUNCH);
+#undef LAUNCH
+    return hipGetLastError();
+}
+
+int64_t norm_grad_parts(int64_t rows, int64_t cols)
+{
+    const int64_t per = norm_rows_per_group(cols);
+    return std::min<int64_t>((rows + per - 1) / per, 512);
+}
+
+hipError_t launch_rms_norm_grad(const NormGradArgs& a, bool bf16, hipStream_t stream)
+{
+    const int64_t cols = a.cols;
+    if (cols < 1 || cols > kNormMaxCols) return hipErrorInvalidValue;
+    const dim3 dw_grid(static_cast<unsigned>((cols + 63) / 64));
+    if (a.rows <= 0) {
+        hipLaunchKernelGGL(k_fill_zero, dim3(static_cast<unsigned>((cols + 255) / 256)), dim3(256),
+                           0, stream, a.dw, cols);
+        return hipGetLastError();
+    }
+    const int64_t parts = norm_grad_parts(a.rows, cols);
+    const int64_t groups = act8_groups(cols);
+    const dim3 grid(static_cast<unsigned>(parts));
+#define LAUNCH(TPR, NV)                                                                    \
+    do {                                                                                   \
+        if (bf16)                                                                          \
+            hipLaunchKernelGGL((k_rms_norm_grad<true, TPR, NV>), grid,                     \
+                               dim3(kNormThreads(TPR)), 0, stream, a, groups);             \
+        else                                                                               \
+            hipLaunchKernelGGL((k_rms_norm_grad<false, TPR, NV>), grid,                    \
+                               dim3(kNormThreads(TPR)), 0, stream, a, groups);             \
+    } while (0)
+    GEFEN_NORM_WIDTHS(LAUNCH);
+#undef LAUNCH
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL(k_norm_dw, dw_grid, dim3(256), 0, stream, a.partial, parts, cols, a.dw);
+    return hipGetLastError();
+}
+
+}  // namespace gefen

@@ -1,0 +1,220 @@
+// Device helpers of the feed-forward operators: eight-element vectors of a row at any alignment,
+// and the 8-bit checkpoint code (ffn_internal.h defines it).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+#include "ffn_internal.h"
+
+namespace gefen {
+
+typedef float f32x2a __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2a __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4a __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2a __attribute__((ext_vector_type(2)));
+
+// 16, 8 bytes from or to any address (a global access of that width at any alignment).
+__device__ __forceinline__ u32x4a load16(const void* p)
+{
+    u32x4a v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+__device__ __forceinline__ u32x2a load8b(const void* p)
+{
+    u32x2a v;
+    __builtin_memcpy(&v, p, 8);
+    return v;
+}
+__device__ __forceinline__ void store16(void* p, const u32x4a& v) { __builtin_memcpy(p, &v, 16); }
+__device__ __forceinline__ void store8b(void* p, const u32x2a& v) { __builtin_memcpy(p, &v, 8); }
+
+__device__ __forceinline__ float bf16_float(uint32_t b) { return __uint_as_float(b << 16); }
+
+// Two float32 to bfloat16, rounded to nearest even (NaN stays NaN), low half first.
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
+{
+    const f32x2a x = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2a));
+}
+__device__ __forceinline__ uint16_t bf16_bits(float x)
+{
+    return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
+}
+
+// Elements e .. e + 7 of a row of n at `row`, as float32; zero from n on.
+template <bool BF16, typename I>
+__device__ __forceinline__ void load_row8(const void* row, I e, I n, float (&v)[8])
+{
+    if (e + 8 <= n) {
+        if constexpr (BF16) {
+            const u32x4a w = load16(static_cast<const uint16_t*>(row) + e);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[2 * j] = bf16_float(w[j]);
+                v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+            }
+        } else {
+            const u32x4a a = load16(static_cast<const float*>(row) + e);
+            const u32x4a b = load16(static_cast<const float*>(row) + e + 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = __uint_as_float(a[j]);
+                v[4 + j] = __uint_as_float(b[j]);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = 0.0f;
+            if (e + j < n)
+                v[j] = BF16 ? bf16_float(static_cast<const uint16_t*>(row)[e + j])
+                            : static_cast<const float*>(row)[e + j];
+        }
+    }
+}
+
+template <bool BF16, typename I>
+__device__ __forceinline__ void store_row8(void* row, I e, I n, const float (&v)[8])
+{
+    if (e + 8 <= n) {
+        if constexpr (BF16) {
+            u32x4a w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = bf16_pair(v[2 * j], v[2 * j + 1]);
+            store16(static_cast<uint16_t*>(row) + e, w);
+        } else {
+            u32x4a a, b;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                a[j] = __float_as_uint(v[j]);
+                b[j] = __float_as_uint(v[4 + j]);
+            }
+            store16(static_cast<float*>(row) + e, a);
+            store16(static_cast<float*>(row) + e + 4, b);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (e + j < n) {
+                if constexpr (BF16)
+                    static_cast<uint16_t*>(row)[e + j] = bf16_bits(v[j]);
+                else
+                    static_cast<float*>(row)[e + j] = v[j];
+            }
+    }
+}
+
+// ---------------------------------------------------------------- the 8-bit code
+// Absolute values are compared by their bits, which order as the values do and put infinity and
+// NaN last, so that a group's largest bits tell whether it holds one.
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// E of a group from its largest bits: the exponent less 6 puts |x| / scale into [64, 128); from
+// 127.5 / 64 in the leading digits on (the carry of 0x10000) one more, so that no code is 128.
+// At most kAct8Top: one more would have 64 stand for 2^128.
+__device__ __forceinline__ int act8_exponent(uint32_t top)
+{
+    const int e = static_cast<int>((top + 0x10000u) >> 23) - 6;
+    return top >= 0x7f800000u ? 255 : min(max(e, 1), kAct8Top);
+}
+
+// 1 / scale: a power of two, so that products with it are exact (0 for the NaN group).
+__device__ __forceinline__ float act8_inverse(int e)
+{
+    return e == 255 ? 0.0f : __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
+}
+
+__device__ __forceinline__ float act8_scale(uint32_t e)
+{
+    return __uint_as_float(e == 255u ? 0x7fc00000u : e << 23);
+}
+
+// rint(x * inv) in the low byte, within +-127 (only kAct8Top needs it): adding 1.5 * 2^23 rounds
+// to a whole number, ties to even, and leaves its two's complement in the low bits.
+__device__ __forceinline__ uint32_t act8_code(float x, float inv)
+{
+    return __float_as_uint(__builtin_amdgcn_fmed3f(x * inv, -127.0f, 127.0f) + 12582912.0f);
+}
+
+__device__ __forceinline__ uint32_t act8_pack(float a, float b, float c, float d, float inv)
+{
+    const uint32_t lo = __builtin_amdgcn_perm(act8_code(b, inv), act8_code(a, inv), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(act8_code(d, inv), act8_code(c, inv), 0x04000c0cu);
+    return lo | hi;
+}
+
+// Code j (0..3) of four packed ones, as float32.
+__device__ __forceinline__ float act8_value(uint32_t w, int j)
+{
+    return static_cast<float>(static_cast<int32_t>(w << (24 - 8 * j)) >> 24);
+}
+
+// Largest over the eight lanes of an aligned run of eight.
+__device__ __forceinline__ uint32_t max_over_8(uint32_t m)
+{
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 1)));
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 2)));
+    return max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 4)));
+}
+
+// One group's eight lanes, each with eight elements e .. e + 7 of a row of n (zero from n on),
+// write the group's codes and its exponent. Every lane of the eight takes part.
+template <typename I>
+__device__ __forceinline__ void act8_write_group(const float (&v)[8], I e, I n,
+                                                 int8_t* __restrict__ codes,
+                                                 uint8_t* __restrict__ exps)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, abs_bits(v[j]));
+    const int ex = act8_exponent(max_over_8(top));
+    const float inv = act8_inverse(ex);
+    u32x2a w = {0u, 0u};   // the codes of a NaN group are zero
+    if (ex != 255) {
+        w.x = act8_pack(v[0], v[1], v[2], v[3], inv);
+        w.y = act8_pack(v[4], v[5], v[6], v[7], inv);
+    }
+    if (e + 8 <= n) {
+        store8b(codes + e, w);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (e + j < n) codes[e + j] = static_cast<int8_t>((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+    }
+    if ((e & 63) == 0 && e < n) exps[e >> 6] = static_cast<uint8_t>(ex);
+}
+
+// Elements e .. e + 7 of a checkpointed row of n; zero from n on.
+template <typename I>
+__device__ __forceinline__ void act8_read8(const int8_t* __restrict__ codes,
+                                           const uint8_t* __restrict__ exps, I e, I n,
+                                           float (&v)[8])
+{
+    u32x2a w = {0u, 0u};
+    float s = 0.0f;
+    if (e < n) s = act8_scale(exps[e >> 6]);
+    if (e + 8 <= n) {
+        w = load8b(codes + e);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (e + j < n) {
+                const uint32_t b = static_cast<uint8_t>(codes[e + j]);
+                if (j < 4) w.x |= b << (8 * j);
+                else w.y |= b << (8 * (j - 4));
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[j] = act8_value(w.x, j) * s;
+        v[4 + j] = act8_value(w.y, j) * s;
+    }
+    if (e + 8 > n) {   // a NaN group's padding is zero too
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (e + j >= n) v[j] = 0.0f;
+    }
+}
+
+}  // namespace gefen

@@ -1,0 +1,114 @@
+// Host-side plan of the gated feed-forward block's products: which tile, over how many parts of
+// the sum, and where the intermediate matrices lie in the caller's workspace. Plain C++ (no
+// HIP), so that it can be checked on a host.
+#pragma once
+#include <algorithm>
+#include <cstdint>
+
+namespace gefen {
+
+constexpr int64_t kFfnMaxTokens = int64_t(1) << 24;
+constexpr int64_t kFfnMaxWidth = int64_t(1) << 20;   // a tile's rows stay within 32-bit offsets
+constexpr int kFfnBigTile = 256, kFfnSmallTile = 128, kFfnDepth = 64;
+
+inline int64_t ffn_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t ffn_up8(int64_t a) { return (a + 7) / 8 * 8; }
+
+struct FfnTile {
+    bool big = false;
+    int32_t splits = 1;
+    int32_t tiles_m = 0, tiles_n = 0, stages = 0;
+    double us = 0.0;
+};
+
+// The tile and split with the least estimated time for C (M x N, `batch` of them), summed over
+// `segments` of K. `halves`: the tile's columns are two matrices' (gate and up). `may_split`:
+// the sum may be cut into parts, joined by a second kernel.
+inline FfnTile ffn_choose(int64_t M, int64_t N, int64_t K, int batch, int segments, bool halves,
+                          bool may_split)
+{
+    FfnTile best;
+    for (int b = 0; b < 2; ++b) {
+        const int64_t t = b ? kFfnBigTile : kFfnSmallTile;
+        const int64_t tm = ffn_ceil(M, t), tn = ffn_ceil(N, halves ? t / 2 : t);
+        const int64_t stages = ffn_ceil(K, kFfnDepth), all = stages * segments;
+        for (int64_t s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (s > 1 && (!may_split || all / s < 4)) break;
+            const int64_t groups = tm * tn * batch * s;
+            const int64_t each = ffn_ceil(all, s);
+            double us;
+            if (b)
+                us = double(ffn_ceil(groups, 256)) * (1.25 * double(each) + 4.0);
+            else if (groups <= 256)
+                us = 0.5 * double(each) + 3.0;
+            else
+                us = double(ffn_ceil(groups, 512)) * (0.8 * double(each) + 3.0);
+            if (s > 1) us += 3.0 + double(M) * double(N) * batch * (8.0 * double(s) + 2.0) / 4.0e6;
+            if (best.tiles_m == 0 || us < best.us) {
+                best.big = b != 0;
+                best.splits = static_cast<int32_t>(s);
+                best.tiles_m = static_cast<int32_t>(tm);
+                best.tiles_n = static_cast<int32_t>(tn);
+                best.stages = static_cast<int32_t>(stages);
+                best.us = us;
+            }
+        }
+    }
+    return best;
+}
+
+// Byte offsets into the workspace; -1: not needed. T tokens, K the block's width, F its inner
+// width; rows of K8 or F8 elements are rounded up to 8 so that 16-byte loads stay aligned.
+struct FfnSpace {
+    int64_t x = -1, dy = -1, w_gate = -1, w_up = -1, w_down = -1;   // padded copies
+    int64_t a = -1, dg = -1, du = -1;                               // T x F8 each
+    int64_t partial = -1;
+    int64_t bytes = 0;
+    FfnTile gate_up, down;                        // forward
+    FfnTile grad_inner, dx, dw_down, dw_inner;    // backward
+};
+
+inline int64_t ffn_partial_bytes(const FfnTile& t, int64_t M, int64_t N, int batch)
+{
+    return t.splits > 1 ? 4 * M * N * batch * t.splits : 0;
+}
+
+// copy_*: the operand's copy is needed (its rows are no multiple of 8, or it is not aligned).
+inline FfnSpace ffn_space(int64_t T, int64_t K, int64_t F, bool backward, bool copy_k, bool copy_f)
+{
+    FfnSpace s;
+    auto take = [&](int64_t bytes) {
+        const int64_t at = s.bytes;
+        s.bytes += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    const int64_t K8 = ffn_up8(K), F8 = ffn_up8(F);
+    int64_t partial = 0;
+    if (copy_k) {
+        if (!backward) s.x = take(2 * T * K8);
+        if (backward) s.dy = take(2 * T * K8);
+        s.w_gate = take(2 * F * K8);
+        s.w_up = take(2 * F * K8);
+    }
+    if (copy_f) s.w_down = take(2 * K * F8);
+    s.a = take(2 * T * F8);
+    if (!backward) {
+        s.gate_up = ffn_choose(T, F, K, 1, 1, true, false);
+        s.down = ffn_choose(T, K, F, 1, 1, false, true);
+        partial = ffn_partial_bytes(s.down, T, K, 1);
+    } else {
+        s.x = take(2 * T * K8);   // decoded, or copied
+        s.dg = take(2 * T * F8);
+        s.du = take(2 * T * F8);
+        s.grad_inner = ffn_choose(T, F, K, 1, 1, false, false);
+        s.dx = ffn_choose(T, K, F, 1, 2, false, true);
+        s.dw_down = ffn_choose(K, F, T, 1, 1, false, true);
+        s.dw_inner = ffn_choose(F, K, T, 2, 1, false, true);
+        partial = std::max({ffn_partial_bytes(s.dx, T, K, 1), ffn_partial_bytes(s.dw_down, K, F, 1),
+                            ffn_partial_bytes(s.dw_inner, F, K, 2)});
+    }
+    if (partial) s.partial = take(partial);
+    return s;
+}
+
+}  // namespace gefen

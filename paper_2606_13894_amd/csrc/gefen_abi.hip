@@ -52,6 +52,8 @@ bool finite_f(double x) { return std::isfinite(x); }
 
 }  // namespace
 
+void gefen::set_last_error(const char* message) { g_err = message; }
+
 struct gefen_state {
     int device = 0;
     int32_t n_tensors = 0;

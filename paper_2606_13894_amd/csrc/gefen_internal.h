@@ -9,6 +9,9 @@
 
 namespace gefen {
 
+// The message that gefen_last_error gives on this thread (gefen_abi.hip).
+void set_last_error(const char* message);
+
 // Kernel classes, tiles and the planner: tile_plan.h (host-only, shared with the
 // host tests).
 

@@ -1,0 +1,338 @@
+"""The feed-forward half of a transformer block on the library's kernels, trained with one byte
+per saved activation.
+
+* :func:`checkpoint8` / :meth:`Checkpoint8.decode` -- 8-bit activation checkpoints.
+* :func:`rms_norm` / :func:`rms_norm_backward` -- the residual's addition and RMS norm, with an
+  8-bit checkpoint of the normalised rows.
+* :func:`gated_ffn` / :func:`gated_ffn_backward` -- the gated block, with 8-bit checkpoints of
+  its gate and up activations.
+* :class:`FeedForward` -- all of it as one module under autograd.
+
+``include/gefen.h`` gives each operator's formula, types and limits. Tensors are device tensors
+of any leading dimensions (rows are all but the last); ones that are not contiguous are copied.
+All calls are asynchronous on ``stream`` (the current torch stream by default), where their
+outputs and workspaces are allocated.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import BF16, F32, _check, load_library
+
+GROUP = 64
+ACTIVATIONS = {"silu": 0, "gelu": 1}
+_BACKWARD, _UNALIGNED = 1, 2
+
+_DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _on(stream, fn, *args):
+    """fn(*args) with `stream` as torch's current stream."""
+    with torch.cuda.stream(stream):
+        return fn(*args)
+
+
+def _handle():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _operand(t, what, dtype=None, shape=None):
+    """t, contiguous, after its checks."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, not on the current device")
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return t if t.is_contiguous() else t.contiguous()
+
+
+def _rows(t, what):
+    """(rows, cols) of a tensor whose last dimension is a row."""
+    if t.dim() < 1 or t.shape[-1] < 1:
+        raise ValueError(f"{what} must have rows of at least one element")
+    cols = t.shape[-1]
+    return t.numel() // cols, cols
+
+
+def _dtype(t, what):
+    d = _DTYPE.get(t.dtype)
+    if d is None:
+        raise TypeError(f"{what} must be float32 or bfloat16, not {t.dtype}")
+    return d
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class Checkpoint8:
+    """An 8-bit checkpoint of a tensor: ``codes`` int8, shaped as it, and ``exponents`` uint8, one
+    per group of 64 elements of the last dimension. Element = code * 2^(exponent - 127)."""
+
+    __slots__ = ("codes", "exponents")
+
+    def __init__(self, codes, exponents):
+        if codes.dtype is not torch.int8 or exponents.dtype is not torch.uint8:
+            raise TypeError("codes must be int8 and exponents uint8")
+        rows, cols = _rows(codes, "codes")
+        if tuple(exponents.shape) != (*codes.shape[:-1], -(-cols // GROUP)):
+            raise ValueError(f"exponents have shape {tuple(exponents.shape)}, expected "
+                             f"{(*codes.shape[:-1], -(-cols // GROUP))}")
+        self.codes = _operand(codes, "codes")
+        self.exponents = _operand(exponents, "exponents")
+
+    @classmethod
+    def empty(cls, shape, device):
+        """One to be written."""
+        self = cls.__new__(cls)
+        self.codes = torch.empty(shape, dtype=torch.int8, device=device)
+        self.exponents = torch.empty((*shape[:-1], -(-shape[-1] // GROUP)), dtype=torch.uint8,
+                                     device=device)
+        return self
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @property
+    def nbytes(self):
+        return self.codes.numel() + self.exponents.numel()
+
+    def decode(self, dtype=torch.bfloat16, gain=None, out=None, stream=None):
+        """The tensor's values (exact in both types), times ``gain`` (float32, one per column)."""
+        if stream is not None:
+            return _on(stream, self.decode, dtype, gain, out)
+        lib = load_library()
+        rows, cols = _rows(self.codes, "codes")
+        if out is None:
+            out = torch.empty(self.codes.shape, dtype=dtype, device=self.codes.device)
+        elif not out.is_contiguous():
+            raise ValueError("out must be contiguous")
+        d = _dtype(_operand(out, "out", None, self.codes.shape), "out")
+        if gain is not None:
+            gain = _operand(gain, "gain", torch.float32, (cols,))
+        _check(lib.gefen_checkpoint_decode(self.codes.data_ptr(), self.exponents.data_ptr(),
+                                           _ptr(gain), rows, cols, out.data_ptr(), d, _handle()))
+        return out
+
+
+def checkpoint8(x, stream=None):
+    """The 8-bit checkpoint of a float32 or bfloat16 tensor, in groups of 64 along its last
+    dimension."""
+    if stream is not None:
+        return _on(stream, checkpoint8, x)
+    lib = load_library()
+    x = _operand(x, "x")
+    d = _dtype(x, "x")
+    rows, cols = _rows(x, "x")
+    c = Checkpoint8.empty(x.shape, x.device)
+    _check(lib.gefen_checkpoint_encode(x.data_ptr(), d, rows, cols, c.codes.data_ptr(),
+                                       c.exponents.data_ptr(), _handle()))
+    return c
+
+
+class RMSNormOutput(NamedTuple):
+    """``y`` the scaled rows; ``h`` = x + residual (x itself without one); ``rstd`` float32, one
+    per row; ``checkpoint`` of h * rstd, or None."""
+    y: torch.Tensor
+    h: torch.Tensor
+    rstd: torch.Tensor
+    checkpoint: Optional[Checkpoint8]
+
+
+def rms_norm(x, weight, residual=None, eps: float = 1e-6, checkpoint: bool = False, stream=None):
+    """RMS norm of each row of x + residual, times weight (float32): an :class:`RMSNormOutput`.
+    With ``checkpoint`` the normalised rows are saved in 8 bits for the backward passes."""
+    if stream is not None:
+        return _on(stream, rms_norm, x, weight, residual, eps, checkpoint)
+    lib = load_library()
+    x = _operand(x, "x")
+    d = _dtype(x, "x")
+    rows, cols = _rows(x, "x")
+    weight = _operand(weight, "weight", torch.float32, (cols,))
+    y = torch.empty_like(x)
+    h = x
+    if residual is not None:
+        residual = _operand(residual, "residual", x.dtype, x.shape)
+        h = torch.empty_like(x)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    c = Checkpoint8.empty(x.shape, x.device) if checkpoint else None
+    _check(lib.gefen_rms_norm(x.data_ptr(), _ptr(residual), d, weight.data_ptr(), rows, cols, eps,
+                              y.data_ptr(), None if residual is None else h.data_ptr(),
+                              rstd.data_ptr(), c and c.codes.data_ptr(),
+                              c and c.exponents.data_ptr(), _handle()))
+    return RMSNormOutput(y, h, rstd, c)
+
+
+def rms_norm_backward(dy, saved, rstd, weight, dh=None, stream=None):
+    """(dx, dweight) of :func:`rms_norm`. ``saved`` is its ``checkpoint`` or its ``h``; ``dh`` the
+    gradient that h gets from its other uses, added to dx (which is the residual's too)."""
+    if stream is not None:
+        return _on(stream, rms_norm_backward, dy, saved, rstd, weight, dh)
+    lib = load_library()
+    dy = _operand(dy, "dy")
+    d = _dtype(dy, "dy")
+    rows, cols = _rows(dy, "dy")
+    weight = _operand(weight, "weight", torch.float32, (cols,))
+    rstd = _operand(rstd, "rstd", torch.float32, dy.shape[:-1])
+    h = codes = exps = None
+    if isinstance(saved, Checkpoint8):
+        if saved.shape != dy.shape:
+            raise ValueError(f"saved has shape {tuple(saved.shape)}, expected {tuple(dy.shape)}")
+        codes, exps = saved.codes.data_ptr(), saved.exponents.data_ptr()
+    else:
+        saved = _operand(saved, "saved", dy.dtype, dy.shape)
+        h = saved.data_ptr()
+    if dh is not None:
+        dh = _operand(dh, "dh", dy.dtype, dy.shape)
+    dx = torch.empty_like(dy)
+    dw = torch.empty(cols, dtype=torch.float32, device=dy.device)
+    n = ctypes.c_int64()
+    _check(lib.gefen_rms_norm_backward_workspace(rows, cols, n))
+    ws = torch.empty(n.value, dtype=torch.uint8, device=dy.device)
+    _check(lib.gefen_rms_norm_backward(dy.data_ptr(), _ptr(dh), d, h, codes, exps, rstd.data_ptr(),
+                                       weight.data_ptr(), rows, cols, dx.data_ptr(),
+                                       dw.data_ptr(), ws.data_ptr(), n.value, _handle()))
+    return dx, dw
+
+
+def _ffn_operands(rows_of, what, w_gate, w_up, w_down, activation):
+    act = ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, not {activation!r}")
+    t = _operand(rows_of, what, torch.bfloat16)
+    tokens, width = _rows(t, what)
+    w_gate = _operand(w_gate, "w_gate", torch.bfloat16)
+    if w_gate.dim() != 2 or w_gate.shape[1] != width or w_gate.shape[0] < 1:
+        raise ValueError(f"w_gate has shape {tuple(w_gate.shape)}, expected (inner, {width})")
+    inner = w_gate.shape[0]
+    w_up = _operand(w_up, "w_up", torch.bfloat16, (inner, width))
+    w_down = _operand(w_down, "w_down", torch.bfloat16, (width, inner))
+    return t, tokens, width, inner, w_gate, w_up, w_down, act
+
+
+def _ffn_space(lib, tokens, width, inner, flags, tensors):
+    if any(t is not None and t.data_ptr() % 16 for t in tensors):
+        flags |= _UNALIGNED
+    n = ctypes.c_int64()
+    _check(lib.gefen_gated_ffn_workspace(tokens, width, inner, flags, n))
+    return torch.empty(n.value, dtype=torch.uint8, device=tensors[0].device), n.value
+
+
+def gated_ffn(x, w_gate, w_up, w_down, activation: str = "silu", checkpoint: bool = False,
+              stream=None):
+    """(act(x w_gate^T) * (x w_up^T)) w_down^T of bfloat16 tensors; weights are [out, in].
+    With ``checkpoint`` returns (y, (gate, up)), the 8-bit checkpoints of both projections for
+    :func:`gated_ffn_backward`."""
+    if stream is not None:
+        return _on(stream, gated_ffn, x, w_gate, w_up, w_down, activation, checkpoint)
+    lib = load_library()
+    x, tokens, width, inner, w_gate, w_up, w_down, act = _ffn_operands(
+        x, "x", w_gate, w_up, w_down, activation)
+    y = torch.empty_like(x)
+    saved, p = None, (None,) * 4
+    if checkpoint:
+        shape = (*x.shape[:-1], inner)
+        saved = Checkpoint8.empty(shape, x.device), Checkpoint8.empty(shape, x.device)
+        p = tuple(q.data_ptr() for c in saved for q in (c.codes, c.exponents))
+    ws, n = _ffn_space(lib, tokens, width, inner, 0, (x, w_gate, w_up, w_down))
+    _check(lib.gefen_gated_ffn(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(),
+                               w_down.data_ptr(), tokens, width, inner, act, y.data_ptr(), *p,
+                               ws.data_ptr(), n, _handle()))
+    return (y, saved) if checkpoint else y
+
+
+def gated_ffn_backward(dy, x, saved, w_gate, w_up, w_down, activation: str = "silu", gain=None,
+                       stream=None):
+    """(dx, dw_gate, dw_up, dw_down) of :func:`gated_ffn` from its checkpoints ``saved``. ``x`` is
+    its input, or a :class:`Checkpoint8` of it, times ``gain`` (float32, one per column): the
+    checkpoint of the :func:`rms_norm` that made x, with that norm's weight."""
+    if stream is not None:
+        return _on(stream, gated_ffn_backward, dy, x, saved, w_gate, w_up, w_down, activation,
+                   gain)
+    lib = load_library()
+    dy, tokens, width, inner, w_gate, w_up, w_down, act = _ffn_operands(
+        dy, "dy", w_gate, w_up, w_down, activation)
+    gate, up = saved
+    for c, what in ((gate, "the gate's checkpoint"), (up, "the up projection's checkpoint")):
+        if not isinstance(c, Checkpoint8) or tuple(c.shape) != (*dy.shape[:-1], inner):
+            raise ValueError(f"{what} must be a Checkpoint8 of shape "
+                             f"{(*dy.shape[:-1], inner)}")
+    xs = codes = exps = None
+    if isinstance(x, Checkpoint8):
+        if x.shape != dy.shape:
+            raise ValueError(f"x has shape {tuple(x.shape)}, expected {tuple(dy.shape)}")
+        codes, exps = x.codes.data_ptr(), x.exponents.data_ptr()
+        if gain is not None:
+            gain = _operand(gain, "gain", torch.float32, (width,))
+    else:
+        if gain is not None:
+            raise ValueError("gain goes with a Checkpoint8 of x")
+        xs = x = _operand(x, "x", torch.bfloat16, dy.shape)
+    dx = torch.empty_like(dy)
+    dwg, dwu, dwd = (torch.empty_like(w) for w in (w_gate, w_up, w_down))
+    ws, n = _ffn_space(lib, tokens, width, inner, _BACKWARD, (dy, xs, w_gate, w_up, w_down))
+    _check(lib.gefen_gated_ffn_backward(
+        dy.data_ptr(), _ptr(xs), codes, exps, _ptr(gain), gate.codes.data_ptr(),
+        gate.exponents.data_ptr(), up.codes.data_ptr(), up.exponents.data_ptr(),
+        w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), tokens, width, inner, act,
+        dx.data_ptr(), dwg.data_ptr(), dwu.data_ptr(), dwd.data_ptr(), ws.data_ptr(), n,
+        _handle()))
+    return dx, dwg, dwu, dwd
+
+
+class _Block(torch.autograd.Function):
+    """y, h = the gated block of rms_norm(x + residual), and h, saved in 8 bits."""
+
+    @staticmethod
+    def forward(ctx, x, residual, norm_weight, w_gate, w_up, w_down, eps, activation):
+        n = rms_norm(x, norm_weight, residual, eps, checkpoint=True)
+        y, (gate, up) = gated_ffn(n.y, w_gate, w_up, w_down, activation, checkpoint=True)
+        ctx.save_for_backward(norm_weight, w_gate, w_up, w_down, n.rstd,
+                              n.checkpoint.codes, n.checkpoint.exponents, gate.codes,
+                              gate.exponents, up.codes, up.exponents)
+        ctx.activation, ctx.residual = activation, residual is not None
+        return y, (n.h if residual is not None else x.view_as(x))
+
+    @staticmethod
+    def backward(ctx, dy, dh):
+        nw, wg, wu, wd, rstd, nc, ne, gc, ge, uc, ue = ctx.saved_tensors
+        saved = Checkpoint8(nc, ne)
+        dn, dwg, dwu, dwd = gated_ffn_backward(
+            dy, saved, (Checkpoint8(gc, ge), Checkpoint8(uc, ue)), wg, wu, wd, ctx.activation,
+            gain=nw)
+        dx, dnw = rms_norm_backward(dn, saved, rstd, nw, dh)
+        return dx, dx if ctx.residual else None, dnw, dwg, dwu, dwd, None, None
+
+
+class FeedForward(torch.nn.Module):
+    """The feed-forward half of a transformer block: ``y, h = ff(x, residual)`` with
+    h = x + residual and y the gated block of the RMS norm of h (so that h + y, or h as the next
+    residual of y, goes on). Parameters are float32, as the optimizers take them, and cast to
+    bfloat16 in each call; x and residual are bfloat16. The backward pass keeps the normalised
+    rows and both projections in 8 bits and nothing else of that size."""
+
+    def __init__(self, width: int, inner: int, activation: str = "silu", eps: float = 1e-6,
+                 device=None):
+        super().__init__()
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
+        self.activation, self.eps = activation, eps
+        self.norm = torch.nn.Parameter(torch.ones(width, device=device))
+
+        def weight(out, into):
+            return torch.nn.Parameter(torch.randn(out, into, device=device) * into ** -0.5)
+
+        self.w_gate, self.w_up = weight(inner, width), weight(inner, width)
+        self.w_down = weight(width, inner)
+
+    def forward(self, x, residual=None):
+        bf16 = torch.bfloat16
+        return _Block.apply(x, residual, self.norm, self.w_gate.to(bf16), self.w_up.to(bf16),
+                            self.w_down.to(bf16), self.eps, self.activation)
