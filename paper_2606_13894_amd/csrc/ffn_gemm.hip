@@ -31,8 +31,6 @@
 #include "act8_device.h"
 #include "ffn_internal.h"
 
-#include <type_traits>
-
 namespace gefen {
 namespace {
 
@@ -41,8 +39,10 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) uint16_t lds_u16;
 
-constexpr int BK = 64;
+constexpr int BK = 32;                    // depth of a stage
+constexpr int kStages = 4;                // stages in LDS: three in flight
 constexpr int NI = 4;                     // 32-column blocks of a wave (128 columns)
 constexpr uint32_t kOut = 0x80000000u;    // a vector offset past every resource's range
 
@@ -55,6 +55,11 @@ struct Shape {
     static constexpr int kStage = 2 * T * BK;       // elements of one LDS stage (A, then B)
 };
 
+// The permutation of a row's eight 16-byte pieces of k: a fragment read takes 16 rows at a time,
+// which are to fill 256 bytes of banks. (With row & 7 as the key, rows 8 apart met in a bank:
+// half of the read cycles were conflicts.)
+__device__ __forceinline__ int chunk_key(int row) { return (row >> 2) & 3; }
+
 // The permutation of a row of k's 32-byte pieces: distinct for four consecutive rows within 128
 // bytes, and within 256 bytes for two neighbouring pieces of each.
 __device__ __forceinline__ int piece_key(int row) { return (row & 3) | ((row & 1) << 2); }
@@ -63,20 +68,20 @@ __device__ __forceinline__ int piece_key(int row) { return (row & 3) | ((row & 1
 template <bool BIG, bool KMAJOR>
 struct Loader {
     using S = Shape<BIG>;
-    uint32_t off[4];     // byte offsets of the lane's 16 bytes
-    int klim;            // rows of n or m: stages from this k on have nothing for this lane
+    uint32_t off[2];     // byte offsets of the lane's 16 bytes
+    int klim;            // rows of n or m: nothing for this lane at stages from k = klim on
 
     // DUAL: LDS rows are 64 of the first matrix, 64 of the second, and so on.
     template <bool DUAL>
     __device__ __forceinline__ void init(int wave, int lane, int64_t ld, int64_t klen)
     {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int q = wave * 4 + j;
+        for (int j = 0; j < 2; ++j) {
+            const int q = wave * 2 + j;
             if constexpr (KMAJOR) {
-                int row = q * 8 + (lane >> 3);
+                int row = q * 16 + (lane >> 2);
                 if constexpr (DUAL) row = (row >> 7) * 64 + (row & 63);
-                const int chunk = (lane & 7) ^ (lane >> 3);
+                const int chunk = (lane & 3) ^ chunk_key(row);
                 off[j] = static_cast<uint32_t>((row * ld + chunk * 8) * 2);
                 klim = static_cast<int>(klen) - chunk * 8;
             } else {
@@ -207,6 +212,119 @@ __device__ __forceinline__ u32x4a read_codes(const int8_t* __restrict__ row, int
     return w;
 }
 
+// Fragments of two 16-deep steps from rows of k (of T elements), N 32-wide blocks at the byte
+// addresses at[]: four transposing reads each, of four rows of k. One block with its own wait,
+// so that the compiler neither uses nor reuses a register that is still to be written. (It
+// would wait for every load to LDS in flight before this instruction's builtin, whatever buffer
+// that is for.)
+template <int T>
+__device__ __forceinline__ void read_t(const uint32_t (&p)[4], u32x2a (&o)[16])
+{
+    asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
+                 "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o4], %[p1]\n\t"
+                 "ds_read_b64_tr_b16 %[o5], %[p1] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o6], %[p1] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o7], %[p1] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o8], %[p2]\n\t"
+                 "ds_read_b64_tr_b16 %[o9], %[p2] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o10], %[p2] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o11], %[p2] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o12], %[p3]\n\t"
+                 "ds_read_b64_tr_b16 %[o13], %[p3] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o14], %[p3] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o15], %[p3] offset:%[s3]\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
+                   "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
+                   "=&v"(o[8]), [o9] "=&v"(o[9]), [o10] "=&v"(o[10]), [o11] "=&v"(o[11]), [o12]
+                   "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15])
+                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [s1] "n"(8 *
+                   T), [s2] "n"(32 * T), [s3] "n"(40 * T)
+                 : "memory");
+}
+
+template <int T>
+__device__ __forceinline__ void read_t(const uint32_t (&p)[5], u32x2a (&o)[20])
+{
+    asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
+                 "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o4], %[p1]\n\t"
+                 "ds_read_b64_tr_b16 %[o5], %[p1] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o6], %[p1] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o7], %[p1] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o8], %[p2]\n\t"
+                 "ds_read_b64_tr_b16 %[o9], %[p2] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o10], %[p2] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o11], %[p2] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o12], %[p3]\n\t"
+                 "ds_read_b64_tr_b16 %[o13], %[p3] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o14], %[p3] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o15], %[p3] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o16], %[p4]\n\t"
+                 "ds_read_b64_tr_b16 %[o17], %[p4] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o18], %[p4] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o19], %[p4] offset:%[s3]\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
+                   "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
+                   "=&v"(o[8]), [o9] "=&v"(o[9]), [o10] "=&v"(o[10]), [o11] "=&v"(o[11]), [o12]
+                   "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15]), [o16]
+                   "=&v"(o[16]), [o17] "=&v"(o[17]), [o18] "=&v"(o[18]), [o19] "=&v"(o[19])
+                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [p4] "v"(p[4]),
+                   [s1] "n"(8 * T), [s2] "n"(32 * T), [s3] "n"(40 * T)
+                 : "memory");
+}
+
+template <int T>
+__device__ __forceinline__ void read_t(const uint32_t (&p)[6], u32x2a (&o)[24])
+{
+    asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
+                 "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o4], %[p1]\n\t"
+                 "ds_read_b64_tr_b16 %[o5], %[p1] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o6], %[p1] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o7], %[p1] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o8], %[p2]\n\t"
+                 "ds_read_b64_tr_b16 %[o9], %[p2] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o10], %[p2] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o11], %[p2] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o12], %[p3]\n\t"
+                 "ds_read_b64_tr_b16 %[o13], %[p3] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o14], %[p3] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o15], %[p3] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o16], %[p4]\n\t"
+                 "ds_read_b64_tr_b16 %[o17], %[p4] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o18], %[p4] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o19], %[p4] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o20], %[p5]\n\t"
+                 "ds_read_b64_tr_b16 %[o21], %[p5] offset:%[s1]\n\t"
+                 "ds_read_b64_tr_b16 %[o22], %[p5] offset:%[s2]\n\t"
+                 "ds_read_b64_tr_b16 %[o23], %[p5] offset:%[s3]\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
+                   "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
+                   "=&v"(o[8]), [o9] "=&v"(o[9]), [o10] "=&v"(o[10]), [o11] "=&v"(o[11]), [o12]
+                   "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15]), [o16]
+                   "=&v"(o[16]), [o17] "=&v"(o[17]), [o18] "=&v"(o[18]), [o19] "=&v"(o[19]), [o20]
+                   "=&v"(o[20]), [o21] "=&v"(o[21]), [o22] "=&v"(o[22]), [o23] "=&v"(o[23])
+                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [p4] "v"(p[4]),
+                   [p5] "v"(p[5]), [s1] "n"(8 * T), [s2] "n"(32 * T), [s3] "n"(40 * T)
+                 : "memory");
+}
+
+__device__ __forceinline__ bf16x8 join(const u32x2a& a, const u32x2a& b)
+{
+    const u32x4a v = {a[0], a[1], b[0], b[1]};
+    return __builtin_bit_cast(bf16x8, v);
+}
+
 template <int KIND, bool AK, bool BKM, bool BIG>
 __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnGemm g)
 {
@@ -216,6 +334,8 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
     // two arrays, so that the compiler sees that reads of one do not wait for loads to the other
     __shared__ __attribute__((aligned(16))) uint16_t lds0[S::kStage];
     __shared__ __attribute__((aligned(16))) uint16_t lds1[S::kStage];
+    __shared__ __attribute__((aligned(16))) uint16_t lds2[S::kStage];
+    __shared__ __attribute__((aligned(16))) uint16_t lds3[S::kStage];
     Work w;
     if (!decode_work(g, w)) return;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -234,92 +354,119 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
     const int first = static_cast<int>(int64_t(all) * w.split / g.splits);
     const int nk = static_cast<int>(int64_t(all) * (w.split + 1) / g.splits) - first;
 
-    auto resource = [](const uint16_t* p, int64_t bytes) {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), 0,
-                                                 static_cast<int>(bytes), 0x00020000);
+    auto resource = [](const uint16_t* p, int bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), 0, bytes, 0x00020000);
     };
-    auto load = [&](uint16_t* lds, int it) {
-        const int st = first + it;
-        const int seg = st >= per_seg ? 1 : 0;
-        const int k0 = (st - seg * per_seg) * BK;
-        const int ia = g.segments > 1 ? seg : w.batch;
-        auto piece = [&](__amdgpu_buffer_rsrc_t r, uint16_t* dst, uint32_t off, int soff) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)dst, 16, off, soff, 0, 0);
-        };
-        {
-            uint16_t* dst = lds + wave * 4 * 512;
-            if constexpr (AK) {
-                const auto r = resource(g.a[ia] + row0 * g.lda,
-                                        2 * min(int64_t(T), g.M - row0) * g.lda);
-                const bool in = k0 < la.klim;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) piece(r, dst + j * 512, in ? la.off[j] : kOut, 2 * k0);
-            } else {
-                const auto r = resource(g.a[ia] + k0 * g.lda + row0,
-                                        2 * (min(int64_t(BK), g.K - k0) * g.lda - row0));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) piece(r, dst + j * 512, la.off[j], 0);
-            }
+    auto load_piece = [](__amdgpu_buffer_rsrc_t r, uint16_t* dst, uint32_t off) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)dst, 16, off, 0, 0, 0);
+    };
+    // Where the next stage's pieces come from, moved on stage by stage in scalar registers; past
+    // the last stage, ranges of no bytes.
+    const int lda = static_cast<int>(g.lda), ldb = static_cast<int>(g.ldb);
+    const int klen = static_cast<int>(g.K), kend = per_seg * BK;
+    const int a_rows = static_cast<int>(min(int64_t(T), g.M - row0));
+    const int b_rows = static_cast<int>(min(int64_t(DUAL ? T / 2 : T), g.N - col0));
+    const int a_col = static_cast<int>(row0), b_col = static_cast<int>(col0);   // rows of k
+    const uint16_t* a_base[2];
+    const uint16_t* b_base[2];
+    a_base[0] = g.a[g.segments > 1 ? 0 : w.batch] + (AK ? row0 * g.lda : row0);
+    a_base[1] = g.a[1] + (AK ? row0 * g.lda : row0);
+    // DUAL: a wave's 32 LDS rows lie in one 64-row half
+    b_base[0] = g.b[DUAL ? (wave * 32) >> 6 & 1 : 0] + (BKM ? col0 * g.ldb : col0);
+    b_base[1] = g.b[1] + (BKM ? col0 * g.ldb : col0);
+    const int64_t a_step = AK ? BK : int64_t(BK) * g.lda, b_step = BKM ? BK : int64_t(BK) * g.ldb;
+    const bool second = first >= per_seg;
+    struct Source {
+        const uint16_t *a, *b;
+        int k0, left;      // left: stages still to be loaded
+    } at;
+    at.k0 = (first - (second ? per_seg : 0)) * BK;
+    at.a = a_base[second] + (AK ? at.k0 : at.k0 * g.lda);
+    at.b = b_base[second] + (BKM ? at.k0 : at.k0 * g.ldb);
+    at.left = nk;
+    auto a_bytes = [&]() {
+        return at.left <= 0 ? 0
+                            : 2 * (AK ? a_rows * lda - at.k0 : min(BK, klen - at.k0) * lda - a_col);
+    };
+    auto b_bytes = [&]() {
+        return at.left <= 0
+                   ? 0
+                   : 2 * (BKM ? b_rows * ldb - at.k0 : min(BK, klen - at.k0) * ldb - b_col);
+    };
+    auto advance = [&]() {
+        --at.left;
+        at.k0 += BK;
+        at.a += a_step;
+        at.b += b_step;
+        if (at.k0 == kend) {   // on to the second segment, if there is one
+            at.k0 = 0;
+            at.a = a_base[1];
+            at.b = b_base[1];
         }
-        {
-            uint16_t* dst = lds + T * BK + wave * 4 * 512;
-            if constexpr (DUAL) {
-                const int64_t bytes = 2 * min(int64_t(T / 2), g.N - col0) * g.ldb;
-                const auto r0 = resource(g.b[0] + col0 * g.ldb, bytes);
-                const auto r1 = resource(g.b[1] + col0 * g.ldb, bytes);
-                const bool in = k0 < lb.klim;
-                // a wave's 32 LDS rows lie in one 64-row half
-                const bool second = (wave * 32) & 64;
+    };
+    // The wave's four pieces of a stage: two of A, two of B.
+    auto load = [&](uint16_t* lds) {
+        const int an = a_bytes(), bn = b_bytes();
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    piece(second ? r1 : r0, dst + j * 512, in ? lb.off[j] : kOut, 2 * k0);
-            } else if constexpr (BKM) {
-                const auto r = resource(g.b[seg] + col0 * g.ldb,
-                                        2 * min(int64_t(T), g.N - col0) * g.ldb);
-                const bool in = k0 < lb.klim;
+        for (int j = 0; j < 2; ++j)
+            load_piece(resource(at.a, an), lds + (wave * 2 + j) * 512,
+                       AK && at.k0 >= la.klim ? kOut : la.off[j]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) piece(r, dst + j * 512, in ? lb.off[j] : kOut, 2 * k0);
-            } else {
-                const auto r = resource(g.b[seg] + k0 * g.ldb + col0,
-                                        2 * (min(int64_t(BK), g.K - k0) * g.ldb - col0));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) piece(r, dst + j * 512, lb.off[j], 0);
-            }
-        }
+        for (int j = 0; j < 2; ++j)
+            load_piece(resource(at.b, bn), lds + T * BK + (wave * 2 + j) * 512,
+                       BKM && at.k0 >= lb.klim ? kOut : lb.off[j]);
+        advance();
     };
 
-    // Fragments of one 16-deep step: lane l holds row l % 32, k = 8 (l / 32) .. + 7.
+    // A stage's fragments, two 16-deep steps: lane l holds row l % 32, k = 8 (l / 32) .. + 7.
     const int half = lane >> 5, l32 = lane & 31;
+    bf16x8 fa[2][MI], fb[2][NI];
     auto frag_k = [&](const uint16_t* t, int row, int ks) -> bf16x8 {
-        const int chunk = (2 * ks + half) ^ (l32 & 7);
+        const int chunk = (2 * ks + half) ^ chunk_key(l32);
         return *reinterpret_cast<const bf16x8*>(t + (row + l32) * BK + chunk * 8);
     };
-    const int trow = 8 * half + ((lane >> 2) & 3);    // row of k this lane reads a piece of
+    // Rows of k: byte address of the lane's 8 bytes of the first step's first four rows.
+    const int trow = 8 * half + ((lane >> 2) & 3);
     const int tkey = piece_key((lane >> 2) & 3);
-    auto frag_t = [&](const uint16_t* t, int col, int ks) -> bf16x8 {
+    auto addr_t = [&](const uint16_t* t, int col) -> uint32_t {
         const int piece = ((col >> 4) + ((lane >> 4) & 1)) ^ tkey;
-        const uint16_t* p = t + (16 * ks + trow) * T + piece * 16 + (lane & 3) * 4;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * T));
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
-        const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        return __builtin_bit_cast(bf16x8, v);
+        return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
+                   (lds_u16*)(t + trow * T + piece * 16 + (lane & 3) * 4)));
     };
-    typedef bf16x8 FragA[MI];
-    typedef bf16x8 FragB[NI];
-    auto frags = [&](FragA& fa, FragB& fb, const uint16_t* lds, int ks) {
+    auto frags = [&](const uint16_t* lds) {
         const uint16_t* sb = lds + T * BK;
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-            const int r = (wm * MI + mi) * 32;
-            fa[mi] = AK ? frag_k(lds, r, ks) : frag_t(lds, r, ks);
-        }
+        for (int ks = 0; ks < 2; ++ks) {
+            if constexpr (AK) {
 #pragma unroll
-        for (int ni = 0; ni < NI; ++ni) {
-            const int c = wn * 128 + ni * 32;
-            fb[ni] = BKM ? frag_k(sb, c, ks) : frag_t(sb, c, ks);
+                for (int mi = 0; mi < MI; ++mi) fa[ks][mi] = frag_k(lds, (wm * MI + mi) * 32, ks);
+            }
+            if constexpr (BKM) {
+#pragma unroll
+                for (int ni = 0; ni < NI; ++ni) fb[ks][ni] = frag_k(sb, wn * 128 + ni * 32, ks);
+            }
         }
+        if constexpr (!BKM) {   // rows of k: B, and A with it
+            constexpr int NA = AK ? 0 : MI;
+            uint32_t at[NI + NA];
+            u32x2a o[4 * (NI + NA)];
+#pragma unroll
+            for (int i = 0; i < NI + NA; ++i)
+                at[i] = i < NI ? addr_t(sb, wn * 128 + i * 32)
+                               : addr_t(lds, (wm * MI + i - NI) * 32);
+            read_t<T>(at, o);
+#pragma unroll
+            for (int i = 0; i < NI + NA; ++i)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    const bf16x8 f = join(o[4 * i + 2 * ks], o[4 * i + 2 * ks + 1]);
+                    if (i < NI) fb[ks][i] = f;
+                    else fa[ks][i - NI] = f;
+                }
+        }
+        __builtin_amdgcn_sched_barrier(0);
     };
+    static_assert(AK || !BKM, "an A of rows of k goes with such a B");
     f32x16 acc[MI][NI];
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi)
@@ -327,63 +474,66 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
         for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[mi][ni][v] = 0.0f;
-    auto mfmas = [&](const FragA& fa, const FragB& fb, int from, int to) {
+    auto mfmas = [&]() {
 #pragma unroll
-        for (int q = from; q < to; ++q)
-            acc[q / NI][q % NI] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                fb[q % NI], fa[q / NI], acc[q / NI][q % NI], 0, 0, 0);
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int q = 0; q < MI * NI; ++q)
+                acc[q / NI][q % NI] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    fb[ks][q % NI], fa[ks][q / NI], acc[q / NI][q % NI], 0, 0, 0);
     };
-    constexpr int kMM = MI * NI;
-    FragA fa[2];
-    FragB fb[2];
-    // Instruction order inside a step, by scheduling groups: one matrix-core op, then its share
-    // of the step's fragment reads, so that no more than two steps' fragments are ever live.
-    constexpr int kMfma = 0x008, kDsRead = 0x100;
-    constexpr int kReads = MI * (AK ? 1 : 2) + NI * (BKM ? 1 : 2);
-    auto interleave = [&](auto ops) {
-        constexpr int n = decltype(ops)::value;
-#pragma unroll
-        for (int q = 0; q < n; ++q) {
-            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-            const int share = (q + 1) * kReads / n - q * kReads / n;
-            if (share == 1) __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
-            if (share == 2) __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
-            if (share == 3) __builtin_amdgcn_sched_group_barrier(kDsRead, 3, 0);
-            if (share == 4) __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
-            if (share == 5) __builtin_amdgcn_sched_group_barrier(kDsRead, 5, 0);
-        }
+    auto barrier = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
     };
-    typedef std::integral_constant<int, kMM> WholeStep;
-    typedef std::integral_constant<int, kMM / 2> HalfStep;
-    // One stage: the next stage's loads go out first; each step's matrix-core ops run while the
-    // next step's fragments are read; in the middle of the last step the barrier, then the next
-    // stage's first fragments under the other half (after the last stage, of what is there).
-    auto body = [&](const uint16_t* cur, uint16_t* nxt, int it) {
-        if (it + 1 < nk) load(nxt, it + 1);
-        __builtin_amdgcn_sched_barrier(0);   // not to be moved behind the matrix-core ops
-#pragma unroll
-        for (int ks = 0; ks < 3; ++ks) {
-            frags(fa[(ks + 1) & 1], fb[(ks + 1) & 1], cur, ks + 1);
-            mfmas(fa[ks & 1], fb[ks & 1], 0, kMM);
-            interleave(WholeStep{});
+    // This wave's LDS reads are done, and its loads but for the newest two stages' (four each).
+    auto settled = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0070 | 4 * (kStages - 2));
+    };
+    // A stage is two phases with a barrier after each: fragments out of LDS and the loads of
+    // the stage three ahead; then the matrix-core ops. With eight waves, two to a SIMD, the
+    // second four run one phase behind the first: each SIMD's matrix core works for one wave
+    // while the other reads. The loads go to the buffer of the stage before this one, whose
+    // reads ended before the last barrier; a stage's loads have settled in every wave before
+    // the barrier that its first readers pass.
+    auto body = [&](const uint16_t* cur, uint16_t* to) {
+        if constexpr (!BIG) {
+            settled();
+            barrier();
         }
-        mfmas(fa[1], fb[1], 0, kMM / 2);
-        __builtin_amdgcn_sched_group_barrier(kMfma, kMM / 2, 0);
-        __syncthreads();
-        frags(fa[0], fb[0], nxt, 0);
-        mfmas(fa[1], fb[1], kMM / 2, kMM);
-        interleave(HalfStep{});
+        frags(cur);
+        load(to);
+        if constexpr (BIG) {
+            settled();
+            barrier();
+            __builtin_amdgcn_s_setprio(1);
+        }
+        mfmas();
+        if constexpr (BIG) {
+            __builtin_amdgcn_s_setprio(0);
+            barrier();
+        }
     };
     if (nk > 0) {
-        load(lds0, 0);
-        __syncthreads();
-        frags(fa[0], fb[0], lds0, 0);
-        for (int it = 0;; it += 2) {
-            body(lds0, lds1, it);
-            if (it + 1 >= nk) break;
-            body(lds1, lds0, it + 1);
-            if (it + 2 >= nk) break;
+        load(lds0);
+        load(lds1);
+        load(lds2);
+        if constexpr (BIG) {
+            settled();
+            barrier();
+            if (wave >= 4) barrier();
         }
+        for (int it = 0; it < nk; it += 4) {
+            body(lds0, lds3);
+            body(lds1, lds0);
+            body(lds2, lds1);
+            body(lds3, lds2);
+        }
+        if (BIG && wave < 4) barrier();
     }
 
     // ------------------------------------------------------------------ epilogues
