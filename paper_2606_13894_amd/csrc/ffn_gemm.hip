@@ -31,6 +31,8 @@
 #include "act8_device.h"
 #include "ffn_internal.h"
 
+#include <type_traits>
+
 namespace gefen {
 namespace {
 
@@ -41,8 +43,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) uint16_t lds_u16;
 
-constexpr int BK = 32;                    // depth of a stage
-constexpr int kStages = 4;                // stages in LDS: three in flight
+constexpr int BK = 64;                    // k of a stage: 128 bytes of a row
 constexpr int NI = 4;                     // 32-column blocks of a wave (128 columns)
 constexpr uint32_t kOut = 0x80000000u;    // a vector offset past every resource's range
 
@@ -52,48 +53,44 @@ struct Shape {
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int T = BIG ? 256 : 128;       // tile rows and columns
     static constexpr int MI = BIG ? 2 : 1;          // 32-row blocks of a wave
-    static constexpr int kStage = 2 * T * BK;       // elements of one LDS stage (A, then B)
 };
 
 // The permutation of a row's eight 16-byte pieces of k: a fragment read takes 16 rows at a time,
 // which are to fill 256 bytes of banks. (With row & 7 as the key, rows 8 apart met in a bank:
 // half of the read cycles were conflicts.)
-__device__ __forceinline__ int chunk_key(int row) { return (row >> 2) & 3; }
+__device__ __forceinline__ int chunk_key(int row) { return (row >> 1) & 7; }
 
-// The permutation of a row of k's 32-byte pieces: distinct for four consecutive rows within 128
-// bytes, and within 256 bytes for two neighbouring pieces of each.
-__device__ __forceinline__ int piece_key(int row) { return (row & 3) | ((row & 1) << 2); }
+// The permutation of a row of k's 32-byte pieces (WIDE / 16 of them): distinct for four
+// consecutive rows within 128 bytes of banks, and within 256 for two neighbouring pieces of each.
+// (Rows of 64 elements alternate between the halves of 256 bytes by themselves.)
+template <int WIDE>
+__device__ __forceinline__ int piece_key(int row)
+{
+    static_assert(WIDE >= 64, "four pieces");
+    return WIDE == 64 ? row & 3 : (row & 3) | ((row & 1) << 2);
+}
 
-// One operand's share of the stage loads: four 1 KiB pieces a wave.
-template <bool BIG, bool KMAJOR>
-struct Loader {
-    using S = Shape<BIG>;
-    uint32_t off[2];     // byte offsets of the lane's 16 bytes
-    int klim;            // rows of n or m: nothing for this lane at stages from k = klim on
-
-    // DUAL: LDS rows are 64 of the first matrix, 64 of the second, and so on.
-    template <bool DUAL>
-    __device__ __forceinline__ void init(int wave, int lane, int64_t ld, int64_t klen)
-    {
+// Where a lane's 16 bytes of its wave's N loads of 1 KiB come from, in bytes from the stage's
+// first element: of a K-major tile 8 rows of 64 k a load, else 1024 / (2 WIDE) rows of WIDE.
+template <bool KMAJOR, int WIDE, int N>
+__device__ __forceinline__ void lane_offsets(int wave, int lane, int64_t ld, uint32_t (&off)[N])
+{
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int q = wave * 2 + j;
-            if constexpr (KMAJOR) {
-                int row = q * 16 + (lane >> 2);
-                if constexpr (DUAL) row = (row >> 7) * 64 + (row & 63);
-                const int chunk = (lane & 3) ^ chunk_key(row);
-                off[j] = static_cast<uint32_t>((row * ld + chunk * 8) * 2);
-                klim = static_cast<int>(klen) - chunk * 8;
-            } else {
-                constexpr int kPer = S::T / 8;            // 16-byte pieces of a row
-                const int row = q * (64 / kPer) + lane / kPer;
-                const int pc = lane % kPer;
-                const int chunk = (((pc >> 1) ^ piece_key(row)) << 1) | (pc & 1);
-                off[j] = static_cast<uint32_t>((row * ld + chunk * 8) * 2);
-            }
+    for (int j = 0; j < N; ++j) {
+        const int q = wave * N + j;
+        int row, chunk;
+        if constexpr (KMAJOR) {
+            row = q * 8 + (lane >> 3);
+            chunk = (lane & 7) ^ chunk_key(row);
+        } else {
+            constexpr int kPer = WIDE / 8;            // 16-byte pieces of a row
+            row = q * (64 / kPer) + lane / kPer;
+            const int pc = lane % kPer;
+            chunk = (((pc >> 1) ^ piece_key<WIDE>(row)) << 1) | (pc & 1);
         }
+        off[j] = static_cast<uint32_t>((row * ld + chunk * 8) * 2);
     }
-};
+}
 
 struct Work {
     int32_t tm, tn, batch, split;
@@ -212,101 +209,68 @@ __device__ __forceinline__ u32x4a read_codes(const int8_t* __restrict__ row, int
     return w;
 }
 
-// Fragments of two 16-deep steps from rows of k (of T elements), N 32-wide blocks at the byte
-// addresses at[]: four transposing reads each, of four rows of k. One block with its own wait,
-// so that the compiler neither uses nor reuses a register that is still to be written. (It
-// would wait for every load to LDS in flight before this instruction's builtin, whatever buffer
-// that is for.)
-template <int T>
-__device__ __forceinline__ void read_t(const uint32_t (&p)[4], u32x2a (&o)[16])
+// Fragments of a stage's four 16-deep steps from rows of k, of 32-wide blocks at the byte
+// addresses p[]: eight transposing reads each, of four rows of k; first A's blocks (rows of SA
+// bytes), then two of B's (rows of SB bytes). One block with its own wait, so that the compiler
+// neither uses nor reuses a register that is still to be written. (It would wait for every load
+// to LDS in flight before this instruction's builtin, whatever buffer that is for.)
+template <int SA, int SB>
+__device__ __forceinline__ void read_t(const uint32_t (&p)[2], u32x2a (&o)[16])
 {
     asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
-                 "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o4], %[p1]\n\t"
-                 "ds_read_b64_tr_b16 %[o5], %[p1] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o6], %[p1] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o7], %[p1] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o8], %[p2]\n\t"
-                 "ds_read_b64_tr_b16 %[o9], %[p2] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o10], %[p2] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o11], %[p2] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o12], %[p3]\n\t"
-                 "ds_read_b64_tr_b16 %[o13], %[p3] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o14], %[p3] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o15], %[p3] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o4], %[p0] offset:%[b4]\n\t"
+                 "ds_read_b64_tr_b16 %[o5], %[p0] offset:%[b5]\n\t"
+                 "ds_read_b64_tr_b16 %[o6], %[p0] offset:%[b6]\n\t"
+                 "ds_read_b64_tr_b16 %[o7], %[p0] offset:%[b7]\n\t"
+                 "ds_read_b64_tr_b16 %[o8], %[p1]\n\t"
+                 "ds_read_b64_tr_b16 %[o9], %[p1] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o10], %[p1] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o11], %[p1] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o12], %[p1] offset:%[b4]\n\t"
+                 "ds_read_b64_tr_b16 %[o13], %[p1] offset:%[b5]\n\t"
+                 "ds_read_b64_tr_b16 %[o14], %[p1] offset:%[b6]\n\t"
+                 "ds_read_b64_tr_b16 %[o15], %[p1] offset:%[b7]\n\t"
                  "s_waitcnt lgkmcnt(0)"
                  : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
                    "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
                    "=&v"(o[8]), [o9] "=&v"(o[9]), [o10] "=&v"(o[10]), [o11] "=&v"(o[11]), [o12]
                    "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15])
-                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [s1] "n"(8 *
-                   T), [s2] "n"(32 * T), [s3] "n"(40 * T)
+                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [b1] "n"(4 * SB), [b2] "n"(16 * SB), [b3]
+                   "n"(20 * SB), [b4] "n"(32 * SB), [b5] "n"(36 * SB), [b6] "n"(48 * SB), [b7]
+                   "n"(52 * SB)
                  : "memory");
 }
 
-template <int T>
-__device__ __forceinline__ void read_t(const uint32_t (&p)[5], u32x2a (&o)[20])
+template <int SA, int SB>
+__device__ __forceinline__ void read_t(const uint32_t (&p)[3], u32x2a (&o)[24])
 {
     asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
-                 "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o4], %[p1]\n\t"
-                 "ds_read_b64_tr_b16 %[o5], %[p1] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o6], %[p1] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o7], %[p1] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o8], %[p2]\n\t"
-                 "ds_read_b64_tr_b16 %[o9], %[p2] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o10], %[p2] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o11], %[p2] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o12], %[p3]\n\t"
-                 "ds_read_b64_tr_b16 %[o13], %[p3] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o14], %[p3] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o15], %[p3] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o16], %[p4]\n\t"
-                 "ds_read_b64_tr_b16 %[o17], %[p4] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o18], %[p4] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o19], %[p4] offset:%[s3]\n\t"
-                 "s_waitcnt lgkmcnt(0)"
-                 : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
-                   "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
-                   "=&v"(o[8]), [o9] "=&v"(o[9]), [o10] "=&v"(o[10]), [o11] "=&v"(o[11]), [o12]
-                   "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15]), [o16]
-                   "=&v"(o[16]), [o17] "=&v"(o[17]), [o18] "=&v"(o[18]), [o19] "=&v"(o[19])
-                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [p4] "v"(p[4]),
-                   [s1] "n"(8 * T), [s2] "n"(32 * T), [s3] "n"(40 * T)
-                 : "memory");
-}
-
-template <int T>
-__device__ __forceinline__ void read_t(const uint32_t (&p)[6], u32x2a (&o)[24])
-{
-    asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
-                 "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o4], %[p1]\n\t"
-                 "ds_read_b64_tr_b16 %[o5], %[p1] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o6], %[p1] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o7], %[p1] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o8], %[p2]\n\t"
-                 "ds_read_b64_tr_b16 %[o9], %[p2] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o10], %[p2] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o11], %[p2] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o12], %[p3]\n\t"
-                 "ds_read_b64_tr_b16 %[o13], %[p3] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o14], %[p3] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o15], %[p3] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o16], %[p4]\n\t"
-                 "ds_read_b64_tr_b16 %[o17], %[p4] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o18], %[p4] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o19], %[p4] offset:%[s3]\n\t"
-                 "ds_read_b64_tr_b16 %[o20], %[p5]\n\t"
-                 "ds_read_b64_tr_b16 %[o21], %[p5] offset:%[s1]\n\t"
-                 "ds_read_b64_tr_b16 %[o22], %[p5] offset:%[s2]\n\t"
-                 "ds_read_b64_tr_b16 %[o23], %[p5] offset:%[s3]\n\t"
+                 "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[a1]\n\t"
+                 "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[a2]\n\t"
+                 "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[a3]\n\t"
+                 "ds_read_b64_tr_b16 %[o4], %[p0] offset:%[a4]\n\t"
+                 "ds_read_b64_tr_b16 %[o5], %[p0] offset:%[a5]\n\t"
+                 "ds_read_b64_tr_b16 %[o6], %[p0] offset:%[a6]\n\t"
+                 "ds_read_b64_tr_b16 %[o7], %[p0] offset:%[a7]\n\t"
+                 "ds_read_b64_tr_b16 %[o8], %[p1]\n\t"
+                 "ds_read_b64_tr_b16 %[o9], %[p1] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o10], %[p1] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o11], %[p1] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o12], %[p1] offset:%[b4]\n\t"
+                 "ds_read_b64_tr_b16 %[o13], %[p1] offset:%[b5]\n\t"
+                 "ds_read_b64_tr_b16 %[o14], %[p1] offset:%[b6]\n\t"
+                 "ds_read_b64_tr_b16 %[o15], %[p1] offset:%[b7]\n\t"
+                 "ds_read_b64_tr_b16 %[o16], %[p2]\n\t"
+                 "ds_read_b64_tr_b16 %[o17], %[p2] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o18], %[p2] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o19], %[p2] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o20], %[p2] offset:%[b4]\n\t"
+                 "ds_read_b64_tr_b16 %[o21], %[p2] offset:%[b5]\n\t"
+                 "ds_read_b64_tr_b16 %[o22], %[p2] offset:%[b6]\n\t"
+                 "ds_read_b64_tr_b16 %[o23], %[p2] offset:%[b7]\n\t"
                  "s_waitcnt lgkmcnt(0)"
                  : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
                    "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
@@ -314,8 +278,62 @@ __device__ __forceinline__ void read_t(const uint32_t (&p)[6], u32x2a (&o)[24])
                    "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15]), [o16]
                    "=&v"(o[16]), [o17] "=&v"(o[17]), [o18] "=&v"(o[18]), [o19] "=&v"(o[19]), [o20]
                    "=&v"(o[20]), [o21] "=&v"(o[21]), [o22] "=&v"(o[22]), [o23] "=&v"(o[23])
-                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [p4] "v"(p[4]),
-                   [p5] "v"(p[5]), [s1] "n"(8 * T), [s2] "n"(32 * T), [s3] "n"(40 * T)
+                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [a1] "n"(4 * SA), [a2] "n"(16 *
+                   SA), [a3] "n"(20 * SA), [a4] "n"(32 * SA), [a5] "n"(36 * SA), [a6] "n"(48 *
+                   SA), [a7] "n"(52 * SA), [b1] "n"(4 * SB), [b2] "n"(16 * SB), [b3] "n"(20 * SB),
+                   [b4] "n"(32 * SB), [b5] "n"(36 * SB), [b6] "n"(48 * SB), [b7] "n"(52 * SB)
+                 : "memory");
+}
+
+template <int SA, int SB>
+__device__ __forceinline__ void read_t(const uint32_t (&p)[4], u32x2a (&o)[32])
+{
+    asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
+                 "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[a1]\n\t"
+                 "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[a2]\n\t"
+                 "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[a3]\n\t"
+                 "ds_read_b64_tr_b16 %[o4], %[p0] offset:%[a4]\n\t"
+                 "ds_read_b64_tr_b16 %[o5], %[p0] offset:%[a5]\n\t"
+                 "ds_read_b64_tr_b16 %[o6], %[p0] offset:%[a6]\n\t"
+                 "ds_read_b64_tr_b16 %[o7], %[p0] offset:%[a7]\n\t"
+                 "ds_read_b64_tr_b16 %[o8], %[p1]\n\t"
+                 "ds_read_b64_tr_b16 %[o9], %[p1] offset:%[a1]\n\t"
+                 "ds_read_b64_tr_b16 %[o10], %[p1] offset:%[a2]\n\t"
+                 "ds_read_b64_tr_b16 %[o11], %[p1] offset:%[a3]\n\t"
+                 "ds_read_b64_tr_b16 %[o12], %[p1] offset:%[a4]\n\t"
+                 "ds_read_b64_tr_b16 %[o13], %[p1] offset:%[a5]\n\t"
+                 "ds_read_b64_tr_b16 %[o14], %[p1] offset:%[a6]\n\t"
+                 "ds_read_b64_tr_b16 %[o15], %[p1] offset:%[a7]\n\t"
+                 "ds_read_b64_tr_b16 %[o16], %[p2]\n\t"
+                 "ds_read_b64_tr_b16 %[o17], %[p2] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o18], %[p2] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o19], %[p2] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o20], %[p2] offset:%[b4]\n\t"
+                 "ds_read_b64_tr_b16 %[o21], %[p2] offset:%[b5]\n\t"
+                 "ds_read_b64_tr_b16 %[o22], %[p2] offset:%[b6]\n\t"
+                 "ds_read_b64_tr_b16 %[o23], %[p2] offset:%[b7]\n\t"
+                 "ds_read_b64_tr_b16 %[o24], %[p3]\n\t"
+                 "ds_read_b64_tr_b16 %[o25], %[p3] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o26], %[p3] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o27], %[p3] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o28], %[p3] offset:%[b4]\n\t"
+                 "ds_read_b64_tr_b16 %[o29], %[p3] offset:%[b5]\n\t"
+                 "ds_read_b64_tr_b16 %[o30], %[p3] offset:%[b6]\n\t"
+                 "ds_read_b64_tr_b16 %[o31], %[p3] offset:%[b7]\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
+                   "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
+                   "=&v"(o[8]), [o9] "=&v"(o[9]), [o10] "=&v"(o[10]), [o11] "=&v"(o[11]), [o12]
+                   "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15]), [o16]
+                   "=&v"(o[16]), [o17] "=&v"(o[17]), [o18] "=&v"(o[18]), [o19] "=&v"(o[19]), [o20]
+                   "=&v"(o[20]), [o21] "=&v"(o[21]), [o22] "=&v"(o[22]), [o23] "=&v"(o[23]), [o24]
+                   "=&v"(o[24]), [o25] "=&v"(o[25]), [o26] "=&v"(o[26]), [o27] "=&v"(o[27]), [o28]
+                   "=&v"(o[28]), [o29] "=&v"(o[29]), [o30] "=&v"(o[30]), [o31] "=&v"(o[31])
+                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [a1] "n"(4 *
+                   SA), [a2] "n"(16 * SA), [a3] "n"(20 * SA), [a4] "n"(32 * SA), [a5] "n"(36 *
+                   SA), [a6] "n"(48 * SA), [a7] "n"(52 * SA), [b1] "n"(4 * SB), [b2] "n"(16 * SB),
+                   [b3] "n"(20 * SB), [b4] "n"(32 * SB), [b5] "n"(36 * SB), [b6] "n"(48 * SB),
+                   [b7] "n"(52 * SB)
                  : "memory");
 }
 
@@ -331,11 +349,11 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
     using S = Shape<BIG>;
     constexpr int T = S::T, MI = S::MI;
     constexpr bool DUAL = KIND == kFfnGateUp;
-    // two arrays, so that the compiler sees that reads of one do not wait for loads to the other
-    __shared__ __attribute__((aligned(16))) uint16_t lds0[S::kStage];
-    __shared__ __attribute__((aligned(16))) uint16_t lds1[S::kStage];
-    __shared__ __attribute__((aligned(16))) uint16_t lds2[S::kStage];
-    __shared__ __attribute__((aligned(16))) uint16_t lds3[S::kStage];
+    // two stages of A, and B's halves, as arrays of their own: so the compiler sees that reads of
+    // one do not wait for loads to the others
+    __shared__ __attribute__((aligned(16))) uint16_t lds_a0[T * BK], lds_a1[T * BK];
+    __shared__ __attribute__((aligned(16))) uint16_t lds_b00[T * BK / 2], lds_b01[T * BK / 2];
+    __shared__ __attribute__((aligned(16))) uint16_t lds_b10[T * BK / 2], lds_b11[T * BK / 2];
     Work w;
     if (!decode_work(g, w)) return;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -344,124 +362,139 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
     const int64_t row0 = int64_t(w.tm) * T;
     const int64_t col0 = int64_t(w.tn) * (DUAL ? T / 2 : T);   // DUAL: columns of each matrix
 
-    Loader<BIG, AK> la;
-    Loader<BIG, BKM> lb;
-    la.template init<false>(wave, lane, g.lda, g.kpad);
-    lb.template init<DUAL>(wave, lane, g.ldb, g.kpad);
-
-    const int per_seg = g.stages;                     // stages of one segment of the sum
-    const int all = per_seg * g.segments;
+    const int stages = g.stages;                      // of one segment of the sum
+    const int all = stages * g.segments;
     const int first = static_cast<int>(int64_t(all) * w.split / g.splits);
     const int nk = static_cast<int>(int64_t(all) * (w.split + 1) / g.splits) - first;
 
+    // A stage's tiles: A (T rows of m), and B's two halves of H = T / 2 columns of n, which are
+    // two parts of one matrix, or of the gate's and the up matrix. Their sources move on stage
+    // by stage in scalar registers; past the last stage they are ranges of no bytes.
+    constexpr int H = T / 2;
+    uint32_t off_a[4], off_b[2];
+    lane_offsets<AK, T>(wave, lane, g.lda, off_a);
+    lane_offsets<BKM, H>(wave, lane, g.ldb, off_b);
+    int klim[2];   // K-major: load j has nothing for this lane at stages from k = klim[j & 1] on
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        klim[j] = static_cast<int>(g.kpad) - 8 * ((lane & 7) ^ chunk_key(8 * j + (lane >> 3)));
+    const int lda = static_cast<int>(g.lda), ldb = static_cast<int>(g.ldb);
+    const int klen = static_cast<int>(g.K), kend = stages * BK;
+    const int a_rows = static_cast<int>(min(int64_t(T), g.M - row0));
+    int b_rows[2], b_col[2];
+    const uint16_t *a_next, *b_next[2];               // where the second segment starts
+    struct Source {
+        const uint16_t* p;
+        int k0, left;                                 // left: stages still to be loaded
+    } at_a, at_b[2];
+    const bool second = first >= stages;
+    const int start = (first - (second ? stages : 0)) * BK;
+    {
+        const int64_t skip = AK ? row0 * g.lda : row0;
+        a_next = g.a[1] + skip;
+        at_a.p = (second ? g.a[1] : g.a[g.segments > 1 ? 0 : w.batch]) + skip +
+                 (AK ? start : start * g.lda);
+        at_a.k0 = start;
+        at_a.left = nk;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t col = DUAL ? col0 : col0 + h * H;
+        const int64_t skip = BKM ? col * g.ldb : col;
+        b_next[h] = g.b[1] + skip;
+        at_b[h].p = g.b[DUAL ? h : second] + skip + (BKM ? start : start * g.ldb);
+        at_b[h].k0 = start;
+        at_b[h].left = nk;
+        b_rows[h] = static_cast<int>(max(int64_t(0), min(int64_t(H), g.N - col)));
+        b_col[h] = static_cast<int>(col);
+    }
     auto resource = [](const uint16_t* p, int bytes) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), 0, bytes, 0x00020000);
     };
     auto load_piece = [](__amdgpu_buffer_rsrc_t r, uint16_t* dst, uint32_t off) {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)dst, 16, off, 0, 0, 0);
     };
-    // Where the next stage's pieces come from, moved on stage by stage in scalar registers; past
-    // the last stage, ranges of no bytes.
-    const int lda = static_cast<int>(g.lda), ldb = static_cast<int>(g.ldb);
-    const int klen = static_cast<int>(g.K), kend = per_seg * BK;
-    const int a_rows = static_cast<int>(min(int64_t(T), g.M - row0));
-    const int b_rows = static_cast<int>(min(int64_t(DUAL ? T / 2 : T), g.N - col0));
-    const int a_col = static_cast<int>(row0), b_col = static_cast<int>(col0);   // rows of k
-    const uint16_t* a_base[2];
-    const uint16_t* b_base[2];
-    a_base[0] = g.a[g.segments > 1 ? 0 : w.batch] + (AK ? row0 * g.lda : row0);
-    a_base[1] = g.a[1] + (AK ? row0 * g.lda : row0);
-    // DUAL: a wave's 32 LDS rows lie in one 64-row half
-    b_base[0] = g.b[DUAL ? (wave * 32) >> 6 & 1 : 0] + (BKM ? col0 * g.ldb : col0);
-    b_base[1] = g.b[1] + (BKM ? col0 * g.ldb : col0);
-    const int64_t a_step = AK ? BK : int64_t(BK) * g.lda, b_step = BKM ? BK : int64_t(BK) * g.ldb;
-    const bool second = first >= per_seg;
-    struct Source {
-        const uint16_t *a, *b;
-        int k0, left;      // left: stages still to be loaded
-    } at;
-    at.k0 = (first - (second ? per_seg : 0)) * BK;
-    at.a = a_base[second] + (AK ? at.k0 : at.k0 * g.lda);
-    at.b = b_base[second] + (BKM ? at.k0 : at.k0 * g.ldb);
-    at.left = nk;
-    auto a_bytes = [&]() {
-        return at.left <= 0 ? 0
-                            : 2 * (AK ? a_rows * lda - at.k0 : min(BK, klen - at.k0) * lda - a_col);
-    };
-    auto b_bytes = [&]() {
-        return at.left <= 0
-                   ? 0
-                   : 2 * (BKM ? b_rows * ldb - at.k0 : min(BK, klen - at.k0) * ldb - b_col);
-    };
-    auto advance = [&]() {
+    auto advance = [&](Source& at, const uint16_t* next, int64_t step) {
         --at.left;
         at.k0 += BK;
-        at.a += a_step;
-        at.b += b_step;
-        if (at.k0 == kend) {   // on to the second segment, if there is one
+        at.p += step;
+        if (at.k0 == kend) {
             at.k0 = 0;
-            at.a = a_base[1];
-            at.b = b_base[1];
+            at.p = next;
         }
     };
-    // The wave's four pieces of a stage: two of A, two of B.
-    auto load = [&](uint16_t* lds) {
-        const int an = a_bytes(), bn = b_bytes();
+    struct Tiles {
+        uint16_t *a, *b[2];
+    };
+    const Tiles t0 = {lds_a0, {lds_b00, lds_b01}}, t1 = {lds_a1, {lds_b10, lds_b11}};
+    auto load_a = [&](const Tiles& t) {               // four loads
+        const int n = AK ? a_rows * lda - at_a.k0
+                         : min(BK, klen - at_a.k0) * lda - static_cast<int>(row0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            load_piece(resource(at_a.p, at_a.left > 0 ? 2 * n : 0), t.a + (wave * 4 + j) * 512,
+                       AK && at_a.k0 >= klim[j & 1] ? kOut : off_a[j]);
+        advance(at_a, a_next, AK ? BK : int64_t(BK) * g.lda);
+    };
+    auto load_b = [&](const Tiles& t, int h) {        // two
+        Source& at = at_b[h];
+        const int n = BKM ? b_rows[h] * ldb - at.k0 : min(BK, klen - at.k0) * ldb - b_col[h];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            load_piece(resource(at.a, an), lds + (wave * 2 + j) * 512,
-                       AK && at.k0 >= la.klim ? kOut : la.off[j]);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            load_piece(resource(at.b, bn), lds + T * BK + (wave * 2 + j) * 512,
-                       BKM && at.k0 >= lb.klim ? kOut : lb.off[j]);
-        advance();
+            load_piece(resource(at.p, at.left > 0 && n > 0 ? 2 * n : 0),
+                       t.b[h] + (wave * 2 + j) * 512,
+                       BKM && at.k0 >= klim[j] ? kOut : off_b[j]);
+        advance(at, b_next[h], BKM ? BK : int64_t(BK) * g.ldb);
     };
 
-    // A stage's fragments, two 16-deep steps: lane l holds row l % 32, k = 8 (l / 32) .. + 7.
+    // Fragments of four 16-deep steps: lane l holds row l % 32, k = 8 (l / 32) .. + 7.
     const int half = lane >> 5, l32 = lane & 31;
-    bf16x8 fa[2][MI], fb[2][NI];
+    bf16x8 fa[4][MI], fb[4][2];
     auto frag_k = [&](const uint16_t* t, int row, int ks) -> bf16x8 {
         const int chunk = (2 * ks + half) ^ chunk_key(l32);
         return *reinterpret_cast<const bf16x8*>(t + (row + l32) * BK + chunk * 8);
     };
-    // Rows of k: byte address of the lane's 8 bytes of the first step's first four rows.
+    // Rows of k: byte address of the lane's 8 bytes of the first four rows.
     const int trow = 8 * half + ((lane >> 2) & 3);
-    const int tkey = piece_key((lane >> 2) & 3);
-    auto addr_t = [&](const uint16_t* t, int col) -> uint32_t {
-        const int piece = ((col >> 4) + ((lane >> 4) & 1)) ^ tkey;
+    auto addr_t = [&](const uint16_t* t, auto width, int col) -> uint32_t {
+        constexpr int wide = decltype(width)::value;
+        const int piece = ((col >> 4) + ((lane >> 4) & 1)) ^ piece_key<wide>((lane >> 2) & 3);
         return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
-                   (lds_u16*)(t + trow * T + piece * 16 + (lane & 3) * 4)));
+                   (lds_u16*)(t + trow * wide + piece * 16 + (lane & 3) * 4)));
     };
-    auto frags = [&](const uint16_t* lds) {
-        const uint16_t* sb = lds + T * BK;
+    // All of A's with B's first half, or B's second half.
+    typedef std::integral_constant<int, T> WideA;
+    typedef std::integral_constant<int, H> WideB;
+    auto frags = [&](const Tiles& t, auto part) {
+        constexpr int h = decltype(part)::value;
+        constexpr int NA = AK || h ? 0 : MI;
+        const uint16_t* sb = t.b[h];
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            if constexpr (AK) {
+        for (int ks = 0; ks < 4; ++ks) {
+            if constexpr (AK && h == 0) {
 #pragma unroll
-                for (int mi = 0; mi < MI; ++mi) fa[ks][mi] = frag_k(lds, (wm * MI + mi) * 32, ks);
+                for (int mi = 0; mi < MI; ++mi) fa[ks][mi] = frag_k(t.a, (wm * MI + mi) * 32, ks);
             }
             if constexpr (BKM) {
 #pragma unroll
-                for (int ni = 0; ni < NI; ++ni) fb[ks][ni] = frag_k(sb, wn * 128 + ni * 32, ks);
+                for (int j = 0; j < 2; ++j) fb[ks][j] = frag_k(sb, wn * 64 + j * 32, ks);
             }
         }
         if constexpr (!BKM) {   // rows of k: B, and A with it
-            constexpr int NA = AK ? 0 : MI;
-            uint32_t at[NI + NA];
-            u32x2a o[4 * (NI + NA)];
+            uint32_t at[NA + 2];
+            u32x2a o[8 * (NA + 2)];
 #pragma unroll
-            for (int i = 0; i < NI + NA; ++i)
-                at[i] = i < NI ? addr_t(sb, wn * 128 + i * 32)
-                               : addr_t(lds, (wm * MI + i - NI) * 32);
-            read_t<T>(at, o);
+            for (int i = 0; i < NA + 2; ++i)
+                at[i] = i < NA ? addr_t(t.a, WideA{}, (wm * MI + i) * 32)
+                               : addr_t(sb, WideB{}, wn * 64 + (i - NA) * 32);
+            read_t<2 * T, 2 * H>(at, o);
 #pragma unroll
-            for (int i = 0; i < NI + NA; ++i)
+            for (int i = 0; i < NA + 2; ++i)
 #pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    const bf16x8 f = join(o[4 * i + 2 * ks], o[4 * i + 2 * ks + 1]);
-                    if (i < NI) fb[ks][i] = f;
-                    else fa[ks][i - NI] = f;
+                for (int ks = 0; ks < 4; ++ks) {
+                    const bf16x8 f = join(o[8 * i + 2 * ks], o[8 * i + 2 * ks + 1]);
+                    if (i < NA) fa[ks][i] = f;
+                    else fb[ks][i - NA] = f;
                 }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -474,13 +507,16 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
         for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[mi][ni][v] = 0.0f;
-    auto mfmas = [&]() {
+    auto mfmas = [&](auto part) {
+        constexpr int h = decltype(part)::value;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+        for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-            for (int q = 0; q < MI * NI; ++q)
-                acc[q / NI][q % NI] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    fb[ks][q % NI], fa[ks][q / NI], acc[q / NI][q % NI], 0, 0, 0);
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[mi][2 * h + j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        fb[ks][j], fa[ks][mi], acc[mi][2 * h + j], 0, 0, 0);
     };
     auto barrier = [&]() {
         __builtin_amdgcn_sched_barrier(0);
@@ -489,49 +525,62 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    // This wave's LDS reads are done, and its loads but for the newest two stages' (four each).
+    // This wave's LDS reads are done, and all but its newest eight loads: those of the phase
+    // after next and later (six with A and B's first half, two with the second).
     auto settled = [&]() {
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x0070 | 4 * (kStages - 2));
+        __builtin_amdgcn_s_waitcnt(0x0070 | 8);
     };
-    // A stage is two phases with a barrier after each: fragments out of LDS and the loads of
-    // the stage three ahead; then the matrix-core ops. With eight waves, two to a SIMD, the
-    // second four run one phase behind the first: each SIMD's matrix core works for one wave
-    // while the other reads. The loads go to the buffer of the stage before this one, whose
-    // reads ended before the last barrier; a stage's loads have settled in every wave before
-    // the barrier that its first readers pass.
-    auto body = [&](const uint16_t* cur, uint16_t* to) {
+    // A stage is two parts, by B's halves; A's fragments stay for the second. A part is two
+    // phases: its fragments out of LDS and loads for a later part; then the matrix-core ops.
+    // With eight waves, two to a SIMD, a barrier follows each phase and the second four run one
+    // phase behind the first: each SIMD's matrix core works for one wave while the other reads.
+    // Three parts' loads are in flight: A and B's first half of the stage after next go out in
+    // the second part, into this stage's buffer, where all waves have read them before the last
+    // barrier; B's second half in the next stage's first part. A part's loads have settled in
+    // every wave before the barrier that its first readers pass.
+    auto part = [&](auto which, const Tiles& cur, const Tiles& to) {
+        constexpr int h = decltype(which)::value;
         if constexpr (!BIG) {
             settled();
             barrier();
         }
-        frags(cur);
-        load(to);
+        frags(cur, which);
+        if constexpr (h == 0) {
+            load_b(to, 1);
+        } else {
+            load_a(to);
+            load_b(to, 0);
+        }
         if constexpr (BIG) {
             settled();
             barrier();
             __builtin_amdgcn_s_setprio(1);
         }
-        mfmas();
+        mfmas(which);
         if constexpr (BIG) {
             __builtin_amdgcn_s_setprio(0);
             barrier();
         }
     };
+    typedef std::integral_constant<int, 0> First;
+    typedef std::integral_constant<int, 1> Second;
     if (nk > 0) {
-        load(lds0);
-        load(lds1);
-        load(lds2);
+        load_a(t0);
+        load_b(t0, 0);
+        load_b(t0, 1);
+        load_a(t1);
+        load_b(t1, 0);
         if constexpr (BIG) {
             settled();
             barrier();
             if (wave >= 4) barrier();
         }
-        for (int it = 0; it < nk; it += 4) {
-            body(lds0, lds3);
-            body(lds1, lds0);
-            body(lds2, lds1);
-            body(lds3, lds2);
+        for (int it = 0; it < nk; it += 2) {
+            part(First{}, t0, t1);
+            part(Second{}, t0, t0);
+            part(First{}, t1, t0);
+            part(Second{}, t1, t1);
         }
         if (BIG && wave < 4) barrier();
     }
@@ -570,7 +619,7 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
             if (!on) continue;
 #pragma unroll
             for (int ni = 0; ni < NI; ++ni) {
-                const int64_t c = col0 + wn * 128 + ni * 32 + 16 * half;
+                const int64_t c = col0 + (ni >> 1) * H + wn * 64 + (ni & 1) * 32 + 16 * half;
                 float d[16], dg[16], du[16], av[16];
                 to_run(acc[mi][ni], d);   // both halves of the wave take part
                 if (c >= g.ldo) continue;
@@ -601,7 +650,7 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
             if (!on) continue;
 #pragma unroll
             for (int ni = 0; ni < NI; ++ni) {
-                const int64_t c = col0 + wn * 128 + ni * 32 + 16 * half;
+                const int64_t c = col0 + (ni >> 1) * H + wn * 64 + (ni & 1) * 32 + 16 * half;
                 float v[16];
                 to_run(acc[mi][ni], v);
                 if (g.partial) {

@@ -9,7 +9,7 @@ namespace gefen {
 
 constexpr int64_t kFfnMaxTokens = int64_t(1) << 24;
 constexpr int64_t kFfnMaxWidth = int64_t(1) << 20;   // a tile's rows stay within 32-bit offsets
-constexpr int kFfnBigTile = 256, kFfnSmallTile = 128, kFfnDepth = 32;
+constexpr int kFfnBigTile = 256, kFfnSmallTile = 128, kFfnDepth = 64;
 
 inline int64_t ffn_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t ffn_up8(int64_t a) { return (a + 7) / 8 * 8; }
@@ -33,16 +33,16 @@ inline FfnTile ffn_choose(int64_t M, int64_t N, int64_t K, int batch, int segmen
         const int64_t tm = ffn_ceil(M, t), tn = ffn_ceil(N, halves ? t / 2 : t);
         const int64_t stages = ffn_ceil(K, kFfnDepth), all = stages * segments;
         for (int64_t s : {1, 2, 3, 4, 6, 8, 12, 16}) {
-            if (s > 1 && (!may_split || all / s < 8)) break;
+            if (s > 1 && (!may_split || all / s < 4)) break;
             const int64_t groups = tm * tn * batch * s;
             const int64_t each = ffn_ceil(all, s);
             double us;
             if (b)
-                us = double(ffn_ceil(groups, 256)) * (0.625 * double(each) + 4.0);
+                us = double(ffn_ceil(groups, 256)) * (1.25 * double(each) + 4.0);
             else if (groups <= 256)
-                us = 0.25 * double(each) + 3.0;
+                us = 0.5 * double(each) + 3.0;
             else
-                us = double(ffn_ceil(groups, 512)) * (0.4 * double(each) + 3.0);
+                us = double(ffn_ceil(groups, 512)) * (0.8 * double(each) + 3.0);
             if (s > 1) us += 3.0 + double(M) * double(N) * batch * (8.0 * double(s) + 2.0) / 4.0e6;
             if (best.tiles_m == 0 || us < best.us) {
                 best.big = b != 0;
