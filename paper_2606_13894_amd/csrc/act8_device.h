@@ -147,7 +147,7 @@ __device__ __forceinline__ uint32_t act8_pack(float a, float b, float c, float d
 // Code j (0..3) of four packed ones, as float32.
 __device__ __forceinline__ float act8_value(uint32_t w, int j)
 {
-    return static_cast<float>(static_cast<int32_t>(w << (24 - 8 * j)) >> 24);
+    return static_cast<float>(static_cast<int8_t>(w >> (8 * j)));
 }
 
 // Largest over the eight lanes of an aligned run of eight.

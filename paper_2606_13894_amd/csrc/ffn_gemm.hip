@@ -38,13 +38,13 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) uint16_t lds_u16;
 
 constexpr int BK = 64;                    // k of a stage: 128 bytes of a row
-constexpr int NI = 4;                     // 32-column blocks of a wave (128 columns)
+constexpr int NJ = 4;                     // 16-column blocks of a wave in each half of B
 constexpr uint32_t kOut = 0x80000000u;    // a vector offset past every resource's range
 
 template <bool BIG>
@@ -52,7 +52,7 @@ struct Shape {
     static constexpr int kWaves = BIG ? 8 : 4;
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int T = BIG ? 256 : 128;       // tile rows and columns
-    static constexpr int MI = BIG ? 2 : 1;          // 32-row blocks of a wave
+    static constexpr int MI = BIG ? 4 : 2;          // 16-row blocks of a wave
 };
 
 // The permutation of a row's eight 16-byte pieces of k: a fragment read takes 16 rows at a time,
@@ -60,14 +60,14 @@ struct Shape {
 // half of the read cycles were conflicts.)
 __device__ __forceinline__ int chunk_key(int row) { return (row >> 1) & 7; }
 
-// The permutation of a row of k's 32-byte pieces (WIDE / 16 of them): distinct for four
-// consecutive rows within 128 bytes of banks, and within 256 for two neighbouring pieces of each.
-// (Rows of 64 elements alternate between the halves of 256 bytes by themselves.)
+// The permutation of a row of k's 32-byte pieces (WIDE / 16 of them): a transposing read takes
+// four consecutive rows, and those eight further on, which are to lie in distinct 32 bytes of
+// 256 bytes of banks. (Rows of 64 elements alternate between its halves by themselves.)
 template <int WIDE>
 __device__ __forceinline__ int piece_key(int row)
 {
     static_assert(WIDE >= 64, "four pieces");
-    return WIDE == 64 ? row & 3 : (row & 3) | ((row & 1) << 2);
+    return WIDE == 64 ? ((row >> 1) & 1) | ((row >> 2) & 2) : (row & 3) | ((row >> 1) & 4);
 }
 
 // Where a lane's 16 bytes of its wave's N loads of 1 KiB come from, in bytes from the stage's
@@ -115,21 +115,24 @@ __device__ __forceinline__ bool decode_work(const FfnGemm& g, Work& w)
     return true;
 }
 
-// A 32 x 32 accumulator block to runs: lane l of half h holds v[0..15] = columns 16 h + 0..15
-// of row l % 32. (Element 4 q + i of a lane is column 8 q + 4 h + i.) The two lanes of a row
-// exchange elements: both are to be active.
-__device__ __forceinline__ void to_run(const f32x16& acc, float (&v)[16])
+// Four 16 x 16 accumulator blocks side by side to runs: lane l, q = l / 16, holds element i of
+// column 16 j + 4 q + i of row l % 16 as acc[j][i], and gets columns 16 q + 0..15 of the same row
+// as v. The four lanes of a row exchange elements: all are to be active.
+__device__ __forceinline__ void to_run(const f32x4 (&acc)[NJ], float (&v)[16])
 {
 #pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const auto s = __builtin_amdgcn_permlane32_swap(
-                __float_as_uint(acc[4 * q + i]), __float_as_uint(acc[4 * (q + 2) + i]), false,
-                false);
-            v[8 * q + i] = __uint_as_float(s[0]);
-            v[8 * q + 4 + i] = __uint_as_float(s[1]);
-        }
+    for (int i = 0; i < 4; ++i) {
+        const auto e = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[0][i]),
+                                                        __float_as_uint(acc[2][i]), false, false);
+        const auto o = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[1][i]),
+                                                        __float_as_uint(acc[3][i]), false, false);
+        const auto lo = __builtin_amdgcn_permlane16_swap(e[0], o[0], false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(e[1], o[1], false, false);
+        v[i] = __uint_as_float(lo[0]);
+        v[4 + i] = __uint_as_float(lo[1]);
+        v[8 + i] = __uint_as_float(hi[0]);
+        v[12 + i] = __uint_as_float(hi[1]);
+    }
 }
 
 // Sixteen consecutive elements of a row of n, from column c on, rounded to bfloat16.
@@ -147,7 +150,11 @@ __device__ __forceinline__ void store_run(uint16_t* __restrict__ row, int64_t c,
 // The activation a = act(g) and its derivative; both from one logistic p = 1 / (1 + e^-z):
 // silu: a = g p, a' = p + a (1 - p);  gelu in its tanh form, (1 + tanh z) / 2 = the logistic
 // of 2 z: a = g p, a' = p + a (1 - p) z', with z = 2 sqrt(2 / pi) (g + 0.044715 g^3).
-__device__ __forceinline__ float logistic(float z) { return 1.0f / (1.0f + __expf(-z)); }
+// (The reciprocal is the hardware's, within one unit in the last place.)
+__device__ __forceinline__ float logistic(float z)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+}
 
 template <bool SLOPE>
 __device__ __forceinline__ float activation(float g, int act, float& slope)
@@ -164,39 +171,34 @@ __device__ __forceinline__ float activation(float g, int act, float& slope)
     return a;
 }
 
-// Sixteen codes of a run and, once a group, its exponent. v2: the wave's other run of the same
-// rows (a lane and its partner in the other half hold a group of 64 between them).
-__device__ __forceinline__ void write_codes(const float (&v0)[16], const float (&v1)[16],
-                                            int64_t c0, int64_t n, int half,
+// The codes of a run and, once a group, its exponent: the four lanes of a row hold a group of 64,
+// from column c - 16 q on.
+__device__ __forceinline__ void write_codes(const float (&v)[16], int64_t c, int64_t n, int q,
                                             int8_t* __restrict__ codes, uint8_t* __restrict__ exps,
                                             bool on)
 {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, max(abs_bits(v0[i]), abs_bits(v1[i])));
+    for (int i = 0; i < 16; ++i) top = max(top, abs_bits(v[i]));
+    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 16)));
     top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32)));
     const int ex = act8_exponent(top);
     const float inv = act8_inverse(ex);
     if (!on) return;
+    u32x4a w = {0u, 0u, 0u, 0u};
+    if (ex != 255) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const float* v = b ? v1 : v0;
-        const int64_t c = c0 + 32 * b + 16 * half;
-        u32x4a w = {0u, 0u, 0u, 0u};
-        if (ex != 255) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                w[q] = act8_pack(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], inv);
-        }
-        if (c + 16 <= n) {
-            store16(codes + c, w);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (c + i < n) codes[c + i] = static_cast<int8_t>(w[i >> 2] >> (8 * (i & 3)));
-        }
+        for (int k = 0; k < 4; ++k)
+            w[k] = act8_pack(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3], inv);
     }
-    if (half == 0 && c0 < n) exps[c0 >> 6] = static_cast<uint8_t>(ex);
+    if (c + 16 <= n) {
+        store16(codes + c, w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (c + i < n) codes[c + i] = static_cast<int8_t>(w[i >> 2] >> (8 * (i & 3)));
+    }
+    if (q == 0 && c < n) exps[c >> 6] = static_cast<uint8_t>(ex);
 }
 
 __device__ __forceinline__ u32x4a read_codes(const int8_t* __restrict__ row, int64_t c, int64_t n)
@@ -209,68 +211,67 @@ __device__ __forceinline__ u32x4a read_codes(const int8_t* __restrict__ row, int
     return w;
 }
 
-// Fragments of a stage's four 16-deep steps from rows of k, of 32-wide blocks at the byte
-// addresses p[]: eight transposing reads each, of four rows of k; first A's blocks (rows of SA
-// bytes), then two of B's (rows of SB bytes). One block with its own wait, so that the compiler
+// Fragments of a stage's two 32-deep steps from rows of k, of 16-wide blocks at the byte
+// addresses p[]: four transposing reads each, of four rows of k; first A's blocks (rows of SA
+// bytes), then four of B's (rows of SB bytes). One block with its own wait, so that the compiler
 // neither uses nor reuses a register that is still to be written. (It would wait for every load
 // to LDS in flight before this instruction's builtin, whatever buffer that is for.)
 template <int SA, int SB>
-__device__ __forceinline__ void read_t(const uint32_t (&p)[2], u32x2a (&o)[16])
+__device__ __forceinline__ void read_t(const uint32_t (&p)[4], u32x2a (&o)[16])
 {
     asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
                  "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[b1]\n\t"
                  "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[b2]\n\t"
                  "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[b3]\n\t"
-                 "ds_read_b64_tr_b16 %[o4], %[p0] offset:%[b4]\n\t"
-                 "ds_read_b64_tr_b16 %[o5], %[p0] offset:%[b5]\n\t"
-                 "ds_read_b64_tr_b16 %[o6], %[p0] offset:%[b6]\n\t"
-                 "ds_read_b64_tr_b16 %[o7], %[p0] offset:%[b7]\n\t"
-                 "ds_read_b64_tr_b16 %[o8], %[p1]\n\t"
-                 "ds_read_b64_tr_b16 %[o9], %[p1] offset:%[b1]\n\t"
-                 "ds_read_b64_tr_b16 %[o10], %[p1] offset:%[b2]\n\t"
-                 "ds_read_b64_tr_b16 %[o11], %[p1] offset:%[b3]\n\t"
-                 "ds_read_b64_tr_b16 %[o12], %[p1] offset:%[b4]\n\t"
-                 "ds_read_b64_tr_b16 %[o13], %[p1] offset:%[b5]\n\t"
-                 "ds_read_b64_tr_b16 %[o14], %[p1] offset:%[b6]\n\t"
-                 "ds_read_b64_tr_b16 %[o15], %[p1] offset:%[b7]\n\t"
+                 "ds_read_b64_tr_b16 %[o4], %[p1]\n\t"
+                 "ds_read_b64_tr_b16 %[o5], %[p1] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o6], %[p1] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o7], %[p1] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o8], %[p2]\n\t"
+                 "ds_read_b64_tr_b16 %[o9], %[p2] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o10], %[p2] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o11], %[p2] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o12], %[p3]\n\t"
+                 "ds_read_b64_tr_b16 %[o13], %[p3] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o14], %[p3] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o15], %[p3] offset:%[b3]\n\t"
                  "s_waitcnt lgkmcnt(0)"
                  : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
                    "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
                    "=&v"(o[8]), [o9] "=&v"(o[9]), [o10] "=&v"(o[10]), [o11] "=&v"(o[11]), [o12]
                    "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15])
-                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [b1] "n"(4 * SB), [b2] "n"(16 * SB), [b3]
-                   "n"(20 * SB), [b4] "n"(32 * SB), [b5] "n"(36 * SB), [b6] "n"(48 * SB), [b7]
-                   "n"(52 * SB)
+                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [b1] "n"(4 *
+                   SB), [b2] "n"(32 * SB), [b3] "n"(36 * SB)
                  : "memory");
 }
 
 template <int SA, int SB>
-__device__ __forceinline__ void read_t(const uint32_t (&p)[3], u32x2a (&o)[24])
+__device__ __forceinline__ void read_t(const uint32_t (&p)[6], u32x2a (&o)[24])
 {
     asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
                  "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[a1]\n\t"
                  "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[a2]\n\t"
                  "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[a3]\n\t"
-                 "ds_read_b64_tr_b16 %[o4], %[p0] offset:%[a4]\n\t"
-                 "ds_read_b64_tr_b16 %[o5], %[p0] offset:%[a5]\n\t"
-                 "ds_read_b64_tr_b16 %[o6], %[p0] offset:%[a6]\n\t"
-                 "ds_read_b64_tr_b16 %[o7], %[p0] offset:%[a7]\n\t"
-                 "ds_read_b64_tr_b16 %[o8], %[p1]\n\t"
-                 "ds_read_b64_tr_b16 %[o9], %[p1] offset:%[b1]\n\t"
-                 "ds_read_b64_tr_b16 %[o10], %[p1] offset:%[b2]\n\t"
-                 "ds_read_b64_tr_b16 %[o11], %[p1] offset:%[b3]\n\t"
-                 "ds_read_b64_tr_b16 %[o12], %[p1] offset:%[b4]\n\t"
-                 "ds_read_b64_tr_b16 %[o13], %[p1] offset:%[b5]\n\t"
-                 "ds_read_b64_tr_b16 %[o14], %[p1] offset:%[b6]\n\t"
-                 "ds_read_b64_tr_b16 %[o15], %[p1] offset:%[b7]\n\t"
-                 "ds_read_b64_tr_b16 %[o16], %[p2]\n\t"
-                 "ds_read_b64_tr_b16 %[o17], %[p2] offset:%[b1]\n\t"
-                 "ds_read_b64_tr_b16 %[o18], %[p2] offset:%[b2]\n\t"
-                 "ds_read_b64_tr_b16 %[o19], %[p2] offset:%[b3]\n\t"
-                 "ds_read_b64_tr_b16 %[o20], %[p2] offset:%[b4]\n\t"
-                 "ds_read_b64_tr_b16 %[o21], %[p2] offset:%[b5]\n\t"
-                 "ds_read_b64_tr_b16 %[o22], %[p2] offset:%[b6]\n\t"
-                 "ds_read_b64_tr_b16 %[o23], %[p2] offset:%[b7]\n\t"
+                 "ds_read_b64_tr_b16 %[o4], %[p1]\n\t"
+                 "ds_read_b64_tr_b16 %[o5], %[p1] offset:%[a1]\n\t"
+                 "ds_read_b64_tr_b16 %[o6], %[p1] offset:%[a2]\n\t"
+                 "ds_read_b64_tr_b16 %[o7], %[p1] offset:%[a3]\n\t"
+                 "ds_read_b64_tr_b16 %[o8], %[p2]\n\t"
+                 "ds_read_b64_tr_b16 %[o9], %[p2] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o10], %[p2] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o11], %[p2] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o12], %[p3]\n\t"
+                 "ds_read_b64_tr_b16 %[o13], %[p3] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o14], %[p3] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o15], %[p3] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o16], %[p4]\n\t"
+                 "ds_read_b64_tr_b16 %[o17], %[p4] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o18], %[p4] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o19], %[p4] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o20], %[p5]\n\t"
+                 "ds_read_b64_tr_b16 %[o21], %[p5] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o22], %[p5] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o23], %[p5] offset:%[b3]\n\t"
                  "s_waitcnt lgkmcnt(0)"
                  : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
                    "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
@@ -278,48 +279,47 @@ __device__ __forceinline__ void read_t(const uint32_t (&p)[3], u32x2a (&o)[24])
                    "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15]), [o16]
                    "=&v"(o[16]), [o17] "=&v"(o[17]), [o18] "=&v"(o[18]), [o19] "=&v"(o[19]), [o20]
                    "=&v"(o[20]), [o21] "=&v"(o[21]), [o22] "=&v"(o[22]), [o23] "=&v"(o[23])
-                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [a1] "n"(4 * SA), [a2] "n"(16 *
-                   SA), [a3] "n"(20 * SA), [a4] "n"(32 * SA), [a5] "n"(36 * SA), [a6] "n"(48 *
-                   SA), [a7] "n"(52 * SA), [b1] "n"(4 * SB), [b2] "n"(16 * SB), [b3] "n"(20 * SB),
-                   [b4] "n"(32 * SB), [b5] "n"(36 * SB), [b6] "n"(48 * SB), [b7] "n"(52 * SB)
+                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [p4] "v"(p[4]),
+                   [p5] "v"(p[5]), [a1] "n"(4 * SA), [a2] "n"(32 * SA), [a3] "n"(36 * SA), [b1]
+                   "n"(4 * SB), [b2] "n"(32 * SB), [b3] "n"(36 * SB)
                  : "memory");
 }
 
 template <int SA, int SB>
-__device__ __forceinline__ void read_t(const uint32_t (&p)[4], u32x2a (&o)[32])
+__device__ __forceinline__ void read_t(const uint32_t (&p)[8], u32x2a (&o)[32])
 {
     asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
                  "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[a1]\n\t"
                  "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[a2]\n\t"
                  "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[a3]\n\t"
-                 "ds_read_b64_tr_b16 %[o4], %[p0] offset:%[a4]\n\t"
-                 "ds_read_b64_tr_b16 %[o5], %[p0] offset:%[a5]\n\t"
-                 "ds_read_b64_tr_b16 %[o6], %[p0] offset:%[a6]\n\t"
-                 "ds_read_b64_tr_b16 %[o7], %[p0] offset:%[a7]\n\t"
-                 "ds_read_b64_tr_b16 %[o8], %[p1]\n\t"
-                 "ds_read_b64_tr_b16 %[o9], %[p1] offset:%[a1]\n\t"
-                 "ds_read_b64_tr_b16 %[o10], %[p1] offset:%[a2]\n\t"
-                 "ds_read_b64_tr_b16 %[o11], %[p1] offset:%[a3]\n\t"
-                 "ds_read_b64_tr_b16 %[o12], %[p1] offset:%[a4]\n\t"
-                 "ds_read_b64_tr_b16 %[o13], %[p1] offset:%[a5]\n\t"
-                 "ds_read_b64_tr_b16 %[o14], %[p1] offset:%[a6]\n\t"
-                 "ds_read_b64_tr_b16 %[o15], %[p1] offset:%[a7]\n\t"
-                 "ds_read_b64_tr_b16 %[o16], %[p2]\n\t"
-                 "ds_read_b64_tr_b16 %[o17], %[p2] offset:%[b1]\n\t"
-                 "ds_read_b64_tr_b16 %[o18], %[p2] offset:%[b2]\n\t"
-                 "ds_read_b64_tr_b16 %[o19], %[p2] offset:%[b3]\n\t"
-                 "ds_read_b64_tr_b16 %[o20], %[p2] offset:%[b4]\n\t"
-                 "ds_read_b64_tr_b16 %[o21], %[p2] offset:%[b5]\n\t"
-                 "ds_read_b64_tr_b16 %[o22], %[p2] offset:%[b6]\n\t"
-                 "ds_read_b64_tr_b16 %[o23], %[p2] offset:%[b7]\n\t"
-                 "ds_read_b64_tr_b16 %[o24], %[p3]\n\t"
-                 "ds_read_b64_tr_b16 %[o25], %[p3] offset:%[b1]\n\t"
-                 "ds_read_b64_tr_b16 %[o26], %[p3] offset:%[b2]\n\t"
-                 "ds_read_b64_tr_b16 %[o27], %[p3] offset:%[b3]\n\t"
-                 "ds_read_b64_tr_b16 %[o28], %[p3] offset:%[b4]\n\t"
-                 "ds_read_b64_tr_b16 %[o29], %[p3] offset:%[b5]\n\t"
-                 "ds_read_b64_tr_b16 %[o30], %[p3] offset:%[b6]\n\t"
-                 "ds_read_b64_tr_b16 %[o31], %[p3] offset:%[b7]\n\t"
+                 "ds_read_b64_tr_b16 %[o4], %[p1]\n\t"
+                 "ds_read_b64_tr_b16 %[o5], %[p1] offset:%[a1]\n\t"
+                 "ds_read_b64_tr_b16 %[o6], %[p1] offset:%[a2]\n\t"
+                 "ds_read_b64_tr_b16 %[o7], %[p1] offset:%[a3]\n\t"
+                 "ds_read_b64_tr_b16 %[o8], %[p2]\n\t"
+                 "ds_read_b64_tr_b16 %[o9], %[p2] offset:%[a1]\n\t"
+                 "ds_read_b64_tr_b16 %[o10], %[p2] offset:%[a2]\n\t"
+                 "ds_read_b64_tr_b16 %[o11], %[p2] offset:%[a3]\n\t"
+                 "ds_read_b64_tr_b16 %[o12], %[p3]\n\t"
+                 "ds_read_b64_tr_b16 %[o13], %[p3] offset:%[a1]\n\t"
+                 "ds_read_b64_tr_b16 %[o14], %[p3] offset:%[a2]\n\t"
+                 "ds_read_b64_tr_b16 %[o15], %[p3] offset:%[a3]\n\t"
+                 "ds_read_b64_tr_b16 %[o16], %[p4]\n\t"
+                 "ds_read_b64_tr_b16 %[o17], %[p4] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o18], %[p4] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o19], %[p4] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o20], %[p5]\n\t"
+                 "ds_read_b64_tr_b16 %[o21], %[p5] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o22], %[p5] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o23], %[p5] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o24], %[p6]\n\t"
+                 "ds_read_b64_tr_b16 %[o25], %[p6] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o26], %[p6] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o27], %[p6] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o28], %[p7]\n\t"
+                 "ds_read_b64_tr_b16 %[o29], %[p7] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o30], %[p7] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o31], %[p7] offset:%[b3]\n\t"
                  "s_waitcnt lgkmcnt(0)"
                  : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
                    "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
@@ -329,11 +329,9 @@ __device__ __forceinline__ void read_t(const uint32_t (&p)[4], u32x2a (&o)[32])
                    "=&v"(o[20]), [o21] "=&v"(o[21]), [o22] "=&v"(o[22]), [o23] "=&v"(o[23]), [o24]
                    "=&v"(o[24]), [o25] "=&v"(o[25]), [o26] "=&v"(o[26]), [o27] "=&v"(o[27]), [o28]
                    "=&v"(o[28]), [o29] "=&v"(o[29]), [o30] "=&v"(o[30]), [o31] "=&v"(o[31])
-                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [a1] "n"(4 *
-                   SA), [a2] "n"(16 * SA), [a3] "n"(20 * SA), [a4] "n"(32 * SA), [a5] "n"(36 *
-                   SA), [a6] "n"(48 * SA), [a7] "n"(52 * SA), [b1] "n"(4 * SB), [b2] "n"(16 * SB),
-                   [b3] "n"(20 * SB), [b4] "n"(32 * SB), [b5] "n"(36 * SB), [b6] "n"(48 * SB),
-                   [b7] "n"(52 * SB)
+                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [p4] "v"(p[4]),
+                   [p5] "v"(p[5]), [p6] "v"(p[6]), [p7] "v"(p[7]), [a1] "n"(4 * SA), [a2] "n"(32 *
+                   SA), [a3] "n"(36 * SA), [b1] "n"(4 * SB), [b2] "n"(32 * SB), [b3] "n"(36 * SB)
                  : "memory");
 }
 
@@ -447,52 +445,52 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
         advance(at, b_next[h], BKM ? BK : int64_t(BK) * g.ldb);
     };
 
-    // Fragments of four 16-deep steps: lane l holds row l % 32, k = 8 (l / 32) .. + 7.
-    const int half = lane >> 5, l32 = lane & 31;
-    bf16x8 fa[4][MI], fb[4][2];
+    // Fragments of two 32-deep steps: lane l holds row l % 16, k = 8 (l / 16) .. + 7.
+    const int q = lane >> 4, l16 = lane & 15;
+    bf16x8 fa[2][MI], fb[2][NJ];
     auto frag_k = [&](const uint16_t* t, int row, int ks) -> bf16x8 {
-        const int chunk = (2 * ks + half) ^ chunk_key(l32);
-        return *reinterpret_cast<const bf16x8*>(t + (row + l32) * BK + chunk * 8);
+        const int chunk = (4 * ks + q) ^ chunk_key(l16);
+        return *reinterpret_cast<const bf16x8*>(t + (row + l16) * BK + chunk * 8);
     };
     // Rows of k: byte address of the lane's 8 bytes of the first four rows.
-    const int trow = 8 * half + ((lane >> 2) & 3);
+    const int trow = 8 * q + (l16 >> 2);
     auto addr_t = [&](const uint16_t* t, auto width, int col) -> uint32_t {
         constexpr int wide = decltype(width)::value;
-        const int piece = ((col >> 4) + ((lane >> 4) & 1)) ^ piece_key<wide>((lane >> 2) & 3);
+        const int piece = (col >> 4) ^ piece_key<wide>(trow);
         return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
                    (lds_u16*)(t + trow * wide + piece * 16 + (lane & 3) * 4)));
     };
-    // All of A's with B's first half, or B's second half.
     typedef std::integral_constant<int, T> WideA;
     typedef std::integral_constant<int, H> WideB;
+    // All of A's with B's first half, or B's second half.
     auto frags = [&](const Tiles& t, auto part) {
         constexpr int h = decltype(part)::value;
         constexpr int NA = AK || h ? 0 : MI;
         const uint16_t* sb = t.b[h];
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
+        for (int ks = 0; ks < 2; ++ks) {
             if constexpr (AK && h == 0) {
 #pragma unroll
-                for (int mi = 0; mi < MI; ++mi) fa[ks][mi] = frag_k(t.a, (wm * MI + mi) * 32, ks);
+                for (int mi = 0; mi < MI; ++mi) fa[ks][mi] = frag_k(t.a, (wm * MI + mi) * 16, ks);
             }
             if constexpr (BKM) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) fb[ks][j] = frag_k(sb, wn * 64 + j * 32, ks);
+                for (int j = 0; j < NJ; ++j) fb[ks][j] = frag_k(sb, wn * 64 + j * 16, ks);
             }
         }
         if constexpr (!BKM) {   // rows of k: B, and A with it
-            uint32_t at[NA + 2];
-            u32x2a o[8 * (NA + 2)];
+            uint32_t at[NA + NJ];
+            u32x2a o[4 * (NA + NJ)];
 #pragma unroll
-            for (int i = 0; i < NA + 2; ++i)
-                at[i] = i < NA ? addr_t(t.a, WideA{}, (wm * MI + i) * 32)
-                               : addr_t(sb, WideB{}, wn * 64 + (i - NA) * 32);
+            for (int i = 0; i < NA + NJ; ++i)
+                at[i] = i < NA ? addr_t(t.a, WideA{}, (wm * MI + i) * 16)
+                               : addr_t(sb, WideB{}, wn * 64 + (i - NA) * 16);
             read_t<2 * T, 2 * H>(at, o);
 #pragma unroll
-            for (int i = 0; i < NA + 2; ++i)
+            for (int i = 0; i < NA + NJ; ++i)
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks) {
-                    const bf16x8 f = join(o[8 * i + 2 * ks], o[8 * i + 2 * ks + 1]);
+                for (int ks = 0; ks < 2; ++ks) {
+                    const bf16x8 f = join(o[4 * i + 2 * ks], o[4 * i + 2 * ks + 1]);
                     if (i < NA) fa[ks][i] = f;
                     else fb[ks][i - NA] = f;
                 }
@@ -500,23 +498,23 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
         __builtin_amdgcn_sched_barrier(0);
     };
     static_assert(AK || !BKM, "an A of rows of k goes with such a B");
-    f32x16 acc[MI][NI];
+    f32x4 acc[MI][2][NJ];
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-        for (int ni = 0; ni < NI; ++ni)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) acc[mi][ni][v] = 0.0f;
+            for (int j = 0; j < NJ; ++j) acc[mi][h][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     auto mfmas = [&](auto part) {
         constexpr int h = decltype(part)::value;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
+        for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    acc[mi][2 * h + j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        fb[ks][j], fa[ks][mi], acc[mi][2 * h + j], 0, 0, 0);
+                for (int j = 0; j < NJ; ++j)
+                    acc[mi][h][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        fb[ks][j], fa[ks][mi], acc[mi][h][j], 0, 0, 0);
     };
     auto barrier = [&]() {
         __builtin_amdgcn_sched_barrier(0);
@@ -588,79 +586,67 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
     // ------------------------------------------------------------------ epilogues
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
-        const int64_t row = row0 + (wm * MI + mi) * 32 + l32;
+        const int64_t row = row0 + (wm * MI + mi) * 16 + l16;
         const bool on = row < g.M;
         if constexpr (KIND == kFfnGateUp) {
-            const int64_t c = col0 + wn * 64;
-            float gv[2][16], uv[2][16];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                to_run(acc[mi][b], gv[b]);
-                to_run(acc[mi][2 + b], uv[b]);
-            }
+            const int64_t c = col0 + wn * 64 + 16 * q;
+            float gv[16], uv[16];
+            to_run(acc[mi][0], gv);
+            to_run(acc[mi][1], uv);
             if (g.gcodes) {
-                write_codes(gv[0], gv[1], c, g.N, half, g.gcodes + row * g.N,
-                            g.gexps + row * g.groups, on);
-                write_codes(uv[0], uv[1], c, g.N, half, g.ucodes + row * g.N,
-                            g.uexps + row * g.groups, on);
+                write_codes(gv, c, g.N, q, g.gcodes + row * g.N, g.gexps + row * g.groups, on);
+                write_codes(uv, c, g.N, q, g.ucodes + row * g.N, g.uexps + row * g.groups, on);
             }
-            if (on) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    float av[16], none;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        av[i] = activation<false>(gv[b][i], g.act, none) * uv[b][i];
-                    // columns from N to ldo are read by the next product as zeros
-                    store_run(g.o[0] + row * g.ldo, c + 32 * b + 16 * half, g.ldo, av);
-                }
-            }
-        } else if constexpr (KIND == kFfnGateGrad) {
             if (!on) continue;
+            float none;
 #pragma unroll
-            for (int ni = 0; ni < NI; ++ni) {
-                const int64_t c = col0 + (ni >> 1) * H + wn * 64 + (ni & 1) * 32 + 16 * half;
-                float d[16], dg[16], du[16], av[16];
-                to_run(acc[mi][ni], d);   // both halves of the wave take part
-                if (c >= g.ldo) continue;
-                u32x4a gw = {0u, 0u, 0u, 0u}, uw = gw;
-                float gs = 0.0f, us = 0.0f;
-                if (c < g.N) {
-                    gw = read_codes(g.gcodes + row * g.N, c, g.N);
-                    uw = read_codes(g.ucodes + row * g.N, c, g.N);
-                    gs = act8_scale(g.gexps[row * g.groups + (c >> 6)]);
-                    us = act8_scale(g.uexps[row * g.groups + (c >> 6)]);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const bool in = c + i < g.N;
-                    const float gv = act8_value(gw[i >> 2], i & 3) * gs;
-                    const float uv = act8_value(uw[i >> 2], i & 3) * us;
-                    float slope;
-                    const float a = activation<true>(gv, g.act, slope);
-                    av[i] = in ? a * uv : 0.0f;
-                    dg[i] = in ? d[i] * uv * slope : 0.0f;
-                    du[i] = in ? d[i] * a : 0.0f;
-                }
-                store_run(g.o[0] + row * g.ldo, c, g.ldo, dg);
-                store_run(g.o[1] + row * g.ldo, c, g.ldo, du);
-                store_run(g.o2 + row * g.ldo, c, g.ldo, av);
-            }
+            for (int i = 0; i < 16; ++i) gv[i] = activation<false>(gv[i], g.act, none) * uv[i];
+            // columns from N to ldo are read by the next product as zeros
+            store_run(g.o[0] + row * g.ldo, c, g.ldo, gv);
         } else {
             if (!on) continue;
 #pragma unroll
-            for (int ni = 0; ni < NI; ++ni) {
-                const int64_t c = col0 + (ni >> 1) * H + wn * 64 + (ni & 1) * 32 + 16 * half;
+            for (int h = 0; h < 2; ++h) {
+                const int64_t c = col0 + h * H + wn * 64 + 16 * q;
                 float v[16];
-                to_run(acc[mi][ni], v);
-                if (g.partial) {
+                to_run(acc[mi][h], v);   // all four lanes of the row take part
+                if constexpr (KIND == kFfnGateGrad) {
+                    if (c >= g.ldo) continue;
+                    u32x4a gw = {0u, 0u, 0u, 0u}, uw = gw;
+                    float gs = 0.0f, us = 0.0f;
+                    if (c < g.N) {
+                        gw = read_codes(g.gcodes + row * g.N, c, g.N);
+                        uw = read_codes(g.ucodes + row * g.N, c, g.N);
+                        gs = act8_scale(g.gexps[row * g.groups + (c >> 6)]);
+                        us = act8_scale(g.uexps[row * g.groups + (c >> 6)]);
+                    }
+                    float dg[16], av[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float gv = act8_value(gw[i >> 2], i & 3) * gs;
+                        const float uv = act8_value(uw[i >> 2], i & 3) * us;
+                        float slope;
+                        const float a = activation<true>(gv, g.act, slope);
+                        av[i] = a * uv;
+                        dg[i] = v[i] * uv * slope;
+                        v[i] *= a;
+                    }
+                    if (c + 16 > g.N) {   // columns from N to ldo are read as zeros
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (c + i >= g.N) av[i] = dg[i] = v[i] = 0.0f;
+                    }
+                    store_run(g.o[0] + row * g.ldo, c, g.ldo, dg);
+                    store_run(g.o[1] + row * g.ldo, c, g.ldo, v);
+                    store_run(g.o2 + row * g.ldo, c, g.ldo, av);
+                } else if (g.partial) {
                     float* __restrict__ p =
                         g.partial + ((int64_t(w.split) * g.batch + w.batch) * g.M + row) * g.N;
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const float* s = v + 8 * q;
+                    for (int b = 0; b < 2; ++b) {
+                        const float* s = v + 8 * b;
                         const float x[8] = {s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]};
-                        store_row8<false>(p, c + 8 * q, g.N, x);
+                        store_row8<false>(p, c + 8 * b, g.N, x);
                     }
                 } else {
                     if (g.col_scale) {
