@@ -135,7 +135,9 @@ __device__ __forceinline__ void to_run(const f32x4 (&acc)[NJ], float (&v)[16])
     }
 }
 
-// Sixteen consecutive elements of a row of n, from column c on, rounded to bfloat16.
+// Sixteen consecutive elements of a row of n, from column c on, rounded to bfloat16. FULL: they
+// are all there (in each of these functions).
+template <bool FULL>
 __device__ __forceinline__ void store_run(uint16_t* __restrict__ row, int64_t c, int64_t n,
                                           const float (&v)[16])
 {
@@ -143,7 +145,7 @@ __device__ __forceinline__ void store_run(uint16_t* __restrict__ row, int64_t c,
     for (int half = 0; half < 2; ++half) {
         const float* p = v + 8 * half;
         const float w[8] = {p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]};
-        store_row8<true>(row, c + 8 * half, n, w);
+        store_row8<true>(row, c + 8 * half, FULL ? c + 8 * half + 8 : n, w);
     }
 }
 
@@ -156,14 +158,14 @@ __device__ __forceinline__ float logistic(float z)
     return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
 }
 
-template <bool SLOPE>
-__device__ __forceinline__ float activation(float g, int act, float& slope)
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ float activation(float g, float& slope)
 {
     float z = g, dz = 1.0f;
-    if (act == kActGelu) {
-        const float q = g * g;
-        z = 1.5957691216057308f * g * fmaf(0.044715f, q, 1.0f);
-        if (SLOPE) dz = 1.5957691216057308f * fmaf(0.134145f, q, 1.0f);
+    if (ACT == kActGelu) {
+        const float s = g * g;
+        z = 1.5957691216057308f * g * fmaf(0.044715f, s, 1.0f);
+        if (SLOPE) dz = 1.5957691216057308f * fmaf(0.134145f, s, 1.0f);
     }
     const float p = logistic(z);
     const float a = g * p;
@@ -173,6 +175,7 @@ __device__ __forceinline__ float activation(float g, int act, float& slope)
 
 // The codes of a run and, once a group, its exponent: the four lanes of a row hold a group of 64,
 // from column c - 16 q on.
+template <bool FULL>
 __device__ __forceinline__ void write_codes(const float (&v)[16], int64_t c, int64_t n, int q,
                                             int8_t* __restrict__ codes, uint8_t* __restrict__ exps,
                                             bool on)
@@ -184,26 +187,27 @@ __device__ __forceinline__ void write_codes(const float (&v)[16], int64_t c, int
     top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32)));
     const int ex = act8_exponent(top);
     const float inv = act8_inverse(ex);
-    if (!on) return;
+    if (!FULL && !on) return;
     u32x4a w = {0u, 0u, 0u, 0u};
     if (ex != 255) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             w[k] = act8_pack(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3], inv);
     }
-    if (c + 16 <= n) {
+    if (FULL || c + 16 <= n) {
         store16(codes + c, w);
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (c + i < n) codes[c + i] = static_cast<int8_t>(w[i >> 2] >> (8 * (i & 3)));
     }
-    if (q == 0 && c < n) exps[c >> 6] = static_cast<uint8_t>(ex);
+    if (q == 0 && (FULL || c < n)) exps[c >> 6] = static_cast<uint8_t>(ex);
 }
 
+template <bool FULL>
 __device__ __forceinline__ u32x4a read_codes(const int8_t* __restrict__ row, int64_t c, int64_t n)
 {
-    if (c + 16 <= n) return load16(row + c);
+    if (FULL || c + 16 <= n) return load16(row + c);
     u32x4a w = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -584,80 +588,138 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
     }
 
     // ------------------------------------------------------------------ epilogues
+    // Tiles that lie wholly inside take a path without bounds.
+    auto gate_up = [&](auto whole, auto act) {
+        constexpr bool FULL = decltype(whole)::value;
+        constexpr int ACT = decltype(act)::value;
+        const int64_t c = col0 + wn * 64 + 16 * q;
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) {
-        const int64_t row = row0 + (wm * MI + mi) * 16 + l16;
-        const bool on = row < g.M;
-        if constexpr (KIND == kFfnGateUp) {
-            const int64_t c = col0 + wn * 64 + 16 * q;
+        for (int mi = 0; mi < MI; ++mi) {
+            const int64_t row = row0 + (wm * MI + mi) * 16 + l16;
+            const bool on = FULL || row < g.M;
             float gv[16], uv[16];
             to_run(acc[mi][0], gv);
             to_run(acc[mi][1], uv);
             if (g.gcodes) {
-                write_codes(gv, c, g.N, q, g.gcodes + row * g.N, g.gexps + row * g.groups, on);
-                write_codes(uv, c, g.N, q, g.ucodes + row * g.N, g.uexps + row * g.groups, on);
+                write_codes<FULL>(gv, c, g.N, q, g.gcodes + row * g.N, g.gexps + row * g.groups,
+                                  on);
+                write_codes<FULL>(uv, c, g.N, q, g.ucodes + row * g.N, g.uexps + row * g.groups,
+                                  on);
             }
             if (!on) continue;
             float none;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) gv[i] = activation<false>(gv[i], g.act, none) * uv[i];
+            for (int i = 0; i < 16; ++i) gv[i] = activation<ACT, false>(gv[i], none) * uv[i];
             // columns from N to ldo are read by the next product as zeros
-            store_run(g.o[0] + row * g.ldo, c, g.ldo, gv);
-        } else {
-            if (!on) continue;
+            store_run<FULL>(g.o[0] + row * g.ldo, c, g.ldo, gv);
+        }
+    };
+    auto gate_grad = [&](auto whole, auto act) {
+        constexpr bool FULL = decltype(whole)::value;
+        constexpr int ACT = decltype(act)::value;
+        // the next rows' codes are loaded while these are worked on
+        u32x4a gw[2][2], uw[2][2];
+        uint32_t ge[2][2], ue[2][2];
+        auto fetch = [&](int mi) {
+            const int64_t row = row0 + (wm * MI + mi) * 16 + l16;
+            const int s = mi & 1;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t c = col0 + h * H + wn * 64 + 16 * q;
+                gw[s][h] = uw[s][h] = u32x4a{0u, 0u, 0u, 0u};
+                ge[s][h] = ue[s][h] = 0;
+                if (FULL || (row < g.M && c < g.N)) {
+                    gw[s][h] = read_codes<FULL>(g.gcodes + row * g.N, c, g.N);
+                    uw[s][h] = read_codes<FULL>(g.ucodes + row * g.N, c, g.N);
+                    ge[s][h] = g.gexps[row * g.groups + (c >> 6)];
+                    ue[s][h] = g.uexps[row * g.groups + (c >> 6)];
+                }
+            }
+        };
+        fetch(0);
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            if (mi + 1 < MI) fetch(mi + 1);
+            const int64_t row = row0 + (wm * MI + mi) * 16 + l16;
+            const int s = mi & 1;
+            if (!FULL && row >= g.M) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t c = col0 + h * H + wn * 64 + 16 * q;
+                float v[16], dg[16], av[16];
+                to_run(acc[mi][h], v);   // all four lanes of the row take part
+                if (!FULL && c >= g.ldo) continue;
+                const float gs = act8_scale(ge[s][h]), us = act8_scale(ue[s][h]);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float gv = act8_value(gw[s][h][i >> 2], i & 3) * gs;
+                    const float uv = act8_value(uw[s][h][i >> 2], i & 3) * us;
+                    float slope;
+                    const float a = activation<ACT, true>(gv, slope);
+                    av[i] = a * uv;
+                    dg[i] = v[i] * uv * slope;
+                    v[i] *= a;
+                }
+                if (!FULL && c + 16 > g.N) {   // columns from N to ldo are read as zeros
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c + i >= g.N) av[i] = dg[i] = v[i] = 0.0f;
+                }
+                store_run<FULL>(g.o[0] + row * g.ldo, c, g.ldo, dg);
+                store_run<FULL>(g.o[1] + row * g.ldo, c, g.ldo, v);
+                store_run<FULL>(g.o2 + row * g.ldo, c, g.ldo, av);
+            }
+        }
+    };
+    auto plain = [&](auto whole) {
+        constexpr bool FULL = decltype(whole)::value;
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            const int64_t row = row0 + (wm * MI + mi) * 16 + l16;
+            if (!FULL && row >= g.M) continue;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t c = col0 + h * H + wn * 64 + 16 * q;
                 float v[16];
-                to_run(acc[mi][h], v);   // all four lanes of the row take part
-                if constexpr (KIND == kFfnGateGrad) {
-                    if (c >= g.ldo) continue;
-                    u32x4a gw = {0u, 0u, 0u, 0u}, uw = gw;
-                    float gs = 0.0f, us = 0.0f;
-                    if (c < g.N) {
-                        gw = read_codes(g.gcodes + row * g.N, c, g.N);
-                        uw = read_codes(g.ucodes + row * g.N, c, g.N);
-                        gs = act8_scale(g.gexps[row * g.groups + (c >> 6)]);
-                        us = act8_scale(g.uexps[row * g.groups + (c >> 6)]);
-                    }
-                    float dg[16], av[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float gv = act8_value(gw[i >> 2], i & 3) * gs;
-                        const float uv = act8_value(uw[i >> 2], i & 3) * us;
-                        float slope;
-                        const float a = activation<true>(gv, g.act, slope);
-                        av[i] = a * uv;
-                        dg[i] = v[i] * uv * slope;
-                        v[i] *= a;
-                    }
-                    if (c + 16 > g.N) {   // columns from N to ldo are read as zeros
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (c + i >= g.N) av[i] = dg[i] = v[i] = 0.0f;
-                    }
-                    store_run(g.o[0] + row * g.ldo, c, g.ldo, dg);
-                    store_run(g.o[1] + row * g.ldo, c, g.ldo, v);
-                    store_run(g.o2 + row * g.ldo, c, g.ldo, av);
-                } else if (g.partial) {
+                to_run(acc[mi][h], v);
+                if (g.partial) {
                     float* __restrict__ p =
                         g.partial + ((int64_t(w.split) * g.batch + w.batch) * g.M + row) * g.N;
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         const float* s = v + 8 * b;
                         const float x[8] = {s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]};
-                        store_row8<false>(p, c + 8 * b, g.N, x);
+                        store_row8<false>(p, c + 8 * b, FULL ? c + 8 * b + 8 : g.N, x);
                     }
                 } else {
                     if (g.col_scale) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            if (c + i < g.N) v[i] *= g.col_scale[c + i];
+                            if (FULL || c + i < g.N) v[i] *= g.col_scale[c + i];
                     }
-                    store_run(g.o[w.batch] + row * g.ldo, c, g.N, v);
+                    store_run<FULL>(g.o[w.batch] + row * g.ldo, c, g.N, v);
                 }
             }
         }
+    };
+    typedef std::integral_constant<bool, true> Whole;
+    typedef std::integral_constant<bool, false> Edge;
+    typedef std::integral_constant<int, kActSilu> Silu;
+    typedef std::integral_constant<int, kActGelu> Gelu;
+    const bool inside = row0 + T <= g.M && col0 + (DUAL ? H : T) <= g.N;
+    if constexpr (KIND == kFfnPlain) {
+        if (inside) plain(Whole{});
+        else plain(Edge{});
+    } else if constexpr (KIND == kFfnGateUp) {
+        if (inside && g.act == kActSilu) gate_up(Whole{}, Silu{});
+        else if (inside) gate_up(Whole{}, Gelu{});
+        else if (g.act == kActSilu) gate_up(Edge{}, Silu{});
+        else gate_up(Edge{}, Gelu{});
+    } else {
+        if (inside && g.act == kActSilu) gate_grad(Whole{}, Silu{});
+        else if (inside) gate_grad(Whole{}, Gelu{});
+        else if (g.act == kActSilu) gate_grad(Edge{}, Silu{});
+        else gate_grad(Edge{}, Gelu{});
     }
 }
 
