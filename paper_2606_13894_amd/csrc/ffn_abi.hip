@@ -249,6 +249,31 @@ int gefen_gated_ffn(const uint16_t* x, const uint16_t* w_gate, const uint16_t* w
     if (!T) return GEFEN_OK;
     if (!x || !w_gate || !w_up || !w_down || !y) return fail(GEFEN_EINVAL, "NULL argument");
     hipStream_t stream = as_stream(stream_);
+    if (T <= kFfnFewTokens && !gate_codes) {
+        if ((rc = check_space(workspace, workspace_bytes, 2 * T * F))) return rc;
+        FfnTokens t{};
+        t.x = x;
+        t.ldx = K;
+        t.w[0] = w_gate;
+        t.w[1] = w_up;
+        t.tokens = T;
+        t.N = F;
+        t.K = K;
+        t.act = activation;
+        t.o = static_cast<uint16_t*>(workspace);
+        t.ldo = F;
+        GEFEN_HIP(launch_ffn_tokens(t, stream));
+        t.x = t.o;
+        t.ldx = F;
+        t.w[0] = w_down;
+        t.w[1] = nullptr;
+        t.N = K;
+        t.K = F;
+        t.o = y;
+        t.ldo = K;
+        GEFEN_HIP(launch_ffn_tokens(t, stream));
+        return GEFEN_OK;
+    }
     const bool copy_k = K % 8 || !aligned16(x) || !aligned16(w_gate) || !aligned16(w_up);
     const bool copy_f = F % 8 || !aligned16(w_down);
     const FfnSpace s = ffn_space(T, K, F, false, copy_k, copy_f);

@@ -89,6 +89,20 @@ struct FfnGemm {
 };
 hipError_t launch_ffn_gemm(const FfnGemm& g, hipStream_t stream);
 
+// One forward product of a few tokens (ffn_tokens.hip): o[t][n] = sum_k x[t][k] w[n][k] over
+// dense rows of K, or act(G) U of two such products where w[1] is given.
+constexpr int64_t kFfnFewTokens = 16;
+struct FfnTokens {
+    const uint16_t* x;
+    int64_t ldx;
+    const uint16_t* w[2];
+    int64_t tokens, N, K;
+    int32_t act;
+    uint16_t* o;
+    int64_t ldo;
+};
+hipError_t launch_ffn_tokens(const FfnTokens& g, hipStream_t stream);
+
 struct FfnPad {
     const uint16_t* src;
     uint16_t* dst;
