@@ -21,11 +21,33 @@ struct FfnTile {
     double us = 0.0;
 };
 
+// What a tile does with its sums, by the time it takes beside the sum itself: a plain store, the
+// gate's activation and checkpoints, or the gate's gradients.
+enum FfnEpilogue : int { kFfnStore = 0, kFfnActivate = 1, kFfnGradient = 2 };
+
+// Estimated time in microseconds of `groups` workgroups that each sum `stages` stages, and of
+// their epilogues, fitted to measurements from 32 to 8192 rows. A stage's time grows with the
+// number of workgroups that load at once: 0.5 us for one small tile, 0.72 for one on every CU,
+// 1.2 for two on every CU; 1.0 to 1.5 us for a large one.
+inline double ffn_sum_us(bool big, int64_t groups, int64_t stages, FfnEpilogue epilogue)
+{
+    static const double small_end[3] = {5.0, 5.0, 14.0}, big_end[3] = {6.0, 9.0, 38.0};
+    const int64_t slots = big ? 256 : 512, full = groups / slots, rest = groups % slots;
+    const double end = big ? big_end[epilogue] : small_end[epilogue];
+    double us = double(full) * ((big ? 1.5 : 1.2) * double(stages) + end);
+    if (rest) {
+        const double load = double(std::min<int64_t>(rest, 256)) / 256.0;
+        const double stage = big ? 1.0 + 0.5 * load : rest > 256 ? 1.2 : 0.5 + 0.22 * load;
+        us += stage * double(stages) + end;
+    }
+    return us;
+}
+
 // The tile and split with the least estimated time for C (M x N, `batch` of them), summed over
 // `segments` of K. `halves`: the tile's columns are two matrices' (gate and up). `may_split`:
-// the sum may be cut into parts, joined by a second kernel.
+// the sum may be cut into parts, whose float32 results are written, and read by a second kernel.
 inline FfnTile ffn_choose(int64_t M, int64_t N, int64_t K, int batch, int segments, bool halves,
-                          bool may_split)
+                          bool may_split, FfnEpilogue epilogue)
 {
     FfnTile best;
     for (int b = 0; b < 2; ++b) {
@@ -34,16 +56,11 @@ inline FfnTile ffn_choose(int64_t M, int64_t N, int64_t K, int batch, int segmen
         const int64_t stages = ffn_ceil(K, kFfnDepth), all = stages * segments;
         for (int64_t s : {1, 2, 3, 4, 6, 8, 12, 16}) {
             if (s > 1 && (!may_split || all / s < 4)) break;
-            const int64_t groups = tm * tn * batch * s;
-            const int64_t each = ffn_ceil(all, s);
-            double us;
-            if (b)
-                us = double(ffn_ceil(groups, 256)) * (1.25 * double(each) + 4.0);
-            else if (groups <= 256)
-                us = 0.5 * double(each) + 3.0;
-            else
-                us = double(ffn_ceil(groups, 512)) * (0.8 * double(each) + 3.0);
-            if (s > 1) us += 3.0 + double(M) * double(N) * batch * (8.0 * double(s) + 2.0) / 4.0e6;
+            double us = ffn_sum_us(b != 0, tm * tn * batch * s, ffn_ceil(all, s), epilogue);
+            if (s > 1) {
+                const double mb = 4e-6 * double(M) * double(N) * batch * double(s);
+                us += 3.5 + mb / 4.0 + mb / 6.0;
+            }
             if (best.tiles_m == 0 || us < best.us) {
                 best.big = b != 0;
                 best.splits = static_cast<int32_t>(s);
@@ -93,17 +110,17 @@ inline FfnSpace ffn_space(int64_t T, int64_t K, int64_t F, bool backward, bool c
     if (copy_f) s.w_down = take(2 * K * F8);
     s.a = take(2 * T * F8);
     if (!backward) {
-        s.gate_up = ffn_choose(T, F, K, 1, 1, true, false);
-        s.down = ffn_choose(T, K, F, 1, 1, false, true);
+        s.gate_up = ffn_choose(T, F, K, 1, 1, true, false, kFfnActivate);
+        s.down = ffn_choose(T, K, F, 1, 1, false, true, kFfnStore);
         partial = ffn_partial_bytes(s.down, T, K, 1);
     } else {
         s.x = take(2 * T * K8);   // decoded, or copied
         s.dg = take(2 * T * F8);
         s.du = take(2 * T * F8);
-        s.grad_inner = ffn_choose(T, F, K, 1, 1, false, false);
-        s.dx = ffn_choose(T, K, F, 1, 2, false, true);
-        s.dw_down = ffn_choose(K, F, T, 1, 1, false, true);
-        s.dw_inner = ffn_choose(F, K, T, 2, 1, false, true);
+        s.grad_inner = ffn_choose(T, F, K, 1, 1, false, false, kFfnGradient);
+        s.dx = ffn_choose(T, K, F, 1, 2, false, true, kFfnStore);
+        s.dw_down = ffn_choose(K, F, T, 1, 1, false, true, kFfnStore);
+        s.dw_inner = ffn_choose(F, K, T, 2, 1, false, true, kFfnStore);
         partial = std::max({ffn_partial_bytes(s.dx, T, K, 1), ffn_partial_bytes(s.dw_down, K, F, 1),
                             ffn_partial_bytes(s.dw_inner, F, K, 2)});
     }
