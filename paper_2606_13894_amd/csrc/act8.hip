@@ -78,8 +78,8 @@ RowGrid row_grid(int64_t rows, int64_t vectors)
 constexpr int kNormThreads(int tpr) { return tpr < 256 ? 256 : tpr; }
 
 // The sum over the row's lanes, in every lane. All threads of the workgroup call it.
-template <int TPR>
-__device__ __forceinline__ float row_sum(float s, float* red)
+template <int TPR, typename F>
+__device__ __forceinline__ F row_sum(F s, F* red)
 {
 #pragma unroll
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
@@ -88,23 +88,36 @@ __device__ __forceinline__ float row_sum(float s, float* red)
         __syncthreads();   // the last row's sum has been read
         if ((threadIdx.x & 63) == 0) red[wave] = s;
         __syncthreads();
-        s = 0.0f;
+        s = red[0];
 #pragma unroll
-        for (int w = 0; w < TPR / 64; ++w) s += red[w];
+        for (int w = 1; w < TPR / 64; ++w) s += red[w];
     }
     return s;
 }
 
+// x^(-1/2): the float32 one with a Newton step in 64 bits. A mean square past float32's range
+// either way goes through the 64-bit functions.
+__device__ __forceinline__ double inverse_root(double x)
+{
+    const float f = static_cast<float>(x);
+    if (!(f > 1e-36f && f < 1e36f)) return 1.0 / sqrt(x);
+    const double r = static_cast<double>(__builtin_amdgcn_rsqf(f));
+    return r * fma(-0.5 * x * r, r, 1.5);
+}
+
+// The sum of squares and rstd are in 64 bits, and so are the products that the codes are rounded
+// from: a checkpoint's code is the formula's, whatever the order of the sum (the pass is bound by
+// memory: no time is lost).
 template <bool BF16, int TPR, int NV>
 __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm(const NormArgs a, int64_t groups)
 {
     constexpr int kRows = kNormThreads(TPR) / TPR;
     constexpr int kSize = BF16 ? 2 : 4;
-    __shared__ float red[TPR / 64];
+    __shared__ double red[TPR / 64];
     const int lane = threadIdx.x & (TPR - 1);
     const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
     const int cols = static_cast<int>(a.cols);
-    const float inv_n = 1.0f / static_cast<float>(cols);
+    const double inv_n = 1.0 / static_cast<double>(cols);
     float w[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) load_row8<false>(a.weight, (i * TPR + lane) * 8, cols, w[i]);
@@ -115,7 +128,7 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm(const NormArgs a
         const int n = on ? cols : 0;
         const int64_t at = on ? row * cols : 0;
         float v[NV][8];
-        float s = 0.0f;
+        double s = 0.0;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             load_row8<BF16>(static_cast<const char*>(a.x) + at * kSize, (i * TPR + lane) * 8, n,
@@ -133,31 +146,76 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm(const NormArgs a
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s = fmaf(v[i][j], v[i][j], s);
+            for (int j = 0; j < 8; ++j)
+                s = fma(static_cast<double>(v[i][j]), static_cast<double>(v[i][j]), s);
         s = row_sum<TPR>(s, red);
-        const float rstd = 1.0f / sqrtf(s * inv_n + a.eps);
+        const double rstd = inverse_root(fma(s, inv_n, a.eps));
+        const float rf = static_cast<float>(rstd);
         if (!on) continue;
-        if (lane == 0) a.rstd[row] = rstd;
+        if (lane == 0) a.rstd[row] = rf;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int e = (i * TPR + lane) * 8;
             if (a.h) store_row8<BF16>(static_cast<char*>(a.h) + at * kSize, e, n, v[i]);
-            float y[8];
+            float f[8], y[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                v[i][j] *= rstd;
-                y[j] = v[i][j] * w[i][j];
+                f[j] = static_cast<float>(static_cast<double>(v[i][j]) * rstd);
+                y[j] = f[j] * w[i][j];
             }
             store_row8<BF16>(static_cast<char*>(a.y) + at * kSize, e, n, y);
-            if (a.codes) act8_write_group(v[i], e, n, a.codes + at, a.exps + row * groups);
+            if (a.codes)
+                act8_write_products(v[i], rstd, f, e, n, a.codes + at, a.exps + row * groups);
         }
     }
 }
 
 // dn = dy w;  dx = rstd (dn - n mean(dn n)) + dh;  dw = the sum over rows of dy n. A workgroup
 // keeps its rows' share of dw in registers and writes it once; k_norm_dw adds the shares in
-// order, so that dw does not depend on timing.
-template <bool BF16, int TPR, int NV>
+// order, so that dw does not depend on timing. The next row's vectors are on their way while a
+// row is worked on.
+template <bool BF16, bool CODES, int NV>
+struct GradRow {
+    u32x4a dy[NV][BF16 ? 1 : 2], dh[NV][BF16 ? 1 : 2], h[NV][BF16 ? 1 : 2];   // h: codes in one half
+    uint32_t ex[NV];
+    float rstd;
+};
+
+template <bool BF16>
+__device__ __forceinline__ void fetch8(const void* row, int e, int n, u32x4a (&v)[BF16 ? 1 : 2])
+{
+    constexpr int kEach = BF16 ? 8 : 4;      // elements of 16 bytes
+#pragma unroll
+    for (int b = 0; b < (BF16 ? 1 : 2); ++b) {
+        v[b] = u32x4a{0u, 0u, 0u, 0u};
+        const int at = e + b * kEach;
+        if (at + kEach <= n) {
+            v[b] = load16(static_cast<const char*>(row) + at * (BF16 ? 2 : 4));
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (at + j < n) {
+                    if constexpr (BF16)
+                        v[b][j >> 1] |= static_cast<uint32_t>(
+                                            static_cast<const uint16_t*>(row)[at + j])
+                                        << (16 * (j & 1));
+                    else
+                        v[b][j] = static_cast<const uint32_t*>(row)[at + j];
+                }
+        }
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ float element(const u32x4a (&v)[BF16 ? 1 : 2], int j)
+{
+    if constexpr (BF16)
+        return j & 1 ? __uint_as_float(v[0][j >> 1] & 0xffff0000u) : bf16_float(v[0][j >> 1]);
+    else
+        return __uint_as_float(v[j >> 2][j & 3]);
+}
+
+template <bool BF16, bool CODES, int TPR, int NV>
 __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormGradArgs a,
                                                                      int64_t groups)
 {
@@ -166,6 +224,7 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
     __shared__ float red[TPR / 64];
     __shared__ float share[kRows > 1 ? kRows - 1 : 1][kRows > 1 ? TPR * NV * 8 : 1];
     const int lane = threadIdx.x & (TPR - 1);
+    const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
     const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
     const int cols = static_cast<int>(a.cols);
     const float inv_n = 1.0f / static_cast<float>(cols);
@@ -176,59 +235,69 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
 #pragma unroll
         for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
     }
-    for (int64_t base = static_cast<int64_t>(blockIdx.x) * kRows; base < a.rows; base += step) {
-        const int64_t row = base + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    typedef GradRow<BF16, CODES, NV> Row;
+    auto fetch = [&](int64_t base, Row& r) {
+        const int64_t row = base + sub;
         const bool on = row < a.rows;
         const int n = on ? cols : 0;
         const int64_t at = on ? row * cols : 0;
-        const float rstd = on ? a.rstd[row] : 0.0f;
-        float d[NV][8], v[NV][8];
-        float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            load_row8<BF16>(static_cast<const char*>(a.dy) + at * kSize, (i * TPR + lane) * 8, n,
-                            d[i]);
-        if (a.h) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                load_row8<BF16>(static_cast<const char*>(a.h) + at * kSize, (i * TPR + lane) * 8,
-                                n, v[i]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] *= rstd;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                act8_read8(a.codes + at, a.exps + (on ? row : 0) * groups, (i * TPR + lane) * 8, n,
-                           v[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                dw[i][j] = fmaf(d[i][j], v[i][j], dw[i][j]);
-                d[i][j] *= w[i][j];
-                s = fmaf(d[i][j], v[i][j], s);
-            }
-        s = row_sum<TPR>(s, red);
-        if (!on) continue;
-        const float c = s * inv_n;
+        r.rstd = on ? a.rstd[row] : 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int e = (i * TPR + lane) * 8;
-            float g[8];
-            if (a.dh) {
-                load_row8<BF16>(static_cast<const char*>(a.dh) + at * kSize, e, n, g);
+            fetch8<BF16>(static_cast<const char*>(a.dy) + at * kSize, e, n, r.dy[i]);
+            if constexpr (CODES) {
+                r.ex[i] = e < n ? a.exps[(on ? row : 0) * groups + (e >> 6)] : 0u;
+                const u32x2a c = act8_codes8(a.codes + at, e, n);
+                r.h[i][0] = u32x4a{c.x, c.y, 0u, 0u};
             } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] = 0.0f;
+                fetch8<BF16>(static_cast<const char*>(a.h) + at * kSize, e, n, r.h[i]);
             }
+            if (a.dh) fetch8<BF16>(static_cast<const char*>(a.dh) + at * kSize, e, n, r.dh[i]);
+        }
+    };
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kRows;
+    Row next;
+    if (first < a.rows) fetch(first, next);
+    for (int64_t base = first; base < a.rows; base += step) {
+        const Row r = next;
+        if (base + step < a.rows) fetch(base + step, next);
+        const int64_t row = base + sub;
+        const bool on = row < a.rows;
+        float d[NV][8], v[NV][8];
+        float s = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] = fmaf(rstd, fmaf(-v[i][j], c, d[i][j]), g[j]);
-            store_row8<BF16>(static_cast<char*>(a.dx) + at * kSize, e, n, g);
+        for (int i = 0; i < NV; ++i) {
+            const float scale = CODES ? act8_scale(r.ex[i]) : r.rstd;
+            // past the row's end dy is zero; a NaN group's scale is not to reach the sum there
+            const bool some = (i * TPR + lane) * 8 < cols;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float n;
+                if constexpr (CODES) n = act8_value(r.h[i][0][j >> 2], j & 3) * scale;
+                else n = element<BF16>(r.h[i], j) * scale;
+                if (CODES && (!some || (i * TPR + lane) * 8 + j >= cols)) n = 0.0f;
+                v[i][j] = n;
+                d[i][j] = element<BF16>(r.dy[i], j);
+                dw[i][j] = fmaf(d[i][j], n, dw[i][j]);
+                d[i][j] *= w[i][j];
+                s = fmaf(d[i][j], n, s);
+            }
+        }
+        s = row_sum<TPR>(s, red);
+        if (!on) continue;
+        const float c = s * inv_n;
+        const int64_t at = row * cols;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float g[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                g[j] = fmaf(r.rstd, fmaf(-v[i][j], c, d[i][j]),
+                            a.dh ? element<BF16>(r.dh[i], j) : 0.0f);
+            store_row8<BF16>(static_cast<char*>(a.dx) + at * kSize, (i * TPR + lane) * 8, cols, g);
         }
     }
-    const int sub = threadIdx.x / TPR;
     if constexpr (kRows > 1) {
         __syncthreads();
         if (sub > 0) {
@@ -251,21 +320,32 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
     for (int i = 0; i < NV; ++i) store_row8<false>(out, (i * TPR + lane) * 8, cols, dw[i]);
 }
 
-// dw[c] = the sum over p of partial[p][c]: 64 columns a workgroup, four waves of every fourth row.
-__global__ __launch_bounds__(256) void k_norm_dw(const float* __restrict__ partial, int64_t parts,
-                                                 int64_t cols, float* __restrict__ dw)
+// dw[c] = the sum over p of partial[p][c]: a workgroup takes 16 columns, 64 threads each, so that
+// a thread's few loads are all in flight at once; the threads' sums are added in order.
+__global__ __launch_bounds__(1024) void k_norm_dw(const float* __restrict__ partial, int64_t parts,
+                                                  int64_t cols, float* __restrict__ dw)
 {
-    __shared__ float t[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+    __shared__ float t[64][17];
+    const int col = threadIdx.x & 15, slot = threadIdx.x >> 4;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 16 + col;
     float s = 0.0f;
     if (c < cols) {
 #pragma unroll 8
-        for (int64_t p = wave; p < parts; p += 4) s += partial[p * cols + c];
+        for (int64_t p = slot; p < parts; p += 64) s += partial[p * cols + c];
     }
-    t[wave][lane] = s;
+    t[slot][col] = s;
     __syncthreads();
-    if (wave == 0 && c < cols) dw[c] = (t[0][lane] + t[1][lane]) + (t[2][lane] + t[3][lane]);
+    if (threadIdx.x >= 256) return;
+    s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s += t[slot * 4 + k][col];
+    // sixteen slots are left, lanes 16 apart in four waves
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    __shared__ float u[4][16];
+    if ((threadIdx.x & 63) < 16) u[threadIdx.x >> 6][col] = s;
+    __syncthreads();
+    if (threadIdx.x < 16 && c < cols) dw[c] = (u[0][col] + u[1][col]) + (u[2][col] + u[3][col]);
 }
 
 __global__ __launch_bounds__(256) void k_fill_zero(float* __restrict__ p, int64_t n)
@@ -358,14 +438,14 @@ hipError_t launch_rms_norm(const NormArgs& a, bool bf16, hipStream_t stream)
 int64_t norm_grad_parts(int64_t rows, int64_t cols)
 {
     const int64_t per = norm_rows_per_group(cols);
-    return std::min<int64_t>((rows + per - 1) / per, 512);
+    return std::min<int64_t>((rows + per - 1) / per, 1024);
 }
 
 hipError_t launch_rms_norm_grad(const NormGradArgs& a, bool bf16, hipStream_t stream)
 {
     const int64_t cols = a.cols;
     if (cols < 1 || cols > kNormMaxCols) return hipErrorInvalidValue;
-    const dim3 dw_grid(static_cast<unsigned>((cols + 63) / 64));
+    const dim3 dw_grid(static_cast<unsigned>((cols + 15) / 16));
     if (a.rows <= 0) {
         hipLaunchKernelGGL(k_fill_zero, dim3(static_cast<unsigned>((cols + 255) / 256)), dim3(256),
                            0, stream, a.dw, cols);
@@ -374,20 +454,22 @@ hipError_t launch_rms_norm_grad(const NormGradArgs& a, bool bf16, hipStream_t st
     const int64_t parts = norm_grad_parts(a.rows, cols);
     const int64_t groups = act8_groups(cols);
     const dim3 grid(static_cast<unsigned>(parts));
+#define LAUNCH_AS(BF, CODES, TPR, NV)                                                       \
+    hipLaunchKernelGGL((k_rms_norm_grad<BF, CODES, TPR, NV>), grid, dim3(kNormThreads(TPR)), 0, \
+                       stream, a, groups)
 #define LAUNCH(TPR, NV)                                                                    \
     do {                                                                                   \
-        if (bf16)                                                                          \
-            hipLaunchKernelGGL((k_rms_norm_grad<true, TPR, NV>), grid,                     \
-                               dim3(kNormThreads(TPR)), 0, stream, a, groups);             \
-        else                                                                               \
-            hipLaunchKernelGGL((k_rms_norm_grad<false, TPR, NV>), grid,                    \
-                               dim3(kNormThreads(TPR)), 0, stream, a, groups);             \
+        if (bf16 && a.codes) LAUNCH_AS(true, true, TPR, NV);                               \
+        else if (bf16) LAUNCH_AS(true, false, TPR, NV);                                    \
+        else if (a.codes) LAUNCH_AS(false, true, TPR, NV);                                 \
+        else LAUNCH_AS(false, false, TPR, NV);                                             \
     } while (0)
     GEFEN_NORM_WIDTHS(LAUNCH);
 #undef LAUNCH
+#undef LAUNCH_AS
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    hipLaunchKernelGGL(k_norm_dw, dw_grid, dim3(256), 0, stream, a.partial, parts, cols, a.dw);
+    hipLaunchKernelGGL(k_norm_dw, dw_grid, dim3(1024), 0, stream, a.partial, parts, cols, a.dw);
     return hipGetLastError();
 }
 

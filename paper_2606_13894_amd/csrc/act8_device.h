@@ -158,6 +158,22 @@ __device__ __forceinline__ uint32_t max_over_8(uint32_t m)
     return max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 4)));
 }
 
+// One group's eight lanes write its codes (w: eight packed ones each) and its exponent.
+template <typename I>
+__device__ __forceinline__ void act8_store_group(const u32x2a& w, int ex, I e, I n,
+                                                 int8_t* __restrict__ codes,
+                                                 uint8_t* __restrict__ exps)
+{
+    if (e + 8 <= n) {
+        store8b(codes + e, w);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (e + j < n) codes[e + j] = static_cast<int8_t>((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+    }
+    if ((e & 63) == 0 && e < n) exps[e >> 6] = static_cast<uint8_t>(ex);
+}
+
 // One group's eight lanes, each with eight elements e .. e + 7 of a row of n (zero from n on),
 // write the group's codes and its exponent. Every lane of the eight takes part.
 template <typename I>
@@ -175,14 +191,49 @@ __device__ __forceinline__ void act8_write_group(const float (&v)[8], I e, I n,
         w.x = act8_pack(v[0], v[1], v[2], v[3], inv);
         w.y = act8_pack(v[4], v[5], v[6], v[7], inv);
     }
-    if (e + 8 <= n) {
-        store8b(codes + e, w);
-    } else {
+    act8_store_group(w, ex, e, n, codes, exps);
+}
+
+// The same of products v[j] * by with `by` in 64 bits: float32 would move about one code in a
+// million across a rounding boundary. f: the products rounded to float32; below kAct8Top.
+template <typename I>
+__device__ __forceinline__ void act8_write_products(const float (&v)[8], double by,
+                                                    const float (&f)[8], I e, I n,
+                                                    int8_t* __restrict__ codes,
+                                                    uint8_t* __restrict__ exps)
+{
+    uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (e + j < n) codes[e + j] = static_cast<int8_t>((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+    for (int j = 0; j < 8; ++j) top = max(top, abs_bits(f[j]));
+    const int ex = act8_exponent(max_over_8(top));
+    const double to = by * static_cast<double>(act8_inverse(ex));
+    u32x2a w = {0u, 0u};
+    if (ex != 255) {
+        uint32_t c[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)   // 1.5 * 2^52, as in act8_code
+            c[j] = static_cast<uint32_t>(__double2loint(
+                fma(static_cast<double>(v[j]), to, 6755399441055744.0)));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t lo = __builtin_amdgcn_perm(c[4 * j + 1], c[4 * j], 0x0c0c0400u);
+            const uint32_t hi = __builtin_amdgcn_perm(c[4 * j + 3], c[4 * j + 2], 0x04000c0cu);
+            w[j] = lo | hi;
+        }
     }
-    if ((e & 63) == 0 && e < n) exps[e >> 6] = static_cast<uint8_t>(ex);
+    act8_store_group(w, ex, e, n, codes, exps);
+}
+
+// Codes e .. e + 7 of a row of n; zero from n on.
+template <typename I>
+__device__ __forceinline__ u32x2a act8_codes8(const int8_t* __restrict__ codes, I e, I n)
+{
+    if (e + 8 <= n) return load8b(codes + e);
+    u32x2a w = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (e + j < n) w[j >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(codes[e + j])) << (8 * (j & 3));
+    return w;
 }
 
 // Elements e .. e + 7 of a checkpointed row of n; zero from n on.
@@ -191,25 +242,10 @@ __device__ __forceinline__ void act8_read8(const int8_t* __restrict__ codes,
                                            const uint8_t* __restrict__ exps, I e, I n,
                                            float (&v)[8])
 {
-    u32x2a w = {0u, 0u};
-    float s = 0.0f;
-    if (e < n) s = act8_scale(exps[e >> 6]);
-    if (e + 8 <= n) {
-        w = load8b(codes + e);
-    } else {
+    const float s = e < n ? act8_scale(exps[e >> 6]) : 0.0f;
+    const u32x2a w = act8_codes8(codes, e, n);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (e + j < n) {
-                const uint32_t b = static_cast<uint8_t>(codes[e + j]);
-                if (j < 4) w.x |= b << (8 * j);
-                else w.y |= b << (8 * (j - 4));
-            }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        v[j] = act8_value(w.x, j) * s;
-        v[4 + j] = act8_value(w.y, j) * s;
-    }
+    for (int j = 0; j < 8; ++j) v[j] = act8_value(w[j >> 2], j & 3) * s;
     if (e + 8 > n) {   // a NaN group's padding is zero too
 #pragma unroll
         for (int j = 0; j < 8; ++j)

@@ -165,7 +165,7 @@ int gefen_rms_norm(const void* x, const void* residual, int32_t dtype, const flo
     a.weight = weight;
     a.rows = rows;
     a.cols = cols;
-    a.eps = static_cast<float>(eps);
+    a.eps = eps;
     a.y = y;
     a.h = h;
     a.rstd = rstd;

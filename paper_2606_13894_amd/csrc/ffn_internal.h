@@ -32,7 +32,7 @@ struct NormArgs {
     const void* r;          // residual, or null
     const float* weight;
     int64_t rows, cols;
-    float eps;
+    double eps;
     void* y;
     void* h;                // x + r, or null
     float* rstd;

@@ -29,35 +29,54 @@ _BACKWARD, _UNALIGNED = 1, 2
 _DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream   # no Stream object: a microsecond less a call
+_lib = None
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        _lib = load_library()
+    return _lib
+
+
 def _on(stream, fn, *args):
     """fn(*args) with `stream` as torch's current stream."""
     with torch.cuda.stream(stream):
         return fn(*args)
 
 
-def _handle():
-    return torch.cuda.current_stream().cuda_stream
+def _device(t, what):
+    """The index of t's device, which is the current one."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    dev = t.get_device()
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, not on the current device")
+    return dev
 
 
-def _operand(t, what, dtype=None, shape=None):
+def _operand(t, what, dev, dtype=None, shape=None):
     """t, contiguous, after its checks."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{what} must be a device tensor")
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != dev:
         raise ValueError(f"{what} is on {t.device}, not on the current device")
     if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     return t if t.is_contiguous() else t.contiguous()
 
 
 def _rows(t, what):
     """(rows, cols) of a tensor whose last dimension is a row."""
-    if t.dim() < 1 or t.shape[-1] < 1:
+    shape = t.shape
+    if len(shape) == 2 and shape[1]:
+        return shape
+    if not shape or not shape[-1]:
         raise ValueError(f"{what} must have rows of at least one element")
-    cols = t.shape[-1]
-    return t.numel() // cols, cols
+    return t.numel() // shape[-1], shape[-1]
 
 
 def _dtype(t, what):
@@ -67,8 +86,9 @@ def _dtype(t, what):
     return d
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _call(code):
+    if code:
+        _check(code)
 
 
 class Checkpoint8:
@@ -84,8 +104,9 @@ class Checkpoint8:
         if tuple(exponents.shape) != (*codes.shape[:-1], -(-cols // GROUP)):
             raise ValueError(f"exponents have shape {tuple(exponents.shape)}, expected "
                              f"{(*codes.shape[:-1], -(-cols // GROUP))}")
-        self.codes = _operand(codes, "codes")
-        self.exponents = _operand(exponents, "exponents")
+        dev = _device(codes, "codes")
+        self.codes = _operand(codes, "codes", dev)
+        self.exponents = _operand(exponents, "exponents", dev)
 
     @classmethod
     def empty(cls, shape, device):
@@ -108,17 +129,22 @@ class Checkpoint8:
         """The tensor's values (exact in both types), times ``gain`` (float32, one per column)."""
         if stream is not None:
             return _on(stream, self.decode, dtype, gain, out)
-        lib = load_library()
-        rows, cols = _rows(self.codes, "codes")
+        codes = self.codes
+        dev = codes.get_device()
+        rows, cols = _rows(codes, "codes")
         if out is None:
-            out = torch.empty(self.codes.shape, dtype=dtype, device=self.codes.device)
+            out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
         elif not out.is_contiguous():
             raise ValueError("out must be contiguous")
-        d = _dtype(_operand(out, "out", None, self.codes.shape), "out")
+        else:
+            _operand(out, "out", dev, None, codes.shape)
+        d = _dtype(out, "out")
+        p = None
         if gain is not None:
-            gain = _operand(gain, "gain", torch.float32, (cols,))
-        _check(lib.gefen_checkpoint_decode(self.codes.data_ptr(), self.exponents.data_ptr(),
-                                           _ptr(gain), rows, cols, out.data_ptr(), d, _handle()))
+            gain = _operand(gain, "gain", dev, torch.float32, (cols,))
+            p = gain.data_ptr()
+        _call(_library().gefen_checkpoint_decode(codes.data_ptr(), self.exponents.data_ptr(), p,
+                                                 rows, cols, out.data_ptr(), d, _raw_stream(dev)))
         return out
 
 
@@ -127,13 +153,14 @@ def checkpoint8(x, stream=None):
     dimension."""
     if stream is not None:
         return _on(stream, checkpoint8, x)
-    lib = load_library()
-    x = _operand(x, "x")
+    dev = _device(x, "x")
+    if not x.is_contiguous():
+        x = x.contiguous()
     d = _dtype(x, "x")
     rows, cols = _rows(x, "x")
     c = Checkpoint8.empty(x.shape, x.device)
-    _check(lib.gefen_checkpoint_encode(x.data_ptr(), d, rows, cols, c.codes.data_ptr(),
-                                       c.exponents.data_ptr(), _handle()))
+    _call(_library().gefen_checkpoint_encode(x.data_ptr(), d, rows, cols, c.codes.data_ptr(),
+                                             c.exponents.data_ptr(), _raw_stream(dev)))
     return c
 
 
@@ -151,22 +178,25 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-6, checkpoint: bool = Fal
     With ``checkpoint`` the normalised rows are saved in 8 bits for the backward passes."""
     if stream is not None:
         return _on(stream, rms_norm, x, weight, residual, eps, checkpoint)
-    lib = load_library()
-    x = _operand(x, "x")
+    dev = _device(x, "x")
+    if not x.is_contiguous():
+        x = x.contiguous()
     d = _dtype(x, "x")
     rows, cols = _rows(x, "x")
-    weight = _operand(weight, "weight", torch.float32, (cols,))
+    weight = _operand(weight, "weight", dev, torch.float32, (cols,))
     y = torch.empty_like(x)
-    h = x
+    h, rp, hp = x, None, None
     if residual is not None:
-        residual = _operand(residual, "residual", x.dtype, x.shape)
+        residual = _operand(residual, "residual", dev, x.dtype, x.shape)
         h = torch.empty_like(x)
+        rp, hp = residual.data_ptr(), h.data_ptr()
     rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    c = Checkpoint8.empty(x.shape, x.device) if checkpoint else None
-    _check(lib.gefen_rms_norm(x.data_ptr(), _ptr(residual), d, weight.data_ptr(), rows, cols, eps,
-                              y.data_ptr(), None if residual is None else h.data_ptr(),
-                              rstd.data_ptr(), c and c.codes.data_ptr(),
-                              c and c.exponents.data_ptr(), _handle()))
+    c = cp = ep = None
+    if checkpoint:
+        c = Checkpoint8.empty(x.shape, x.device)
+        cp, ep = c.codes.data_ptr(), c.exponents.data_ptr()
+    _call(_library().gefen_rms_norm(x.data_ptr(), rp, d, weight.data_ptr(), rows, cols, eps,
+                                    y.data_ptr(), hp, rstd.data_ptr(), cp, ep, _raw_stream(dev)))
     return RMSNormOutput(y, h, rstd, c)
 
 
@@ -175,30 +205,34 @@ def rms_norm_backward(dy, saved, rstd, weight, dh=None, stream=None):
     gradient that h gets from its other uses, added to dx (which is the residual's too)."""
     if stream is not None:
         return _on(stream, rms_norm_backward, dy, saved, rstd, weight, dh)
-    lib = load_library()
-    dy = _operand(dy, "dy")
+    dev = _device(dy, "dy")
+    if not dy.is_contiguous():
+        dy = dy.contiguous()
     d = _dtype(dy, "dy")
     rows, cols = _rows(dy, "dy")
-    weight = _operand(weight, "weight", torch.float32, (cols,))
-    rstd = _operand(rstd, "rstd", torch.float32, dy.shape[:-1])
+    weight = _operand(weight, "weight", dev, torch.float32, (cols,))
+    rstd = _operand(rstd, "rstd", dev, torch.float32, dy.shape[:-1])
     h = codes = exps = None
     if isinstance(saved, Checkpoint8):
-        if saved.shape != dy.shape:
+        if saved.codes.shape != dy.shape:
             raise ValueError(f"saved has shape {tuple(saved.shape)}, expected {tuple(dy.shape)}")
         codes, exps = saved.codes.data_ptr(), saved.exponents.data_ptr()
     else:
-        saved = _operand(saved, "saved", dy.dtype, dy.shape)
+        saved = _operand(saved, "saved", dev, dy.dtype, dy.shape)
         h = saved.data_ptr()
+    p = None
     if dh is not None:
-        dh = _operand(dh, "dh", dy.dtype, dy.shape)
+        dh = _operand(dh, "dh", dev, dy.dtype, dy.shape)
+        p = dh.data_ptr()
+    lib = _library()
     dx = torch.empty_like(dy)
     dw = torch.empty(cols, dtype=torch.float32, device=dy.device)
     n = ctypes.c_int64()
-    _check(lib.gefen_rms_norm_backward_workspace(rows, cols, n))
+    _call(lib.gefen_rms_norm_backward_workspace(rows, cols, n))
     ws = torch.empty(n.value, dtype=torch.uint8, device=dy.device)
-    _check(lib.gefen_rms_norm_backward(dy.data_ptr(), _ptr(dh), d, h, codes, exps, rstd.data_ptr(),
-                                       weight.data_ptr(), rows, cols, dx.data_ptr(),
-                                       dw.data_ptr(), ws.data_ptr(), n.value, _handle()))
+    _call(lib.gefen_rms_norm_backward(dy.data_ptr(), p, d, h, codes, exps, rstd.data_ptr(),
+                                      weight.data_ptr(), rows, cols, dx.data_ptr(), dw.data_ptr(),
+                                      ws.data_ptr(), n.value, _raw_stream(dev)))
     return dx, dw
 
 
@@ -206,23 +240,27 @@ def _ffn_operands(rows_of, what, w_gate, w_up, w_down, activation):
     act = ACTIVATIONS.get(activation)
     if act is None:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, not {activation!r}")
-    t = _operand(rows_of, what, torch.bfloat16)
+    dev = _device(rows_of, what)
+    bf16 = torch.bfloat16
+    t = _operand(rows_of, what, dev, bf16)
     tokens, width = _rows(t, what)
-    w_gate = _operand(w_gate, "w_gate", torch.bfloat16)
-    if w_gate.dim() != 2 or w_gate.shape[1] != width or w_gate.shape[0] < 1:
-        raise ValueError(f"w_gate has shape {tuple(w_gate.shape)}, expected (inner, {width})")
+    w_gate = _operand(w_gate, "w_gate", dev, bf16)
     inner = w_gate.shape[0]
-    w_up = _operand(w_up, "w_up", torch.bfloat16, (inner, width))
-    w_down = _operand(w_down, "w_down", torch.bfloat16, (width, inner))
-    return t, tokens, width, inner, w_gate, w_up, w_down, act
+    if w_gate.dim() != 2 or w_gate.shape[1] != width or inner < 1:
+        raise ValueError(f"w_gate has shape {tuple(w_gate.shape)}, expected (inner, {width})")
+    w_up = _operand(w_up, "w_up", dev, bf16, (inner, width))
+    w_down = _operand(w_down, "w_down", dev, bf16, (width, inner))
+    return dev, t, tokens, width, inner, w_gate, w_up, w_down, act
 
 
-def _ffn_space(lib, tokens, width, inner, flags, tensors):
-    if any(t is not None and t.data_ptr() % 16 for t in tensors):
-        flags |= _UNALIGNED
+def _ffn_space(lib, like, tokens, width, inner, flags, pointers):
+    """The workspace for operands at `pointers`, and its size."""
+    for p in pointers:
+        if p is not None and p & 15:
+            flags |= _UNALIGNED
     n = ctypes.c_int64()
-    _check(lib.gefen_gated_ffn_workspace(tokens, width, inner, flags, n))
-    return torch.empty(n.value, dtype=torch.uint8, device=tensors[0].device), n.value
+    _call(lib.gefen_gated_ffn_workspace(tokens, width, inner, flags, n))
+    return torch.empty(n.value, dtype=torch.uint8, device=like.device), n.value
 
 
 def gated_ffn(x, w_gate, w_up, w_down, activation: str = "silu", checkpoint: bool = False,
@@ -232,19 +270,19 @@ def gated_ffn(x, w_gate, w_up, w_down, activation: str = "silu", checkpoint: boo
     :func:`gated_ffn_backward`."""
     if stream is not None:
         return _on(stream, gated_ffn, x, w_gate, w_up, w_down, activation, checkpoint)
-    lib = load_library()
-    x, tokens, width, inner, w_gate, w_up, w_down, act = _ffn_operands(
+    dev, x, tokens, width, inner, w_gate, w_up, w_down, act = _ffn_operands(
         x, "x", w_gate, w_up, w_down, activation)
+    lib = _library()
     y = torch.empty_like(x)
     saved, p = None, (None,) * 4
     if checkpoint:
         shape = (*x.shape[:-1], inner)
         saved = Checkpoint8.empty(shape, x.device), Checkpoint8.empty(shape, x.device)
         p = tuple(q.data_ptr() for c in saved for q in (c.codes, c.exponents))
-    ws, n = _ffn_space(lib, tokens, width, inner, 0, (x, w_gate, w_up, w_down))
-    _check(lib.gefen_gated_ffn(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(),
-                               w_down.data_ptr(), tokens, width, inner, act, y.data_ptr(), *p,
-                               ws.data_ptr(), n, _handle()))
+    ops = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr()
+    ws, n = _ffn_space(lib, x, tokens, width, inner, 0, ops)
+    _call(lib.gefen_gated_ffn(*ops, tokens, width, inner, act, y.data_ptr(), *p, ws.data_ptr(), n,
+                              _raw_stream(dev)))
     return (y, saved) if checkpoint else y
 
 
@@ -256,34 +294,36 @@ def gated_ffn_backward(dy, x, saved, w_gate, w_up, w_down, activation: str = "si
     if stream is not None:
         return _on(stream, gated_ffn_backward, dy, x, saved, w_gate, w_up, w_down, activation,
                    gain)
-    lib = load_library()
-    dy, tokens, width, inner, w_gate, w_up, w_down, act = _ffn_operands(
+    dev, dy, tokens, width, inner, w_gate, w_up, w_down, act = _ffn_operands(
         dy, "dy", w_gate, w_up, w_down, activation)
     gate, up = saved
     for c, what in ((gate, "the gate's checkpoint"), (up, "the up projection's checkpoint")):
-        if not isinstance(c, Checkpoint8) or tuple(c.shape) != (*dy.shape[:-1], inner):
+        if not isinstance(c, Checkpoint8) or c.codes.shape != (*dy.shape[:-1], inner):
             raise ValueError(f"{what} must be a Checkpoint8 of shape "
                              f"{(*dy.shape[:-1], inner)}")
-    xs = codes = exps = None
+    xp = codes = exps = gp = None
     if isinstance(x, Checkpoint8):
-        if x.shape != dy.shape:
+        if x.codes.shape != dy.shape:
             raise ValueError(f"x has shape {tuple(x.shape)}, expected {tuple(dy.shape)}")
         codes, exps = x.codes.data_ptr(), x.exponents.data_ptr()
         if gain is not None:
-            gain = _operand(gain, "gain", torch.float32, (width,))
+            gain = _operand(gain, "gain", dev, torch.float32, (width,))
+            gp = gain.data_ptr()
     else:
         if gain is not None:
             raise ValueError("gain goes with a Checkpoint8 of x")
-        xs = x = _operand(x, "x", torch.bfloat16, dy.shape)
+        x = _operand(x, "x", dev, torch.bfloat16, dy.shape)
+        xp = x.data_ptr()
+    lib = _library()
     dx = torch.empty_like(dy)
     dwg, dwu, dwd = (torch.empty_like(w) for w in (w_gate, w_up, w_down))
-    ws, n = _ffn_space(lib, tokens, width, inner, _BACKWARD, (dy, xs, w_gate, w_up, w_down))
-    _check(lib.gefen_gated_ffn_backward(
-        dy.data_ptr(), _ptr(xs), codes, exps, _ptr(gain), gate.codes.data_ptr(),
-        gate.exponents.data_ptr(), up.codes.data_ptr(), up.exponents.data_ptr(),
-        w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), tokens, width, inner, act,
+    dp, w = dy.data_ptr(), (w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr())
+    ws, n = _ffn_space(lib, dy, tokens, width, inner, _BACKWARD, (dp, xp, *w))
+    _call(lib.gefen_gated_ffn_backward(
+        dp, xp, codes, exps, gp, gate.codes.data_ptr(), gate.exponents.data_ptr(),
+        up.codes.data_ptr(), up.exponents.data_ptr(), *w, tokens, width, inner, act,
         dx.data_ptr(), dwg.data_ptr(), dwu.data_ptr(), dwd.data_ptr(), ws.data_ptr(), n,
-        _handle()))
+        _raw_stream(dev)))
     return dx, dwg, dwu, dwd
 
 
