@@ -191,16 +191,19 @@ __device__ __forceinline__ void fetch8(const void* row, int e, int n, u32x4a (&v
         const int at = e + b * kEach;
         if (at + kEach <= n) {
             v[b] = load16(static_cast<const char*>(row) + at * (BF16 ? 2 : 4));
-        } else {
+        } else if (at < n) {   // all loads together, the last element for those past it
+            uint32_t t[kEach];
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                const int i = at + j < n ? at + j : n - 1;
+                t[j] = BF16 ? static_cast<uint32_t>(static_cast<const uint16_t*>(row)[i])
+                            : static_cast<const uint32_t*>(row)[i];
+            }
 #pragma unroll
             for (int j = 0; j < kEach; ++j)
                 if (at + j < n) {
-                    if constexpr (BF16)
-                        v[b][j >> 1] |= static_cast<uint32_t>(
-                                            static_cast<const uint16_t*>(row)[at + j])
-                                        << (16 * (j & 1));
-                    else
-                        v[b][j] = static_cast<const uint32_t*>(row)[at + j];
+                    if constexpr (BF16) v[b][j >> 1] |= t[j] << (16 * (j & 1));
+                    else v[b][j] = t[j];
                 }
         }
     }

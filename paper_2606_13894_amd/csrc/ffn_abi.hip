@@ -84,7 +84,7 @@ FfnGemm product(int32_t kind, const FfnTile& t, int64_t M, int64_t N, int64_t K,
 {
     FfnGemm g{};
     g.kind = kind;
-    g.big = t.big;
+    g.tile = t.tile;
     g.M = M;
     g.N = N;
     g.K = K;

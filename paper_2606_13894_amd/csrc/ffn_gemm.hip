@@ -8,8 +8,8 @@
 // rows of k go through the transposing LDS read (ds_read_b64_tr_b16), which gives a lane four
 // consecutive k of its column.
 //
-// A workgroup computes a 256 x 256 tile with eight waves (4 x 2 of 64 x 128), or a 128 x 128
-// tile with four (4 x 1 of 32 x 128) where that fills the chip better. Tiles of 64 k are loaded
+// A workgroup computes a 256 x 256 tile with eight waves (4 x 2 of 64 x 128), or a 128 x 128 or
+// 64 x 128 tile with four (4 x 1 of 32 x 128, 16 x 128) where that fills the chip better. Tiles of 64 k are loaded
 // straight into LDS (no registers) through buffer resources, whose range check gives zeros past
 // the operand's rows; two LDS stages, the next one in flight while the current one feeds the
 // matrix cores, one barrier per stage. LDS rows are not padded: 16-byte pieces (32-byte ones
@@ -47,12 +47,16 @@ constexpr int BK = 64;                    // k of a stage: 128 bytes of a row
 constexpr int NJ = 4;                     // 16-column blocks of a wave in each half of B
 constexpr uint32_t kOut = 0x80000000u;    // a vector offset past every resource's range
 
-template <bool BIG>
+// The tiles (kFfnTile*): rows of C, and columns in two halves.
+template <int SIZE>
 struct Shape {
-    static constexpr int kWaves = BIG ? 8 : 4;
+    static constexpr bool kPhases = SIZE == kFfnTile256;        // two waves to a SIMD, in turn
+    static constexpr int kWaves = kPhases ? 8 : 4;
     static constexpr int kThreads = 64 * kWaves;
-    static constexpr int T = BIG ? 256 : 128;       // tile rows and columns
-    static constexpr int MI = BIG ? 4 : 2;          // 16-row blocks of a wave
+    static constexpr int TM = SIZE == kFfnTile256 ? 256 : SIZE == kFfnTile128 ? 128 : 64;
+    static constexpr int H = kPhases ? 128 : 64;                // columns of each half
+    static constexpr int MI = TM / 64;                          // 16-row blocks of a wave
+    static constexpr int kLoadsA = TM / (8 * kWaves);           // 1 KiB loads of a wave and stage
 };
 
 // The permutation of a row's eight 16-byte pieces of k: a fragment read takes 16 rows at a time,
@@ -208,11 +212,9 @@ template <bool FULL>
 __device__ __forceinline__ u32x4a read_codes(const int8_t* __restrict__ row, int64_t c, int64_t n)
 {
     if (FULL || c + 16 <= n) return load16(row + c);
-    u32x4a w = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (c + i < n) w[i >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(row[c + i])) << (8 * (i & 3));
-    return w;
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    if (c < n) load_tail<16>(row, c, n, w);
+    return u32x4a{w[0], w[1], w[2], w[3]};
 }
 
 // Fragments of a stage's two 32-deep steps from rows of k, of 16-wide blocks at the byte
@@ -246,6 +248,41 @@ __device__ __forceinline__ void read_t(const uint32_t (&p)[4], u32x2a (&o)[16])
                    "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15])
                  : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [b1] "n"(4 *
                    SB), [b2] "n"(32 * SB), [b3] "n"(36 * SB)
+                 : "memory");
+}
+
+template <int SA, int SB>
+__device__ __forceinline__ void read_t(const uint32_t (&p)[5], u32x2a (&o)[20])
+{
+    asm volatile("ds_read_b64_tr_b16 %[o0], %[p0]\n\t"
+                 "ds_read_b64_tr_b16 %[o1], %[p0] offset:%[a1]\n\t"
+                 "ds_read_b64_tr_b16 %[o2], %[p0] offset:%[a2]\n\t"
+                 "ds_read_b64_tr_b16 %[o3], %[p0] offset:%[a3]\n\t"
+                 "ds_read_b64_tr_b16 %[o4], %[p1]\n\t"
+                 "ds_read_b64_tr_b16 %[o5], %[p1] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o6], %[p1] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o7], %[p1] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o8], %[p2]\n\t"
+                 "ds_read_b64_tr_b16 %[o9], %[p2] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o10], %[p2] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o11], %[p2] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o12], %[p3]\n\t"
+                 "ds_read_b64_tr_b16 %[o13], %[p3] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o14], %[p3] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o15], %[p3] offset:%[b3]\n\t"
+                 "ds_read_b64_tr_b16 %[o16], %[p4]\n\t"
+                 "ds_read_b64_tr_b16 %[o17], %[p4] offset:%[b1]\n\t"
+                 "ds_read_b64_tr_b16 %[o18], %[p4] offset:%[b2]\n\t"
+                 "ds_read_b64_tr_b16 %[o19], %[p4] offset:%[b3]\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : [o0] "=&v"(o[0]), [o1] "=&v"(o[1]), [o2] "=&v"(o[2]), [o3] "=&v"(o[3]), [o4]
+                   "=&v"(o[4]), [o5] "=&v"(o[5]), [o6] "=&v"(o[6]), [o7] "=&v"(o[7]), [o8]
+                   "=&v"(o[8]), [o9] "=&v"(o[9]), [o10] "=&v"(o[10]), [o11] "=&v"(o[11]), [o12]
+                   "=&v"(o[12]), [o13] "=&v"(o[13]), [o14] "=&v"(o[14]), [o15] "=&v"(o[15]), [o16]
+                   "=&v"(o[16]), [o17] "=&v"(o[17]), [o18] "=&v"(o[18]), [o19] "=&v"(o[19])
+                 : [p0] "v"(p[0]), [p1] "v"(p[1]), [p2] "v"(p[2]), [p3] "v"(p[3]), [p4] "v"(p[4]),
+                   [a1] "n"(4 * SA), [a2] "n"(32 * SA), [a3] "n"(36 * SA), [b1] "n"(4 * SB), [b2]
+                   "n"(32 * SB), [b3] "n"(36 * SB)
                  : "memory");
 }
 
@@ -345,36 +382,36 @@ __device__ __forceinline__ bf16x8 join(const u32x2a& a, const u32x2a& b)
     return __builtin_bit_cast(bf16x8, v);
 }
 
-template <int KIND, bool AK, bool BKM, bool BIG>
-__global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnGemm g)
+template <int KIND, bool AK, bool BKM, int SIZE>
+__global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const FfnGemm g)
 {
-    using S = Shape<BIG>;
-    constexpr int T = S::T, MI = S::MI;
+    using S = Shape<SIZE>;
+    constexpr int TM = S::TM, H = S::H, MI = S::MI, LA = S::kLoadsA;
+    constexpr bool PHASES = S::kPhases;
     constexpr bool DUAL = KIND == kFfnGateUp;
     // two stages of A, and B's halves, as arrays of their own: so the compiler sees that reads of
     // one do not wait for loads to the others
-    __shared__ __attribute__((aligned(16))) uint16_t lds_a0[T * BK], lds_a1[T * BK];
-    __shared__ __attribute__((aligned(16))) uint16_t lds_b00[T * BK / 2], lds_b01[T * BK / 2];
-    __shared__ __attribute__((aligned(16))) uint16_t lds_b10[T * BK / 2], lds_b11[T * BK / 2];
+    __shared__ __attribute__((aligned(16))) uint16_t lds_a0[TM * BK], lds_a1[TM * BK];
+    __shared__ __attribute__((aligned(16))) uint16_t lds_b00[H * BK], lds_b01[H * BK];
+    __shared__ __attribute__((aligned(16))) uint16_t lds_b10[H * BK], lds_b11[H * BK];
     Work w;
     if (!decode_work(g, w)) return;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = BIG ? wave >> 1 : wave, wn = BIG ? wave & 1 : 0;
-    const int64_t row0 = int64_t(w.tm) * T;
-    const int64_t col0 = int64_t(w.tn) * (DUAL ? T / 2 : T);   // DUAL: columns of each matrix
+    const int wm = PHASES ? wave >> 1 : wave, wn = PHASES ? wave & 1 : 0;
+    const int64_t row0 = int64_t(w.tm) * TM;
+    const int64_t col0 = int64_t(w.tn) * (DUAL ? H : 2 * H);   // DUAL: columns of each matrix
 
     const int stages = g.stages;                      // of one segment of the sum
     const int all = stages * g.segments;
     const int first = static_cast<int>(int64_t(all) * w.split / g.splits);
     const int nk = static_cast<int>(int64_t(all) * (w.split + 1) / g.splits) - first;
 
-    // A stage's tiles: A (T rows of m), and B's two halves of H = T / 2 columns of n, which are
-    // two parts of one matrix, or of the gate's and the up matrix. Their sources move on stage
+    // A stage's tiles: A (TM rows of m), and B's two halves of H columns of n, which are two
+    // parts of one matrix, or of the gate's and the up matrix. Their sources move on stage
     // by stage in scalar registers; past the last stage they are ranges of no bytes.
-    constexpr int H = T / 2;
-    uint32_t off_a[4], off_b[2];
-    lane_offsets<AK, T>(wave, lane, g.lda, off_a);
+    uint32_t off_a[LA], off_b[2];
+    lane_offsets<AK, TM>(wave, lane, g.lda, off_a);
     lane_offsets<BKM, H>(wave, lane, g.ldb, off_b);
     int klim[2];   // K-major: load j has nothing for this lane at stages from k = klim[j & 1] on
 #pragma unroll
@@ -382,7 +419,7 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
         klim[j] = static_cast<int>(g.kpad) - 8 * ((lane & 7) ^ chunk_key(8 * j + (lane >> 3)));
     const int lda = static_cast<int>(g.lda), ldb = static_cast<int>(g.ldb);
     const int klen = static_cast<int>(g.K), kend = stages * BK;
-    const int a_rows = static_cast<int>(min(int64_t(T), g.M - row0));
+    const int a_rows = static_cast<int>(min(int64_t(TM), g.M - row0));
     int b_rows[2], b_col[2];
     const uint16_t *a_next, *b_next[2];               // where the second segment starts
     struct Source {
@@ -429,12 +466,12 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
         uint16_t *a, *b[2];
     };
     const Tiles t0 = {lds_a0, {lds_b00, lds_b01}}, t1 = {lds_a1, {lds_b10, lds_b11}};
-    auto load_a = [&](const Tiles& t) {               // four loads
+    auto load_a = [&](const Tiles& t) {               // LA loads
         const int n = AK ? a_rows * lda - at_a.k0
                          : min(BK, klen - at_a.k0) * lda - static_cast<int>(row0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            load_piece(resource(at_a.p, at_a.left > 0 ? 2 * n : 0), t.a + (wave * 4 + j) * 512,
+        for (int j = 0; j < LA; ++j)
+            load_piece(resource(at_a.p, at_a.left > 0 ? 2 * n : 0), t.a + (wave * LA + j) * 512,
                        AK && at_a.k0 >= klim[j & 1] ? kOut : off_a[j]);
         advance(at_a, a_next, AK ? BK : int64_t(BK) * g.lda);
     };
@@ -464,7 +501,7 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
         return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
                    (lds_u16*)(t + trow * wide + piece * 16 + (lane & 3) * 4)));
     };
-    typedef std::integral_constant<int, T> WideA;
+    typedef std::integral_constant<int, TM> WideA;
     typedef std::integral_constant<int, H> WideB;
     // All of A's with B's first half, or B's second half.
     auto frags = [&](const Tiles& t, auto part) {
@@ -489,7 +526,7 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
             for (int i = 0; i < NA + NJ; ++i)
                 at[i] = i < NA ? addr_t(t.a, WideA{}, (wm * MI + i) * 16)
                                : addr_t(sb, WideB{}, wn * 64 + (i - NA) * 16);
-            read_t<2 * T, 2 * H>(at, o);
+            read_t<2 * TM, 2 * H>(at, o);
 #pragma unroll
             for (int i = 0; i < NA + NJ; ++i)
 #pragma unroll
@@ -527,11 +564,11 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    // This wave's LDS reads are done, and all but its newest eight loads: those of the phase
-    // after next and later (six with A and B's first half, two with the second).
+    // This wave's LDS reads are done, and all but its newest loads, two parts' worth: A and B's
+    // first half, and B's second half.
     auto settled = [&]() {
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x0070 | 8);
+        __builtin_amdgcn_s_waitcnt(0x0070 | (LA + 4));
     };
     // A stage is two parts, by B's halves; A's fragments stay for the second. A part is two
     // phases: its fragments out of LDS and loads for a later part; then the matrix-core ops.
@@ -543,7 +580,7 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
     // every wave before the barrier that its first readers pass.
     auto part = [&](auto which, const Tiles& cur, const Tiles& to) {
         constexpr int h = decltype(which)::value;
-        if constexpr (!BIG) {
+        if constexpr (!PHASES) {
             settled();
             barrier();
         }
@@ -554,13 +591,13 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
             load_a(to);
             load_b(to, 0);
         }
-        if constexpr (BIG) {
+        if constexpr (PHASES) {
             settled();
             barrier();
             __builtin_amdgcn_s_setprio(1);
         }
         mfmas(which);
-        if constexpr (BIG) {
+        if constexpr (PHASES) {
             __builtin_amdgcn_s_setprio(0);
             barrier();
         }
@@ -573,7 +610,7 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
         load_b(t0, 1);
         load_a(t1);
         load_b(t1, 0);
-        if constexpr (BIG) {
+        if constexpr (PHASES) {
             settled();
             barrier();
             if (wave >= 4) barrier();
@@ -584,7 +621,7 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
             part(First{}, t1, t0);
             part(Second{}, t1, t1);
         }
-        if (BIG && wave < 4) barrier();
+        if (PHASES && wave < 4) barrier();
     }
 
     // ------------------------------------------------------------------ epilogues
@@ -706,7 +743,7 @@ __global__ __launch_bounds__(Shape<BIG>::kThreads, 2) void k_ffn_gemm(const FfnG
     typedef std::integral_constant<bool, false> Edge;
     typedef std::integral_constant<int, kActSilu> Silu;
     typedef std::integral_constant<int, kActGelu> Gelu;
-    const bool inside = row0 + T <= g.M && col0 + (DUAL ? H : T) <= g.N;
+    const bool inside = row0 + TM <= g.M && col0 + (DUAL ? H : 2 * H) <= g.N;
     if constexpr (KIND == kFfnPlain) {
         if (inside) plain(Whole{});
         else plain(Edge{});
@@ -745,17 +782,34 @@ __global__ __launch_bounds__(256) void k_ffn_join(const FfnGemm g)
     store_row8<true>(g.o[b], e, plane, s);   // the output is dense
 }
 
-// dst (rows of ldd, a multiple of 8) = src (dense rows of `cols`), zero past them.
+// dst (rows of ldd, a multiple of 8) = src (dense rows of `cols`), zero past them. A thread takes
+// four vectors of eight, 256 apart in the flat order, all loaded before the first is stored.
 __global__ __launch_bounds__(256) void k_ffn_pad(const FfnPads p)
 {
-    const FfnPad& m = p.m[blockIdx.z];
-    const int64_t e = (static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63)) * 8;
-    if (e >= m.ldd) return;
-    for (int64_t r = static_cast<int64_t>(blockIdx.y) * 4 + (threadIdx.x >> 6); r < m.rows;
-         r += static_cast<int64_t>(gridDim.y) * 4) {
-        float v[8];
-        load_row8<true>(m.src + r * m.cols, e, m.cols, v);
-        store_row8<true>(m.dst + r * m.ldd, e, m.ldd, v);
+    const FfnPad& m = p.m[blockIdx.y];
+    const int64_t vectors = m.ldd / 8, all = m.rows * vectors;
+    for (int64_t base = static_cast<int64_t>(blockIdx.x) * 1024; base < all;
+         base += static_cast<int64_t>(gridDim.x) * 1024) {
+        const int64_t first = base + threadIdx.x;
+        int64_t row[4], e[4];
+        row[0] = first / vectors;
+        e[0] = first - row[0] * vectors;
+#pragma unroll
+        for (int i = 1; i < 4; ++i) {
+            row[i] = row[i - 1];
+            e[i] = e[i - 1] + 256;
+            while (e[i] >= vectors) {
+                e[i] -= vectors;
+                ++row[i];
+            }
+        }
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            load_row8<true>(m.src + row[i] * m.cols, 8 * e[i], row[i] < m.rows ? m.cols : 0, v[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (row[i] < m.rows) store_row8<true>(m.dst + row[i] * m.ldd, 8 * e[i], m.ldd, v[i]);
     }
 }
 
@@ -770,12 +824,15 @@ hipError_t launch_kind(const FfnGemm& g, hipStream_t stream)
 {
     const int64_t total = int64_t(g.tiles_m) * g.tiles_n * g.batch * g.splits;
     const dim3 grid(static_cast<unsigned>((total + 7) / 8 * 8));
-    if (g.big)
-        hipLaunchKernelGGL((k_ffn_gemm<KIND, AK, BKM, true>), grid, dim3(Shape<true>::kThreads), 0,
-                           stream, g);
+    if (g.tile == kFfnTile256)
+        hipLaunchKernelGGL((k_ffn_gemm<KIND, AK, BKM, kFfnTile256>), grid,
+                           dim3(Shape<kFfnTile256>::kThreads), 0, stream, g);
+    else if (g.tile == kFfnTile128)
+        hipLaunchKernelGGL((k_ffn_gemm<KIND, AK, BKM, kFfnTile128>), grid,
+                           dim3(Shape<kFfnTile128>::kThreads), 0, stream, g);
     else
-        hipLaunchKernelGGL((k_ffn_gemm<KIND, AK, BKM, false>), grid, dim3(Shape<false>::kThreads),
-                           0, stream, g);
+        hipLaunchKernelGGL((k_ffn_gemm<KIND, AK, BKM, kFfnTile64>), grid,
+                           dim3(Shape<kFfnTile64>::kThreads), 0, stream, g);
     return hipGetLastError();
 }
 
@@ -804,16 +861,14 @@ hipError_t launch_ffn_gemm(const FfnGemm& g, hipStream_t stream)
 
 hipError_t launch_ffn_pads(const FfnPads& p, hipStream_t stream)
 {
-    int64_t rows = 0, ldd = 0;
+    int64_t most = 0;
     for (int i = 0; i < p.n; ++i) {
-        rows = p.m[i].rows > rows ? p.m[i].rows : rows;
-        ldd = p.m[i].ldd > ldd ? p.m[i].ldd : ldd;
+        const int64_t vectors = p.m[i].rows * (p.m[i].ldd / 8);
+        most = vectors > most ? vectors : most;
     }
-    if (!p.n || !rows) return hipSuccess;
-    const int64_t gy = (rows + 3) / 4;
-    hipLaunchKernelGGL(k_ffn_pad,
-                       dim3(static_cast<unsigned>((ldd + 511) / 512),
-                            static_cast<unsigned>(gy < 65535 ? gy : 65535), p.n),
+    if (!most) return hipSuccess;
+    const int64_t groups = (most + 1023) / 1024;
+    hipLaunchKernelGGL(k_ffn_pad, dim3(static_cast<unsigned>(groups < 65536 ? groups : 65536), p.n),
                        dim3(256), 0, stream, p);
     return hipGetLastError();
 }

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <cstdint>
 
+#include "ffn_plan.h"
+
 namespace gefen {
 
 // ---------------------------------------------------------------- 8-bit activation checkpoints
@@ -66,7 +68,7 @@ enum : int32_t { kFfnGateUp = 0, kFfnPlain = 1, kFfnGateGrad = 2 };
 struct FfnGemm {
     int32_t kind;
     int32_t act;
-    bool big;                    // 256 x 256 tiles, else 128 x 128
+    int32_t tile;                // kFfnTile*
     bool a_rows_k, b_rows_k;     // the operand is stored as rows of k
     const uint16_t* a[2];        // by segment of the sum, or by batch entry
     const uint16_t* b[2];        // by segment of the sum, or gate and up

@@ -9,13 +9,18 @@ namespace gefen {
 
 constexpr int64_t kFfnMaxTokens = int64_t(1) << 24;
 constexpr int64_t kFfnMaxWidth = int64_t(1) << 20;   // a tile's rows stay within 32-bit offsets
-constexpr int kFfnBigTile = 256, kFfnSmallTile = 128, kFfnDepth = 64;
+constexpr int kFfnDepth = 64;                       // k of a stage
+
+// The products' tiles: 64 x 128 (three workgroups to a CU), 128 x 128 (two), 256 x 256 (one).
+enum FfnTileSize : int32_t { kFfnTile64 = 0, kFfnTile128 = 1, kFfnTile256 = 2 };
+inline int64_t ffn_tile_rows(int32_t size) { return size == kFfnTile256 ? 256 : size == kFfnTile128 ? 128 : 64; }
+inline int64_t ffn_tile_cols(int32_t size) { return size == kFfnTile256 ? 256 : 128; }
 
 inline int64_t ffn_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t ffn_up8(int64_t a) { return (a + 7) / 8 * 8; }
 
 struct FfnTile {
-    bool big = false;
+    int32_t tile = kFfnTile128;
     int32_t splits = 1;
     int32_t tiles_m = 0, tiles_n = 0, stages = 0;
     double us = 0.0;
@@ -27,19 +32,24 @@ enum FfnEpilogue : int { kFfnStore = 0, kFfnActivate = 1, kFfnGradient = 2 };
 
 // Estimated time in microseconds of `groups` workgroups that each sum `stages` stages, and of
 // their epilogues, fitted to measurements from 32 to 8192 rows. A stage's time grows with the
-// number of workgroups that load at once: 0.5 us for one small tile, 0.72 for one on every CU,
-// 1.2 for two on every CU; 1.0 to 1.5 us for a large one.
-inline double ffn_sum_us(bool big, int64_t groups, int64_t stages, FfnEpilogue epilogue)
+// number of workgroups that load at once: from 0.38 us alone to 0.48 with one on every CU and 1.2
+// with three for the 64-row tile, 0.5, 0.72 and (with two) 1.2 for the 128-row one, 1.0 to 1.5
+// for the largest.
+inline double ffn_stage_us(int32_t tile, int64_t groups)
 {
-    static const double small_end[3] = {5.0, 5.0, 14.0}, big_end[3] = {6.0, 9.0, 38.0};
-    const int64_t slots = big ? 256 : 512, full = groups / slots, rest = groups % slots;
-    const double end = big ? big_end[epilogue] : small_end[epilogue];
-    double us = double(full) * ((big ? 1.5 : 1.2) * double(stages) + end);
-    if (rest) {
-        const double load = double(std::min<int64_t>(rest, 256)) / 256.0;
-        const double stage = big ? 1.0 + 0.5 * load : rest > 256 ? 1.2 : 0.5 + 0.22 * load;
-        us += stage * double(stages) + end;
-    }
+    const double cu = double(groups) / 256.0;
+    if (tile == kFfnTile256) return 1.0 + 0.5 * cu;
+    if (tile == kFfnTile128) return cu <= 1.0 ? 0.5 + 0.22 * cu : 0.72 + 0.48 * (cu - 1.0);
+    return cu <= 1.0 ? 0.38 + 0.1 * cu : 0.48 + 0.36 * (cu - 1.0);
+}
+
+inline double ffn_sum_us(int32_t tile, int64_t groups, int64_t stages, FfnEpilogue epilogue)
+{
+    static const double ends[3][3] = {{3.5, 4.0, 7.0}, {5.0, 5.0, 14.0}, {6.0, 9.0, 38.0}};
+    const int64_t slots = tile == kFfnTile256 ? 256 : tile == kFfnTile128 ? 512 : 768;
+    const int64_t full = groups / slots, rest = groups % slots;
+    double us = double(full) * (ffn_stage_us(tile, slots) * double(stages) + ends[tile][epilogue]);
+    if (rest) us += ffn_stage_us(tile, rest) * double(stages) + ends[tile][epilogue];
     return us;
 }
 
@@ -50,19 +60,19 @@ inline FfnTile ffn_choose(int64_t M, int64_t N, int64_t K, int batch, int segmen
                           bool may_split, FfnEpilogue epilogue)
 {
     FfnTile best;
-    for (int b = 0; b < 2; ++b) {
-        const int64_t t = b ? kFfnBigTile : kFfnSmallTile;
-        const int64_t tm = ffn_ceil(M, t), tn = ffn_ceil(N, halves ? t / 2 : t);
+    for (int32_t tile : {kFfnTile64, kFfnTile128, kFfnTile256}) {
+        const int64_t cols = ffn_tile_cols(tile);
+        const int64_t tm = ffn_ceil(M, ffn_tile_rows(tile)), tn = ffn_ceil(N, halves ? cols / 2 : cols);
         const int64_t stages = ffn_ceil(K, kFfnDepth), all = stages * segments;
         for (int64_t s : {1, 2, 3, 4, 6, 8, 12, 16}) {
             if (s > 1 && (!may_split || all / s < 4)) break;
-            double us = ffn_sum_us(b != 0, tm * tn * batch * s, ffn_ceil(all, s), epilogue);
+            double us = ffn_sum_us(tile, tm * tn * batch * s, ffn_ceil(all, s), epilogue);
             if (s > 1) {
                 const double mb = 4e-6 * double(M) * double(N) * batch * double(s);
                 us += 3.5 + mb / 4.0 + mb / 6.0;
             }
             if (best.tiles_m == 0 || us < best.us) {
-                best.big = b != 0;
+                best.tile = tile;
                 best.splits = static_cast<int32_t>(s);
                 best.tiles_m = static_cast<int32_t>(tm);
                 best.tiles_n = static_cast<int32_t>(tn);

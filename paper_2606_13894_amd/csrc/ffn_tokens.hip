@@ -23,10 +23,13 @@ __device__ __forceinline__ bf16x8 row_piece(const uint16_t* __restrict__ row, in
     u32x4a v = {0u, 0u, 0u, 0u};
     if (k + 8 <= n) {
         v = load16(row + k);
-    } else {
+    } else if (k < n) {   // all loads together, the last element for those past it
+        uint32_t t[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = row[k + j < n ? k + j : n - 1];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (k + j < n) v[j >> 1] |= static_cast<uint32_t>(row[k + j]) << (16 * (j & 1));
+            if (k + j < n) v[j >> 1] |= t[j] << (16 * (j & 1));
     }
     return __builtin_bit_cast(bf16x8, v);
 }

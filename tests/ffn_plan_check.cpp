@@ -20,7 +20,7 @@ static void need(bool ok, const char* what, int64_t a, int64_t b, int64_t c)
 static void check_tile(const FfnTile& t, int64_t M, int64_t N, int64_t K, int batch, int segments,
                        bool halves, bool may_split)
 {
-    const int64_t side = t.big ? kFfnBigTile : kFfnSmallTile, cols = halves ? side / 2 : side;
+    const int64_t side = ffn_tile_rows(t.tile), wide = ffn_tile_cols(t.tile), cols = halves ? wide / 2 : wide;
     need(int64_t(t.tiles_m) * side >= M && (t.tiles_m - 1) * side < M, "tile rows", M, N, K);
     need(int64_t(t.tiles_n) * cols >= N && (t.tiles_n - 1) * cols < N, "tile columns", M, N, K);
     need(int64_t(t.stages) * kFfnDepth >= K && (t.stages - 1) * int64_t(kFfnDepth) < K, "stages", M,
