@@ -421,7 +421,7 @@ hipError_t launch_rms_norm(const NormArgs& a, bool bf16, hipStream_t stream)
     if (cols < 1 || cols > kNormMaxCols) return hipErrorInvalidValue;
     if (a.rows <= 0) return hipSuccess;
     const int64_t per = norm_rows_per_group(cols);
-    const int64_t blocks = std::min<int64_t>((a.rows + per - 1) / per, 2048);
+    const int64_t blocks = std::min<int64_t>((a.rows + per - 1) / per, 4096);
     const int64_t groups = act8_groups(cols);
     const dim3 grid(static_cast<unsigned>(blocks));
 #define LAUNCH(TPR, NV)                                                                    \
@@ -441,7 +441,7 @@ hipError_t launch_rms_norm(const NormArgs& a, bool bf16, hipStream_t stream)
 int64_t norm_grad_parts(int64_t rows, int64_t cols)
 {
     const int64_t per = norm_rows_per_group(cols);
-    return std::min<int64_t>((rows + per - 1) / per, 1024);
+    return std::min<int64_t>((rows + per - 1) / per, 768);
 }
 
 hipError_t launch_rms_norm_grad(const NormGradArgs& a, bool bf16, hipStream_t stream)
