@@ -91,17 +91,22 @@ FfnGemm product(int32_t kind, const FfnTile& t, int64_t M, int64_t N, int64_t K,
     g.kpad = ffn_up8(K);
     g.segments = g.batch = 1;
     g.stages = t.stages;
-    g.tiles_m = t.tiles_m;
-    g.tiles_n = t.tiles_n;
+    g.tiles_m = static_cast<int32_t>(ffn_ceil(M, ffn_tile_rows(t.tile)));
+    g.tiles_n = static_cast<int32_t>(
+        ffn_ceil(N, ffn_tile_cols(t.tile) / (kind == kFfnGateUp ? 2 : 1)));
     g.splits = t.splits;
     g.partial = t.splits > 1 ? at<float>(ws, partial) : nullptr;
     return g;
 }
 
+bool fits(const FfnGemm& g)
+{
+    return int64_t(g.tiles_m) * g.tiles_n * g.batch * g.splits <= 0x3ffffff0LL;
+}
+
 int run(const FfnGemm& g, hipStream_t stream)
 {
-    if (int64_t(g.tiles_m) * g.tiles_n * g.batch * g.splits > 0x7ffffff0LL)
-        return fail(GEFEN_EINVAL, "too many tiles");
+    if (!fits(g)) return fail(GEFEN_EINVAL, "too many tiles");
     GEFEN_HIP(launch_ffn_gemm(g, stream));
     return GEFEN_OK;
 }
@@ -377,29 +382,27 @@ int gefen_gated_ffn_backward(const uint16_t* dy, const uint16_t* x, const int8_t
     g.groups = act8_groups(F);
     if ((rc = run(g, stream))) return rc;
 
-    g = product(kFfnPlain, s.dw_down, K, F, T, workspace, s.partial);   // dy^T A
-    g.a_rows_k = g.b_rows_k = true;
+    g = product(kFfnPlain, s.dw, K, F, T, workspace, s.partial);        // dy^T A
     g.a[0] = dyp;
     g.lda = K8;
     g.b[0] = a;
     g.ldb = F8;
     g.o[0] = dw_down;
     g.ldo = F;
-    if ((rc = run(g, stream))) return rc;
-
-    g = product(kFfnPlain, s.dw_inner, F, K, T, workspace, s.partial);  // dG^T x, dU^T x
-    g.batch = 2;
-    g.a_rows_k = g.b_rows_k = true;
-    g.a[0] = dg;
-    g.a[1] = du;
-    g.lda = F8;
-    g.b[0] = xp;
-    g.ldb = K8;
-    g.col_scale = gain;
-    g.o[0] = dw_gate;
-    g.o[1] = dw_up;
-    g.ldo = K;
-    if ((rc = run(g, stream))) return rc;
+    FfnGemm gi = product(kFfnPlain, s.dw, F, K, T, workspace,           // dG^T x, dU^T x
+                         s.partial + ffn_partial_bytes(s.dw, K, F, 1));
+    gi.batch = 2;
+    gi.a[0] = dg;
+    gi.a[1] = du;
+    gi.lda = F8;
+    gi.b[0] = xp;
+    gi.ldb = K8;
+    gi.col_scale = gain;
+    gi.o[0] = dw_gate;
+    gi.o[1] = dw_up;
+    gi.ldo = K;
+    if (!fits(g) || !fits(gi)) return fail(GEFEN_EINVAL, "too many tiles");
+    GEFEN_HIP(launch_ffn_weight_grads(g, gi, stream));
 
     g = product(kFfnPlain, s.dx, T, K, F, workspace, s.partial);        // dG Wg + dU Wu
     g.segments = 2;

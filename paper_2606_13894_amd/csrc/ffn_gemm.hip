@@ -102,13 +102,13 @@ struct Work {
 
 // Work items are dealt to the eight XCDs in contiguous runs; a run walks bands of eight tile
 // rows column by column, so that the tiles that run together share panels in the XCD's L2.
-__device__ __forceinline__ bool decode_work(const FfnGemm& g, Work& w)
+__device__ __forceinline__ bool decode_work(const FfnGemm& g, uint32_t block, Work& w)
 {
     const uint32_t tiles = static_cast<uint32_t>(g.tiles_m * g.tiles_n);
     const uint32_t total = tiles * g.batch * g.splits;
     const uint32_t per = (total + 7) / 8;
-    const uint32_t id = (blockIdx.x % 8) * per + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= per || id >= total) return false;
+    const uint32_t id = (block % 8) * per + block / 8;
+    if (block / 8 >= per || id >= total) return false;
     const uint32_t t = id % tiles, rest = id / tiles;
     w.batch = rest % g.batch;
     w.split = rest / g.batch;
@@ -383,7 +383,7 @@ __device__ __forceinline__ bf16x8 join(const u32x2a& a, const u32x2a& b)
 }
 
 template <int KIND, bool AK, bool BKM, int SIZE>
-__global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const FfnGemm g)
+__global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const FfnGemms gs)
 {
     using S = Shape<SIZE>;
     constexpr int TM = S::TM, H = S::H, MI = S::MI, LA = S::kLoadsA;
@@ -394,8 +394,11 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
     __shared__ __attribute__((aligned(16))) uint16_t lds_a0[TM * BK], lds_a1[TM * BK];
     __shared__ __attribute__((aligned(16))) uint16_t lds_b00[H * BK], lds_b01[H * BK];
     __shared__ __attribute__((aligned(16))) uint16_t lds_b10[H * BK], lds_b11[H * BK];
+    // the weight gradients' two products are one launch
+    const bool other = !AK && blockIdx.x >= gs.blocks;
+    const FfnGemm& g = gs.g[other];
     Work w;
-    if (!decode_work(g, w)) return;
+    if (!decode_work(g, blockIdx.x - (other ? gs.blocks : 0), w)) return;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = PHASES ? wave >> 1 : wave, wn = PHASES ? wave & 1 : 0;
@@ -820,14 +823,20 @@ __global__ __launch_bounds__(256) void k_ffn_zero(uint16_t* __restrict__ p, int6
 }
 
 template <int KIND, bool AK, bool BKM>
-hipError_t launch_kind(const FfnGemm& g, hipStream_t stream)
+hipError_t launch_kind(const FfnGemm& one, const FfnGemm* two, hipStream_t stream)
 {
-    const int64_t total = int64_t(g.tiles_m) * g.tiles_n * g.batch * g.splits;
-    const dim3 grid(static_cast<unsigned>((total + 7) / 8 * 8));
-    if (g.tile == kFfnTile256)
+    auto blocks = [](const FfnGemm& g) {   // whole rounds over the XCDs
+        return (int64_t(g.tiles_m) * g.tiles_n * g.batch * g.splits + 7) / 8 * 8;
+    };
+    FfnGemms g{};
+    g.g[0] = one;
+    g.blocks = static_cast<uint32_t>(blocks(one));
+    if (two) g.g[1] = *two;
+    const dim3 grid(g.blocks + static_cast<uint32_t>(two ? blocks(*two) : 0));
+    if (one.tile == kFfnTile256)
         hipLaunchKernelGGL((k_ffn_gemm<KIND, AK, BKM, kFfnTile256>), grid,
                            dim3(Shape<kFfnTile256>::kThreads), 0, stream, g);
-    else if (g.tile == kFfnTile128)
+    else if (one.tile == kFfnTile128)
         hipLaunchKernelGGL((k_ffn_gemm<KIND, AK, BKM, kFfnTile128>), grid,
                            dim3(Shape<kFfnTile128>::kThreads), 0, stream, g);
     else
@@ -838,25 +847,35 @@ hipError_t launch_kind(const FfnGemm& g, hipStream_t stream)
 
 }  // namespace
 
+static hipError_t launch_join(const FfnGemm& g, hipStream_t stream)
+{
+    if (!g.partial) return hipSuccess;
+    const int64_t vectors = (g.M * g.N + 7) / 8;
+    hipLaunchKernelGGL(k_ffn_join, dim3(static_cast<unsigned>((vectors + 255) / 256), g.batch),
+                       dim3(256), 0, stream, g);
+    return hipGetLastError();
+}
+
 hipError_t launch_ffn_gemm(const FfnGemm& g, hipStream_t stream)
 {
     hipError_t err;
     if (g.kind == kFfnGateUp)
-        err = launch_kind<kFfnGateUp, true, true>(g, stream);
+        err = launch_kind<kFfnGateUp, true, true>(g, nullptr, stream);
     else if (g.kind == kFfnGateGrad)
-        err = launch_kind<kFfnGateGrad, true, false>(g, stream);
-    else if (g.a_rows_k)
-        err = launch_kind<kFfnPlain, false, false>(g, stream);
+        err = launch_kind<kFfnGateGrad, true, false>(g, nullptr, stream);
     else if (g.b_rows_k)
-        err = launch_kind<kFfnPlain, true, false>(g, stream);
+        err = launch_kind<kFfnPlain, true, false>(g, nullptr, stream);
     else
-        err = launch_kind<kFfnPlain, true, true>(g, stream);
-    if (err != hipSuccess || !g.partial) return err;
-    const int64_t vectors = (g.M * g.N + 7) / 8;
-    hipLaunchKernelGGL(k_ffn_join,
-                       dim3(static_cast<unsigned>((vectors + 255) / 256), g.batch),
-                       dim3(256), 0, stream, g);
-    return hipGetLastError();
+        err = launch_kind<kFfnPlain, true, true>(g, nullptr, stream);
+    return err == hipSuccess ? launch_join(g, stream) : err;
+}
+
+hipError_t launch_ffn_weight_grads(const FfnGemm& one, const FfnGemm& two, hipStream_t stream)
+{
+    if (one.tile != two.tile) return hipErrorInvalidValue;
+    hipError_t err = launch_kind<kFfnPlain, false, false>(one, &two, stream);
+    if (err == hipSuccess) err = launch_join(one, stream);
+    return err == hipSuccess ? launch_join(two, stream) : err;
 }
 
 hipError_t launch_ffn_pads(const FfnPads& p, hipStream_t stream)

@@ -69,7 +69,7 @@ struct FfnGemm {
     int32_t kind;
     int32_t act;
     int32_t tile;                // kFfnTile*
-    bool a_rows_k, b_rows_k;     // the operand is stored as rows of k
+    bool b_rows_k;               // B is stored as rows of k (with A in the weight gradients)
     const uint16_t* a[2];        // by segment of the sum, or by batch entry
     const uint16_t* b[2];        // by segment of the sum, or gate and up
     int64_t lda, ldb;
@@ -89,7 +89,13 @@ struct FfnGemm {
     uint8_t* uexps;
     int64_t groups;              // exponents per row
 };
+struct FfnGemms {
+    FfnGemm g[2];
+    uint32_t blocks;             // workgroups of the first
+};
 hipError_t launch_ffn_gemm(const FfnGemm& g, hipStream_t stream);
+// Two plain products whose operands are both stored as rows of k, of one tile size.
+hipError_t launch_ffn_weight_grads(const FfnGemm& one, const FfnGemm& two, hipStream_t stream);
 
 // One forward product of a few tokens (ffn_tokens.hip): o[t][n] = sum_k x[t][k] w[n][k] over
 // dense rows of K, or act(G) U of two such products where w[1] is given.

@@ -22,7 +22,7 @@ inline int64_t ffn_up8(int64_t a) { return (a + 7) / 8 * 8; }
 struct FfnTile {
     int32_t tile = kFfnTile128;
     int32_t splits = 1;
-    int32_t tiles_m = 0, tiles_n = 0, stages = 0;
+    int32_t stages = 0;
     double us = 0.0;
 };
 
@@ -53,29 +53,38 @@ inline double ffn_sum_us(int32_t tile, int64_t groups, int64_t stages, FfnEpilog
     return us;
 }
 
-// The tile and split with the least estimated time for C (M x N, `batch` of them), summed over
-// `segments` of K. `halves`: the tile's columns are two matrices' (gate and up). `may_split`:
-// the sum may be cut into parts, whose float32 results are written, and read by a second kernel.
-inline FfnTile ffn_choose(int64_t M, int64_t N, int64_t K, int batch, int segments, bool halves,
+// One launch's results: C of M x N, `batch` of them.
+struct FfnResult {
+    int64_t M, N;
+    int batch;
+};
+
+// The tile and split with the least estimated time for `n` results (one, or two in one launch)
+// summed over `segments` of K. `halves`: the tile's columns are two matrices' (gate and up).
+// `may_split`: the sum may be cut into parts, whose float32 results are written, and read by a
+// second kernel.
+inline FfnTile ffn_choose(const FfnResult* r, int n, int64_t K, int segments, bool halves,
                           bool may_split, FfnEpilogue epilogue)
 {
     FfnTile best;
+    const int64_t stages = ffn_ceil(K, kFfnDepth), all = stages * segments;
     for (int32_t tile : {kFfnTile64, kFfnTile128, kFfnTile256}) {
-        const int64_t cols = ffn_tile_cols(tile);
-        const int64_t tm = ffn_ceil(M, ffn_tile_rows(tile)), tn = ffn_ceil(N, halves ? cols / 2 : cols);
-        const int64_t stages = ffn_ceil(K, kFfnDepth), all = stages * segments;
+        const int64_t rows = ffn_tile_rows(tile), cols = ffn_tile_cols(tile) / (halves ? 2 : 1);
+        int64_t groups = 0, elems = 0;
+        for (int i = 0; i < n; ++i) {
+            groups += ffn_ceil(r[i].M, rows) * ffn_ceil(r[i].N, cols) * r[i].batch;
+            elems += r[i].M * r[i].N * r[i].batch;
+        }
         for (int64_t s : {1, 2, 3, 4, 6, 8, 12, 16}) {
             if (s > 1 && (!may_split || all / s < 4)) break;
-            double us = ffn_sum_us(tile, tm * tn * batch * s, ffn_ceil(all, s), epilogue);
+            double us = ffn_sum_us(tile, groups * s, ffn_ceil(all, s), epilogue);
             if (s > 1) {
-                const double mb = 4e-6 * double(M) * double(N) * batch * double(s);
-                us += 3.5 + mb / 4.0 + mb / 6.0;
+                const double mb = 4e-6 * double(elems) * double(s);
+                us += 3.5 * n + mb / 4.0 + mb / 6.0;
             }
-            if (best.tiles_m == 0 || us < best.us) {
+            if (best.stages == 0 || us < best.us) {
                 best.tile = tile;
                 best.splits = static_cast<int32_t>(s);
-                best.tiles_m = static_cast<int32_t>(tm);
-                best.tiles_n = static_cast<int32_t>(tn);
                 best.stages = static_cast<int32_t>(stages);
                 best.us = us;
             }
@@ -92,7 +101,7 @@ struct FfnSpace {
     int64_t partial = -1;
     int64_t bytes = 0;
     FfnTile gate_up, down;                        // forward
-    FfnTile grad_inner, dx, dw_down, dw_inner;    // backward
+    FfnTile grad_inner, dx, dw;                   // backward
 };
 
 inline int64_t ffn_partial_bytes(const FfnTile& t, int64_t M, int64_t N, int batch)
@@ -120,19 +129,20 @@ inline FfnSpace ffn_space(int64_t T, int64_t K, int64_t F, bool backward, bool c
     if (copy_f) s.w_down = take(2 * K * F8);
     s.a = take(2 * T * F8);
     if (!backward) {
-        s.gate_up = ffn_choose(T, F, K, 1, 1, true, false, kFfnActivate);
-        s.down = ffn_choose(T, K, F, 1, 1, false, true, kFfnStore);
+        const FfnResult inner = {T, F, 1}, y = {T, K, 1};
+        s.gate_up = ffn_choose(&inner, 1, K, 1, true, false, kFfnActivate);
+        s.down = ffn_choose(&y, 1, F, 1, false, true, kFfnStore);
         partial = ffn_partial_bytes(s.down, T, K, 1);
     } else {
         s.x = take(2 * T * K8);   // decoded, or copied
         s.dg = take(2 * T * F8);
         s.du = take(2 * T * F8);
-        s.grad_inner = ffn_choose(T, F, K, 1, 1, false, false, kFfnGradient);
-        s.dx = ffn_choose(T, K, F, 1, 2, false, true, kFfnStore);
-        s.dw_down = ffn_choose(K, F, T, 1, 1, false, true, kFfnStore);
-        s.dw_inner = ffn_choose(F, K, T, 2, 1, false, true, kFfnStore);
-        partial = std::max({ffn_partial_bytes(s.dx, T, K, 1), ffn_partial_bytes(s.dw_down, K, F, 1),
-                            ffn_partial_bytes(s.dw_inner, F, K, 2)});
+        const FfnResult inner = {T, F, 1}, dx = {T, K, 1}, dw[2] = {{K, F, 1}, {F, K, 2}};
+        s.grad_inner = ffn_choose(&inner, 1, K, 1, false, false, kFfnGradient);
+        s.dx = ffn_choose(&dx, 1, F, 2, false, true, kFfnStore);
+        s.dw = ffn_choose(dw, 2, T, 1, false, true, kFfnStore);
+        // the weight gradients' parts lie one after the other
+        partial = std::max(ffn_partial_bytes(s.dx, T, K, 1), ffn_partial_bytes(s.dw, K, F, 3));
     }
     if (partial) s.partial = take(partial);
     return s;

@@ -17,18 +17,14 @@ static void need(bool ok, const char* what, int64_t a, int64_t b, int64_t c)
     std::exit(1);
 }
 
-static void check_tile(const FfnTile& t, int64_t M, int64_t N, int64_t K, int batch, int segments,
-                       bool halves, bool may_split)
+static void check_tile(const FfnTile& t, int64_t M, int64_t N, int64_t K, int segments,
+                       bool may_split)
 {
-    const int64_t side = ffn_tile_rows(t.tile), wide = ffn_tile_cols(t.tile), cols = halves ? wide / 2 : wide;
-    need(int64_t(t.tiles_m) * side >= M && (t.tiles_m - 1) * side < M, "tile rows", M, N, K);
-    need(int64_t(t.tiles_n) * cols >= N && (t.tiles_n - 1) * cols < N, "tile columns", M, N, K);
+    need(t.tile == kFfnTile64 || t.tile == kFfnTile128 || t.tile == kFfnTile256, "tile", M, N, K);
     need(int64_t(t.stages) * kFfnDepth >= K && (t.stages - 1) * int64_t(kFfnDepth) < K, "stages", M,
          N, K);
     need(t.splits >= 1 && (may_split || t.splits == 1), "splits", M, N, K);
-    need(t.splits == 1 || int64_t(t.stages) * segments / t.splits >= 1, "an empty part", M, N, K);
-    need(int64_t(t.tiles_m) * t.tiles_n * batch * t.splits < 0x7ffffff0LL || M * N > (1LL << 40),
-         "tiles", M, N, K);
+    need(t.splits == 1 || int64_t(t.stages) * segments / t.splits >= 4, "a short part", M, N, K);
 }
 
 struct Region {
@@ -57,17 +53,17 @@ static void check_space(int64_t T, int64_t K, int64_t F, bool backward, bool una
     add(s.du, 2 * T * F8, backward);
     int64_t partial = 0;
     if (!backward) {
-        check_tile(s.gate_up, T, F, K, 1, 1, true, false);
-        check_tile(s.down, T, K, F, 1, 1, false, true);
+        check_tile(s.gate_up, T, F, K, 1, false);
+        check_tile(s.down, T, K, F, 1, true);
         partial = ffn_partial_bytes(s.down, T, K, 1);
     } else {
-        check_tile(s.grad_inner, T, F, K, 1, 1, false, false);
-        check_tile(s.dx, T, K, F, 1, 2, false, true);
-        check_tile(s.dw_down, K, F, T, 1, 1, false, true);
-        check_tile(s.dw_inner, F, K, T, 2, 1, false, true);
-        for (int64_t p : {ffn_partial_bytes(s.dx, T, K, 1), ffn_partial_bytes(s.dw_down, K, F, 1),
-                          ffn_partial_bytes(s.dw_inner, F, K, 2)})
-            partial = p > partial ? p : partial;
+        check_tile(s.grad_inner, T, F, K, 1, false);
+        check_tile(s.dx, T, K, F, 2, true);
+        check_tile(s.dw, K, F, T, 1, true);
+        // the two weight gradients' parts are live together
+        partial = ffn_partial_bytes(s.dx, T, K, 1);
+        const int64_t both = ffn_partial_bytes(s.dw, K, F, 1) + ffn_partial_bytes(s.dw, F, K, 2);
+        partial = both > partial ? both : partial;
     }
     add(s.partial, partial, partial > 0);
     for (size_t i = 0; i < r.size(); ++i)
