@@ -109,12 +109,16 @@ class Checkpoint8:
         self.exponents = _operand(exponents, "exponents", dev)
 
     @classmethod
-    def empty(cls, shape, device):
-        """One to be written."""
+    def like(cls, t, cols=None):
+        """One of t's shape (its last dimension `cols`, if given) and device, to be written."""
         self = cls.__new__(cls)
-        self.codes = torch.empty(shape, dtype=torch.int8, device=device)
-        self.exponents = torch.empty((*shape[:-1], -(-shape[-1] // GROUP)), dtype=torch.uint8,
-                                     device=device)
+        shape = t.shape
+        if cols is None or cols == shape[-1]:
+            cols = shape[-1]
+            self.codes = torch.empty_like(t, dtype=torch.int8)
+        else:
+            self.codes = t.new_empty((*shape[:-1], cols), dtype=torch.int8)
+        self.exponents = t.new_empty((*shape[:-1], -(-cols // GROUP)), dtype=torch.uint8)
         return self
 
     @property
@@ -133,7 +137,7 @@ class Checkpoint8:
         dev = codes.get_device()
         rows, cols = _rows(codes, "codes")
         if out is None:
-            out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+            out = torch.empty_like(codes, dtype=dtype)
         elif not out.is_contiguous():
             raise ValueError("out must be contiguous")
         else:
@@ -158,7 +162,7 @@ def checkpoint8(x, stream=None):
         x = x.contiguous()
     d = _dtype(x, "x")
     rows, cols = _rows(x, "x")
-    c = Checkpoint8.empty(x.shape, x.device)
+    c = Checkpoint8.like(x)
     _call(_library().gefen_checkpoint_encode(x.data_ptr(), d, rows, cols, c.codes.data_ptr(),
                                              c.exponents.data_ptr(), _raw_stream(dev)))
     return c
@@ -190,10 +194,10 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-6, checkpoint: bool = Fal
         residual = _operand(residual, "residual", dev, x.dtype, x.shape)
         h = torch.empty_like(x)
         rp, hp = residual.data_ptr(), h.data_ptr()
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = x.new_empty(x.shape[:-1], dtype=torch.float32)
     c = cp = ep = None
     if checkpoint:
-        c = Checkpoint8.empty(x.shape, x.device)
+        c = Checkpoint8.like(x)
         cp, ep = c.codes.data_ptr(), c.exponents.data_ptr()
     _call(_library().gefen_rms_norm(x.data_ptr(), rp, d, weight.data_ptr(), rows, cols, eps,
                                     y.data_ptr(), hp, rstd.data_ptr(), cp, ep, _raw_stream(dev)))
@@ -226,10 +230,10 @@ def rms_norm_backward(dy, saved, rstd, weight, dh=None, stream=None):
         p = dh.data_ptr()
     lib = _library()
     dx = torch.empty_like(dy)
-    dw = torch.empty(cols, dtype=torch.float32, device=dy.device)
+    dw = torch.empty_like(weight)
     n = ctypes.c_int64()
     _call(lib.gefen_rms_norm_backward_workspace(rows, cols, n))
-    ws = torch.empty(n.value, dtype=torch.uint8, device=dy.device)
+    ws = dy.new_empty(n.value, dtype=torch.uint8)
     _call(lib.gefen_rms_norm_backward(dy.data_ptr(), p, d, h, codes, exps, rstd.data_ptr(),
                                       weight.data_ptr(), rows, cols, dx.data_ptr(), dw.data_ptr(),
                                       ws.data_ptr(), n.value, _raw_stream(dev)))
@@ -260,7 +264,7 @@ def _ffn_space(lib, like, tokens, width, inner, flags, pointers):
             flags |= _UNALIGNED
     n = ctypes.c_int64()
     _call(lib.gefen_gated_ffn_workspace(tokens, width, inner, flags, n))
-    return torch.empty(n.value, dtype=torch.uint8, device=like.device), n.value
+    return like.new_empty(n.value, dtype=torch.uint8), n.value
 
 
 def gated_ffn(x, w_gate, w_up, w_down, activation: str = "silu", checkpoint: bool = False,
@@ -276,8 +280,7 @@ def gated_ffn(x, w_gate, w_up, w_down, activation: str = "silu", checkpoint: boo
     y = torch.empty_like(x)
     saved, p = None, (None,) * 4
     if checkpoint:
-        shape = (*x.shape[:-1], inner)
-        saved = Checkpoint8.empty(shape, x.device), Checkpoint8.empty(shape, x.device)
+        saved = Checkpoint8.like(x, inner), Checkpoint8.like(x, inner)
         p = tuple(q.data_ptr() for c in saved for q in (c.codes, c.exponents))
     ops = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr()
     ws, n = _ffn_space(lib, x, tokens, width, inner, 0, ops)
