@@ -118,9 +118,12 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm(const NormArgs a
     const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
     const int cols = static_cast<int>(a.cols);
     const double inv_n = 1.0 / static_cast<double>(cols);
+    constexpr bool kHold = TPR * NV < 2048;   // the widest rows read the weight again each time
     float w[NV][8];
+    if constexpr (kHold) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) load_row8<false>(a.weight, (i * TPR + lane) * 8, cols, w[i]);
+        for (int i = 0; i < NV; ++i) load_row8<false>(a.weight, (i * TPR + lane) * 8, cols, w[i]);
+    }
     // rows advance together in a workgroup: every thread takes part in the row's sum
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * kRows; base < a.rows; base += step) {
         const int64_t row = base + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
@@ -157,6 +160,7 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm(const NormArgs a
         for (int i = 0; i < NV; ++i) {
             const int e = (i * TPR + lane) * 8;
             if (a.h) store_row8<BF16>(static_cast<char*>(a.h) + at * kSize, e, n, v[i]);
+            if constexpr (!kHold) load_row8<false>(a.weight, e, cols, w[i]);
             float f[8], y[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -184,29 +188,8 @@ struct GradRow {
 template <bool BF16>
 __device__ __forceinline__ void fetch8(const void* row, int e, int n, u32x4a (&v)[BF16 ? 1 : 2])
 {
-    constexpr int kEach = BF16 ? 8 : 4;      // elements of 16 bytes
 #pragma unroll
-    for (int b = 0; b < (BF16 ? 1 : 2); ++b) {
-        v[b] = u32x4a{0u, 0u, 0u, 0u};
-        const int at = e + b * kEach;
-        if (at + kEach <= n) {
-            v[b] = load16(static_cast<const char*>(row) + at * (BF16 ? 2 : 4));
-        } else if (at < n) {   // all loads together, the last element for those past it
-            uint32_t t[kEach];
-#pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                const int i = at + j < n ? at + j : n - 1;
-                t[j] = BF16 ? static_cast<uint32_t>(static_cast<const uint16_t*>(row)[i])
-                            : static_cast<const uint32_t*>(row)[i];
-            }
-#pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (at + j < n) {
-                    if constexpr (BF16) v[b][j >> 1] |= t[j] << (16 * (j & 1));
-                    else v[b][j] = t[j];
-                }
-        }
-    }
+    for (int b = 0; b < (BF16 ? 1 : 2); ++b) v[b] = load_vector<BF16 ? 2 : 4>(row, e + 4 * b, n);
 }
 
 template <bool BF16>
@@ -231,10 +214,11 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
     const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
     const int cols = static_cast<int>(a.cols);
     const float inv_n = 1.0f / static_cast<float>(cols);
+    constexpr bool kHold = TPR * NV < 2048;
     float w[NV][8], dw[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        load_row8<false>(a.weight, (i * TPR + lane) * 8, cols, w[i]);
+        if constexpr (kHold) load_row8<false>(a.weight, (i * TPR + lane) * 8, cols, w[i]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
     }
@@ -263,8 +247,10 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
     Row next;
     if (first < a.rows) fetch(first, next);
     for (int64_t base = first; base < a.rows; base += step) {
+        // the widest rows' registers hold one row: it is fetched here
+        if (!kHold && base != first) fetch(base, next);
         const Row r = next;
-        if (base + step < a.rows) fetch(base + step, next);
+        if (kHold && base + step < a.rows) fetch(base + step, next);
         const int64_t row = base + sub;
         const bool on = row < a.rows;
         float d[NV][8], v[NV][8];
@@ -274,6 +260,7 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
             const float scale = CODES ? act8_scale(r.ex[i]) : r.rstd;
             // past the row's end dy is zero; a NaN group's scale is not to reach the sum there
             const bool some = (i * TPR + lane) * 8 < cols;
+            if constexpr (!kHold) load_row8<false>(a.weight, (i * TPR + lane) * 8, cols, w[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 float n;
@@ -405,13 +392,13 @@ hipError_t launch_act8_decode(const int8_t* codes, const uint8_t* exps, const fl
 }
 
 // The kernel for a row width: a wave per row while the row fits its registers, else a workgroup.
-#define GEFEN_NORM_WIDTHS(LAUNCH)                                                          \
+#define GEFEN_NORM_WIDTHS(LAUNCH, T8, N8)                                                  \
     do {                                                                                   \
         if (cols <= 512) LAUNCH(64, 1);                                                    \
         else if (cols <= 1024) LAUNCH(64, 2);                                              \
         else if (cols <= 2048) LAUNCH(256, 1);                                             \
         else if (cols <= 4096) LAUNCH(256, 2);                                             \
-        else if (cols <= 8192) LAUNCH(512, 2);                                             \
+        else if (cols <= 8192) LAUNCH(T8, N8);                                             \
         else LAUNCH(1024, 2);                                                              \
     } while (0)
 
@@ -433,7 +420,7 @@ hipError_t launch_rms_norm(const NormArgs& a, bool bf16, hipStream_t stream)
             hipLaunchKernelGGL((k_rms_norm<false, TPR, NV>), grid,                         \
                                dim3(kNormThreads(TPR)), 0, stream, a, groups);             \
     } while (0)
-    GEFEN_NORM_WIDTHS(LAUNCH);
+    GEFEN_NORM_WIDTHS(LAUNCH, 1024, 1);
 #undef LAUNCH
     return hipGetLastError();
 }
@@ -467,7 +454,7 @@ hipError_t launch_rms_norm_grad(const NormGradArgs& a, bool bf16, hipStream_t st
         else if (a.codes) LAUNCH_AS(false, true, TPR, NV);                                 \
         else LAUNCH_AS(false, false, TPR, NV);                                             \
     } while (0)
-    GEFEN_NORM_WIDTHS(LAUNCH);
+    GEFEN_NORM_WIDTHS(LAUNCH, 512, 2);
 #undef LAUNCH
 #undef LAUNCH_AS
     hipError_t err = hipGetLastError();

@@ -42,57 +42,71 @@ __device__ __forceinline__ uint16_t bf16_bits(float x)
     return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
 }
 
-// Elements e .. e + 7 of a row of n at `row`, as float32; zero from n on. At a row's end the last
-// element is read in the place of those past it: all loads go out together, where a branch round
-// each waited for the one before (the 15 last codes of a row took 10 us).
+// At a row's end the last whole vector of the row is loaded instead and shifted down, so that
+// every vector is one load (element by element, each waiting for the one before, the 15 last
+// codes of a row took 10 us). w >> bits, zeros from above; bits from 128 on give 0.
+__device__ __forceinline__ u32x4a shift_down(const u32x4a& w, uint32_t bits)
+{
+    uint64_t lo = w[0] | (static_cast<uint64_t>(w[1]) << 32);
+    uint64_t hi = w[2] | (static_cast<uint64_t>(w[3]) << 32);
+    if (bits >= 64) {
+        lo = bits >= 128 ? 0 : hi >> (bits - 64);
+        hi = 0;
+    } else if (bits > 0) {
+        lo = (lo >> bits) | (hi << (64 - bits));
+        hi >>= bits;
+    }
+    return u32x4a{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32),
+                  static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
+}
+
+// The 16 bytes of elements of SIZE bytes from element e of a row of n on; zero from n on. (e is a
+// multiple of their number.)
+template <int SIZE, typename I>
+__device__ __forceinline__ u32x4a load_vector(const void* row, I e, I n)
+{
+    constexpr int kCount = 16 / SIZE;
+    const char* p = static_cast<const char*>(row);
+    if (n >= kCount) {
+        const I at = e < n - kCount ? e : n - kCount;
+        const u32x4a w = load16(p + at * SIZE);
+        if (e == at) return w;
+        return shift_down(w, e - at < kCount ? static_cast<uint32_t>(e - at) * 8 * SIZE : 128u);
+    }
+    u32x4a w = {0u, 0u, 0u, 0u};   // a row shorter than a vector
+    if (e == 0) {
+#pragma unroll
+        for (int j = 0; j < kCount - 1; ++j)
+            if (j < n) {
+                if constexpr (SIZE == 4) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+                else if constexpr (SIZE == 2)
+                    w[j >> 1] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[j])
+                                 << (16 * (j & 1));
+                else w[j >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(p[j])) << (8 * (j & 3));
+            }
+    }
+    return w;
+}
+
+// Elements e .. e + 7 of a row of n at `row`, as float32; zero from n on.
 template <bool BF16, typename I>
 __device__ __forceinline__ void load_row8(const void* row, I e, I n, float (&v)[8])
 {
-    if (e + 8 <= n) {
-        if constexpr (BF16) {
-            const u32x4a w = load16(static_cast<const uint16_t*>(row) + e);
+    if constexpr (BF16) {
+        const u32x4a w = load_vector<2>(row, e, n);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[2 * j] = bf16_float(w[j]);
-                v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-            }
-        } else {
-            const u32x4a a = load16(static_cast<const float*>(row) + e);
-            const u32x4a b = load16(static_cast<const float*>(row) + e + 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] = __uint_as_float(a[j]);
-                v[4 + j] = __uint_as_float(b[j]);
-            }
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = bf16_float(w[j]);
+            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-        if (e < n) {
-            float t[8];
+        for (int b = 0; b < 2; ++b) {
+            const u32x4a w = load_vector<4>(row, static_cast<I>(e + 4 * b), n);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const I at = e + j < n ? e + j : n - 1;
-                t[j] = BF16 ? bf16_float(static_cast<const uint16_t*>(row)[at])
-                            : static_cast<const float*>(row)[at];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = e + j < n ? t[j] : 0.0f;
+            for (int j = 0; j < 4; ++j) v[4 * b + j] = __uint_as_float(w[j]);
         }
     }
-}
-
-// COUNT consecutive bytes of a row of n from e < n on, packed, zero from n on; in the same way.
-template <int COUNT, typename I>
-__device__ __forceinline__ void load_tail(const int8_t* __restrict__ row, I e, I n, uint32_t* w)
-{
-    uint32_t t[COUNT];
-#pragma unroll
-    for (int j = 0; j < COUNT; ++j)
-        t[j] = static_cast<uint8_t>(row[e + j < n ? e + j : n - 1]);
-#pragma unroll
-    for (int j = 0; j < COUNT; ++j)
-        if (e + j < n) w[j >> 2] |= t[j] << (8 * (j & 3));
 }
 
 template <bool BF16, typename I>
@@ -249,10 +263,21 @@ __device__ __forceinline__ void act8_write_products(const float (&v)[8], double 
 template <typename I>
 __device__ __forceinline__ u32x2a act8_codes8(const int8_t* __restrict__ codes, I e, I n)
 {
-    if (e + 8 <= n) return load8b(codes + e);
-    uint32_t w[2] = {0u, 0u};
-    if (e < n) load_tail<8>(codes, e, n, w);
-    return u32x2a{w[0], w[1]};
+    if (n >= 8) {
+        const I at = e < n - 8 ? e : n - 8;
+        const u32x2a w = load8b(codes + at);
+        if (e == at) return w;
+        const uint64_t v = (w.x | (static_cast<uint64_t>(w.y) << 32));
+        const uint64_t r = e - at < 8 ? v >> (8 * static_cast<uint32_t>(e - at)) : 0;
+        return u32x2a{static_cast<uint32_t>(r), static_cast<uint32_t>(r >> 32)};
+    }
+    u32x2a w = {0u, 0u};
+    if (e == 0) {
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < n) w[j >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(codes[j])) << (8 * (j & 3));
+    }
+    return w;
 }
 
 // Elements e .. e + 7 of a checkpointed row of n; zero from n on.

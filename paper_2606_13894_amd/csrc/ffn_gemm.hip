@@ -167,7 +167,7 @@ __device__ __forceinline__ float activation(float g, float& slope)
 {
     float z = g, dz = 1.0f;
     if (ACT == kActGelu) {
-        const float s = g * g;
+        const float s = fminf(g * g, 1e30f);   // an infinite z' times a zero would be NaN
         z = 1.5957691216057308f * g * fmaf(0.044715f, s, 1.0f);
         if (SLOPE) dz = 1.5957691216057308f * fmaf(0.134145f, s, 1.0f);
     }
@@ -211,10 +211,7 @@ __device__ __forceinline__ void write_codes(const float (&v)[16], int64_t c, int
 template <bool FULL>
 __device__ __forceinline__ u32x4a read_codes(const int8_t* __restrict__ row, int64_t c, int64_t n)
 {
-    if (FULL || c + 16 <= n) return load16(row + c);
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-    if (c < n) load_tail<16>(row, c, n, w);
-    return u32x4a{w[0], w[1], w[2], w[3]};
+    return FULL ? load16(row + c) : load_vector<1>(row, c, n);
 }
 
 // Fragments of a stage's two 32-deep steps from rows of k, of 16-wide blocks at the byte
@@ -640,6 +637,11 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
             float gv[16], uv[16];
             to_run(acc[mi][0], gv);
             to_run(acc[mi][1], uv);
+            if (!FULL && c + 16 > g.N) {   // (an infinity in x makes NaN of the zeros there)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (c + i >= g.N) gv[i] = uv[i] = 0.0f;
+            }
             if (g.gcodes) {
                 write_codes<FULL>(gv, c, g.N, q, g.gcodes + row * g.N, g.gexps + row * g.groups,
                                   on);

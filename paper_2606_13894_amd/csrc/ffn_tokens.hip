@@ -20,18 +20,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // Elements k .. k + 7 of a row of `n`; zero from n on.
 __device__ __forceinline__ bf16x8 row_piece(const uint16_t* __restrict__ row, int k, int n)
 {
-    u32x4a v = {0u, 0u, 0u, 0u};
-    if (k + 8 <= n) {
-        v = load16(row + k);
-    } else if (k < n) {   // all loads together, the last element for those past it
-        uint32_t t[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = row[k + j < n ? k + j : n - 1];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (k + j < n) v[j >> 1] |= t[j] << (16 * (j & 1));
-    }
-    return __builtin_bit_cast(bf16x8, v);
+    return __builtin_bit_cast(bf16x8, load_vector<2>(row, k, n));
 }
 
 template <bool DUAL, int R, int W>

@@ -438,6 +438,47 @@ def test_ffn_edges(dev):
     assert all(torch.isfinite(g).all() for g in gb)
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_ffn_huge_gates(dev, act):
+    """Gates whose square passes float32: the activation is the gate or zero, its slope one or
+    zero, as the formulas' limits are."""
+    T, K, F = 40, 64, 96
+    x, wg, wu, wd, dy = _ffn_inputs(dev, T, K, F, seed=7)
+    wg, wd = (wg.float() * 2.0 ** 70).to(BF16), (wd.float() * 2.0 ** -70).to(BF16)
+    y, saved = gf.gated_ffn(x, wg, wu, wd, act, checkpoint=True)
+    assert torch.isfinite(y).all()
+    grads = gf.gated_ffn_backward(dy, x, saved, wg, wu, wd, act)
+    assert all(torch.isfinite(g).all() for g in grads)
+    g, u = _decode64(saved[0]), _decode64(saved[1])
+    big = g.abs() > 2.0 ** 40            # all but the codes 0
+    on = (big & (g > 0)).to(F64)
+    da = dy.to(F64) @ wd.to(F64)
+    keep = big | (g == 0)
+    assert keep.all()
+    slope = torch.where(g == 0, torch.full_like(g, 0.5), on)
+    dg = da * u * slope
+    want = dg.t() @ x.to(F64)
+    _within(grads[1], want, ROUND * want.abs() * 1.02 + (2 * ROUND * dg.abs()).t() @ x.to(F64).abs(),
+            "dw_gate")
+    a = torch.where(g > 0, g, torch.zeros_like(g)) * u
+    want = dy.to(F64).t() @ a
+    _within(grads[3], want, ROUND * want.abs() * 1.02 + dy.to(F64).abs().t() @ (2 * ROUND * a.abs()),
+            "dw_down")
+
+
+def test_ffn_infinity_stays_infinity(dev):
+    """An infinite input and positive weights: infinite outputs, whatever is padded."""
+    T, K, F = 3, 20, 13
+    x = torch.ones(T, K, dtype=BF16, device=dev)
+    x[1, 4] = math.inf
+    w = torch.full((F, K), 0.5, dtype=BF16, device=dev)
+    wd = torch.full((K, F), 0.5, dtype=BF16, device=dev)
+    for save in (False, True):           # the kernels for a few tokens, and the tiles
+        y = gf.gated_ffn(x, w, w, wd, checkpoint=save)
+        y = y[0] if save else y
+        assert torch.isinf(y[1]).all() and torch.isfinite(y[[0, 2]]).all()
+
+
 def test_rows_past_32_bits(dev):
     """More than 2^31 elements: the last rows are what the same rows give alone. (The block's
     products take other tiles and splits then, so that their sums' order differs.)"""
