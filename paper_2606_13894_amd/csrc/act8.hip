@@ -132,18 +132,24 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm(const NormArgs a
         const int64_t at = on ? row * cols : 0;
         float v[NV][8];
         double s = 0.0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            load_row8<BF16>(static_cast<const char*>(a.x) + at * kSize, (i * TPR + lane) * 8, n,
-                            v[i]);
-        if (a.r) {
+        {
+            u32x4a x[NV][BF16 ? 1 : 2], r[NV][BF16 ? 1 : 2];
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                float q[8];
-                load_row8<BF16>(static_cast<const char*>(a.r) + at * kSize, (i * TPR + lane) * 8,
-                                n, q);
+                const int e = (i * TPR + lane) * 8;
+                fetch8<BF16>(static_cast<const char*>(a.x) + at * kSize, e, n, x[i]);
+                if (a.r) fetch8<BF16>(static_cast<const char*>(a.r) + at * kSize, e, n, r[i]);
+            }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] += q[j];
+            for (int i = 0; i < NV; ++i) {
+                const int e = (i * TPR + lane) * 8;
+                settle8<BF16>(x[i], e, n, v[i]);
+                if (a.r) {
+                    float q[8];
+                    settle8<BF16>(r[i], e, n, q);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[i][j] += q[j];
+                }
             }
         }
 #pragma unroll
@@ -185,22 +191,6 @@ struct GradRow {
     float rstd;
 };
 
-template <bool BF16>
-__device__ __forceinline__ void fetch8(const void* row, int e, int n, u32x4a (&v)[BF16 ? 1 : 2])
-{
-#pragma unroll
-    for (int b = 0; b < (BF16 ? 1 : 2); ++b) v[b] = load_vector<BF16 ? 2 : 4>(row, e + 4 * b, n);
-}
-
-template <bool BF16>
-__device__ __forceinline__ float element(const u32x4a (&v)[BF16 ? 1 : 2], int j)
-{
-    if constexpr (BF16)
-        return j & 1 ? __uint_as_float(v[0][j >> 1] & 0xffff0000u) : bf16_float(v[0][j >> 1]);
-    else
-        return __uint_as_float(v[j >> 2][j & 3]);
-}
-
 template <bool BF16, bool CODES, int TPR, int NV>
 __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormGradArgs a,
                                                                      int64_t groups)
@@ -235,7 +225,7 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
             fetch8<BF16>(static_cast<const char*>(a.dy) + at * kSize, e, n, r.dy[i]);
             if constexpr (CODES) {
                 r.ex[i] = e < n ? a.exps[(on ? row : 0) * groups + (e >> 6)] : 0u;
-                const u32x2a c = act8_codes8(a.codes + at, e, n);
+                const u32x2a c = fetch_codes8(a.codes + at, e, n);
                 r.h[i][0] = u32x4a{c.x, c.y, 0u, 0u};
             } else {
                 fetch8<BF16>(static_cast<const char*>(a.h) + at * kSize, e, n, r.h[i]);
@@ -257,21 +247,25 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const float scale = CODES ? act8_scale(r.ex[i]) : r.rstd;
-            // past the row's end dy is zero; a NaN group's scale is not to reach the sum there
-            const bool some = (i * TPR + lane) * 8 < cols;
-            if constexpr (!kHold) load_row8<false>(a.weight, (i * TPR + lane) * 8, cols, w[i]);
+            const int e = (i * TPR + lane) * 8, n = on ? cols : 0;
+            settle8<BF16>(r.dy[i], e, n, d[i]);
+            if constexpr (CODES) {
+                const float scale = act8_scale(r.ex[i]);
+                const u32x2a c = settle_codes8(u32x2a{r.h[i][0].x, r.h[i][0].y}, e, n);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)   // a NaN group's scale is not to reach past the row
+                    v[i][j] = e + j < n ? act8_value(c[j >> 2], j & 3) * scale : 0.0f;
+            } else {
+                settle8<BF16>(r.h[i], e, n, v[i]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] *= r.rstd;
+            }
+            if constexpr (!kHold) load_row8<false>(a.weight, e, cols, w[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float n;
-                if constexpr (CODES) n = act8_value(r.h[i][0][j >> 2], j & 3) * scale;
-                else n = element<BF16>(r.h[i], j) * scale;
-                if (CODES && (!some || (i * TPR + lane) * 8 + j >= cols)) n = 0.0f;
-                v[i][j] = n;
-                d[i][j] = element<BF16>(r.dy[i], j);
-                dw[i][j] = fmaf(d[i][j], n, dw[i][j]);
+                dw[i][j] = fmaf(d[i][j], v[i][j], dw[i][j]);
                 d[i][j] *= w[i][j];
-                s = fmaf(d[i][j], n, s);
+                s = fmaf(d[i][j], v[i][j], s);
             }
         }
         s = row_sum<TPR>(s, red);
@@ -280,12 +274,12 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
         const int64_t at = row * cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float g[8];
+            const int e = (i * TPR + lane) * 8;
+            float g[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            if (a.dh) settle8<BF16>(r.dh[i], e, cols, g);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                g[j] = fmaf(r.rstd, fmaf(-v[i][j], c, d[i][j]),
-                            a.dh ? element<BF16>(r.dh[i], j) : 0.0f);
-            store_row8<BF16>(static_cast<char*>(a.dx) + at * kSize, (i * TPR + lane) * 8, cols, g);
+            for (int j = 0; j < 8; ++j) g[j] = fmaf(r.rstd, fmaf(-v[i][j], c, d[i][j]), g[j]);
+            store_row8<BF16>(static_cast<char*>(a.dx) + at * kSize, e, cols, g);
         }
     }
     if constexpr (kRows > 1) {

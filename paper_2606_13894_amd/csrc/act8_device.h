@@ -61,18 +61,14 @@ __device__ __forceinline__ u32x4a shift_down(const u32x4a& w, uint32_t bits)
 }
 
 // The 16 bytes of elements of SIZE bytes from element e of a row of n on; zero from n on. (e is a
-// multiple of their number.)
+// multiple of their number.) In two steps, so that several vectors' loads can go out before the
+// first is shifted: what lies at e or, past the row's last whole vector, that one; and its shift.
 template <int SIZE, typename I>
-__device__ __forceinline__ u32x4a load_vector(const void* row, I e, I n)
+__device__ __forceinline__ u32x4a fetch_vector(const void* row, I e, I n)
 {
     constexpr int kCount = 16 / SIZE;
     const char* p = static_cast<const char*>(row);
-    if (n >= kCount) {
-        const I at = e < n - kCount ? e : n - kCount;
-        const u32x4a w = load16(p + at * SIZE);
-        if (e == at) return w;
-        return shift_down(w, e - at < kCount ? static_cast<uint32_t>(e - at) * 8 * SIZE : 128u);
-    }
+    if (n >= kCount) return load16(p + (e < n - kCount ? e : n - kCount) * SIZE);
     u32x4a w = {0u, 0u, 0u, 0u};   // a row shorter than a vector
     if (e == 0) {
 #pragma unroll
@@ -87,26 +83,55 @@ __device__ __forceinline__ u32x4a load_vector(const void* row, I e, I n)
     }
     return w;
 }
+template <int SIZE, typename I>
+__device__ __forceinline__ u32x4a settle_vector(const u32x4a& w, I e, I n)
+{
+    constexpr int kCount = 16 / SIZE;
+    if (n < kCount || e + kCount <= n) return w;
+    const I past = e + kCount - n;
+    return shift_down(w, past < kCount ? static_cast<uint32_t>(past) * 8 * SIZE : 128u);
+}
+template <int SIZE, typename I>
+__device__ __forceinline__ u32x4a load_vector(const void* row, I e, I n)
+{
+    return settle_vector<SIZE>(fetch_vector<SIZE>(row, e, n), e, n);
+}
+
+// Eight elements, bfloat16 or float32, in the same two steps.
+template <bool BF16, typename I>
+__device__ __forceinline__ void fetch8(const void* row, I e, I n, u32x4a (&v)[BF16 ? 1 : 2])
+{
+#pragma unroll
+    for (int b = 0; b < (BF16 ? 1 : 2); ++b)
+        v[b] = fetch_vector<BF16 ? 2 : 4>(row, static_cast<I>(e + 4 * b), n);
+}
+template <bool BF16, typename I>
+__device__ __forceinline__ void settle8(const u32x4a (&w)[BF16 ? 1 : 2], I e, I n, float (&v)[8])
+{
+    if constexpr (BF16) {
+        const u32x4a t = settle_vector<2>(w[0], e, n);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = bf16_float(t[j]);
+            v[2 * j + 1] = __uint_as_float(t[j] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const u32x4a t = settle_vector<4>(w[b], static_cast<I>(e + 4 * b), n);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * b + j] = __uint_as_float(t[j]);
+        }
+    }
+}
 
 // Elements e .. e + 7 of a row of n at `row`, as float32; zero from n on.
 template <bool BF16, typename I>
 __device__ __forceinline__ void load_row8(const void* row, I e, I n, float (&v)[8])
 {
-    if constexpr (BF16) {
-        const u32x4a w = load_vector<2>(row, e, n);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[2 * j] = bf16_float(w[j]);
-            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const u32x4a w = load_vector<4>(row, static_cast<I>(e + 4 * b), n);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[4 * b + j] = __uint_as_float(w[j]);
-        }
-    }
+    u32x4a w[BF16 ? 1 : 2];
+    fetch8<BF16>(row, e, n, w);
+    settle8<BF16>(w, e, n, v);
 }
 
 template <bool BF16, typename I>
@@ -259,18 +284,11 @@ __device__ __forceinline__ void act8_write_products(const float (&v)[8], double 
     act8_store_group(w, ex, e, n, codes, exps);
 }
 
-// Codes e .. e + 7 of a row of n; zero from n on.
+// Codes e .. e + 7 of a row of n; zero from n on; in the same two steps.
 template <typename I>
-__device__ __forceinline__ u32x2a act8_codes8(const int8_t* __restrict__ codes, I e, I n)
+__device__ __forceinline__ u32x2a fetch_codes8(const int8_t* __restrict__ codes, I e, I n)
 {
-    if (n >= 8) {
-        const I at = e < n - 8 ? e : n - 8;
-        const u32x2a w = load8b(codes + at);
-        if (e == at) return w;
-        const uint64_t v = (w.x | (static_cast<uint64_t>(w.y) << 32));
-        const uint64_t r = e - at < 8 ? v >> (8 * static_cast<uint32_t>(e - at)) : 0;
-        return u32x2a{static_cast<uint32_t>(r), static_cast<uint32_t>(r >> 32)};
-    }
+    if (n >= 8) return load8b(codes + (e < n - 8 ? e : n - 8));
     u32x2a w = {0u, 0u};
     if (e == 0) {
 #pragma unroll
@@ -278,6 +296,15 @@ __device__ __forceinline__ u32x2a act8_codes8(const int8_t* __restrict__ codes, 
             if (j < n) w[j >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(codes[j])) << (8 * (j & 3));
     }
     return w;
+}
+template <typename I>
+__device__ __forceinline__ u32x2a settle_codes8(const u32x2a& w, I e, I n)
+{
+    if (n < 8 || e + 8 <= n) return w;
+    const I past = e + 8 - n;
+    const uint64_t v = w.x | (static_cast<uint64_t>(w.y) << 32);
+    const uint64_t r = past < 8 ? v >> (8 * static_cast<uint32_t>(past)) : 0;
+    return u32x2a{static_cast<uint32_t>(r), static_cast<uint32_t>(r >> 32)};
 }
 
 // Elements e .. e + 7 of a checkpointed row of n; zero from n on.
@@ -287,7 +314,7 @@ __device__ __forceinline__ void act8_read8(const int8_t* __restrict__ codes,
                                            float (&v)[8])
 {
     const float s = e < n ? act8_scale(exps[e >> 6]) : 0.0f;
-    const u32x2a w = act8_codes8(codes, e, n);
+    const u32x2a w = settle_codes8(fetch_codes8(codes, e, n), e, n);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = act8_value(w[j >> 2], j & 3) * s;
     if (e + 8 > n) {   // a NaN group's padding is zero too

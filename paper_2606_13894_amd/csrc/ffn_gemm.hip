@@ -808,13 +808,14 @@ __global__ __launch_bounds__(256) void k_ffn_pad(const FfnPads p)
                 ++row[i];
             }
         }
-        float v[4][8];
+        u32x4a v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            load_row8<true>(m.src + row[i] * m.cols, 8 * e[i], row[i] < m.rows ? m.cols : 0, v[i]);
+            v[i] = fetch_vector<2>(m.src + row[i] * m.cols, 8 * e[i], row[i] < m.rows ? m.cols : 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (row[i] < m.rows) store_row8<true>(m.dst + row[i] * m.ldd, 8 * e[i], m.ldd, v[i]);
+            if (row[i] < m.rows)
+                store16(m.dst + row[i] * m.ldd + 8 * e[i], settle_vector<2>(v[i], 8 * e[i], m.cols));
     }
 }
 
