@@ -14,6 +14,8 @@ namespace {
 // ---------------------------------------------------------------- encode and decode
 // A workgroup takes 256 vectors: 2^lx lanes along a row (a whole number of groups) by
 // 256 >> lx rows. Rows that are whole groups long are one long row to these kernels.
+// 8192 x 8192 bfloat16: encode 41.0 us, decode 39.2 (5 TB/s each, a large copy's rate); one
+// row of 2048 1.8 and 3.8, a launch's time.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_act8_encode(const void* __restrict__ x, int64_t rows,
                                                      int64_t cols, int64_t groups, int lx,
@@ -107,7 +109,10 @@ __device__ __forceinline__ double inverse_root(double x)
 
 // The sum of squares and rstd are in 64 bits, and so are the products that the codes are rounded
 // from: a checkpoint's code is the formula's, whatever the order of the sum (the pass is bound by
-// memory: no time is lost).
+// memory: no time is lost). A row's vectors are all fetched before the first is used; 4096
+// workgroups at most, so that a row's wait is covered by other workgroups'. 8192 x 2048 bfloat16
+// with a residual and a checkpoint: 26.6 us (5.7 TB/s); 1000 x 1601 float32 6.5. Rows of 4096
+// run at 5.4 TB/s, of 8192 to 16384 at 4.2.
 template <bool BF16, int TPR, int NV>
 __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm(const NormArgs a, int64_t groups)
 {
@@ -180,10 +185,7 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm(const NormArgs a
     }
 }
 
-// dn = dy w;  dx = rstd (dn - n mean(dn n)) + dh;  dw = the sum over rows of dy n. A workgroup
-// keeps its rows' share of dw in registers and writes it once; k_norm_dw adds the shares in
-// order, so that dw does not depend on timing. The next row's vectors are on their way while a
-// row is worked on.
+// A row's vectors as they were loaded.
 template <bool BF16, bool CODES, int NV>
 struct GradRow {
     u32x4a dy[NV][BF16 ? 1 : 2], dh[NV][BF16 ? 1 : 2], h[NV][BF16 ? 1 : 2];   // h: codes in one half
@@ -191,6 +193,13 @@ struct GradRow {
     float rstd;
 };
 
+// dn = dy w;  dx = rstd (dn - n mean(dn n)) + dh;  dw = the sum over rows of dy n. A workgroup
+// keeps its rows' share of dw in registers and writes it once; k_norm_dw adds the shares in
+// order, so that dw does not depend on timing. The next row's vectors are on their way while a
+// row is worked on, so few workgroups are enough (768: three to a CU) and the shares stay small.
+// Bound by memory: 8192 x 2048 bfloat16 from codes 23.8 us (4.9 TB/s) and 4.2 for k_norm_dw;
+// 1023 x 768 float32 5.5 and 3.4, launches. Rows of 4096 and 8192 run at 4.4 TB/s, wider ones at
+// 2.0: their vectors do not all fit the 128 registers of a 1024-thread workgroup.
 template <bool BF16, bool CODES, int TPR, int NV>
 __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormGradArgs a,
                                                                      int64_t groups)
@@ -305,7 +314,8 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
 }
 
 // dw[c] = the sum over p of partial[p][c]: a workgroup takes 16 columns, 64 threads each, so that
-// a thread's few loads are all in flight at once; the threads' sums are added in order.
+// a thread's few loads are all in flight at once; the threads' sums are added in order. 768 shares
+// of 2048 columns (6.3 MB, from the L2 and the last-level cache): 4.2 us.
 __global__ __launch_bounds__(1024) void k_norm_dw(const float* __restrict__ partial, int64_t parts,
                                                   int64_t cols, float* __restrict__ dw)
 {

@@ -9,16 +9,29 @@
 // consecutive k of its column.
 //
 // A workgroup computes a 256 x 256 tile with eight waves (4 x 2 of 64 x 128), or a 128 x 128 or
-// 64 x 128 tile with four (4 x 1 of 32 x 128, 16 x 128) where that fills the chip better. Tiles of 64 k are loaded
-// straight into LDS (no registers) through buffer resources, whose range check gives zeros past
-// the operand's rows; two LDS stages, the next one in flight while the current one feeds the
-// matrix cores, one barrier per stage. LDS rows are not padded: 16-byte pieces (32-byte ones
-// for rows of k) are permuted within a row by its low bits, on the loading side through the
-// lane's global address, so that fragment reads hit distinct banks.
+// 64 x 128 tile with four (4 x 1 of 32 x 128, 16 x 128) where that fills the chip better. Stages
+// of 64 k are loaded straight into LDS (no registers) through buffer resources, whose range
+// check gives zeros past the operand's rows; a stage is used in two parts (B's column halves)
+// and the loads of the next parts stay in flight while one feeds the matrix cores. In the
+// largest tile the waves are two groups, one part behind the other, so that one group's matrix
+// instructions cover the other's LDS reads. LDS rows are not padded: 16-byte pieces (32-byte
+// ones for rows of k) are permuted within a row by its low bits, on the loading side through
+// the lane's global address, so that fragment reads hit distinct banks (counters: no conflict).
 //
 // The products are computed as C^T (the n fragment is the instruction's first operand), so
-// that after one exchange between the wave's halves a lane holds 16 consecutive n of one row
+// that after an exchange among the four lanes of a row a lane holds 16 consecutive n of one row
 // m: the epilogues work on such runs and store them as whole 16-byte pieces, without LDS.
+//
+// Bound by the matrix cores and the card's power at large sizes. 8192 tokens, 2048 to 8192
+// columns and back (flops of the product alone; the card's plain large product reaches 1.42
+// PFLOP/s, the library's six products of these sizes 1.16 to 1.60):
+//   gate/up 446 us (1.23 PFLOP/s with the checkpoints), down 187 (1.47), the gradients of the
+//   gate 325 (0.85: over a quarter of it is the epilogue, whose reads and writes come in bursts since
+//   all workgroups reach it together), weight gradients 642 (1.28), dx 396 (1.39).
+// Smaller ones are bound by latency per stage and by the partial sums of a split product: 1000
+// tokens take 54 us for gate/up and 48 + 6 for down, of 72 at the large product's rate.
+// Measured and slower: loads between the matrix instructions, a stage's A loaded for two parts
+// at once, 32-k stages, 32 x 32 x 16 instructions, smaller tiles for the gate's gradients.
 //
 // Epilogues:
 //   gate/up   the wave's 128 columns are 64 of the gate and the same 64 of the up product:
@@ -765,7 +778,8 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
     }
 }
 
-// o[b] = the sum over the splits, in order, of the partial products, times the column factors.
+// o[b] = the sum over the splits, in order, of the partial products, times the column factors. The
+// partial sums come from the L2 and the last-level cache: 5.6 us for 1000 x 2048.
 __global__ __launch_bounds__(256) void k_ffn_join(const FfnGemm g)
 {
     const int64_t e = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
@@ -787,8 +801,11 @@ __global__ __launch_bounds__(256) void k_ffn_join(const FfnGemm g)
     store_row8<true>(g.o[b], e, plane, s);   // the output is dense
 }
 
-// dst (rows of ldd, a multiple of 8) = src (dense rows of `cols`), zero past them. A thread takes
-// four vectors of eight, 256 apart in the flat order, all loaded before the first is stored.
+// dst (rows of ldd, a multiple of 8) = src (dense rows of `cols`), zero past them: rows of odd
+// widths are copied to 16-byte alignment once, so that the products' loads to LDS are whole. A
+// thread takes four vectors of eight, 256 apart in the flat order, all loaded before the first is
+// stored. Memory and a launch: 9.7 us a pass for 777 tokens and three weights of 765 x 2047 (21 MB
+// read and written).
 __global__ __launch_bounds__(256) void k_ffn_pad(const FfnPads p)
 {
     const FfnPad& m = p.m[blockIdx.y];

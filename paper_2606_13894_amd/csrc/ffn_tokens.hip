@@ -6,8 +6,12 @@
 // R = 8, for up to 8 tokens: 8 rows x 64 k, the second 32 k as eight more rows against eight more
 // columns of the same tokens, whose other halves are not used: a row's cache line is loaded whole
 // by one instruction, and twice as many workgroups share the matrix. Rows need no alignment and k
-// no multiple: a lane's 16 bytes are loaded at any address, the last ones of a row element by
-// element. The waves' float32 sums are added through LDS, in order.
+// no multiple: a lane's 16 bytes are loaded at any address, the row's last whole
+// vector shifted at its end. The waves' float32 sums are added through LDS, in order.
+//
+// One token, 2048 to 8192 columns and back: gate/up 12.9 us (67 MB, 5.2 TB/s), down 7.8 (34 MB,
+// 4.3 TB/s). Weight loads that bypass the caches were 2 % faster on cold weights (27.4 us against
+// 28.0 a call) and 20 % slower where a small model's weights stay in the caches, so they are plain.
 #include "act8_device.h"
 #include "ffn_internal.h"
 
