@@ -193,13 +193,31 @@ struct GradRow {
     float rstd;
 };
 
+// The compiler no longer knows what a row's vectors hold.
+template <bool BF16, bool CODES, int NV>
+__device__ __forceinline__ void hide(GradRow<BF16, CODES, NV>& r)
+{
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int b = 0; b < (BF16 ? 1 : 2); ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t p = r.dy[i][b][j], q = r.h[i][b][j];
+                asm volatile("" : "+v"(p), "+v"(q));
+                r.dy[i][b][j] = p;
+                r.h[i][b][j] = q;
+            }
+}
+
 // dn = dy w;  dx = rstd (dn - n mean(dn n)) + dh;  dw = the sum over rows of dy n. A workgroup
 // keeps its rows' share of dw in registers and writes it once; k_norm_dw adds the shares in
 // order, so that dw does not depend on timing. The next row's vectors are on their way while a
 // row is worked on, so few workgroups are enough (768: three to a CU) and the shares stay small.
 // Bound by memory: 8192 x 2048 bfloat16 from codes 23.8 us (4.9 TB/s) and 4.2 for k_norm_dw;
-// 1023 x 768 float32 5.5 and 3.4, launches. Rows of 4096 and 8192 run at 4.4 TB/s, wider ones at
-// 2.0: their vectors do not all fit the 128 registers of a 1024-thread workgroup.
+// 1023 x 768 float32 5.5 and 3.4, launches. Rows of 4096 and 8192 run at 4.4 TB/s, of 16384 at
+// 3.1 (2.8 in float32; 2.0 before their values were formed twice): a 1024-thread workgroup has 128
+// registers to a lane, which hold one row as it was loaded and dw.
 template <bool BF16, bool CODES, int TPR, int NV>
 __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormGradArgs a,
                                                                      int64_t groups)
@@ -213,7 +231,7 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
     const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
     const int cols = static_cast<int>(a.cols);
     const float inv_n = 1.0f / static_cast<float>(cols);
-    constexpr bool kHold = TPR * NV < 2048;
+    constexpr bool kHold = TPR * NV < 2048;   // the widest rows: one to a workgroup
     float w[NV][8], dw[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -239,23 +257,24 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
             } else {
                 fetch8<BF16>(static_cast<const char*>(a.h) + at * kSize, e, n, r.h[i]);
             }
-            if (a.dh) fetch8<BF16>(static_cast<const char*>(a.dh) + at * kSize, e, n, r.dh[i]);
+            if (kHold && a.dh)   // else when dx is formed
+                fetch8<BF16>(static_cast<const char*>(a.dh) + at * kSize, e, n, r.dh[i]);
         }
     };
     const int64_t first = static_cast<int64_t>(blockIdx.x) * kRows;
     Row next;
-    if (first < a.rows) fetch(first, next);
+    if (kHold && first < a.rows) fetch(first, next);
     for (int64_t base = first; base < a.rows; base += step) {
-        // the widest rows' registers hold one row: it is fetched here
-        if (!kHold && base != first) fetch(base, next);
-        const Row r = next;
+        // the widest rows' registers do not hold two rows: the row is fetched here, and what is
+        // formed of it is formed again after its sum
+        if constexpr (!kHold) fetch(base, next);
+        Row r = next;
         if (kHold && base + step < a.rows) fetch(base + step, next);
         const int64_t row = base + sub;
         const bool on = row < a.rows;
         float d[NV][8], v[NV][8];
         float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
+        auto values = [&](int i) {   // d = dy and v = n of the row's vector i
             const int e = (i * TPR + lane) * 8, n = on ? cols : 0;
             settle8<BF16>(r.dy[i], e, n, d[i]);
             if constexpr (CODES) {
@@ -270,6 +289,11 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
                 for (int j = 0; j < 8; ++j) v[i][j] *= r.rstd;
             }
             if constexpr (!kHold) load_row8<false>(a.weight, e, cols, w[i]);
+        };
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            values(i);
+            if constexpr (!kHold) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 dw[i][j] = fmaf(d[i][j], v[i][j], dw[i][j]);
@@ -278,13 +302,22 @@ __global__ __launch_bounds__(kNormThreads(TPR)) void k_rms_norm_grad(const NormG
             }
         }
         s = row_sum<TPR>(s, red);
+        if constexpr (!kHold) hide(r);   // so that the values are formed again, not kept
         if (!on) continue;
         const float c = s * inv_n;
         const int64_t at = row * cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int e = (i * TPR + lane) * 8;
+            if constexpr (!kHold) {
+                __builtin_amdgcn_sched_barrier(0);
+                values(i);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[i][j] *= w[i][j];
+            }
             float g[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            if (!kHold && a.dh)   // dx may be dh: of a shifted vector only the lane's own count
+                fetch8<BF16>(static_cast<const char*>(a.dh) + at * kSize, e, cols, r.dh[i]);
             if (a.dh) settle8<BF16>(r.dh[i], e, cols, g);
 #pragma unroll
             for (int j = 0; j < 8; ++j) g[j] = fmaf(r.rstd, fmaf(-v[i][j], c, d[i][j]), g[j]);

@@ -6,6 +6,7 @@ by at most n 2^-24 of the sum of their magnitudes. Matrix products of rounded ma
 bounded by those two, term by term: with A rounded, |error of A W| <= 2^-8 |A| |W| + (n 2^-24) |A|
 |W|, and 2^-8 of the result for the output's own rounding. float32 functions (exp, division,
 square root) are taken as 16 units in the last place, 2^-20."""
+import ctypes
 import math
 
 import pytest
@@ -250,6 +251,48 @@ def test_norm_edges(dev):
     off = _randn(dev, 3 * 101 + 1, seed=4).to(BF16)[1:].view(3, 101)
     w1 = torch.ones(102, device=dev)[1:]
     assert torch.equal(gf.rms_norm(off, w1).y, gf.rms_norm(off.clone(), w1.clone()).y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [5, 100, 777, 1601, 2048, 4099, 8191, 8201, 8205, 12289, 16384])
+def test_norm_in_place(dev, cols, dtype):
+    """y and h may be x or the residual, dx may be dy or dh: the same bits either way."""
+    lib, p = gf.load_library(), lambda t: None if t is None else t.data_ptr()
+    rows, dt = 1000 if cols < 4000 else 300, {"bf16": BF16, "f32": F32}[dtype]
+    d = gf.BF16 if dt is BF16 else gf.F32
+    stream = torch.cuda.current_stream().cuda_stream
+    x, r, dy, dh = (_randn(dev, rows, cols, seed=i, dtype=dt) for i in range(4))
+    w = 1 + 0.1 * _randn(dev, cols, seed=5)
+    rstd = torch.empty(rows, device=dev)
+
+    def forward(a, b, y, h):
+        assert lib.gefen_rms_norm(p(a), p(b), d, p(w), rows, cols, 1e-6, p(y), p(h), p(rstd), None,
+                                  None, stream) == 0
+        return y, h
+
+    y, h = forward(x, r, torch.empty_like(x), torch.empty_like(x))
+    for swap in (False, True):
+        a, b = x.clone(), r.clone()
+        got = forward(a, b, b, a) if swap else forward(a, b, a, b)
+        assert torch.equal(got[0], y) and torch.equal(got[1], h)
+
+    n = ctypes.c_int64()
+    assert lib.gefen_rms_norm_backward_workspace(rows, cols, ctypes.byref(n)) == 0
+    ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
+    code = gf.checkpoint8(h.float() * rstd[:, None])
+
+    def backward(a, b, dx, saved):
+        dw = torch.empty(cols, device=dev)
+        of = (p(h), None, None) if saved == "h" else (None, p(code.codes), p(code.exponents))
+        assert lib.gefen_rms_norm_backward(p(a), p(b), d, *of, p(rstd), p(w), rows, cols, p(dx),
+                                           p(dw), p(ws), n.value, stream) == 0
+        return dx, dw
+
+    for saved in ("h", "codes"):
+        want = backward(dy, dh, torch.empty_like(dy), saved)
+        a, b = dy.clone(), dh.clone()
+        for got in (backward(a, dh, a, saved), backward(dy, b, b, saved)):
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 # ------------------------------------------------------------------ the gated block
