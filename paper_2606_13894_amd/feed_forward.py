@@ -91,6 +91,15 @@ def _call(code):
         _check(code)
 
 
+def _saved(c, what, dev, shape):
+    """The codes' and exponents' addresses of checkpoint c, after its checks."""
+    if not isinstance(c, Checkpoint8) or c.codes.shape != shape:
+        raise ValueError(f"{what} must be a Checkpoint8 of shape {tuple(shape)}")
+    if c.codes.get_device() != dev:
+        raise ValueError(f"{what} is on {c.codes.device}, not on the current device")
+    return c.codes.data_ptr(), c.exponents.data_ptr()
+
+
 class Checkpoint8:
     """An 8-bit checkpoint of a tensor: ``codes`` int8, shaped as it, and ``exponents`` uint8, one
     per group of 64 elements of the last dimension. Element = code * 2^(exponent - 127)."""
@@ -134,7 +143,7 @@ class Checkpoint8:
         if stream is not None:
             return _on(stream, self.decode, dtype, gain, out)
         codes = self.codes
-        dev = codes.get_device()
+        dev = _device(codes, "codes")
         rows, cols = _rows(codes, "codes")
         if out is None:
             out = torch.empty_like(codes, dtype=dtype)
@@ -218,9 +227,7 @@ def rms_norm_backward(dy, saved, rstd, weight, dh=None, stream=None):
     rstd = _operand(rstd, "rstd", dev, torch.float32, dy.shape[:-1])
     h = codes = exps = None
     if isinstance(saved, Checkpoint8):
-        if saved.codes.shape != dy.shape:
-            raise ValueError(f"saved has shape {tuple(saved.shape)}, expected {tuple(dy.shape)}")
-        codes, exps = saved.codes.data_ptr(), saved.exponents.data_ptr()
+        codes, exps = _saved(saved, "saved", dev, dy.shape)
     else:
         saved = _operand(saved, "saved", dev, dy.dtype, dy.shape)
         h = saved.data_ptr()
@@ -300,15 +307,12 @@ def gated_ffn_backward(dy, x, saved, w_gate, w_up, w_down, activation: str = "si
     dev, dy, tokens, width, inner, w_gate, w_up, w_down, act = _ffn_operands(
         dy, "dy", w_gate, w_up, w_down, activation)
     gate, up = saved
-    for c, what in ((gate, "the gate's checkpoint"), (up, "the up projection's checkpoint")):
-        if not isinstance(c, Checkpoint8) or c.codes.shape != (*dy.shape[:-1], inner):
-            raise ValueError(f"{what} must be a Checkpoint8 of shape "
-                             f"{(*dy.shape[:-1], inner)}")
+    inside = (*dy.shape[:-1], inner)
+    gate = _saved(gate, "the gate's checkpoint", dev, inside)
+    up = _saved(up, "the up projection's checkpoint", dev, inside)
     xp = codes = exps = gp = None
     if isinstance(x, Checkpoint8):
-        if x.codes.shape != dy.shape:
-            raise ValueError(f"x has shape {tuple(x.shape)}, expected {tuple(dy.shape)}")
-        codes, exps = x.codes.data_ptr(), x.exponents.data_ptr()
+        codes, exps = _saved(x, "x", dev, dy.shape)
         if gain is not None:
             gain = _operand(gain, "gain", dev, torch.float32, (width,))
             gp = gain.data_ptr()
@@ -323,10 +327,8 @@ def gated_ffn_backward(dy, x, saved, w_gate, w_up, w_down, activation: str = "si
     dp, w = dy.data_ptr(), (w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr())
     ws, n = _ffn_space(lib, dy, tokens, width, inner, _BACKWARD, (dp, xp, *w))
     _call(lib.gefen_gated_ffn_backward(
-        dp, xp, codes, exps, gp, gate.codes.data_ptr(), gate.exponents.data_ptr(),
-        up.codes.data_ptr(), up.exponents.data_ptr(), *w, tokens, width, inner, act,
-        dx.data_ptr(), dwg.data_ptr(), dwu.data_ptr(), dwd.data_ptr(), ws.data_ptr(), n,
-        _raw_stream(dev)))
+        dp, xp, codes, exps, gp, *gate, *up, *w, tokens, width, inner, act, dx.data_ptr(),
+        dwg.data_ptr(), dwu.data_ptr(), dwd.data_ptr(), ws.data_ptr(), n, _raw_stream(dev)))
     return dx, dwg, dwu, dwd
 
 
