@@ -332,6 +332,24 @@ def gated_ffn_backward(dy, x, saved, w_gate, w_up, w_down, activation: str = "si
     return dx, dwg, dwu, dwd
 
 
+class _NoGraph(torch.autograd.Function):
+    """Kernel results under autograd: they carry no graph, so that a gradient through them is an
+    error and not a missing share."""
+
+    @staticmethod
+    def forward(ctx, anchor, what, *results):
+        ctx.what = what
+        return tuple(r.view_as(r) for r in results)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(ctx.what)
+
+
+def _no_graph(what, *results):
+    return _NoGraph.apply(torch.ones((), requires_grad=True), what, *results)
+
+
 class _Block(torch.autograd.Function):
     """y, h = the gated block of rms_norm(x + residual), and h, saved in 8 bits."""
 
@@ -348,11 +366,15 @@ class _Block(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy, dh):
         nw, wg, wu, wd, rstd, nc, ne, gc, ge, uc, ue = ctx.saved_tensors
-        saved = Checkpoint8(nc, ne)
-        dn, dwg, dwu, dwd = gated_ffn_backward(
-            dy, saved, (Checkpoint8(gc, ge), Checkpoint8(uc, ue)), wg, wu, wd, ctx.activation,
-            gain=nw)
-        dx, dnw = rms_norm_backward(dn, saved, rstd, nw, dh)
+        with torch.no_grad():
+            saved = Checkpoint8(nc, ne)
+            dn, dwg, dwu, dwd = gated_ffn_backward(
+                dy, saved, (Checkpoint8(gc, ge), Checkpoint8(uc, ue)), wg, wu, wd,
+                ctx.activation, gain=nw)
+            dx, dnw = rms_norm_backward(dn, saved, rstd, nw, dh)
+        if torch.is_grad_enabled():   # create_graph
+            dx, dnw, dwg, dwu, dwd = _no_graph("FeedForward has no second derivative",
+                                               dx, dnw, dwg, dwu, dwd)
         return dx, dx if ctx.residual else None, dnw, dwg, dwu, dwd, None, None
 
 
@@ -360,8 +382,9 @@ class FeedForward(torch.nn.Module):
     """The feed-forward half of a transformer block: ``y, h = ff(x, residual)`` with
     h = x + residual and y the gated block of the RMS norm of h (so that h + y, or h as the next
     residual of y, goes on). Parameters are float32, as the optimizers take them, and cast to
-    bfloat16 in each call; x and residual are bfloat16. The backward pass keeps the normalised
-    rows and both projections in 8 bits and nothing else of that size."""
+    bfloat16 in each call; x and residual are bfloat16. A second derivative is an error. The
+    backward pass keeps the normalised rows and both projections in 8 bits and nothing else of that
+    size."""
 
     def __init__(self, width: int, inner: int, activation: str = "silu", eps: float = 1e-6,
                  device=None):

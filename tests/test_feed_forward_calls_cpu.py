@@ -84,3 +84,52 @@ def test_backward_takes_checkpoints_of_its_device_only(launched):
         with pytest.raises(ValueError, match="current device"):
             call()
     assert launched == []
+
+
+# ------------------------------------------------------------------ second derivatives
+@pytest.fixture
+def block(monkeypatch):
+    """``FeedForward`` with y = 3 x in the place of its kernels: their results, made of raw memory,
+    carry no graph."""
+    class Saved:
+        def __init__(self, codes, exponents):
+            self.codes, self.exponents = codes, exponents
+
+    def norm(x, weight, residual=None, eps=1e-6, checkpoint=False, stream=None):
+        return gf.RMSNormOutput(x.detach().clone(), x if residual is None else (x + residual).detach(),
+                                x.detach()[..., 0], Saved(x.detach(), x.detach()))
+
+    def ffn(x, *weights, checkpoint=False, **kw):
+        y = 3.0 * x.detach()
+        return (y, (Saved(y, y), Saved(y, y))) if checkpoint else y
+
+    def ffn_backward(dy, x, saved, wg, wu, wd, *a, **kw):
+        return 3.0 * dy.detach(), *(torch.zeros_like(w) for w in (wg, wu, wd))
+
+    def norm_backward(dy, saved, rstd, weight, dh=None):
+        return dy.detach() + dh.detach(), torch.zeros_like(weight)
+
+    for name, f in (("Checkpoint8", Saved), ("rms_norm", norm), ("gated_ffn", ffn),
+                    ("gated_ffn_backward", ffn_backward), ("rms_norm_backward", norm_backward)):
+        monkeypatch.setattr(ff, name, f)
+    return ff.FeedForward(8, 4)
+
+
+@pytest.mark.parametrize("linear", [False, True])
+def test_second_derivative_is_an_error(block, linear):
+    """A gradient penalty whose gradient has another path to x: the block's share was left out."""
+    x = torch.randn(3, 8, requires_grad=True)
+    y, h = block(x)
+    out = y.sum() if linear else y.square().sum()
+    (g,) = torch.autograd.grad(out + h.pow(3).sum() + x.pow(3).sum(), x, create_graph=True)
+    assert torch.isfinite(g).all()                  # the gradient itself is there
+    with pytest.raises(RuntimeError, match="second derivative"):
+        g.square().sum().backward()
+
+
+def test_first_derivative_keeps_no_graph(block):
+    x = torch.randn(3, 8, requires_grad=True)
+    y, h = block(x)
+    (y.sum() + h.sum()).backward()
+    assert torch.equal(x.grad, torch.full_like(x, 4.0)) and x.grad.grad_fn is None
+    assert block.w_up.grad is not None and not block.w_up.grad.requires_grad
