@@ -11,7 +11,8 @@ per saved activation.
 ``include/gefen.h`` gives each operator's formula, types and limits. Tensors are device tensors
 of any leading dimensions (rows are all but the last); ones that are not contiguous are copied.
 All calls are asynchronous on ``stream`` (the current torch stream by default), where their
-outputs and workspaces are allocated.
+outputs and workspaces are allocated. Only ``FeedForward`` has an autograd form: where an
+argument of the other calls wants a gradient, a gradient through their results is an error.
 """
 from __future__ import annotations
 
@@ -100,6 +101,40 @@ def _saved(c, what, dev, shape):
     return c.codes.data_ptr(), c.exponents.data_ptr()
 
 
+class _NoGraph(torch.autograd.Function):
+    """A kernel's result under autograd: it carries no graph, so that a gradient through it is an
+    error and not a missing share. The tensor itself is returned."""
+
+    @staticmethod
+    def forward(ctx, anchor, what, result):
+        ctx.what = what
+        ctx.mark_dirty(result)
+        return result
+
+    @staticmethod
+    def backward(ctx, grad):
+        raise RuntimeError(ctx.what)
+
+
+def _no_graph(what, *results):
+    anchor = torch.ones((), requires_grad=True)
+    for r in results:
+        _NoGraph.apply(anchor, what, r)
+
+
+def _tracked(*tensors):
+    """Whether autograd would want a graph from them to the results."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
+
+
+_FORWARD = " has no gradient of its own: FeedForward has (or call it under torch.no_grad())"
+_BACKWARD_ONLY = "the results of {} cannot be differentiated"
+
+
 class Checkpoint8:
     """An 8-bit checkpoint of a tensor: ``codes`` int8, shaped as it, and ``exponents`` uint8, one
     per group of 64 elements of the last dimension. Element = code * 2^(exponent - 127)."""
@@ -158,6 +193,8 @@ class Checkpoint8:
             p = gain.data_ptr()
         _call(_library().gefen_checkpoint_decode(codes.data_ptr(), self.exponents.data_ptr(), p,
                                                  rows, cols, out.data_ptr(), d, _raw_stream(dev)))
+        if _tracked(gain):
+            _no_graph("decode" + _FORWARD, out)
         return out
 
 
@@ -210,6 +247,8 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-6, checkpoint: bool = Fal
         cp, ep = c.codes.data_ptr(), c.exponents.data_ptr()
     _call(_library().gefen_rms_norm(x.data_ptr(), rp, d, weight.data_ptr(), rows, cols, eps,
                                     y.data_ptr(), hp, rstd.data_ptr(), cp, ep, _raw_stream(dev)))
+    if _tracked(x, weight, residual):
+        _no_graph("rms_norm" + _FORWARD, y, rstd, *(() if h is x else (h,)))
     return RMSNormOutput(y, h, rstd, c)
 
 
@@ -244,6 +283,8 @@ def rms_norm_backward(dy, saved, rstd, weight, dh=None, stream=None):
     _call(lib.gefen_rms_norm_backward(dy.data_ptr(), p, d, h, codes, exps, rstd.data_ptr(),
                                       weight.data_ptr(), rows, cols, dx.data_ptr(), dw.data_ptr(),
                                       ws.data_ptr(), n.value, _raw_stream(dev)))
+    if _tracked(dy, dh):
+        _no_graph(_BACKWARD_ONLY.format("rms_norm_backward"), dx, dw)
     return dx, dw
 
 
@@ -293,6 +334,8 @@ def gated_ffn(x, w_gate, w_up, w_down, activation: str = "silu", checkpoint: boo
     ws, n = _ffn_space(lib, x, tokens, width, inner, 0, ops)
     _call(lib.gefen_gated_ffn(*ops, tokens, width, inner, act, y.data_ptr(), *p, ws.data_ptr(), n,
                               _raw_stream(dev)))
+    if _tracked(x, w_gate, w_up, w_down):
+        _no_graph("gated_ffn" + _FORWARD, y)
     return (y, saved) if checkpoint else y
 
 
@@ -329,25 +372,9 @@ def gated_ffn_backward(dy, x, saved, w_gate, w_up, w_down, activation: str = "si
     _call(lib.gefen_gated_ffn_backward(
         dp, xp, codes, exps, gp, *gate, *up, *w, tokens, width, inner, act, dx.data_ptr(),
         dwg.data_ptr(), dwu.data_ptr(), dwd.data_ptr(), ws.data_ptr(), n, _raw_stream(dev)))
+    if _tracked(dy):
+        _no_graph(_BACKWARD_ONLY.format("gated_ffn_backward"), dx, dwg, dwu, dwd)
     return dx, dwg, dwu, dwd
-
-
-class _NoGraph(torch.autograd.Function):
-    """Kernel results under autograd: they carry no graph, so that a gradient through them is an
-    error and not a missing share."""
-
-    @staticmethod
-    def forward(ctx, anchor, what, *results):
-        ctx.what = what
-        return tuple(r.view_as(r) for r in results)
-
-    @staticmethod
-    def backward(ctx, *grads):
-        raise RuntimeError(ctx.what)
-
-
-def _no_graph(what, *results):
-    return _NoGraph.apply(torch.ones((), requires_grad=True), what, *results)
 
 
 class _Block(torch.autograd.Function):
@@ -373,8 +400,7 @@ class _Block(torch.autograd.Function):
                 ctx.activation, gain=nw)
             dx, dnw = rms_norm_backward(dn, saved, rstd, nw, dh)
         if torch.is_grad_enabled():   # create_graph
-            dx, dnw, dwg, dwu, dwd = _no_graph("FeedForward has no second derivative",
-                                               dx, dnw, dwg, dwu, dwd)
+            _no_graph("FeedForward has no second derivative", dx, dnw, dwg, dwu, dwd)
         return dx, dx if ctx.residual else None, dnw, dwg, dwu, dwd, None, None
 
 

@@ -133,3 +133,58 @@ def test_first_derivative_keeps_no_graph(block):
     (y.sum() + h.sum()).backward()
     assert torch.equal(x.grad, torch.full_like(x, 4.0)) and x.grad.grad_fn is None
     assert block.w_up.grad is not None and not block.w_up.grad.requires_grad
+
+
+# ------------------------------------------------------------------ plain calls under autograd
+def _calls(x, w, wg, wd):
+    n = gf.rms_norm(x, w, residual=x, checkpoint=True)
+    yield from ((n.y, "rms_norm"), (n.h, "rms_norm"), (n.rstd, "rms_norm"))
+    yield gf.rms_norm(x, w).y, "rms_norm"
+    yield gf.gated_ffn(x, wg, wg, wd), "gated_ffn"
+    yield gf.gated_ffn(x, wg, wg, wd, checkpoint=True)[0], "gated_ffn"
+
+
+@pytest.mark.parametrize("which", range(3))
+def test_plain_calls_do_not_cut_the_graph_silently(launched, which):
+    """The calls have no autograd form: a gradient through one is refused instead of missing."""
+    ops = [_tensor(_On0, 3, 100), _tensor(_On0, 100, dtype=F32), _tensor(_On0, 40, 100),
+           _tensor(_On0, 100, 40)]
+    ops[which].requires_grad_(True)
+    flagged = [name for y, name in _calls(*ops) if y.requires_grad]
+    assert flagged == {0: ["rms_norm"] * 4 + ["gated_ffn"] * 2, 1: ["rms_norm"] * 4,
+                       2: ["gated_ffn"] * 2}[which]
+    for y, name in _calls(*ops):
+        if y.requires_grad:
+            with pytest.raises(RuntimeError, match=name + ".* FeedForward"):
+                y.float().sum().backward()
+    with torch.no_grad():
+        assert not any(y.requires_grad for y, _ in _calls(*ops))
+
+
+def test_norm_without_residual_passes_x_on(launched):
+    x = _tensor(_On0, 3, 100).requires_grad_(True)
+    assert gf.rms_norm(x, _tensor(_On0, 100, dtype=F32)).h is x
+
+
+def test_decode_and_backward_calls_do_not_cut_the_graph_silently(launched):
+    x = _checkpoint(_On0, 3, 100)
+    gain = _tensor(_On0, 100, dtype=F32).requires_grad_(True)
+    assert not x.decode().requires_grad
+    with pytest.raises(RuntimeError, match="decode"):
+        x.decode(gain=gain).float().sum().backward()
+    w, rstd = _tensor(_On0, 40, 100).requires_grad_(True), _tensor(_On0, 3, dtype=F32)
+    dy, inner = _tensor(_On0, 3, 100), _checkpoint(_On0, 3, 40)
+    wd = _tensor(_On0, 100, 40)
+
+    def results(dy, dh=None):
+        return (*gf.rms_norm_backward(dy, x, rstd, gain, dh=dh),
+                *gf.gated_ffn_backward(dy, x, (inner, inner), w, w, wd))
+
+    # parameters are what a hand-written step holds: its gradients stay plain tensors
+    assert not any(t.requires_grad for t in results(dy))
+    for t in results(dy.clone().requires_grad_(True)):
+        with pytest.raises(RuntimeError, match="backward"):
+            t.float().sum().backward()
+    dx = results(dy, dy.clone().requires_grad_(True))[0]
+    with pytest.raises(RuntimeError, match="rms_norm_backward"):
+        dx.float().sum().backward()
