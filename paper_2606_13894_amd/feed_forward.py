@@ -410,7 +410,7 @@ class FeedForward(torch.nn.Module):
     residual of y, goes on). Parameters are float32, as the optimizers take them, and cast to
     bfloat16 in each call; x and residual are bfloat16. A second derivative is an error. The
     backward pass keeps the normalised rows and both projections in 8 bits and nothing else of that
-    size."""
+    size; where no gradient is wanted nothing is saved, and few tokens take the kernels for them."""
 
     def __init__(self, width: int, inner: int, activation: str = "silu", eps: float = 1e-6,
                  device=None):
@@ -428,5 +428,9 @@ class FeedForward(torch.nn.Module):
 
     def forward(self, x, residual=None):
         bf16 = torch.bfloat16
-        return _Block.apply(x, residual, self.norm, self.w_gate.to(bf16), self.w_up.to(bf16),
-                            self.w_down.to(bf16), self.eps, self.activation)
+        weights = self.w_gate.to(bf16), self.w_up.to(bf16), self.w_down.to(bf16)
+        if _tracked(x, residual, self.norm, *weights):
+            return _Block.apply(x, residual, self.norm, *weights, self.eps, self.activation)
+        n = rms_norm(x, self.norm, residual, self.eps)
+        y = gated_ffn(n.y, *weights, self.activation)
+        return y, (n.h if residual is not None else x.view_as(x))
