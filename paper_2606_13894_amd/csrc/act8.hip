@@ -13,17 +13,17 @@ namespace {
 
 // ---------------------------------------------------------------- encode and decode
 // A workgroup takes 256 vectors: 2^lx lanes along a row (a whole number of groups) by
-// 256 >> lx rows. Rows that are whole groups long are one long row to these kernels.
+// 256 >> lx rows, from the workgroup `first` along a row on (RowGrid). Rows that are whole groups
+// long are one long row to these kernels.
 // 8192 x 8192 bfloat16: encode 41.0 us, decode 39.2 (5 TB/s each, a large copy's rate); one
 // row of 2048 1.8 and 3.8, a launch's time.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_act8_encode(const void* __restrict__ x, int64_t rows,
                                                      int64_t cols, int64_t groups, int lx,
-                                                     int8_t* __restrict__ codes,
+                                                     int64_t first, int8_t* __restrict__ codes,
                                                      uint8_t* __restrict__ exps)
 {
-    const int64_t e = ((static_cast<int64_t>(blockIdx.x) << lx) +
-                       (threadIdx.x & ((1 << lx) - 1))) * 8;
+    const int64_t e = (((first + blockIdx.x) << lx) + (threadIdx.x & ((1 << lx) - 1))) * 8;
     const int64_t step = static_cast<int64_t>(gridDim.y) << (8 - lx);
     for (int64_t r = (static_cast<int64_t>(blockIdx.y) << (8 - lx)) + (threadIdx.x >> lx);
          r < rows; r += step) {
@@ -39,10 +39,10 @@ __global__ __launch_bounds__(256) void k_act8_decode(const int8_t* __restrict__ 
                                                      const uint8_t* __restrict__ exps,
                                                      const float* __restrict__ gain, int64_t rows,
                                                      int64_t cols, int64_t groups, int lx,
-                                                     void* __restrict__ out, int64_t ldo)
+                                                     int64_t first, void* __restrict__ out,
+                                                     int64_t ldo)
 {
-    const int64_t e = ((static_cast<int64_t>(blockIdx.x) << lx) +
-                       (threadIdx.x & ((1 << lx) - 1))) * 8;
+    const int64_t e = (((first + blockIdx.x) << lx) + (threadIdx.x & ((1 << lx) - 1))) * 8;
     const int64_t step = static_cast<int64_t>(gridDim.y) << (8 - lx);
     float g[8];
     if (gain) load_row8<false>(gain, e, cols, g);
@@ -58,20 +58,17 @@ __global__ __launch_bounds__(256) void k_act8_decode(const int8_t* __restrict__ 
     }
 }
 
-// lx, grid for `rows` rows of `vectors` vectors, a whole number of groups.
-struct RowGrid {
-    int lx;
-    dim3 grid;
-};
-RowGrid row_grid(int64_t rows, int64_t vectors)
+// launch(grid, first workgroup along a row), until all of them have had their launch.
+template <typename Launch>
+hipError_t launch_along(const RowGrid& g, const Launch& launch)
 {
-    RowGrid g;
-    g.lx = 3;
-    while (g.lx < 8 && (int64_t(1) << g.lx) < vectors) ++g.lx;
-    const int64_t gx = (vectors + (int64_t(1) << g.lx) - 1) >> g.lx;
-    const int64_t gy = (rows + (256 >> g.lx) - 1) / (256 >> g.lx);
-    g.grid = dim3(static_cast<unsigned>(gx), static_cast<unsigned>(std::min<int64_t>(gy, 65535)));
-    return g;
+    for (int64_t first = 0; first < g.gx; first += g.most) {
+        launch(dim3(static_cast<unsigned>(std::min(g.most, g.gx - first)),
+                    static_cast<unsigned>(g.gy)), first);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
 }
 
 // ---------------------------------------------------------------- RMS norm
@@ -394,15 +391,15 @@ hipError_t launch_act8_encode(const void* x, bool bf16, int64_t rows, int64_t co
         rows = 1;
     }
     const int64_t groups = act8_groups(cols);
-    if (groups > 0x7fffffffLL) return hipErrorInvalidValue;
     const RowGrid g = row_grid(rows, groups * 8);
-    if (bf16)
-        hipLaunchKernelGGL(k_act8_encode<true>, g.grid, dim3(256), 0, stream, x, rows, cols,
-                           groups, g.lx, codes, exps);
-    else
-        hipLaunchKernelGGL(k_act8_encode<false>, g.grid, dim3(256), 0, stream, x, rows, cols,
-                           groups, g.lx, codes, exps);
-    return hipGetLastError();
+    return launch_along(g, [&](dim3 grid, int64_t first) {
+        if (bf16)
+            hipLaunchKernelGGL(k_act8_encode<true>, grid, dim3(256), 0, stream, x, rows, cols,
+                               groups, g.lx, first, codes, exps);
+        else
+            hipLaunchKernelGGL(k_act8_encode<false>, grid, dim3(256), 0, stream, x, rows, cols,
+                               groups, g.lx, first, codes, exps);
+    });
 }
 
 hipError_t launch_act8_decode(const int8_t* codes, const uint8_t* exps, const float* gain,
@@ -417,15 +414,15 @@ hipError_t launch_act8_decode(const int8_t* codes, const uint8_t* exps, const fl
         rows = 1;
     }
     const int64_t groups = act8_groups(cols);
-    if (groups > 0x7fffffffLL) return hipErrorInvalidValue;
     const RowGrid g = row_grid(rows, groups * 8);
-    if (bf16)
-        hipLaunchKernelGGL(k_act8_decode<true>, g.grid, dim3(256), 0, stream, codes, exps, gain,
-                           rows, cols, groups, g.lx, out, ldo);
-    else
-        hipLaunchKernelGGL(k_act8_decode<false>, g.grid, dim3(256), 0, stream, codes, exps, gain,
-                           rows, cols, groups, g.lx, out, ldo);
-    return hipGetLastError();
+    return launch_along(g, [&](dim3 grid, int64_t first) {
+        if (bf16)
+            hipLaunchKernelGGL(k_act8_decode<true>, grid, dim3(256), 0, stream, codes, exps, gain,
+                               rows, cols, groups, g.lx, first, out, ldo);
+        else
+            hipLaunchKernelGGL(k_act8_decode<false>, grid, dim3(256), 0, stream, codes, exps, gain,
+                               rows, cols, groups, g.lx, first, out, ldo);
+    });
 }
 
 // The kernel for a row width: a wave per row while the row fits its registers, else a workgroup.

@@ -93,6 +93,27 @@ inline FfnTile ffn_choose(const FfnResult* r, int n, int64_t K, int segments, bo
     return best;
 }
 
+// ---------------------------------------------------------------- launches
+// The checkpoint kernels' launches for `rows` rows of `vectors` vectors of eight, a whole number
+// of groups: 2^lx lanes along a row by 256 >> lx rows to a workgroup. A dispatch has fewer than
+// 2^32 threads along an axis (one row of 2^35 elements would have as many), so that of the gx
+// workgroups along a row each launch takes the next `most`. (One launch whose workgroups went on
+// along the row took 6 to 15 % longer at 8192 x 8192.) gy workgroups walk down the rows.
+struct RowGrid {
+    int lx;
+    int64_t gx, most, gy;
+};
+inline RowGrid row_grid(int64_t rows, int64_t vectors)
+{
+    RowGrid g;
+    g.lx = 3;
+    while (g.lx < 8 && (int64_t(1) << g.lx) < vectors) ++g.lx;
+    g.gx = (vectors + (int64_t(1) << g.lx) - 1) >> g.lx;
+    g.most = std::min<int64_t>(g.gx, int64_t(1) << 23);
+    g.gy = std::min<int64_t>((rows + (256 >> g.lx) - 1) / (256 >> g.lx), 65535);
+    return g;
+}
+
 // Byte offsets into the workspace; -1: not needed. T tokens, K the block's width, F its inner
 // width; rows of K8 or F8 elements are rounded up to 8 so that 16-byte loads stay aligned.
 struct FfnSpace {
