@@ -99,15 +99,18 @@ FfnGemm product(int32_t kind, const FfnTile& t, int64_t M, int64_t N, int64_t K,
     return g;
 }
 
-bool fits(const FfnGemm& g)
+// Each launch's threads are fewer than 2^32, as a dispatch has them.
+int check_launch(const FfnGemm& one, const FfnGemm* two = nullptr)
 {
-    return int64_t(g.tiles_m) * g.tiles_n * g.batch * g.splits <= 0x3ffffff0LL;
-}
-
-int run(const FfnGemm& g, hipStream_t stream)
-{
-    if (!fits(g)) return fail(GEFEN_EINVAL, "too many tiles");
-    GEFEN_HIP(launch_ffn_gemm(g, stream));
+    const int64_t threads = one.tile == kFfnTile256 ? 512 : 256;
+    int64_t groups = 0;
+    for (const FfnGemm* g : {&one, two}) {
+        if (!g) continue;
+        groups += ffn_ceil(int64_t(g->tiles_m) * g->tiles_n * g->batch * g->splits, 8) * 8;
+        if (g->partial && ffn_ceil(g->M * g->N, 8 * 256) * 256 > 0xffffffffLL)   // the parts' sum
+            return fail(GEFEN_EINVAL, "too many elements of a split sum");
+    }
+    if (groups * threads > 0xffffffffLL) return fail(GEFEN_EINVAL, "too many tiles");
     return GEFEN_OK;
 }
 
@@ -288,30 +291,33 @@ int gefen_gated_ffn(const uint16_t* x, const uint16_t* w_gate, const uint16_t* w
     const uint16_t* gp = operand(w_gate, F, K, copy_k, workspace, s.w_gate, pads);
     const uint16_t* up = operand(w_up, F, K, copy_k, workspace, s.w_up, pads);
     const uint16_t* dp = operand(w_down, K, F, copy_f, workspace, s.w_down, pads);
+
+    FfnGemm inner_product = product(kFfnGateUp, s.gate_up, T, F, K, workspace, s.partial);
+    inner_product.act = activation;
+    inner_product.a[0] = xp;
+    inner_product.b[0] = gp;
+    inner_product.b[1] = up;
+    inner_product.lda = inner_product.ldb = ffn_up8(K);
+    inner_product.o[0] = at<uint16_t>(workspace, s.a);
+    inner_product.ldo = ffn_up8(F);
+    inner_product.gcodes = gate_codes;
+    inner_product.ucodes = up_codes;
+    inner_product.gexps = gate_exponents;
+    inner_product.uexps = up_exponents;
+    inner_product.groups = act8_groups(F);
+
+    FfnGemm down = product(kFfnPlain, s.down, T, K, F, workspace, s.partial);
+    down.a[0] = at<uint16_t>(workspace, s.a);
+    down.b[0] = dp;
+    down.lda = down.ldb = ffn_up8(F);
+    down.o[0] = y;
+    down.ldo = K;
+
+    if ((rc = check_launch(inner_product)) || (rc = check_launch(down))) return rc;
     GEFEN_HIP(launch_ffn_pads(pads, stream));
-
-    FfnGemm g = product(kFfnGateUp, s.gate_up, T, F, K, workspace, s.partial);
-    g.act = activation;
-    g.a[0] = xp;
-    g.b[0] = gp;
-    g.b[1] = up;
-    g.lda = g.ldb = ffn_up8(K);
-    g.o[0] = at<uint16_t>(workspace, s.a);
-    g.ldo = ffn_up8(F);
-    g.gcodes = gate_codes;
-    g.ucodes = up_codes;
-    g.gexps = gate_exponents;
-    g.uexps = up_exponents;
-    g.groups = act8_groups(F);
-    if ((rc = run(g, stream))) return rc;
-
-    g = product(kFfnPlain, s.down, T, K, F, workspace, s.partial);
-    g.a[0] = at<uint16_t>(workspace, s.a);
-    g.b[0] = dp;
-    g.lda = g.ldb = ffn_up8(F);
-    g.o[0] = y;
-    g.ldo = K;
-    return run(g, stream);
+    GEFEN_HIP(launch_ffn_gemm(inner_product, stream));
+    GEFEN_HIP(launch_ffn_gemm(down, stream));
+    return GEFEN_OK;
 }
 
 int gefen_gated_ffn_backward(const uint16_t* dy, const uint16_t* x, const int8_t* x_codes,
@@ -355,67 +361,71 @@ int gefen_gated_ffn_backward(const uint16_t* dy, const uint16_t* x, const int8_t
     const uint16_t* dp = operand(w_down, K, F, copy_f, workspace, s.w_down, pads);
     const uint16_t* xp = x ? operand(x, T, K, copy_k, workspace, s.x, pads)
                            : at<uint16_t>(workspace, s.x);
+    uint16_t* a = at<uint16_t>(workspace, s.a);
+    uint16_t* dg = at<uint16_t>(workspace, s.dg);
+    uint16_t* du = at<uint16_t>(workspace, s.du);
+
+    FfnGemm grad_inner = product(kFfnGateGrad, s.grad_inner, T, F, K, workspace, s.partial);
+    grad_inner.act = activation;
+    grad_inner.a[0] = dyp;
+    grad_inner.lda = K8;
+    grad_inner.b[0] = dp;
+    grad_inner.b_rows_k = true;
+    grad_inner.ldb = F8;
+    grad_inner.o[0] = dg;
+    grad_inner.o[1] = du;
+    grad_inner.o2 = a;
+    grad_inner.ldo = F8;
+    grad_inner.gcodes = const_cast<int8_t*>(gate_codes);
+    grad_inner.ucodes = const_cast<int8_t*>(up_codes);
+    grad_inner.gexps = const_cast<uint8_t*>(gate_exponents);
+    grad_inner.uexps = const_cast<uint8_t*>(up_exponents);
+    grad_inner.groups = act8_groups(F);
+
+    FfnGemm dwd = product(kFfnPlain, s.dw, K, F, T, workspace, s.partial);      // dy^T A
+    dwd.a[0] = dyp;
+    dwd.lda = K8;
+    dwd.b[0] = a;
+    dwd.ldb = F8;
+    dwd.o[0] = dw_down;
+    dwd.ldo = F;
+    FfnGemm dwi = product(kFfnPlain, s.dw, F, K, T, workspace,                  // dG^T x, dU^T x
+                          s.partial + ffn_partial_bytes(s.dw, K, F, 1));
+    dwi.batch = 2;
+    dwi.a[0] = dg;
+    dwi.a[1] = du;
+    dwi.lda = F8;
+    dwi.b[0] = xp;
+    dwi.ldb = K8;
+    dwi.col_scale = gain;
+    dwi.o[0] = dw_gate;
+    dwi.o[1] = dw_up;
+    dwi.ldo = K;
+
+    FfnGemm dxp = product(kFfnPlain, s.dx, T, K, F, workspace, s.partial);      // dG Wg + dU Wu
+    dxp.segments = 2;
+    dxp.b_rows_k = true;
+    dxp.a[0] = dg;
+    dxp.a[1] = du;
+    dxp.lda = F8;
+    dxp.b[0] = gp;
+    dxp.b[1] = up;
+    dxp.ldb = K8;
+    dxp.o[0] = dx;
+    dxp.ldo = K;
+
+    if ((rc = check_launch(grad_inner)) || (rc = check_launch(dwd, &dwi)) ||
+        (rc = check_launch(dxp)))
+        return rc;
     GEFEN_HIP(launch_ffn_pads(pads, stream));
     // The input's values are exact in bfloat16; its gain goes into the weight gradients' columns.
     if (!x)
         GEFEN_HIP(launch_act8_decode(x_codes, x_exponents, nullptr, T, K, at<void>(workspace, s.x),
                                      true, K8, stream));
-    uint16_t* a = at<uint16_t>(workspace, s.a);
-    uint16_t* dg = at<uint16_t>(workspace, s.dg);
-    uint16_t* du = at<uint16_t>(workspace, s.du);
-
-    FfnGemm g = product(kFfnGateGrad, s.grad_inner, T, F, K, workspace, s.partial);
-    g.act = activation;
-    g.a[0] = dyp;
-    g.lda = K8;
-    g.b[0] = dp;
-    g.b_rows_k = true;
-    g.ldb = F8;
-    g.o[0] = dg;
-    g.o[1] = du;
-    g.o2 = a;
-    g.ldo = F8;
-    g.gcodes = const_cast<int8_t*>(gate_codes);
-    g.ucodes = const_cast<int8_t*>(up_codes);
-    g.gexps = const_cast<uint8_t*>(gate_exponents);
-    g.uexps = const_cast<uint8_t*>(up_exponents);
-    g.groups = act8_groups(F);
-    if ((rc = run(g, stream))) return rc;
-
-    g = product(kFfnPlain, s.dw, K, F, T, workspace, s.partial);        // dy^T A
-    g.a[0] = dyp;
-    g.lda = K8;
-    g.b[0] = a;
-    g.ldb = F8;
-    g.o[0] = dw_down;
-    g.ldo = F;
-    FfnGemm gi = product(kFfnPlain, s.dw, F, K, T, workspace,           // dG^T x, dU^T x
-                         s.partial + ffn_partial_bytes(s.dw, K, F, 1));
-    gi.batch = 2;
-    gi.a[0] = dg;
-    gi.a[1] = du;
-    gi.lda = F8;
-    gi.b[0] = xp;
-    gi.ldb = K8;
-    gi.col_scale = gain;
-    gi.o[0] = dw_gate;
-    gi.o[1] = dw_up;
-    gi.ldo = K;
-    if (!fits(g) || !fits(gi)) return fail(GEFEN_EINVAL, "too many tiles");
-    GEFEN_HIP(launch_ffn_weight_grads(g, gi, stream));
-
-    g = product(kFfnPlain, s.dx, T, K, F, workspace, s.partial);        // dG Wg + dU Wu
-    g.segments = 2;
-    g.b_rows_k = true;
-    g.a[0] = dg;
-    g.a[1] = du;
-    g.lda = F8;
-    g.b[0] = gp;
-    g.b[1] = up;
-    g.ldb = K8;
-    g.o[0] = dx;
-    g.ldo = K;
-    return run(g, stream);
+    GEFEN_HIP(launch_ffn_gemm(grad_inner, stream));
+    GEFEN_HIP(launch_ffn_weight_grads(dwd, dwi, stream));
+    GEFEN_HIP(launch_ffn_gemm(dxp, stream));
+    return GEFEN_OK;
 }
 
 }  // extern "C"

@@ -188,3 +188,21 @@ def test_decode_and_backward_calls_do_not_cut_the_graph_silently(launched):
     dx = results(dy, dy.clone().requires_grad_(True))[0]
     with pytest.raises(RuntimeError, match="rms_norm_backward"):
         dx.float().sum().backward()
+
+
+# ------------------------------------------------------------------ sizes past a launch
+def test_products_past_a_launch_are_refused():
+    """2^24 x 2^16 sums are more workgroups than a dispatch has threads for: an argument error,
+    before anything is launched."""
+    import os
+    if not os.path.exists(gf.LIB_PATH):
+        pytest.skip("libgefen.so is not built (run __graft_entry__.build())")
+    if torch.cuda.is_available():
+        pytest.skip("host pointers: without a device only")
+    lib, p = gf.load_library(), 0x1000
+    rc = lib.gefen_gated_ffn(p, p, p, p, 1 << 24, 8, 1 << 16, 0, p, None, None, None, None, p,
+                             1 << 60, None)
+    assert rc == -1 and b"too many" in lib.gefen_last_error(), lib.gefen_last_error()
+    rc = lib.gefen_gated_ffn_backward(p, p, None, None, None, p, p, p, p, p, p, p, 64, 1 << 20,
+                                      1 << 20, 0, p, p, p, p, p, 1 << 60, None)
+    assert rc == -1 and b"too many" in lib.gefen_last_error(), lib.gefen_last_error()
