@@ -173,15 +173,18 @@ class Checkpoint8:
     def nbytes(self):
         return self.codes.numel() + self.exponents.numel()
 
-    def decode(self, dtype=torch.bfloat16, gain=None, out=None, stream=None):
-        """The tensor's values (exact in both types), times ``gain`` (float32, one per column)."""
+    def decode(self, dtype=None, gain=None, out=None, stream=None):
+        """The tensor's values (exact in both types), times ``gain`` (float32, one per column), as
+        ``dtype``: bfloat16 by default, or ``out``'s, which it is to agree with."""
         if stream is not None:
             return _on(stream, self.decode, dtype, gain, out)
         codes = self.codes
         dev = _device(codes, "codes")
         rows, cols = _rows(codes, "codes")
         if out is None:
-            out = torch.empty_like(codes, dtype=dtype)
+            out = torch.empty_like(codes, dtype=dtype or torch.bfloat16)
+        elif dtype is not None and out.dtype is not dtype:
+            raise TypeError(f"out must be {dtype}, not {out.dtype}")
         elif not out.is_contiguous():
             raise ValueError("out must be contiguous")
         else:

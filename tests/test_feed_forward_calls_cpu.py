@@ -206,3 +206,16 @@ def test_products_past_a_launch_are_refused():
     rc = lib.gefen_gated_ffn_backward(p, p, None, None, None, p, p, p, p, p, p, p, 64, 1 << 20,
                                       1 << 20, 0, p, p, p, p, p, 1 << 60, None)
     assert rc == -1 and b"too many" in lib.gefen_last_error(), lib.gefen_last_error()
+
+
+# ------------------------------------------------------------------ arguments that disagree
+def test_decode_type_and_out_agree(launched):
+    c = _checkpoint(_On0, 3, 100)
+    assert c.decode().dtype is BF16 and c.decode(F32).dtype is F32
+    for dtype in (BF16, F32):
+        out = _tensor(_On0, 3, 100, dtype=dtype)
+        assert c.decode(out=out) is out and c.decode(dtype, out=out) is out
+        del launched[:]
+        with pytest.raises(TypeError, match="out"):
+            c.decode(F32 if dtype is BF16 else BF16, out=out)
+        assert launched == []
