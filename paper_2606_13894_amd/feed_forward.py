@@ -300,9 +300,9 @@ def _ffn_operands(rows_of, what, w_gate, w_up, w_down, activation):
     t = _operand(rows_of, what, dev, bf16)
     tokens, width = _rows(t, what)
     w_gate = _operand(w_gate, "w_gate", dev, bf16)
-    inner = w_gate.shape[0]
-    if w_gate.dim() != 2 or w_gate.shape[1] != width or inner < 1:
+    if w_gate.dim() != 2 or w_gate.shape[1] != width or w_gate.shape[0] < 1:
         raise ValueError(f"w_gate has shape {tuple(w_gate.shape)}, expected (inner, {width})")
+    inner = w_gate.shape[0]
     w_up = _operand(w_up, "w_up", dev, bf16, (inner, width))
     w_down = _operand(w_down, "w_down", dev, bf16, (width, inner))
     return dev, t, tokens, width, inner, w_gate, w_up, w_down, act

@@ -219,3 +219,11 @@ def test_decode_type_and_out_agree(launched):
         with pytest.raises(TypeError, match="out"):
             c.decode(F32 if dtype is BF16 else BF16, out=out)
         assert launched == []
+
+
+def test_gate_weight_of_no_matrix_is_refused(launched):
+    x, wd = _tensor(_On0, 3, 100), _tensor(_On0, 100, 40)
+    for bad in (_tensor(_On0, 1)[0], _tensor(_On0, 100), _tensor(_On0, 0, 100), _tensor(_On0, 2, 20, 100)):
+        with pytest.raises(ValueError, match="w_gate has shape"):
+            gf.gated_ffn(x, bad, bad, wd)
+    assert launched == []
