@@ -99,7 +99,6 @@ hipError_t launch_ffn_weight_grads(const FfnGemm& one, const FfnGemm& two, hipSt
 
 // One forward product of a few tokens (ffn_tokens.hip): o[t][n] = sum_k x[t][k] w[n][k] over
 // dense rows of K, or act(G) U of two such products where w[1] is given.
-constexpr int64_t kFfnFewTokens = 16;
 struct FfnTokens {
     const uint16_t* x;
     int64_t ldx;

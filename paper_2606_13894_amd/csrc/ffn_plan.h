@@ -94,6 +94,18 @@ inline FfnTile ffn_choose(const FfnResult* r, int n, int64_t K, int segments, bo
 }
 
 // ---------------------------------------------------------------- launches
+// The few-token products (ffn_tokens.hip): rows of the weights to a workgroup, and its waves, which
+// share the sum over k: about sixteen a CU in all, at least 128 k each.
+constexpr int64_t kFfnFewTokens = 16;
+inline int ffn_token_rows(int64_t tokens) { return tokens <= 8 ? 8 : 16; }
+inline int ffn_token_waves(int64_t N, int64_t K, int rows)
+{
+    const int64_t groups = ffn_ceil(N, rows);
+    int waves = 4;
+    while (waves < 16 && groups * waves < 4096 && K >= 256 * waves) waves *= 2;
+    return waves;
+}
+
 // The checkpoint kernels' launches for `rows` rows of `vectors` vectors of eight, a whole number
 // of groups: 2^lx lanes along a row by 256 >> lx rows to a workgroup. A dispatch has fewer than
 // 2^32 threads along an axis (one row of 2^35 elements would have as many), so that of the gx

@@ -99,11 +99,8 @@ __global__ __launch_bounds__(64 * W) void k_ffn_tokens(const FfnTokens g)
 template <bool DUAL, int R>
 hipError_t launch_waves(const FfnTokens& g, hipStream_t stream)
 {
-    // waves for the sum: about sixteen a CU in all, at least 128 k each
-    const int64_t groups = (g.N + R - 1) / R;
-    int waves = 4;
-    while (waves < 16 && groups * waves < 4096 && g.K >= 256 * waves) waves *= 2;
-    const dim3 grid(static_cast<unsigned>(groups));
+    const int waves = ffn_token_waves(g.N, g.K, R);
+    const dim3 grid(static_cast<unsigned>(ffn_ceil(g.N, R)));
     if (waves == 4)
         hipLaunchKernelGGL((k_ffn_tokens<DUAL, R, 4>), grid, dim3(256), 0, stream, g);
     else if (waves == 8)
@@ -118,7 +115,7 @@ hipError_t launch_waves(const FfnTokens& g, hipStream_t stream)
 hipError_t launch_ffn_tokens(const FfnTokens& g, hipStream_t stream)
 {
     if (g.tokens < 1 || g.tokens > kFfnFewTokens) return hipErrorInvalidValue;
-    if (g.tokens <= 8)
+    if (ffn_token_rows(g.tokens) == 8)
         return g.w[1] ? launch_waves<true, 8>(g, stream) : launch_waves<false, 8>(g, stream);
     return g.w[1] ? launch_waves<true, 16>(g, stream) : launch_waves<false, 16>(g, stream);
 }
