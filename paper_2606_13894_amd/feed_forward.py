@@ -31,6 +31,7 @@ _DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
 
 
 _raw_stream = torch._C._cuda_getCurrentRawStream   # no Stream object: a microsecond less a call
+_current_device = torch._C._cuda_getDevice         # for callers that hold a device tensor already
 _lib = None
 
 
@@ -52,7 +53,7 @@ def _device(t, what):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{what} must be a device tensor")
     dev = t.get_device()
-    if dev != torch.cuda.current_device():
+    if dev != _current_device():
         raise ValueError(f"{what} is on {t.device}, not on the current device")
     return dev
 
@@ -179,7 +180,9 @@ class Checkpoint8:
         if stream is not None:
             return _on(stream, self.decode, dtype, gain, out)
         codes = self.codes
-        dev = _device(codes, "codes")
+        dev = codes.get_device()
+        if dev != _current_device():
+            raise ValueError(f"codes are on {codes.device}, not on the current device")
         rows, cols = _rows(codes, "codes")
         if out is None:
             out = torch.empty_like(codes, dtype=dtype or torch.bfloat16)

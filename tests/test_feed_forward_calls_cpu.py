@@ -47,7 +47,7 @@ def launched(monkeypatch):
 
     monkeypatch.setattr(ff, "_library", Library)
     monkeypatch.setattr(ff, "_raw_stream", lambda dev: 0)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(ff, "_current_device", lambda: 0)
     return names
 
 
