@@ -7,8 +7,8 @@ Each block is h = x + residual, y = its gated block of the RMS norm of h (``Feed
 go on as the next block's x and residual, so that the residual's addition is always the norm
 kernel's. The task is synthetic: a random teacher of the same shape to be matched. After training
 the stack answers single tokens without saving anything. Prints the loss, the time of a step, and
-the bytes kept for the backward pass beside those of a bfloat16 implementation (h, its norm, both
-projections and their product).
+the bytes of activations kept for the backward pass beside those of a bfloat16 implementation (h,
+its norm, both projections and their product), and those of the bfloat16 weights kept with them.
 """
 import argparse
 import os
@@ -85,14 +85,15 @@ def main(argv=None):
             print(f"step {step}: loss {last:.4f} (first {first:.4f})", flush=True)
     torch.cuda.synchronize()
     ms = 1e3 * (time.perf_counter() - begin) / max(1, a.steps - 1)
-    saved = sum(t.numel() * t.element_size() for t in kept if t.shape[0] == a.tokens)
+    copies = sum(2 * t.numel() for t in kept if t.dtype is torch.bfloat16)
+    saved = sum(t.numel() * t.element_size() for t in kept
+                if t.dtype in (torch.int8, torch.uint8) or t.shape == (a.tokens,))
     plain = a.layers * a.tokens * 2 * (2 * a.width + 3 * a.inner)
     print(f"{ms:.2f} ms a step; kept for the backward pass: {saved / 2**20:.1f} MiB "
-          f"(bfloat16: {plain / 2**20:.1f} MiB)")
+          f"(bfloat16: {plain / 2**20:.1f} MiB), and {copies / 2**20:.1f} MiB of weights")
     answer = serve(stack, x)
     one = answer(x[:1])
-    with torch.no_grad():
-        same = stack(x[:1])
+    same = stack(x[:1]).detach()   # with gradients: the kernels that save
     err = (one.float() - same.float()).norm() / same.float().norm()
     print(f"one token served: {tuple(one.shape)}, {err:.1e} off the training path")
     return first, last, err.item()

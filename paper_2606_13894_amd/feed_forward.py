@@ -324,6 +324,7 @@ def _ffn_space(lib, like, tokens, width, inner, flags, pointers):
 def gated_ffn(x, w_gate, w_up, w_down, activation: str = "silu", checkpoint: bool = False,
               stream=None):
     """(act(x w_gate^T) * (x w_up^T)) w_down^T of bfloat16 tensors; weights are [out, in].
+    ``activation`` is "silu" or "gelu", the latter in its tanh form (torch's default is the other).
     With ``checkpoint`` returns (y, (gate, up)), the 8-bit checkpoints of both projections for
     :func:`gated_ffn_backward`."""
     if stream is not None:
@@ -414,9 +415,14 @@ class FeedForward(torch.nn.Module):
     """The feed-forward half of a transformer block: ``y, h = ff(x, residual)`` with
     h = x + residual and y the gated block of the RMS norm of h (so that h + y, or h as the next
     residual of y, goes on). Parameters are float32, as the optimizers take them, and cast to
-    bfloat16 in each call; x and residual are bfloat16. A second derivative is an error. The
-    backward pass keeps the normalised rows and both projections in 8 bits and nothing else of that
-    size; where no gradient is wanted nothing is saved, and few tokens take the kernels for them."""
+    bfloat16 in each call; x and residual are bfloat16. A second derivative is an error.
+
+    Kept for the backward pass: the normalised rows and both projections in 8 bits, a float per
+    row, and the call's bfloat16 copies of the three weights (6 width inner bytes, more than the
+    activations below about 6 width inner / (width + 2 inner) tokens; casting them again in the
+    backward pass took 53 us at 2048 and 8192). Where no gradient is wanted nothing is kept, and
+    few tokens take the kernels for them. A program that serves casts the weights once and calls
+    :func:`rms_norm` and :func:`gated_ffn` itself."""
 
     def __init__(self, width: int, inner: int, activation: str = "silu", eps: float = 1e-6,
                  device=None):

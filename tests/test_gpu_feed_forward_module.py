@@ -63,3 +63,17 @@ def test_module_without_gradients_saves_nothing(dev, monkeypatch, T, act, residu
         assert torch.equal(y1, y)
     else:
         assert (y1.double() - y.double()).norm() <= 2 * 2.0 ** -8 * y.double().norm()
+
+
+def test_everything_kept_for_the_backward_pass(dev):
+    """Bytes an element in 8 bits, a float per row, and the bfloat16 copies of the weights that the
+    call made; the norm's weight is the parameter itself."""
+    T, K, F = 256, 512, 1024
+    block = gf.FeedForward(K, F, device=dev)
+    x = _rows(dev, T, K, 1).requires_grad_(True)
+    kept = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: (kept.append(t), t)[1], lambda t: t):
+        block(x)
+    own = [t for t in kept if t.data_ptr() != block.norm.data_ptr()]
+    assert sum(t.numel() * t.element_size() for t in own) == \
+        T * (K + K // 64 + 2 * (F + F // 64) + 4) + 3 * 2 * K * F
