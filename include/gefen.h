@@ -379,7 +379,7 @@ int gefen_stream_mix(float* theta, const void* grad, int32_t grad_dtype, uint8_t
  * trained with one byte per saved activation. None of them needs a state, allocates or
  * synchronises: every device operation is enqueued on `stream`, workspaces are the caller's
  * (16-byte aligned; their contents need not be kept between calls), outputs must not overlap
- * inputs. Matrices are dense and row-major; pointers may have any alignment that their type has.
+ * inputs unless an entry says that they may. Matrices are dense and row-major; pointers may have any alignment that their type has.
  * A call with no rows (tokens) writes nothing but zero weight gradients.
  *
  * 8-bit activation checkpoint of a rows x cols matrix: int8 codes[rows * cols] and uint8
@@ -387,9 +387,10 @@ int gefen_stream_mix(float* theta, const void* grad, int32_t grad_dtype, uint8_t
  * group of a row may be shorter). With E the group's exponent an element stands for
  * code * 2^(E - 127), |code| <= 127; E is the smallest number >= 1 for which every
  * |element| / 2^(E - 127) rounds to at most 127, and codes are rounded to nearest, ties to
- * even. (E ends at 248, where codes of elements from 127.5 * 2^121 on are held at 127.) Scales are powers of two so that every value is exact in bfloat16 (a scale of
- * absmax / 127 would save about half a bit of rounding error and cost another rounding where a
- * bfloat16 matrix product reads the values). A group that holds an infinity or NaN has E = 255
+ * even. (E ends at 248, where codes of elements from 127.5 * 2^121 on are held at 127.) Scales
+ * are powers of two so that every value is exact in bfloat16 (a scale of absmax / 127 would save
+ * about half a bit of rounding error and cost another rounding where a bfloat16 matrix product
+ * reads the values). A group that holds an infinity or NaN has E = 255
  * and codes 0 and stands for NaN throughout.
  * ---------------------------------------------------------------------------- */
 

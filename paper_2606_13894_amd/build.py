@@ -2,8 +2,9 @@
 
 Every kernel's register and scratch use is taken from the compiler's
 kernel-resource-usage remarks and written next to the library
-(``libgefen.resources.txt``); a kernel that spills to scratch fails the build, since a
-spill turns the HBM-bound step into a scratch-memory-bound one.
+(``libgefen.resources.txt``); a step kernel that spills to scratch fails the build, since a
+spill turns the HBM-bound step into a scratch-memory-bound one. (Of the others the RMS norm of
+rows past 8192 columns and the largest tile of the gate's gradients do; the file shows how much.)
 """
 from __future__ import annotations
 

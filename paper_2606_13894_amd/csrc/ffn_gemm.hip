@@ -27,9 +27,10 @@
 // PFLOP/s, the library's six products of these sizes 1.16 to 1.60):
 //   gate/up 446 us (1.23 PFLOP/s with the checkpoints), down 187 (1.47), the gradients of the
 //   gate 325 (0.85: over a quarter of it is the epilogue, whose reads and writes come in bursts since
-//   all workgroups reach it together), weight gradients 642 (1.28), dx 396 (1.39).
+//   all workgroups reach it together, and whose values leave no register free: 48 bytes a lane go
+//   through scratch), weight gradients 642 (1.28), dx 396 (1.39).
 // Smaller ones are bound by latency per stage and by the partial sums of a split product: 1000
-// tokens take 54 us for gate/up and 48 + 6 for down, of 72 at the large product's rate.
+// tokens take 54 us for gate/up and 51 + 6 for down, of 72 at the large product's rate.
 // Measured and slower: loads between the matrix instructions, a stage's A loaded for two parts
 // at once, 32-k stages, 32 x 32 x 16 instructions, smaller tiles for the gate's gradients.
 //
@@ -41,6 +42,9 @@
 //             gradient, so that neither A nor dA is kept.
 //   plain     bfloat16, times a factor per column where given; or float32 partial sums of a
 //             product split over k, which k_ffn_join adds in order.
+// A, dG and dU are rounded to bfloat16, as the next product's matrix instructions read them (float32
+// operands run at a sixteenth of the rate): an output then lies 0.0024 of its norm from the formula,
+// where its own rounding alone leaves 0.0017.
 #include "act8_device.h"
 #include "ffn_internal.h"
 
@@ -804,7 +808,7 @@ __global__ __launch_bounds__(256) void k_ffn_join(const FfnGemm g)
 // dst (rows of ldd, a multiple of 8) = src (dense rows of `cols`), zero past them: rows of odd
 // widths are copied to 16-byte alignment once, so that the products' loads to LDS are whole. A
 // thread takes four vectors of eight, 256 apart in the flat order, all loaded before the first is
-// stored. Memory and a launch: 9.7 us a pass for 777 tokens and three weights of 765 x 2047 (21 MB
+// stored. Memory and a launch: 6.7 us a pass for 777 tokens and three weights of 765 x 2047 (21 MB
 // read and written).
 __global__ __launch_bounds__(256) void k_ffn_pad(const FfnPads p)
 {
