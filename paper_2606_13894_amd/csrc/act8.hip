@@ -15,8 +15,8 @@ namespace {
 // A workgroup takes 256 vectors: 2^lx lanes along a row (a whole number of groups) by
 // 256 >> lx rows, from the workgroup `first` along a row on (RowGrid). Rows that are whole groups
 // long are one long row to these kernels.
-// 8192 x 8192 bfloat16: encode 42.4 us, decode 38.4 (4.8 and 5.3 TB/s, a large copy's rate); 8192 x
-// 2048 decode 12.0 (4.2 TB/s); one row of 2048 1.8 and 1.7, a launch's time.
+// 8192 x 8192 bfloat16: encode 39.8 us, decode 38.2 (5.1 and 5.3 TB/s, a large copy's rate); 8192 x
+// 2048 decode 11.8 (4.3 TB/s); one row of 2048 1.9 and 1.7, a launch's time.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_act8_encode(const void* __restrict__ x, int64_t rows,
                                                      int64_t cols, int64_t groups, int lx,
@@ -108,7 +108,7 @@ __device__ __forceinline__ double inverse_root(double x)
 // from: a checkpoint's code is the formula's, whatever the order of the sum (the pass is bound by
 // memory: no time is lost). A row's vectors are all fetched before the first is used; 4096
 // workgroups at most, so that a row's wait is covered by other workgroups'. 8192 x 2048 bfloat16
-// with a residual and a checkpoint: 26.8 us (5.6 TB/s); 1000 x 1601 float32 6.4. Rows of 4096
+// with a residual and a checkpoint: 26.2 us (5.8 TB/s); 1000 x 1601 float32 6.6. Rows of 4096
 // run at 5.4 TB/s, of 8192 to 16384 at 4.2 (past 8192 with 20 bytes a lane through scratch, 44 in
 // float32).
 template <bool BF16, int TPR, int NV>
@@ -212,8 +212,8 @@ __device__ __forceinline__ void hide(GradRow<BF16, CODES, NV>& r)
 // keeps its rows' share of dw in registers and writes it once; k_norm_dw adds the shares in
 // order, so that dw does not depend on timing. The next row's vectors are on their way while a
 // row is worked on, so few workgroups are enough (768: three to a CU) and the shares stay small.
-// Bound by memory: 8192 x 2048 bfloat16 from codes 23.2 us (5.1 TB/s) and 4.0 for k_norm_dw;
-// 1023 x 768 float32 5.5 and 3.5, launches. Rows of 4096 and 8192 run at 4.4 TB/s, of 16384 at
+// Bound by memory: 8192 x 2048 bfloat16 from codes 23.5 us (5.0 TB/s) and 4.0 for k_norm_dw;
+// 1023 x 768 float32 5.6 and 3.5, launches. Rows of 4096 and 8192 run at 4.4 TB/s, of 16384 at
 // 3.1 (2.8 in float32; 2.0 before their values were formed twice): a 1024-thread workgroup has 128
 // registers to a lane, which hold one row as it was loaded and dw, and 12 to 172 bytes of a lane
 // go through scratch all the same.

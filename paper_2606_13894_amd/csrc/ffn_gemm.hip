@@ -25,12 +25,12 @@
 // Bound by the matrix cores and the card's power at large sizes. 8192 tokens, 2048 to 8192
 // columns and back (flops of the product alone; the card's plain large product reaches 1.42
 // PFLOP/s, the library's six products of these sizes 1.16 to 1.60):
-//   gate/up 446 us (1.23 PFLOP/s with the checkpoints), down 187 (1.47), the gradients of the
+//   gate/up 438 us (1.26 PFLOP/s with the checkpoints), down 187 (1.47), the gradients of the
 //   gate 325 (0.85: over a quarter of it is the epilogue, whose reads and writes come in bursts since
 //   all workgroups reach it together, and whose values leave no register free: 48 bytes a lane go
-//   through scratch), weight gradients 642 (1.28), dx 396 (1.39).
+//   through scratch), weight gradients 632 (1.30), dx 382 (1.44).
 // Smaller ones are bound by latency per stage and by the partial sums of a split product: 1000
-// tokens take 54 us for gate/up and 51 + 6 for down, of 72 at the large product's rate.
+// tokens take 53 us for gate/up and 48 + 6 for down, of 72 at the large product's rate.
 // Measured and slower: loads between the matrix instructions, a stage's A loaded for two parts
 // at once, 32-k stages, 32 x 32 x 16 instructions, smaller tiles for the gate's gradients.
 //

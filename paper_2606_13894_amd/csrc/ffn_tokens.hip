@@ -10,7 +10,7 @@
 // vector shifted at its end. The waves' float32 sums are added through LDS, in order.
 //
 // One token, 2048 to 8192 columns and back, on weights that change from call to call (2.4 GB of
-// them): gate/up 14.4 us (67 MB, 4.7 TB/s), down 8.2 (34 MB, 4.1), 22.6 a call; on the same ones
+// them): gate/up 14.3 us (67 MB, 4.7 TB/s), down 8.3 (34 MB, 4.0), 22.5 a call; on the same ones
 // again, which the last-level cache holds, 12.6 and 7.8, 20.0 a call. Weight loads that bypass the
 // caches were 2 % faster on cold weights and 20 % slower where a small model's weights stay in the
 // caches, so they are plain. A is rounded to bfloat16 as in ffn_gemm.hip.
