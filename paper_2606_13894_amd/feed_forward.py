@@ -419,8 +419,8 @@ class FeedForward(torch.nn.Module):
 
     Kept for the backward pass: the normalised rows and both projections in 8 bits, a float per
     row, and the call's bfloat16 copies of the three weights (6 width inner bytes, more than the
-    activations below about 6 width inner / (width + 2 inner) tokens; casting them again in the
-    backward pass took 53 us at 2048 and 8192). Where no gradient is wanted nothing is kept, and
+    activations below about 6 width inner / (width + 2 inner) tokens; the casts take 53 us at 2048
+    and 8192, and are not done again in the backward pass). Where no gradient is wanted nothing is kept, and
     few tokens take the kernels for them. A program that serves casts the weights once and calls
     :func:`rms_norm` and :func:`gated_ffn` itself."""
 

@@ -77,3 +77,24 @@ def test_everything_kept_for_the_backward_pass(dev):
     own = [t for t in kept if t.data_ptr() != block.norm.data_ptr()]
     assert sum(t.numel() * t.element_size() for t in own) == \
         T * (K + K // 64 + 2 * (F + F // 64) + 4) + 3 * 2 * K * F
+
+
+def test_gradients_that_are_not_there_are_errors(dev):
+    """On the device as with stand-ins: under create_graph the gradients are the same bits, and
+    going through them, or through a plain call's result, raises."""
+    torch.manual_seed(0)
+    block = gf.FeedForward(64, 96, device=dev)
+    x = _rows(dev, 20, 64, 1).requires_grad_(True)
+    (want,) = torch.autograd.grad(block(x)[0].sum(), x)
+    (got,) = torch.autograd.grad(block(x)[0].sum(), x, create_graph=True)
+    assert torch.equal(got, want) and not want.requires_grad
+    with pytest.raises(RuntimeError, match="second derivative"):
+        got.float().square().sum().backward()
+    n = gf.rms_norm(x, block.norm)
+    assert torch.equal(n.y, gf.rms_norm(x.detach(), block.norm.detach()).y)
+    with pytest.raises(RuntimeError, match="FeedForward"):
+        n.y.float().sum().backward()
+    w = [p.detach().to(BF16) for p in (block.w_gate, block.w_up, block.w_down)]
+    with pytest.raises(RuntimeError, match="FeedForward"):
+        gf.gated_ffn(x, *w).float().sum().backward()
+    assert not gf.gated_ffn(x.detach(), *w).requires_grad
