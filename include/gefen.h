@@ -487,6 +487,116 @@ int gefen_gated_ffn_backward(const uint16_t* dy, const uint16_t* x, const int8_t
                              uint16_t* dx, uint16_t* dw_gate, uint16_t* dw_up, uint16_t* dw_down,
                              void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------
+ * The operators at a language model's two ends, around the blocks: tokens to rows of the embedding
+ * table, dropout, and log probabilities over the vocabulary, with their gradients. As the
+ * feed-forward operators they need no state, neither allocate nor synchronise, enqueue all work on
+ * `stream` and take workspaces of the caller's (16-byte aligned; contents need not be kept); outputs
+ * must not overlap inputs unless an entry says that they may. Matrices are dense and row-major
+ * where no leading dimension is given; pointers may have any alignment that their type has.
+ *
+ * Tokens are whole numbers of token_bytes (4 or 8, signed), at most 2^24 of them in a call but for
+ * gefen_token_logprobs and its backward pass (any number of rows). A token below 0 stands for
+ * none (padding, or a position that no loss is taken on); one from vocab on is a mistake, which
+ * makes NaN of the results that it asks for and takes no gradient. vocab in [1, 2^24], width in
+ * [1, 2^20], matrices of at most 2^40 elements. Sums are float32 (log-sums, entropies and
+ * gradients' among them) and do not depend on timing: equal calls give equal bits.
+ * ---------------------------------------------------------------------------- */
+
+/* gefen_embedding -- y_r = scale * table[tokens[r]], rounded once to `dtype`.
+ *  table  vocab x width of table_dtype;  y  n x width of dtype (GEFEN_F32 or GEFEN_BF16 each).
+ *  scale  finite, rounded to float32. A token below 0 gives a row of zeros.
+ * Errors: EINVAL, EDTYPE, EHIP. */
+int gefen_embedding(const void* tokens, int32_t token_bytes, int64_t n, const void* table,
+                    int32_t table_dtype, int64_t vocab, int64_t width, double scale, void* y,
+                    int32_t dtype, void* stream);
+
+/* gefen_embedding_backward -- dtable[v] = scale * (the sum of dy_r over the r with tokens[r] = v),
+ * in an order that depends on the tokens alone; every row of dtable is written, zeros where
+ * no token asked for it.
+ *  dy      n x width of dtype;  dtable  vocab x width of table_dtype.
+ *  workspace  gefen_embedding_backward_workspace(n, vocab, width) bytes: the sorted tokens, and
+ *          sums of parts of long runs of one token.
+ * Errors: EINVAL, EDTYPE, EHIP. */
+int gefen_embedding_backward_workspace(int64_t n, int64_t vocab, int64_t width, int64_t* bytes);
+int gefen_embedding_backward(const void* dy, int32_t dtype, const void* tokens,
+                             int32_t token_bytes, int64_t n, int64_t vocab, int64_t width,
+                             double scale, void* dtable, int32_t table_dtype, void* workspace,
+                             int64_t workspace_bytes, void* stream);
+
+/* gefen_dropout -- y_i = (i is kept ? x_i * 65536 / (65536 - q) : 0) + residual_i, rounded once,
+ * with q = round(65536 p): p in [0, 1] counts in steps of 2^-16, and the factor keeps the mean for
+ * the p that counts. Element i is kept where 16-bit piece i mod 8 (each word's low half first) of
+ * the Philox-4x32-10 block with counter words (i / 8 low, high, offset low, high) and key words
+ * (seed low, high) is at least q. The gradient of x is the same call on that of y, without residual.
+ *  x, y, residual  n elements of dtype, n at most 2^40; residual may be NULL, y may be x or residual.
+ *  state  device int64[2], or NULL: seed is state[0] in the place of `seed`, and state[1] is added to
+ *         offset, both read when the kernel runs, so that a captured call can be replayed with new
+ *         numbers.
+ * Errors: EINVAL, EDTYPE, EHIP. */
+int gefen_dropout(const void* x, const void* residual, int32_t dtype, int64_t n, double p,
+                  uint64_t seed, uint64_t offset, const int64_t* state, void* y, void* stream);
+
+/* gefen_token_logprobs -- of each row z of scores:
+ *   lse = log sum_j exp(z_j);  logprob = z_token - lse;  entropy = -sum_j p_j log p_j, p = exp(z - lse)
+ * and its `top` largest log probabilities with their tokens, from the largest down, equal ones from
+ * the lowest token up.
+ *  logits  rows x vocab of dtype, rows ld >= vocab elements apart.
+ *  tokens  rows of them. One below 0: logprob is 0.
+ *  logprob, entropy, lse  device float[rows].
+ *  top     in [0, min(32, vocab)]; top_logprobs, top_tokens  rows x top (NULL where top is 0).
+ *  workspace  gefen_token_logprobs_workspace(dtype, rows, vocab, top) bytes.
+ * Scores of -inf (masked ones) have probability 0. A row of nothing else: lse and logprob -inf,
+ * entropy 0. A row that holds a NaN or +inf: lse, logprob and entropy NaN, top_logprobs NaN,
+ * top_tokens -1.
+ * Errors: EINVAL, EDTYPE, EHIP. */
+int gefen_token_logprobs_workspace(int32_t dtype, int64_t rows, int64_t vocab, int32_t top,
+                                   int64_t* bytes);
+int gefen_token_logprobs(const void* logits, int64_t ld, int32_t dtype, int64_t rows,
+                         int64_t vocab, const void* tokens, int32_t token_bytes, int32_t top,
+                         float* logprob, float* entropy, float* lse, float* top_logprobs,
+                         int64_t* top_tokens, void* workspace, int64_t workspace_bytes,
+                         void* stream);
+
+/* gefen_token_logprobs_backward -- with g = dlogprob (0 for a token outside the vocabulary) and
+ * h = dentropy of a row, and lse and entropy from the forward pass:
+ *   dlogits_j = g ([j = token] - p_j) - h p_j (log p_j + entropy)
+ * 0 where p_j is 0 and in a row with nothing left.
+ *  dentropy  device float[rows], or NULL (0).
+ *  dlogits   rows x vocab of dtype, rows ldd elements apart; may be logits itself (ldd = ld).
+ * Errors: EINVAL, EDTYPE, EHIP. */
+int gefen_token_logprobs_backward(const void* logits, int64_t ld, int32_t dtype, int64_t rows,
+                                  int64_t vocab, const void* tokens, int32_t token_bytes,
+                                  const float* lse, const float* entropy, const float* dlogprob,
+                                  const float* dentropy, void* dlogits, int64_t ldd, void* stream);
+
+/* gefen_head_logprobs -- the same logprob, entropy and lse of the scores z = x weight^T, which are
+ * formed tile by tile in float32, not rounded, and never stored.
+ *  x  n x width;  weight  vocab x width, bfloat16 (uint16 bit patterns).
+ *  workspace  gefen_head_logprobs_workspace(...) bytes: flags as for gefen_gated_ffn_workspace. It
+ *          holds the tiles' statistics (backward: the scores' gradients of a range of the vocabulary in
+ *          bfloat16, at most 2^30 bytes or 256 columns, and float32 sums of products that are
+ *          split), and a copy of matrices whose rows are no multiple of 8 elements long.
+ * Errors: EINVAL, EHIP. */
+int gefen_head_logprobs_workspace(int64_t tokens, int64_t width, int64_t vocab, int32_t flags,
+                                  int64_t* bytes);
+int gefen_head_logprobs(const uint16_t* x, const uint16_t* weight, const void* tokens,
+                        int32_t token_bytes, int64_t n, int64_t width, int64_t vocab,
+                        float* logprob, float* entropy, float* lse, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
+/* gefen_head_logprobs_backward -- the scores again, their gradients dz as in
+ * gefen_token_logprobs_backward, rounded to bfloat16 for the products that read them, and
+ *   dx = dz weight;  dweight = dz^T x
+ * with float32 accumulation, each rounded once.
+ *  dx  n x width;  dweight  vocab x width. dentropy may be NULL.
+ * Errors: EINVAL, EHIP. */
+int gefen_head_logprobs_backward(const uint16_t* x, const uint16_t* weight, const void* tokens,
+                                 int32_t token_bytes, int64_t n, int64_t width, int64_t vocab,
+                                 const float* lse, const float* entropy, const float* dlogprob,
+                                 const float* dentropy, uint16_t* dx, uint16_t* dweight,
+                                 void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Free the state and every device buffer it owns. NULL is a no-op. */
 void gefen_destroy(gefen_state* st);
 

@@ -17,6 +17,10 @@ Entry points mirror ``include/gefen.h``:
   checkpoints (:class:`Checkpoint8`, :func:`checkpoint8`), :func:`rms_norm`,
   :func:`gated_ffn`, their backward passes, and :class:`FeedForward`, the block of both under
   autograd.
+* the operators at a language model's two ends of ``language.py``, loaded likewise:
+  :func:`embedding`, :func:`dropout`, :func:`token_logprobs`, :func:`head_logprobs`, their
+  backward passes, and the modules :class:`Embedding`, :class:`Dropout`, :class:`LogProbs` and
+  :class:`Head` under autograd.
 """
 from __future__ import annotations
 
@@ -43,6 +47,10 @@ SYMBOLS = [
     "gefen_dp_codebook_static", "gefen_checkpoint_encode", "gefen_checkpoint_decode",
     "gefen_rms_norm", "gefen_rms_norm_backward", "gefen_rms_norm_backward_workspace",
     "gefen_gated_ffn", "gefen_gated_ffn_backward", "gefen_gated_ffn_workspace",
+    "gefen_embedding", "gefen_embedding_backward", "gefen_embedding_backward_workspace",
+    "gefen_dropout", "gefen_token_logprobs", "gefen_token_logprobs_workspace",
+    "gefen_token_logprobs_backward", "gefen_head_logprobs", "gefen_head_logprobs_workspace",
+    "gefen_head_logprobs_backward",
 ]
 
 
@@ -114,6 +122,21 @@ def load_library(path: str = LIB_PATH):
     lib.gefen_gated_ffn.argtypes = [vp] * 4 + [i64] * 3 + [i32] + [vp] * 6 + [i64, vp]
     lib.gefen_gated_ffn_backward.argtypes = [vp] * 12 + [i64] * 3 + [i32] + [vp] * 5 + [i64, vp]
     lib.gefen_gated_ffn_workspace.argtypes = [i64, i64, i64, i32, P(i64)]
+    u64 = ctypes.c_uint64
+    lib.gefen_embedding.argtypes = [vp, i32, i64, vp, i32, i64, i64, f64, vp, i32, vp]
+    lib.gefen_embedding_backward_workspace.argtypes = [i64, i64, i64, P(i64)]
+    lib.gefen_embedding_backward.argtypes = [vp, i32, vp, i32, i64, i64, i64, f64, vp, i32, vp,
+                                             i64, vp]
+    lib.gefen_dropout.argtypes = [vp, vp, i32, i64, f64, u64, u64, vp, vp, vp]
+    lib.gefen_token_logprobs_workspace.argtypes = [i32, i64, i64, i32, P(i64)]
+    lib.gefen_token_logprobs.argtypes = [vp, i64, i32, i64, i64, vp, i32, i32] + [vp] * 6 + [i64,
+                                                                                            vp]
+    lib.gefen_token_logprobs_backward.argtypes = [vp, i64, i32, i64, i64, vp, i32] + [vp] * 5 + [
+        i64, vp]
+    lib.gefen_head_logprobs_workspace.argtypes = [i64, i64, i64, i32, P(i64)]
+    lib.gefen_head_logprobs.argtypes = [vp, vp, vp, i32, i64, i64, i64] + [vp] * 4 + [i64, vp]
+    lib.gefen_head_logprobs_backward.argtypes = [vp, vp, vp, i32, i64, i64, i64] + [vp] * 7 + [
+        i64, vp]
     lib.gefen_destroy.argtypes = [vp]
     lib.gefen_destroy.restype = None
     lib.gefen_last_error.argtypes = []
@@ -529,11 +552,17 @@ _FEED_FORWARD = ("Checkpoint8", "checkpoint8", "RMSNormOutput", "rms_norm", "rms
                  "gated_ffn", "gated_ffn_backward", "FeedForward")
 
 
+_LANGUAGE = ("embedding", "embedding_backward", "Embedding", "dropout", "Dropout",
+             "TokenLogProbs", "token_logprobs", "token_logprobs_backward", "LogProbs",
+             "HeadLogProbs", "head_logprobs", "head_logprobs_backward", "Head")
+
+
 def __getattr__(name):
-    if name in _FEED_FORWARD:   # needs torch, which importing the binding does not
-        import importlib
-        mod = importlib.import_module(__name__ + ".feed_forward")
-        for n in _FEED_FORWARD:
-            globals()[n] = getattr(mod, n)
-        return globals()[name]
+    for module, names in (("feed_forward", _FEED_FORWARD), ("language", _LANGUAGE)):
+        if name in names:   # needs torch, which importing the binding does not
+            import importlib
+            mod = importlib.import_module(__name__ + "." + module)
+            for n in names:
+                globals()[n] = getattr(mod, n)
+            return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

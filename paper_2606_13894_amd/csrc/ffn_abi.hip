@@ -1,62 +1,14 @@
 // C ABI of the feed-forward operators: argument checks, workspace layout and launches.
-#include "gefen.h"
+#include "abi_checks.h"
 #include "ffn_internal.h"
+#include "ffn_launch.h"
 #include "ffn_plan.h"
-#include "gefen_internal.h"
 
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 
 using namespace gefen;
 
 namespace {
-
-int fail(int code, const char* fmt, ...)
-{
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    set_last_error(buf);
-    return code;
-}
-
-#define GEFEN_HIP(call)                                                                  \
-    do {                                                                                 \
-        hipError_t e_ = (call);                                                          \
-        if (e_ != hipSuccess)                                                            \
-            return fail(GEFEN_EHIP, "%s failed: %s", #call, hipGetErrorString(e_));      \
-    } while (0)
-
-hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
-
-constexpr int64_t kMaxElems = int64_t(1) << 40;
-
-int check_rows(int64_t rows, int64_t cols, int64_t max_cols)
-{
-    if (rows < 0) return fail(GEFEN_EINVAL, "rows must not be negative");
-    if (cols < 1 || cols > max_cols)
-        return fail(GEFEN_EINVAL, "cols must be in [1, %lld]", (long long)max_cols);
-    if (rows > kMaxElems / cols) return fail(GEFEN_EINVAL, "more than 2^40 elements");
-    return GEFEN_OK;
-}
-
-int check_dtype(int32_t dtype)
-{
-    if (dtype != GEFEN_F32 && dtype != GEFEN_BF16)
-        return fail(GEFEN_EDTYPE, "dtype must be GEFEN_F32 or GEFEN_BF16");
-    return GEFEN_OK;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
-template <typename P>
-P* at(void* ws, int64_t off)
-{
-    return reinterpret_cast<P*>(static_cast<char*>(ws) + off);
-}
 
 int check_ffn(int64_t T, int64_t K, int64_t F)
 {
@@ -67,65 +19,6 @@ int check_ffn(int64_t T, int64_t K, int64_t F)
     if (T > 0 && std::max(K, F) > kMaxElems / T)
         return fail(GEFEN_EINVAL, "more than 2^40 elements");
     return GEFEN_OK;
-}
-
-int check_space(const void* ws, int64_t have, int64_t need)
-{
-    if (need > 0 && (!ws || have < need))
-        return fail(GEFEN_EINVAL, "workspace of %lld bytes, %lld needed", (long long)have,
-                    (long long)need);
-    if (!aligned16(ws)) return fail(GEFEN_EINVAL, "workspace must be 16-byte aligned");
-    return GEFEN_OK;
-}
-
-// A product over the plan's tile.
-FfnGemm product(int32_t kind, const FfnTile& t, int64_t M, int64_t N, int64_t K, void* ws,
-                int64_t partial)
-{
-    FfnGemm g{};
-    g.kind = kind;
-    g.tile = t.tile;
-    g.M = M;
-    g.N = N;
-    g.K = K;
-    g.kpad = ffn_up8(K);
-    g.segments = g.batch = 1;
-    g.stages = t.stages;
-    g.tiles_m = static_cast<int32_t>(ffn_ceil(M, ffn_tile_rows(t.tile)));
-    g.tiles_n = static_cast<int32_t>(
-        ffn_ceil(N, ffn_tile_cols(t.tile) / (kind == kFfnGateUp ? 2 : 1)));
-    g.splits = t.splits;
-    g.partial = t.splits > 1 ? at<float>(ws, partial) : nullptr;
-    return g;
-}
-
-// Each launch's threads are fewer than 2^32, as a dispatch has them.
-int check_launch(const FfnGemm& one, const FfnGemm* two = nullptr)
-{
-    const int64_t threads = one.tile == kFfnTile256 ? 512 : 256;
-    int64_t groups = 0;
-    for (const FfnGemm* g : {&one, two}) {
-        if (!g) continue;
-        groups += ffn_ceil(int64_t(g->tiles_m) * g->tiles_n * g->batch * g->splits, 8) * 8;
-        if (g->partial && ffn_ceil(g->M * g->N, 8 * 256) * 256 > 0xffffffffLL)   // the parts' sum
-            return fail(GEFEN_EINVAL, "too many elements of a split sum");
-    }
-    if (groups * threads > 0xffffffffLL) return fail(GEFEN_EINVAL, "too many tiles");
-    return GEFEN_OK;
-}
-
-// The operand itself, or its padded copy in the workspace, noted in `pads`.
-const uint16_t* operand(const void* p, int64_t rows, int64_t cols, bool copy, void* ws, int64_t off,
-                        FfnPads& pads)
-{
-    if (!copy) return static_cast<const uint16_t*>(p);
-    FfnPad& m = pads.m[pads.n++];
-    m.src = static_cast<const uint16_t*>(p);
-    m.dst = at<uint16_t>(ws, off);
-    m.rows = rows;
-    m.cols = cols;
-    m.ldd = ffn_up8(cols);
-    return m.dst;
 }
 
 }  // namespace

@@ -47,6 +47,7 @@
 // where its own rounding alone leaves 0.0017.
 #include "act8_device.h"
 #include "ffn_internal.h"
+#include "token_device.h"
 
 #include <type_traits>
 
@@ -747,7 +748,13 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         const float* s = v + 8 * b;
-                        const float x[8] = {s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]};
+                        float x[8] = {s[0], s[1], s[2], s[3], s[4], s[5], s[6], s[7]};
+                        if (g.add) {
+                            float old[8];
+                            load_row8<false>(p, c + 8 * b, FULL ? c + 8 * b + 8 : g.N, old);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[i] += old[i];
+                        }
                         store_row8<false>(p, c + 8 * b, FULL ? c + 8 * b + 8 : g.N, x);
                     }
                 } else {
@@ -761,6 +768,92 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
             }
         }
     };
+    // A wave's share of each row's statistics: over its columns c < N the largest score m, the sum
+    // of exp(z - m) and that of (z - m) exp(z - m); and the score of the row's token.
+    auto head_stats = [&](auto whole) {
+        constexpr bool FULL = decltype(whole)::value;
+        const int64_t first = col0 + wn * 64;
+        const int64_t slot = PHASES ? 2 * int64_t(w.tn) + wn : w.tn;
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            const int64_t row = row0 + (wm * MI + mi) * 16 + l16;
+            const bool on = FULL || row < g.M;
+            float m = -INFINITY;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (!FULL && first + h * H + 16 * j + 4 * q + i >= g.N)
+                            acc[mi][h][j][i] = -INFINITY;
+                        m = fmaxf(m, acc[mi][h][j][i]);
+                    }
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const float base = score_base(m);
+            float s = 0.0f, t = 0.0f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) score_add(acc[mi][h][j][i], base, s, t);
+            s += __shfl_xor(s, 16);
+            t += __shfl_xor(t, 16);
+            s += __shfl_xor(s, 32);
+            t += __shfl_xor(t, 32);
+            if (!on) continue;
+            if (q == 0) {
+                float* __restrict__ o = g.head.stats + slot * 3 * g.M + row;
+                o[0] = m;
+                o[g.M] = s;
+                o[2 * g.M] = t;
+            }
+            const int64_t at = token_at(g.head.tokens, g.head.wide, row) - g.head.first;
+            const int64_t in = at - first;
+            if (at < g.N && in >= 0 && in < H + 64 && (in & (H - 1)) < 64) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (in == h * H + 16 * j + 4 * q + i)
+                                g.head.taken[row] = acc[mi][h][j][i];
+            }
+        }
+    };
+    // The scores' gradients, rounded to bfloat16 as the two products that read them take them.
+    auto head_grad = [&](auto whole) {
+        constexpr bool FULL = decltype(whole)::value;
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            const int64_t row = row0 + (wm * MI + mi) * 16 + l16;
+            const bool on = FULL || row < g.M;
+            ScoreGrad r = {0.0f, 0.0f, 0.0f, 0.0f, -1};
+            if (on)
+                r = score_grad_row(g.head.tokens, g.head.wide, row, g.head.lse, g.head.entropy,
+                                   g.head.dlogprob, g.head.dentropy);
+            const int64_t at = r.token - g.head.first;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t c = col0 + h * H + wn * 64 + 16 * q;
+                float v[16];
+                to_run(acc[mi][h], v);   // all four lanes of the row take part
+                if (!FULL && (!on || c >= g.ldo)) continue;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    v[i] = score_gradient(v[i], r, r.token >= 0 && at == c + i);
+                if (!FULL && c + 16 > g.N) {   // columns from N to ldo are read as zeros
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c + i >= g.N) v[i] = 0.0f;
+                }
+                store_run<FULL>(g.o[0] + row * g.ldo, c, g.ldo, v);
+            }
+        }
+    };
     typedef std::integral_constant<bool, true> Whole;
     typedef std::integral_constant<bool, false> Edge;
     typedef std::integral_constant<int, kActSilu> Silu;
@@ -769,6 +862,12 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
     if constexpr (KIND == kFfnPlain) {
         if (inside) plain(Whole{});
         else plain(Edge{});
+    } else if constexpr (KIND == kHeadStats) {
+        if (inside) head_stats(Whole{});
+        else head_stats(Edge{});
+    } else if constexpr (KIND == kHeadGrad) {
+        if (inside) head_grad(Whole{});
+        else head_grad(Edge{});
     } else if constexpr (KIND == kFfnGateUp) {
         if (inside && g.act == kActSilu) gate_up(Whole{}, Silu{});
         else if (inside) gate_up(Whole{}, Gelu{});
@@ -871,7 +970,7 @@ hipError_t launch_kind(const FfnGemm& one, const FfnGemm* two, hipStream_t strea
 
 }  // namespace
 
-static hipError_t launch_join(const FfnGemm& g, hipStream_t stream)
+hipError_t launch_ffn_join(const FfnGemm& g, hipStream_t stream)
 {
     if (!g.partial) return hipSuccess;
     const int64_t vectors = (g.M * g.N + 7) / 8;
@@ -880,26 +979,34 @@ static hipError_t launch_join(const FfnGemm& g, hipStream_t stream)
     return hipGetLastError();
 }
 
+hipError_t launch_ffn_parts(const FfnGemm& g, hipStream_t stream)
+{
+    if (g.kind == kFfnGateUp) return launch_kind<kFfnGateUp, true, true>(g, nullptr, stream);
+    if (g.kind == kFfnGateGrad) return launch_kind<kFfnGateGrad, true, false>(g, nullptr, stream);
+    if (g.kind == kHeadStats) return launch_kind<kHeadStats, true, true>(g, nullptr, stream);
+    if (g.kind == kHeadGrad) return launch_kind<kHeadGrad, true, true>(g, nullptr, stream);
+    if (g.b_rows_k) return launch_kind<kFfnPlain, true, false>(g, nullptr, stream);
+    return launch_kind<kFfnPlain, true, true>(g, nullptr, stream);
+}
+
 hipError_t launch_ffn_gemm(const FfnGemm& g, hipStream_t stream)
 {
-    hipError_t err;
-    if (g.kind == kFfnGateUp)
-        err = launch_kind<kFfnGateUp, true, true>(g, nullptr, stream);
-    else if (g.kind == kFfnGateGrad)
-        err = launch_kind<kFfnGateGrad, true, false>(g, nullptr, stream);
-    else if (g.b_rows_k)
-        err = launch_kind<kFfnPlain, true, false>(g, nullptr, stream);
-    else
-        err = launch_kind<kFfnPlain, true, true>(g, nullptr, stream);
-    return err == hipSuccess ? launch_join(g, stream) : err;
+    const hipError_t err = launch_ffn_parts(g, stream);
+    return err == hipSuccess ? launch_ffn_join(g, stream) : err;
+}
+
+hipError_t launch_ffn_weight_grad(const FfnGemm& g, hipStream_t stream)
+{
+    const hipError_t err = launch_kind<kFfnPlain, false, false>(g, nullptr, stream);
+    return err == hipSuccess ? launch_ffn_join(g, stream) : err;
 }
 
 hipError_t launch_ffn_weight_grads(const FfnGemm& one, const FfnGemm& two, hipStream_t stream)
 {
     if (one.tile != two.tile) return hipErrorInvalidValue;
     hipError_t err = launch_kind<kFfnPlain, false, false>(one, &two, stream);
-    if (err == hipSuccess) err = launch_join(one, stream);
-    return err == hipSuccess ? launch_join(two, stream) : err;
+    if (err == hipSuccess) err = launch_ffn_join(one, stream);
+    return err == hipSuccess ? launch_ffn_join(two, stream) : err;
 }
 
 hipError_t launch_ffn_pads(const FfnPads& p, hipStream_t stream)

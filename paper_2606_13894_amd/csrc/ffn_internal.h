@@ -61,7 +61,21 @@ hipError_t launch_rms_norm_grad(const NormGradArgs& a, bool bf16, hipStream_t st
 
 // ---------------------------------------------------------------- gated feed-forward block
 enum : int32_t { kActSilu = 0, kActGelu = 1 };
-enum : int32_t { kFfnGateUp = 0, kFfnPlain = 1, kFfnGateGrad = 2 };
+enum : int32_t { kFfnGateUp = 0, kFfnPlain = 1, kFfnGateGrad = 2, kHeadStats = 3, kHeadGrad = 4 };
+
+// The output head's products: what their epilogues read and write beside the sums (token_internal.h
+// gives the formulas).
+struct HeadRows {
+    const void* tokens;          // of the rows
+    bool wide;                   // 64-bit ones
+    int64_t first;               // the vocabulary entry of column 0
+    float* stats;                // [head_slots][3][M]
+    float* taken;                // [M]: the tokens' scores
+    const float* lse;
+    const float* entropy;
+    const float* dlogprob;
+    const float* dentropy;       // or null
+};
 
 // One product (ffn_gemm.hip). Leading dimensions are multiples of 8 and operands 16-byte
 // aligned; an operand with rows of m or n is zero in its columns K .. kpad - 1.
@@ -88,12 +102,19 @@ struct FfnGemm {
     uint8_t* gexps;
     uint8_t* uexps;
     int64_t groups;              // exponents per row
+    bool add;                    // to what `partial` holds
+    HeadRows head;
 };
 struct FfnGemms {
     FfnGemm g[2];
     uint32_t blocks;             // workgroups of the first
 };
 hipError_t launch_ffn_gemm(const FfnGemm& g, hipStream_t stream);
+// The same without the join of its parts, and the join alone.
+hipError_t launch_ffn_parts(const FfnGemm& g, hipStream_t stream);
+hipError_t launch_ffn_join(const FfnGemm& g, hipStream_t stream);
+// One plain product whose operands are both stored as rows of k.
+hipError_t launch_ffn_weight_grad(const FfnGemm& g, hipStream_t stream);
 // Two plain products whose operands are both stored as rows of k, of one tile size.
 hipError_t launch_ffn_weight_grads(const FfnGemm& one, const FfnGemm& two, hipStream_t stream);
 

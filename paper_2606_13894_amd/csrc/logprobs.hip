@@ -1,0 +1,436 @@
+// Log probabilities of given tokens, their entropy and best alternatives, and the gradients, from rows
+// of scores; and the output head's rows from its tiles' statistics.
+//
+// One pass over a row: each lane keeps the largest score m of what it has read, s = sum exp(z - m) and
+// t = sum (z - m) exp(z - m), so that lse = m + log s, the entropy is log s - t / s, and a token's
+// log probability (z - m) - log s. Lanes, waves and, where rows are few, workgroups that share a row
+// are joined in a fixed order.
+//
+// Best alternatives, by value and among equals by the lower index: a lane also keeps where its
+// largest score first stood. Its k lanes with the largest ones hold k scores at least as large as
+// the k-th of them, so only their vectors, a k-th of a row by the number of lanes, are read again, and the
+// few scores that reach that one are ranked by counting. (They go to a list in LDS; where it does
+// not hold them, the k best are taken one by one.) A score and its place are one 64-bit key, the
+// place inverted, so that no two are equal and no order of arrival counts.
+//
+// Gradients: dz_j = g ([j = token] - p_j) - h p_j (log p_j + H), p_j = exp(z_j - lse), elementwise.
+#include "token_internal.h"
+
+#include "token_device.h"
+
+#include <type_traits>
+
+namespace gefen {
+namespace {
+
+constexpr int L = kScoreThreads;
+constexpr int kWaves = L / 64;
+constexpr int kList = 1024;              // keys of a row that LDS holds beside the lanes'
+
+// Scores order as these do; -0 is 0.
+__device__ __forceinline__ uint32_t ordered(float v)
+{
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t u)
+{
+    return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+__device__ __forceinline__ uint64_t score_key(float v, int64_t place)
+{
+    return (static_cast<uint64_t>(ordered(v)) << 32) | static_cast<uint32_t>(~place);
+}
+
+// 16 bytes of a row of n as scores.
+template <bool BF16>
+struct Vec {
+    static constexpr int N = BF16 ? 8 : 4;
+    static __device__ __forceinline__ u32x4a fetch(const void* row, int64_t v, int64_t n)
+    {
+        return fetch_vector<BF16 ? 2 : 4>(row, v * N, n);
+    }
+    static __device__ __forceinline__ void unpack(const u32x4a& w, float (&z)[N])
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            z[j] = BF16 ? __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16)
+                        : __uint_as_float(w[j]);
+    }
+    // With -inf from n on.
+    static __device__ __forceinline__ void settle(const u32x4a& w, int64_t v, int64_t n,
+                                                  float (&z)[N])
+    {
+        unpack(settle_vector<BF16 ? 2 : 4>(w, v * N, n), z);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (v * N + j >= n) z[j] = -INFINITY;
+    }
+};
+
+__device__ __forceinline__ ScoreSum wave_join(ScoreSum a)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        ScoreSum b;
+        b.m = __shfl_xor(a.m, d);
+        b.s = __shfl_xor(a.s, d);
+        b.t = __shfl_xor(a.t, d);
+        a = score_join(a, b);
+    }
+    return a;
+}
+
+struct ListSpace {
+    uint64_t lane_keys[L];
+    uint64_t list[kList];
+    uint64_t best[kWaves];
+    int lanes[kScoreMaxTop];
+    int count;
+};
+
+// The number of keys[0 .. n) above `key`.
+__device__ __forceinline__ int count_above(const uint64_t* keys, int n, uint64_t key)
+{
+    int above = 0;
+    for (int i = 0; i < n; ++i) above += keys[i] > key;
+    return above;
+}
+
+// The k largest keys of vectors v0 .. v1 - 1 of a row, in order, to out; 0 where there are fewer.
+// `key`: of the lane's largest score, its place that vector's number; 0 where it has read none.
+template <bool BF16>
+__device__ void select_top(const void* row, int64_t n, int64_t v0, int64_t v1, int k, uint64_t key,
+                           ListSpace& s, uint64_t* __restrict__ out)
+{
+    constexpr int N = Vec<BF16>::N;
+    const int tid = threadIdx.x;
+    s.lane_keys[tid] = key;
+    if (tid == 0) s.count = 0;
+    const int have = __syncthreads_count(key != 0);
+    const int rank = key ? count_above(s.lane_keys, L, key) : L;
+    if (rank < k) s.lanes[rank] = tid;
+    const int taken = min(have, k);
+    __syncthreads();
+    const uint64_t least = have >= k ? s.lane_keys[s.lanes[k - 1]] : 0;
+    const int64_t per = (v1 - v0 + L - 1) / L;
+    for (int64_t i = tid; i < taken * per; i += L) {
+        const int64_t v = v0 + s.lanes[i / per] + (i % per) * L;
+        if (v >= v1) continue;
+        float z[N];
+        Vec<BF16>::settle(Vec<BF16>::fetch(row, v, n), v, n, z);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (v * N + j < n && score_key(z[j], v) >= least) {
+                const int at = atomicAdd(&s.count, 1);
+                if (at < kList) s.list[at] = score_key(z[j], v * N + j);
+            }
+    }
+    __syncthreads();
+    const int count = s.count;
+    if (count <= kList) {
+        for (int i = tid; i < count; i += L) {
+            const int at = count_above(s.list, count, s.list[i]);
+            if (at < k) out[at] = s.list[i];
+        }
+        for (int i = count + tid; i < k; i += L) out[i] = 0;
+    } else {
+        uint64_t before = ~uint64_t(0);
+        for (int r = 0; r < k; ++r) {
+            uint64_t best = 0;
+            for (int64_t v = v0 + tid; v < v1; v += L) {
+                float z[N];
+                Vec<BF16>::settle(Vec<BF16>::fetch(row, v, n), v, n, z);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const uint64_t q = score_key(z[j], v * N + j);
+                    if (v * N + j < n && q < before && q > best) best = q;
+                }
+            }
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const uint64_t other = __shfl_xor(static_cast<unsigned long long>(best), d);
+                best = other > best ? other : best;
+            }
+            if ((tid & 63) == 0) s.best[tid >> 6] = best;
+            __syncthreads();
+            for (int w = 0; w < kWaves; ++w) best = s.best[w] > best ? s.best[w] : best;
+            if (tid == 0) out[r] = best;
+            before = best;
+            __syncthreads();
+        }
+    }
+    __syncthreads();
+}
+
+// The row's best alternatives from their keys in order.
+__device__ __forceinline__ void write_top(const ScoreArgs& a, int64_t row, const ScoreSum& sum,
+                                          int i, uint64_t key)
+{
+    const int64_t o = row * a.top + i;
+    const float v = unordered(static_cast<uint32_t>(key >> 32));
+    const bool bad = sum.s != sum.s;
+    a.top_logprob[o] = bad ? sum.s : v == -INFINITY ? v : (v - sum.m) - logf(sum.s);
+    a.top_token[o] = bad ? -1 : static_cast<int64_t>(~static_cast<uint32_t>(key));
+}
+
+__device__ __forceinline__ void write_row(const ScoreArgs& a, int64_t row, const ScoreSum& sum,
+                                          int64_t token, float taken)
+{
+    const ScoreRow r = score_row(sum, token, a.vocab, taken);
+    a.logprob[row] = r.logprob;
+    a.entropy[row] = r.entropy;
+    a.lse[row] = r.lse;
+}
+
+template <bool BF16>
+__device__ __forceinline__ float score_at(const void* z, int64_t i)
+{
+    if constexpr (BF16) return bf16_float(static_cast<const uint16_t*>(z)[i]);
+    else return static_cast<const float*>(z)[i];
+}
+
+template <bool BF16, bool TOP>
+__global__ __launch_bounds__(L) void k_scores(const ScoreArgs a)
+{
+    using V = Vec<BF16>;
+    constexpr int N = V::N, U = 4, S = BF16 ? 2 : 4;
+    __shared__ ScoreSum sums[kWaves];
+    __shared__ typename std::conditional<TOP, ListSpace, int>::type list;
+    __shared__ uint64_t best[TOP ? kScoreMaxTop : 1];
+    const int tid = threadIdx.x;
+    const int64_t vectors = (a.vocab + N - 1) / N, whole = a.vocab / N;
+    const int64_t items = a.rows * a.plan.parts;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t r = item / a.plan.parts, part = item % a.plan.parts;
+        const char* row = static_cast<const char*>(a.z) + r * a.ld * S;
+        const int64_t v0 = part * a.plan.per, v1 = min(vectors, v0 + a.plan.per);
+        const bool one = a.plan.parts == 1;
+        int64_t token = -1;
+        float taken = 0.0f;
+        if (one && tid == 0) {
+            token = token_at(a.tokens.p, a.tokens.wide, r);
+            if (token >= 0 && token < a.vocab) taken = score_at<BF16>(row, token);
+        }
+        ScoreSum c = {-INFINITY, 0.0f, 0.0f};
+        float top = -INFINITY;
+        int64_t place = -1;
+        // A lane's vectors are L apart, U of them loaded before the first is used.
+        for (int64_t b = v0; b < v1; b += U * L) {
+            const bool full = b + U * L <= min(v1, whole);
+            u32x4a w[U];
+            float z[U][N];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t v = b + u * L + tid;
+                if (full || v < v1) w[u] = V::fetch(row, v, a.vocab);
+            }
+            float m = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t v = b + u * L + tid;
+                if (full) {
+                    V::unpack(w[u], z[u]);
+                } else if (v < v1) {
+                    V::settle(w[u], v, a.vocab, z[u]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) z[u][j] = -INFINITY;
+                }
+                float vm = z[u][0];
+#pragma unroll
+                for (int j = 1; j < N; ++j) vm = fmaxf(vm, z[u][j]);
+                m = fmaxf(m, vm);
+                if constexpr (TOP) {
+                    if ((full || v < v1) && (place < 0 || vm > top)) {
+                        top = vm;
+                        place = v;
+                    }
+                }
+            }
+            const float old = c.m;
+            c.m = fmaxf(old, m);
+            const float base = score_base(c.m);
+            score_rebase(old, base, c.s, c.t);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < N; ++j) score_add(z[u][j], base, c.s, c.t);
+        }
+        c = wave_join(c);
+        if ((tid & 63) == 0) sums[tid >> 6] = c;
+        __syncthreads();
+        c = sums[0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) c = score_join(c, sums[w]);
+        if constexpr (TOP) {
+            // (a NaN as the largest of a vector ends in a row whose alternatives are not given)
+            const uint64_t key = place >= 0 ? score_key(top, place) : 0;
+            select_top<BF16>(row, a.vocab, v0, v1, a.top, key, list, best);
+            if (tid < a.top) {
+                if (one) write_top(a, r, c, tid, best[tid]);
+                else a.keys[item * a.top + tid] = best[tid];
+            }
+        }
+        if (tid == 0) {
+            if (one) {
+                write_row(a, r, c, token, taken);
+            } else {
+                a.stats[3 * item] = c.m;
+                a.stats[3 * item + 1] = c.s;
+                a.stats[3 * item + 2] = c.t;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// A row from its parts: their sums in order, and the best of their best. A wave a row.
+template <bool BF16>
+__global__ __launch_bounds__(64) void k_scores_join(const ScoreArgs a)
+{
+    __shared__ uint64_t keys[kScoreMaxParts * kScoreMaxTop];
+    __shared__ uint64_t list[kScoreMaxParts * kScoreMaxTop];
+    const int lane = threadIdx.x;
+    const int parts = static_cast<int>(a.plan.parts);
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        ScoreSum c = {-INFINITY, 0.0f, 0.0f};
+        if (lane < parts) {
+            const float* p = a.stats + 3 * (r * parts + lane);
+            c = ScoreSum{p[0], p[1], p[2]};
+        }
+        c = wave_join(c);
+        if (lane == 0) {
+            const int64_t token = token_at(a.tokens.p, a.tokens.wide, r);
+            float taken = 0.0f;
+            if (token >= 0 && token < a.vocab) taken = score_at<BF16>(a.z, r * a.ld + token);
+            write_row(a, r, c, token, taken);
+        }
+        if (a.top) {
+            const int n = parts * a.top;
+            for (int i = lane; i < n; i += 64) keys[i] = a.keys[r * n + i];
+            __syncthreads();
+            // no key below the k-th largest of the parts' largest ones is among the k largest
+            const uint64_t mine = lane < parts ? keys[lane * a.top] : 0;
+            int above = 0;
+            for (int p = 0; p < parts; ++p) above += keys[p * a.top] > mine;
+            const uint64_t at = __ballot(lane < parts && above == a.top - 1);
+            const uint64_t least = at ? __shfl(static_cast<unsigned long long>(mine),
+                                               __ffsll(static_cast<unsigned long long>(at)) - 1) : 1;
+            int count = 0;
+            for (int i = 0; i < n; i += 64) {
+                const uint64_t key = i + lane < n ? keys[i + lane] : 0;
+                const uint64_t hits = __ballot(key >= least);
+                if (key >= least)
+                    list[count + __popcll(hits & ((uint64_t(1) << lane) - 1))] = key;
+                count += __popcll(hits);
+            }
+            __syncthreads();
+            for (int i = lane; i < count; i += 64) {
+                const int rank = count_above(list, count, list[i]);
+                if (rank < a.top) write_top(a, r, c, rank, list[i]);
+            }
+            __syncthreads();
+        }
+    }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_score_grad(const ScoreGradArgs a, int64_t segments)
+{
+    constexpr int U = 2, S = BF16 ? 2 : 4;
+    const int64_t items = a.rows * segments;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t r = item / segments;
+        const int64_t e0 = (item % segments) * (256 * 8 * U) + 8 * threadIdx.x;
+        const ScoreGrad g = score_grad_row(a.tokens.p, a.tokens.wide, r, a.lse, a.entropy,
+                                           a.dlogprob, a.dentropy);
+        const char* z = static_cast<const char*>(a.z) + r * a.ld * S;
+        char* dz = static_cast<char*>(a.dz) + r * a.ldd * S;
+        u32x4a w[U][BF16 ? 1 : 2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (e0 + 2048 * u < a.vocab) fetch8<BF16>(z, e0 + 2048 * u, a.vocab, w[u]);
+        // (in place: the lane that ends a row may find gradients of the lane before it in its
+        // vector, in the elements that it shifts out)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t e = e0 + 2048 * u;
+            if (e >= a.vocab) continue;
+            float v[8];
+            settle8<BF16>(w[u], e, a.vocab, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[j] = score_gradient(v[j], g, g.token >= 0 && g.token == e + j);
+            store_row8<BF16>(dz, e, a.vocab, v);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- output head
+// A workgroup joins 16 rows, 64 lanes to a row by the slots.
+constexpr int kJoinRows = 16, kJoinWays = 16;
+
+__global__ __launch_bounds__(kJoinRows * kJoinWays) void k_head_join(const HeadJoinArgs a)
+{
+    __shared__ ScoreSum sums[kJoinWays][kJoinRows];
+    const int in = threadIdx.x % kJoinRows, way = threadIdx.x / kJoinRows;
+    const int64_t r = int64_t(blockIdx.x) * kJoinRows + in;
+    ScoreSum c = {-INFINITY, 0.0f, 0.0f};
+    if (r < a.rows)
+        for (int64_t s = way; s < a.slots; s += kJoinWays) {
+            const float* p = a.stats + s * 3 * a.rows + r;
+            c = score_join(c, ScoreSum{p[0], p[a.rows], p[2 * a.rows]});
+        }
+    sums[way][in] = c;
+    __syncthreads();
+    if (way > 0 || r >= a.rows) return;
+    for (int w = 1; w < kJoinWays; ++w) c = score_join(c, sums[w][in]);
+    const int64_t token = token_at(a.tokens.p, a.tokens.wide, r);
+    const float taken = token >= 0 && token < a.vocab ? a.taken[r] : 0.0f;
+    const ScoreRow o = score_row(c, token, a.vocab, taken);
+    a.logprob[r] = o.logprob;
+    a.entropy[r] = o.entropy;
+    a.lse[r] = o.lse;
+}
+
+}  // namespace
+
+hipError_t launch_scores(const ScoreArgs& a, bool bf16, hipStream_t stream)
+{
+    if (a.rows == 0) return hipSuccess;
+    const int64_t items = a.rows * a.plan.parts;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(items, 1 << 20)));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(L), 0, stream, a); };
+    if (bf16 && a.top) go(k_scores<true, true>);
+    else if (bf16) go(k_scores<true, false>);
+    else if (a.top) go(k_scores<false, true>);
+    else go(k_scores<false, false>);
+    if (a.plan.parts > 1) {
+        const dim3 rows(static_cast<unsigned>(std::min<int64_t>(a.rows, 1 << 20)));
+        if (bf16) hipLaunchKernelGGL(k_scores_join<true>, rows, dim3(64), 0, stream, a);
+        else hipLaunchKernelGGL(k_scores_join<false>, rows, dim3(64), 0, stream, a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_score_grad(const ScoreGradArgs& a, bool bf16, hipStream_t stream)
+{
+    if (a.rows == 0) return hipSuccess;
+    const int64_t segments = (a.vocab + 4095) / 4096;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(a.rows * segments, 1 << 22)));
+    if (bf16) hipLaunchKernelGGL(k_score_grad<true>, grid, dim3(256), 0, stream, a, segments);
+    else hipLaunchKernelGGL(k_score_grad<false>, grid, dim3(256), 0, stream, a, segments);
+    return hipGetLastError();
+}
+
+hipError_t launch_head_join(const HeadJoinArgs& a, hipStream_t stream)
+{
+    const int64_t groups = (a.rows + kJoinRows - 1) / kJoinRows;
+    if (groups == 0) return hipSuccess;
+    hipLaunchKernelGGL(k_head_join, dim3(static_cast<unsigned>(groups)), dim3(kJoinRows * kJoinWays),
+                       0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace gefen

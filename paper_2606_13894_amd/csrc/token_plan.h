@@ -1,0 +1,154 @@
+// Host-side plans of the operators at a language model's two ends: how work is cut, and where
+// what lies between the kernels stands in the caller's workspace. Plain C++ (no HIP), so that it can
+// be checked on a host.
+#pragma once
+#include <algorithm>
+#include <cstdint>
+
+#include "ffn_plan.h"
+
+namespace gefen {
+
+// ---------------------------------------------------------------- embedding
+// Sorting by digits of at most kSortBits: passes, and the bits of each, for keys 0 .. most.
+constexpr int kSortBits = 9;
+struct SortPlan {
+    int passes;
+    int bits[4];
+};
+inline SortPlan sort_plan(int64_t most)
+{
+    int all = 1;
+    while (most >> all) ++all;
+    SortPlan s{};
+    s.passes = (all + kSortBits - 1) / kSortBits;
+    for (int p = 0, left = all; p < s.passes; ++p) {
+        s.bits[p] = (left + s.passes - p - 1) / (s.passes - p);
+        left -= s.bits[p];
+    }
+    return s;
+}
+
+// Sorted positions are summed in aligned chunks where one token fills a whole chunk.
+inline int64_t embed_chunk(int64_t n) { return n <= 65536 ? 32 : 256; }
+
+struct EmbedSpace {
+    int64_t keys[2], rows[2], partial, bytes = 0;
+};
+inline EmbedSpace embed_space(int64_t n, int64_t width)
+{
+    EmbedSpace s;
+    auto take = [&](int64_t bytes) {
+        const int64_t at = s.bytes;
+        s.bytes += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    for (int i = 0; i < 2; ++i) {
+        s.keys[i] = take(4 * n);
+        s.rows[i] = take(4 * n);
+    }
+    s.partial = take(4 * (n / embed_chunk(n)) * width);
+    return s;
+}
+
+// ---------------------------------------------------------------- log probabilities
+constexpr int64_t kScoreMaxTop = 32;
+constexpr int64_t kScoreMaxParts = 64;
+constexpr int kScoreThreads = 256;
+
+// A row is taken by `parts` workgroups, each `per` vectors of 16 bytes of it.
+struct ScorePlan {
+    int64_t parts = 1;
+    int64_t per = 0;
+};
+inline ScorePlan score_plan(int64_t rows, int64_t vocab, bool bf16)
+{
+    const int64_t vectors = ffn_ceil(vocab, bf16 ? 8 : 4);
+    ScorePlan p;
+    const int64_t most = std::min(kScoreMaxParts, ffn_ceil(vectors, 2 * kScoreThreads));
+    p.parts = std::max<int64_t>(1, std::min(most, ffn_ceil(1024, std::max<int64_t>(rows, 1))));
+    p.per = ffn_ceil(vectors, p.parts);
+    p.parts = ffn_ceil(vectors, p.per);
+    return p;
+}
+
+struct ScoreSpace {
+    int64_t stats = -1, keys = -1, bytes = 0;
+};
+inline ScoreSpace score_space(const ScorePlan& p, int64_t rows, int64_t top)
+{
+    ScoreSpace s;
+    if (p.parts > 1) {
+        s.keys = 0;
+        s.stats = 8 * rows * p.parts * top;
+        s.bytes = s.stats + 12 * rows * p.parts;
+    }
+    return s;
+}
+
+// ---------------------------------------------------------------- output head
+// Statistics of a row and tile: one for each wave's 128 columns.
+inline int64_t head_slots(int32_t tile, int64_t vocab)
+{
+    return ffn_ceil(vocab, ffn_tile_cols(tile)) * (tile == kFfnTile256 ? 2 : 1);
+}
+
+// The scores' gradients exist for a range of the vocabulary at a time, of at most this many bytes
+// (or 256 columns), and of rows whose tiles stay within 32-bit offsets.
+constexpr int64_t kHeadGradBytes = int64_t(1) << 30;
+
+struct HeadSpace {
+    int64_t x = -1, w = -1;            // padded copies
+    int64_t stats = -1, taken = -1;    // forward
+    int64_t dz = -1, partial = -1;     // backward
+    int64_t bytes = 0;
+    int64_t columns = 0, chunks = 1;   // of the vocabulary, in the backward pass
+    int64_t ldz = 0;
+    FfnTile score, dx, dw;
+};
+
+// copy: the operands' rows are no multiple of 8, or not aligned.
+inline HeadSpace head_space(int64_t T, int64_t K, int64_t V, bool backward, bool copy)
+{
+    HeadSpace s;
+    auto take = [&](int64_t bytes) {
+        const int64_t at = s.bytes;
+        s.bytes += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    const int64_t K8 = ffn_up8(K);
+    if (copy) {
+        s.x = take(2 * T * K8);
+        s.w = take(2 * V * K8);
+    }
+    if (!backward) {
+        const FfnResult z = {T, V, 1};
+        s.score = ffn_choose(&z, 1, K, 1, false, false, kFfnActivate);
+        s.stats = take(12 * T * head_slots(s.score.tile, V));
+        s.taken = take(4 * T);
+        return s;
+    }
+    const int64_t most = std::min(
+        kFfnMaxWidth, std::max<int64_t>(256, kHeadGradBytes / (2 * T) / 256 * 256));
+    s.columns = V;
+    if (V > most) {
+        s.columns = ffn_ceil(ffn_ceil(V, ffn_ceil(V, most)), 256) * 256;
+        s.chunks = ffn_ceil(V, s.columns);
+    }
+    s.ldz = ffn_up8(s.columns);
+    s.dz = take(2 * T * s.ldz);
+    const FfnResult z = {T, s.columns, 1}, dx = {T, K, 1}, dw = {s.columns, K, 1};
+    s.score = ffn_choose(&z, 1, K, 1, false, false, kFfnActivate);
+    s.dx = ffn_choose(&dx, 1, s.columns, 1, false, true, kFfnStore);
+    s.dw = ffn_choose(&dw, 1, T, 1, false, true, kFfnStore);
+    // the sums over the ranges are kept in float32; dx's and dw's parts are not there at once but
+    // where there are ranges
+    const int64_t parts_x = s.chunks > 1 ? 4 * T * K * s.dx.splits
+                                         : ffn_partial_bytes(s.dx, T, K, 1);
+    const int64_t parts_w = ffn_partial_bytes(s.dw, s.columns, K, 1);
+    const int64_t partial = parts_x + parts_w;
+    if (partial) s.partial = take(partial);
+    return s;
+}
+
+}  // namespace gefen
