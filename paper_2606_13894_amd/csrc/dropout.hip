@@ -7,7 +7,7 @@
 // serves eight elements, what a lane loads at once.
 #include "token_internal.h"
 
-#include "act8_device.h"
+#include "token_device.h"
 
 namespace gefen {
 namespace {
@@ -39,13 +39,13 @@ __global__ __launch_bounds__(256) void k_dropout(const DropoutArgs a)
         seed = static_cast<uint64_t>(a.state[0]);
         offset += static_cast<uint64_t>(a.state[1]);
     }
-    const int64_t blocks = (a.n + 7) / 8;
+    const int64_t blocks = (a.n + 7) / 8, n = by_lane(a.n);
     const int64_t step = int64_t(gridDim.x) * 256;
     for (int64_t b = int64_t(blockIdx.x) * 256 + threadIdx.x; b < blocks; b += step) {
         const int64_t e = 8 * b;
         float x[8], r[8];
-        load_row8<BF16>(a.x, e, a.n, x);
-        if constexpr (RESIDUAL) load_row8<BF16>(a.residual, e, a.n, r);
+        load_row8<BF16>(a.x, e, n, x);
+        if constexpr (RESIDUAL) load_row8<BF16>(a.residual, e, n, r);
         const u32x4a w = philox(static_cast<uint64_t>(b), offset, seed);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(256) void k_dropout(const DropoutArgs a)
             const float v = piece >= a.least ? x[j] * a.scale : 0.0f;
             x[j] = RESIDUAL ? v + r[j] : v;
         }
-        store_row8<BF16>(a.y, e, a.n, x);
+        store_row8<BF16>(a.y, e, n, x);
     }
 }
 

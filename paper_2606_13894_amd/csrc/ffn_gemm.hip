@@ -778,7 +778,7 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
         for (int mi = 0; mi < MI; ++mi) {
             const int64_t row = row0 + (wm * MI + mi) * 16 + l16;
             const bool on = FULL || row < g.M;
-            float m = -INFINITY;
+            float m = -INFINITY, low = INFINITY;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -788,17 +788,28 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
                         if (!FULL && first + h * H + 16 * j + 4 * q + i >= g.N)
                             acc[mi][h][j][i] = -INFINITY;
                         m = fmaxf(m, acc[mi][h][j][i]);
+                        low = fminf(low, acc[mi][h][j][i]);
                     }
             m = fmaxf(m, __shfl_xor(m, 16));
             m = fmaxf(m, __shfl_xor(m, 32));
-            const float base = score_base(m);
+            const ScoreBase base = score_base(m);
             float s = 0.0f, t = 0.0f;
+            if (__all(!base.huge && low > -kScoreHuge)) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int j = 0; j < NJ; ++j)
+                    for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) score_add(acc[mi][h][j][i], base, s, t);
+                        for (int i = 0; i < 4; ++i)
+                            score_add_plain(acc[mi][h][j][i], base.b, s, t);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) score_add(acc[mi][h][j][i], base, s, t);
+            }
             s += __shfl_xor(s, 16);
             t += __shfl_xor(t, 16);
             s += __shfl_xor(s, 32);

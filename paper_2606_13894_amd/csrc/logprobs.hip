@@ -1,10 +1,10 @@
 // Log probabilities of given tokens, their entropy and best alternatives, and the gradients, from rows
 // of scores; and the output head's rows from its tiles' statistics.
 //
-// One pass over a row: each lane keeps the largest score m of what it has read, s = sum exp(z - m) and
-// t = sum (z - m) exp(z - m), so that lse = m + log s, the entropy is log s - t / s, and a token's
-// log probability (z - m) - log s. Lanes, waves and, where rows are few, workgroups that share a row
-// are joined in a fixed order.
+// One pass over a row: each lane keeps the largest score m of what it has read, s = sum 2^d and
+// t = sum d 2^d with d = (z - m) log2 e (token_device.h), so that lse = m + ln 2 log2 s, the entropy is
+// ln 2 (log2 s - t / s), and a token's log probability ln 2 (d - log2 s). Lanes, waves and, where
+// rows are few, workgroups that share a row are joined in a fixed order.
 //
 // Best alternatives, by value and among equals by the lower index: a lane also keeps where its
 // largest score first stood. Its k lanes with the largest ones hold k scores at least as large as
@@ -42,11 +42,11 @@ __device__ __forceinline__ uint64_t score_key(float v, int64_t place)
     return (static_cast<uint64_t>(ordered(v)) << 32) | static_cast<uint32_t>(~place);
 }
 
-// 16 bytes of a row of n as scores.
+// 16 bytes of a row of n as scores. (A row has 2^24 of them at most.)
 template <bool BF16>
 struct Vec {
     static constexpr int N = BF16 ? 8 : 4;
-    static __device__ __forceinline__ u32x4a fetch(const void* row, int64_t v, int64_t n)
+    static __device__ __forceinline__ u32x4a fetch(const void* row, int v, int n)
     {
         return fetch_vector<BF16 ? 2 : 4>(row, v * N, n);
     }
@@ -58,8 +58,7 @@ struct Vec {
                         : __uint_as_float(w[j]);
     }
     // With -inf from n on.
-    static __device__ __forceinline__ void settle(const u32x4a& w, int64_t v, int64_t n,
-                                                  float (&z)[N])
+    static __device__ __forceinline__ void settle(const u32x4a& w, int v, int n, float (&z)[N])
     {
         unpack(settle_vector<BF16 ? 2 : 4>(w, v * N, n), z);
 #pragma unroll
@@ -85,37 +84,63 @@ struct ListSpace {
     uint64_t lane_keys[L];
     uint64_t list[kList];
     uint64_t best[kWaves];
+    uint64_t least;
     int lanes[kScoreMaxTop];
-    int count;
+    int found, count;
 };
 
 // The number of keys[0 .. n) above `key`.
 __device__ __forceinline__ int count_above(const uint64_t* keys, int n, uint64_t key)
 {
     int above = 0;
+#pragma unroll 4
     for (int i = 0; i < n; ++i) above += keys[i] > key;
     return above;
+}
+
+// A bound that exactly k of the distinct keys that the lanes of a wave hold reach, bit by bit
+// from the top; 0 where they are fewer than k (keys of 0 are none).
+template <int M>
+__device__ __forceinline__ uint64_t least_of_top(const uint64_t (&key)[M], int k)
+{
+    uint64_t least = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+        const uint64_t with = least | (uint64_t(1) << bit);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < M; ++i) n += __popcll(__ballot(key[i] >= with));
+        if (n >= k) least = with;
+        if (n == k) break;
+    }
+    return least;
 }
 
 // The k largest keys of vectors v0 .. v1 - 1 of a row, in order, to out; 0 where there are fewer.
 // `key`: of the lane's largest score, its place that vector's number; 0 where it has read none.
 template <bool BF16>
-__device__ void select_top(const void* row, int64_t n, int64_t v0, int64_t v1, int k, uint64_t key,
+__device__ void select_top(const void* row, int n, int v0, int v1, int k, uint64_t key,
                            ListSpace& s, uint64_t* __restrict__ out)
 {
     constexpr int N = Vec<BF16>::N;
     const int tid = threadIdx.x;
+    n = by_lane(n);
     s.lane_keys[tid] = key;
-    if (tid == 0) s.count = 0;
-    const int have = __syncthreads_count(key != 0);
-    const int rank = key ? count_above(s.lane_keys, L, key) : L;
-    if (rank < k) s.lanes[rank] = tid;
-    const int taken = min(have, k);
+    if (tid == 0) s.found = s.count = 0;
     __syncthreads();
-    const uint64_t least = have >= k ? s.lane_keys[s.lanes[k - 1]] : 0;
-    const int64_t per = (v1 - v0 + L - 1) / L;
-    for (int64_t i = tid; i < taken * per; i += L) {
-        const int64_t v = v0 + s.lanes[i / per] + (i % per) * L;
+    if (tid < 64) {
+        uint64_t some[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) some[w] = s.lane_keys[64 * w + tid];
+        const uint64_t least = least_of_top(some, k);
+        if (tid == 0) s.least = least;
+    }
+    __syncthreads();
+    const uint64_t least = s.least;
+    if (key && key >= least) s.lanes[atomicAdd(&s.found, 1)] = tid;   // k of them at most
+    __syncthreads();
+    const int per = (v1 - v0 + L - 1) / L;
+    for (int i = tid; i < s.found * per; i += L) {
+        const int v = v0 + s.lanes[i / per] + (i % per) * L;
         if (v >= v1) continue;
         float z[N];
         Vec<BF16>::settle(Vec<BF16>::fetch(row, v, n), v, n, z);
@@ -138,7 +163,7 @@ __device__ void select_top(const void* row, int64_t n, int64_t v0, int64_t v1, i
         uint64_t before = ~uint64_t(0);
         for (int r = 0; r < k; ++r) {
             uint64_t best = 0;
-            for (int64_t v = v0 + tid; v < v1; v += L) {
+            for (int v = v0 + tid; v < v1; v += L) {
                 float z[N];
                 Vec<BF16>::settle(Vec<BF16>::fetch(row, v, n), v, n, z);
 #pragma unroll
@@ -170,7 +195,8 @@ __device__ __forceinline__ void write_top(const ScoreArgs& a, int64_t row, const
     const int64_t o = row * a.top + i;
     const float v = unordered(static_cast<uint32_t>(key >> 32));
     const bool bad = sum.s != sum.s;
-    a.top_logprob[o] = bad ? sum.s : v == -INFINITY ? v : (v - sum.m) - logf(sum.s);
+    a.top_logprob[o] = bad ? sum.s : v == -INFINITY ? v
+                                   : score_logprob(v, score_base(sum.m), log2f(sum.s));
     a.top_token[o] = bad ? -1 : static_cast<int64_t>(~static_cast<uint32_t>(key));
 }
 
@@ -199,50 +225,57 @@ __global__ __launch_bounds__(L) void k_scores(const ScoreArgs a)
     __shared__ typename std::conditional<TOP, ListSpace, int>::type list;
     __shared__ uint64_t best[TOP ? kScoreMaxTop : 1];
     const int tid = threadIdx.x;
-    const int64_t vectors = (a.vocab + N - 1) / N, whole = a.vocab / N;
+    const int vocab = static_cast<int>(a.vocab);
+    const int vectors = (vocab + N - 1) / N, whole = vocab / N;
     const int64_t items = a.rows * a.plan.parts;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t r = item / a.plan.parts, part = item % a.plan.parts;
         const char* row = static_cast<const char*>(a.z) + r * a.ld * S;
-        const int64_t v0 = part * a.plan.per, v1 = min(vectors, v0 + a.plan.per);
+        const int v0 = static_cast<int>(part * a.plan.per);
+        const int v1 = min(vectors, v0 + static_cast<int>(a.plan.per));
         const bool one = a.plan.parts == 1;
         int64_t token = -1;
         float taken = 0.0f;
         if (one && tid == 0) {
             token = token_at(a.tokens.p, a.tokens.wide, r);
-            if (token >= 0 && token < a.vocab) taken = score_at<BF16>(row, token);
+            if (token >= 0 && token < vocab) taken = score_at<BF16>(row, token);
         }
         ScoreSum c = {-INFINITY, 0.0f, 0.0f};
         float top = -INFINITY;
-        int64_t place = -1;
-        // A lane's vectors are L apart, U of them loaded before the first is used.
-        for (int64_t b = v0; b < v1; b += U * L) {
-            const bool full = b + U * L <= min(v1, whole);
-            u32x4a w[U];
+        int place = -1;
+        // A lane's vectors are L apart; U of them are worked on while the next U are on their way.
+        // (A vector past the end is the last one again, and left out below.)
+        u32x4a next[U];
+        auto load = [&](int b) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                next[u] = V::fetch(row, min(b + u * L + tid, vectors - 1), vocab);
+        };
+        auto work = [&](const u32x4a (&w)[U], int b, auto is_full) {
+            constexpr bool FULL = decltype(is_full)::value;
             float z[U][N];
+            float m = -INFINITY, low = INFINITY;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int64_t v = b + u * L + tid;
-                if (full || v < v1) w[u] = V::fetch(row, v, a.vocab);
-            }
-            float m = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t v = b + u * L + tid;
-                if (full) {
+                const int v = b + u * L + tid;
+                if constexpr (FULL) {
                     V::unpack(w[u], z[u]);
                 } else if (v < v1) {
-                    V::settle(w[u], v, a.vocab, z[u]);
+                    V::settle(w[u], v, vocab, z[u]);
                 } else {
 #pragma unroll
                     for (int j = 0; j < N; ++j) z[u][j] = -INFINITY;
                 }
-                float vm = z[u][0];
+                float vm = z[u][0], vl = z[u][0];
 #pragma unroll
-                for (int j = 1; j < N; ++j) vm = fmaxf(vm, z[u][j]);
+                for (int j = 1; j < N; ++j) {
+                    vm = fmaxf(vm, z[u][j]);
+                    vl = fminf(vl, z[u][j]);
+                }
                 m = fmaxf(m, vm);
+                low = fminf(low, vl);
                 if constexpr (TOP) {
-                    if ((full || v < v1) && (place < 0 || vm > top)) {
+                    if ((FULL || v < v1) && (place < 0 || vm > top)) {
                         top = vm;
                         place = v;
                     }
@@ -250,12 +283,28 @@ __global__ __launch_bounds__(L) void k_scores(const ScoreArgs a)
             }
             const float old = c.m;
             c.m = fmaxf(old, m);
-            const float base = score_base(c.m);
+            const ScoreBase base = score_base(c.m);
             score_rebase(old, base, c.s, c.t);
+            if (__all(!base.huge && low > -kScoreHuge)) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int j = 0; j < N; ++j) score_add(z[u][j], base, c.s, c.t);
+                    for (int j = 0; j < N; ++j) score_add_plain(z[u][j], base.b, c.s, c.t);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) score_add(z[u][j], base, c.s, c.t);
+            }
+        };
+        load(v0);
+        for (int b = v0; b < v1; b += U * L) {
+            u32x4a w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) w[u] = next[u];
+            if (b + U * L < v1) load(b + U * L);
+            if (b + U * L <= min(v1, whole)) work(w, b, std::integral_constant<bool, true>{});
+            else work(w, b, std::integral_constant<bool, false>{});
         }
         c = wave_join(c);
         if ((tid & 63) == 0) sums[tid >> 6] = c;
@@ -266,7 +315,7 @@ __global__ __launch_bounds__(L) void k_scores(const ScoreArgs a)
         if constexpr (TOP) {
             // (a NaN as the largest of a vector ends in a row whose alternatives are not given)
             const uint64_t key = place >= 0 ? score_key(top, place) : 0;
-            select_top<BF16>(row, a.vocab, v0, v1, a.top, key, list, best);
+            select_top<BF16>(row, vocab, v0, v1, a.top, key, list, best);
             if (tid < a.top) {
                 if (one) write_top(a, r, c, tid, best[tid]);
                 else a.keys[item * a.top + tid] = best[tid];
@@ -311,12 +360,8 @@ __global__ __launch_bounds__(64) void k_scores_join(const ScoreArgs a)
             for (int i = lane; i < n; i += 64) keys[i] = a.keys[r * n + i];
             __syncthreads();
             // no key below the k-th largest of the parts' largest ones is among the k largest
-            const uint64_t mine = lane < parts ? keys[lane * a.top] : 0;
-            int above = 0;
-            for (int p = 0; p < parts; ++p) above += keys[p * a.top] > mine;
-            const uint64_t at = __ballot(lane < parts && above == a.top - 1);
-            const uint64_t least = at ? __shfl(static_cast<unsigned long long>(mine),
-                                               __ffsll(static_cast<unsigned long long>(at)) - 1) : 1;
+            const uint64_t first[1] = {lane < parts ? keys[lane * a.top] : 0};
+            const uint64_t least = max(least_of_top(first, a.top), uint64_t(1));
             int count = 0;
             for (int i = 0; i < n; i += 64) {
                 const uint64_t key = i + lane < n ? keys[i + lane] : 0;
@@ -368,8 +413,8 @@ __global__ __launch_bounds__(256) void k_score_grad(const ScoreGradArgs a, int64
 }
 
 // ---------------------------------------------------------------- output head
-// A workgroup joins 16 rows, 64 lanes to a row by the slots.
-constexpr int kJoinRows = 16, kJoinWays = 16;
+// A workgroup joins 16 rows, 64 lanes to a row by the slots, four of a lane's on their way at once.
+constexpr int kJoinRows = 16, kJoinWays = 64;
 
 __global__ __launch_bounds__(kJoinRows * kJoinWays) void k_head_join(const HeadJoinArgs a)
 {
@@ -378,14 +423,28 @@ __global__ __launch_bounds__(kJoinRows * kJoinWays) void k_head_join(const HeadJ
     const int64_t r = int64_t(blockIdx.x) * kJoinRows + in;
     ScoreSum c = {-INFINITY, 0.0f, 0.0f};
     if (r < a.rows)
-        for (int64_t s = way; s < a.slots; s += kJoinWays) {
-            const float* p = a.stats + s * 3 * a.rows + r;
-            c = score_join(c, ScoreSum{p[0], p[a.rows], p[2 * a.rows]});
+        for (int64_t s = way; s < a.slots; s += 4 * kJoinWays) {
+            ScoreSum v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t at = min(s + u * kJoinWays, a.slots - 1);
+                const float* p = a.stats + at * 3 * a.rows + r;
+                v[u] = ScoreSum{p[0], p[a.rows], p[2 * a.rows]};
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (s + u * kJoinWays < a.slots) c = score_join(c, v[u]);
         }
     sums[way][in] = c;
-    __syncthreads();
+#pragma unroll
+    for (int half = kJoinWays / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (way < half) {
+            c = score_join(c, sums[way + half][in]);
+            sums[way][in] = c;
+        }
+    }
     if (way > 0 || r >= a.rows) return;
-    for (int w = 1; w < kJoinWays; ++w) c = score_join(c, sums[w][in]);
     const int64_t token = token_at(a.tokens.p, a.tokens.wide, r);
     const float taken = token >= 0 && token < a.vocab ? a.taken[r] : 0.0f;
     const ScoreRow o = score_row(c, token, a.vocab, taken);

@@ -13,32 +13,79 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, bool wide, int64
                 : static_cast<int64_t>(static_cast<const int32_t*>(tokens)[i]);
 }
 
-// ---------------------------------------------------------------- sums of exponentials
-// Over a set of scores z: m the largest, s the sum of exp(z - base), t that of (z - base) times it,
-// with base = m; 0 where no score is above -inf, so that no difference of infinities is formed:
-// each term is then 0. A NaN or an infinity among the scores makes s NaN (inf - inf), and keeps it
-// so. In t the difference is held at -1e4, far below where exp is 0, so that -inf adds 0.
-constexpr float kLog2E = 1.4426950408889634f;
-
-__device__ __forceinline__ float score_base(float m) { return m == -INFINITY ? 0.0f : m; }
-
-__device__ __forceinline__ void score_add(float z, float base, float& s, float& t)
+// The number, which the compiler is to take as one that differs from lane to lane. A row's length is
+// the same in all of them, and so are comparisons with it; but where such a comparison stands in
+// a loop that lanes leave at different times, this compiler (ROCm 7.2) kept its outcome as a mask of
+// the lanes that were still there, and used that mask after the loop for the lanes that had left:
+// they took the path of rows shorter than a vector.
+__device__ __forceinline__ int64_t by_lane(int64_t n)
 {
-    const float d = z - base;
-    const float e = __builtin_amdgcn_exp2f(d * kLog2E);
+    asm("" : "+v"(n));
+    return n;
+}
+__device__ __forceinline__ int by_lane(int n)
+{
+    asm("" : "+v"(n));
+    return n;
+}
+
+// ---------------------------------------------------------------- sums of exponentials
+// Over a set of scores z with m the largest: s = sum 2^d and t = sum d 2^d, d = z log2 e - B, where
+// the base B is m log2 e as rounded to float32. One multiply-add forms d from the exact product; that
+// B is rounded does not matter, since whatever is made of s and t takes the same B.
+// From 2^126 on in magnitude, where z log2 e may overflow, d = (z - m) log2 e instead. Where no score
+// is above -inf, B is 0: no difference of infinities is formed and each term is 0. In t, d is held at
+// -1e4, far below where 2^d is 0, so that -inf adds 0. A NaN or +inf among the scores makes s NaN
+// (inf - inf), and nothing that follows takes that away.
+constexpr float kLog2E = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kScoreHuge = 8.507059173023462e37f;   // 2^126
+
+struct ScoreBase {
+    float m, b;
+    bool huge;
+};
+__device__ __forceinline__ ScoreBase score_base(float m)
+{
+    ScoreBase r;
+    r.m = m == -INFINITY ? 0.0f : m;
+    r.b = r.m * kLog2E;
+    r.huge = fabsf(r.m) >= kScoreHuge;
+    return r;
+}
+__device__ __forceinline__ float score_far(float z, const ScoreBase& r)
+{
+    return r.huge ? (z - r.m) * kLog2E : fmaf(z, kLog2E, -r.b);
+}
+
+// One score, whatever it and the base are.
+__device__ __forceinline__ void score_add(float z, const ScoreBase& r, float& s, float& t)
+{
+    const float d = score_far(z, r);
+    const float e = __builtin_amdgcn_exp2f(d);
     s += e;
     t = fmaf(e, fmaxf(d, -1e4f), t);
+}
+// One whose base is not huge, above -2^126.
+__device__ __forceinline__ void score_add_plain(float z, float b, float& s, float& t)
+{
+    const float d = fmaf(z, kLog2E, -b);
+    const float e = __builtin_amdgcn_exp2f(d);
+    s += e;
+    t = fmaf(e, d, t);
 }
 
 struct ScoreSum {
     float m, s, t;
 };
 
-// The same sums with a larger base.
-__device__ __forceinline__ void score_rebase(float m, float base, float& s, float& t)
+// The same sums from another, larger m.
+__device__ __forceinline__ void score_rebase(float old, const ScoreBase& to, float& s, float& t)
 {
-    const float d = fmaxf(m - base, -1e4f);   // also where nothing was summed yet
-    const float e = __builtin_amdgcn_exp2f(d * kLog2E);
+    const ScoreBase from = score_base(old);
+    const float gap = to.huge || from.huge ? (from.m - to.m) * kLog2E : from.b - to.b;
+    const float d = old == -INFINITY ? -1e4f : fmaxf(gap, -1e4f);   // (nothing was summed yet)
+    const float e = __builtin_amdgcn_exp2f(d);
     t = e * fmaf(s, d, t);
     s *= e;
 }
@@ -47,12 +94,18 @@ __device__ __forceinline__ ScoreSum score_join(ScoreSum a, ScoreSum b)
 {
     ScoreSum r;
     r.m = fmaxf(a.m, b.m);
-    const float base = score_base(r.m);
+    const ScoreBase base = score_base(r.m);
     score_rebase(a.m, base, a.s, a.t);
     score_rebase(b.m, base, b.s, b.t);
     r.s = a.s + b.s;
     r.t = a.t + b.t;
     return r;
+}
+
+// log2 p of a score from the row's sums and log2 s; lse = m + ln 2 (log2 s + (B - m log2 e)).
+__device__ __forceinline__ float score_logprob(float z, const ScoreBase& base, float log2s)
+{
+    return kLn2 * (score_far(z, base) - log2s);
 }
 
 // A row's results. `taken`: its token's score.
@@ -69,10 +122,11 @@ __device__ __forceinline__ ScoreRow score_row(const ScoreSum& a, int64_t token, 
         r.lse = r.logprob = -INFINITY;
         r.entropy = 0.0f;
     } else {
-        const float l = logf(a.s);
-        r.lse = a.m + l;
-        r.entropy = fmaxf(l - a.t / a.s, 0.0f);
-        r.logprob = (taken - a.m) - l;
+        const ScoreBase base = score_base(a.m);
+        const float l = log2f(a.s);
+        r.lse = fmaf(kLn2, base.huge ? l : l - fmaf(a.m, kLog2E, -base.b), a.m);
+        r.entropy = fmaxf(kLn2 * (l - a.t / a.s), 0.0f);
+        r.logprob = score_logprob(taken, base, l);
     }
     if (token < 0) r.logprob = 0.0f;
     if (token >= vocab) r.logprob = __uint_as_float(0x7fc00000u);
