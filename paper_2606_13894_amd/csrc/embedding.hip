@@ -3,11 +3,13 @@
 // Forward: y_r = scale E[t_r], one pass over the rows asked for.
 //
 // Backward: dE[v] = scale sum_{r: t_r = v} dy_r, in float32 in increasing r, rounded once. The tokens
-// are sorted (stably, so that the order of a sum depends on the tokens alone), then a wave owns a
-// few rows of the table: it finds its first one among the sorted tokens, 64 probes at a time, and
-// writes every row once, zeros where no token asked for it. A token that stands often would leave its
-// row's wave with a long sum: wherever one token fills a whole aligned chunk of sorted positions, that
-// chunk's sum is formed before, by a wave of its own, and the row takes it as one term.
+// are sorted (stably, so that the order of a sum depends on the tokens alone), and the sorted
+// positions cut into chunks of equal length, a wave for each (and 512 columns). A token that lies in
+// one chunk altogether gets its row of the table from there; one that goes over an end leaves the sum
+// of its part, and a second launch adds such parts in order: a token that stands often, as some
+// always do, is shared by as many waves as it fills chunks. Most rows of a table are asked for by no
+// token: the whole table is set to zero by workgroups beside those of the sort, which wait for
+// memory most of their time.
 //
 // Sort: by digits of up to nine bits from the lowest; one workgroup for each value of the digit
 // reads all the tokens, counts those with a smaller digit, which is where its own begin, and those
@@ -51,6 +53,23 @@ __global__ __launch_bounds__(256) void k_embedding(const EmbedArgs a, int lanes)
     }
 }
 
+// ---------------------------------------------------------------- zeros
+// Bytes [from, to) of the table, by `groups` workgroups of T threads.
+struct Zeros {
+    char* table;
+    int64_t from, to;
+    uint32_t groups;
+};
+template <int T>
+__device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t group)
+{
+    const u32x4a none = {0u, 0u, 0u, 0u};
+    const int64_t step = int64_t(z.groups) * T * 16;
+    int64_t at = z.from + (int64_t(group) * T + threadIdx.x) * 16;
+    for (; at + 16 <= z.to; at += step) store16(z.table + at, none);
+    for (; at < z.to; at += 2) *reinterpret_cast<uint16_t*>(z.table + at) = 0;
+}
+
 // ---------------------------------------------------------------- sort
 struct SortPass {
     Tokens tokens;               // the first pass's keys; p null: keys
@@ -61,6 +80,7 @@ struct SortPass {
     int64_t n;
     uint32_t vocab;              // the key of a token outside 0 .. vocab - 1
     int shift, bits;
+    Zeros zeros;                 // the first workgroups write them
 };
 
 __device__ __forceinline__ uint32_t sort_key(const SortPass& a, int64_t i)
@@ -72,12 +92,16 @@ __device__ __forceinline__ uint32_t sort_key(const SortPass& a, int64_t i)
 
 constexpr int kSortWaves = 16, kSortKeys = 8;   // keys of a lane that are loaded together
 
-__global__ __launch_bounds__(64 * kSortWaves) void k_sort_pass(const SortPass a)
+__global__ __launch_bounds__(64 * kSortWaves, 8) void k_sort_pass(const SortPass a)
 {
     __shared__ int64_t below[kSortWaves], mine[kSortWaves];
+    if (blockIdx.x < a.zeros.groups) {
+        write_zeros<64 * kSortWaves>(a.zeros, blockIdx.x);
+        return;
+    }
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t digit = blockIdx.x, mask = (1u << a.bits) - 1;
+    const uint32_t digit = blockIdx.x - a.zeros.groups, mask = (1u << a.bits) - 1;
     const int64_t from = a.n * wave / kSortWaves, to = a.n * (wave + 1) / kSortWaves;
     constexpr int kStep = 64 * kSortKeys;
     uint32_t key[kSortKeys];
@@ -137,154 +161,125 @@ struct EmbedSum {
     const uint32_t* rows;
     const void* dy;
     int64_t n, vocab, width;
-    int64_t chunk;               // a power of two
-    float* partial;              // [n / chunk][width]
+    int64_t chunk, chunks;       // sorted positions of a chunk
+    float* head;                 // [chunks][width]: of the token that a chunk begins with, where it
+                                 // came from the chunk before
+    float* tail;                 // of the one that it ends with, where it goes on
     float scale;
     void* dtable;
-    int lanes;                   // along a row, a power of two, 256 at most
-    int64_t per;                 // rows of the table for a workgroup
 };
 
-// acc += the rows at sorted positions p .. to - 1, eight elements from e on, in order. U rows are on
-// their way at a time.
-template <bool DY16, int U>
-__device__ __forceinline__ void add_rows(const EmbedSum& a, int64_t width, int64_t p, int64_t to,
-                                         int64_t e, float (&acc)[8])
+template <bool T16>
+__device__ __forceinline__ void store_sum(const EmbedSum& a, uint32_t key, int64_t e,
+                                          const float (&acc)[8])
 {
-    constexpr int S = DY16 ? 2 : 4;
-    const char* dy = static_cast<const char*>(a.dy);
-    for (; p < to; p += U) {
-        uint32_t r[U];
-        u32x4a w[U][DY16 ? 1 : 2];
+    float v[8];
 #pragma unroll
-        for (int u = 0; u < U; ++u) r[u] = a.rows[p + u < to ? p + u : to - 1];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p + u < to) fetch8<DY16>(dy + int64_t(r[u]) * width * S, e, width, w[u]);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p + u < to) {
-                float v[8];
-                settle8<DY16>(w[u], e, width, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += v[j];
-            }
-    }
+    for (int j = 0; j < 8; ++j) v[j] = acc[j] * a.scale;
+    store_row8<T16>(static_cast<char*>(a.dtable) + int64_t(key) * a.width * (T16 ? 2 : 4), e,
+                    a.width, v);
 }
 
-// acc += rows c .. to - 1 of the chunks' sums.
-__device__ __forceinline__ void add_chunks(const EmbedSum& a, int64_t width, int64_t c, int64_t to,
-                                           int64_t e, float (&acc)[8])
-{
-    constexpr int U = 4;
-    for (; c < to; c += U) {
-        u32x4a w[U][2];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (c + u < to) fetch8<false>(a.partial + (c + u) * width, e, width, w[u]);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (c + u < to) {
-                float v[8];
-                settle8<false>(w[u], e, width, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += v[j];
-            }
-    }
-}
-
-// The sums of whole chunks of one token. A wave takes 512 columns of a chunk.
-template <bool DY16>
+// A wave's chunk: what it does depends on the keys alone, so that its lanes stay together; U rows
+// are on their way at a time.
+template <bool DY16, bool T16>
 __global__ __launch_bounds__(64) void k_embed_chunks(const EmbedSum a, int64_t slabs)
 {
-    const int64_t width = by_lane(a.width);
-    const int64_t all = a.n / a.chunk * slabs;
+    constexpr int U = 16, S = DY16 ? 2 : 4;
+    const char* dy = static_cast<const char*>(a.dy);
+    const int64_t all = a.chunks * slabs;
+    for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
+        const int64_t c = i / slabs, p0 = c * a.chunk, p1 = min(a.n, p0 + a.chunk);
+        const int64_t e = (i % slabs) * 512 + 8 * threadIdx.x;
+        const int64_t mine = min(e, (a.width - 1) / 8 * 8);   // lanes past the row read its end again
+        const bool on = e < a.width;
+        // lane l has the key at position p - 1 + l and the row at p + l, U of them used
+        auto keys_at = [&](int64_t p) {
+            const int64_t at = p - 1 + static_cast<int>(threadIdx.x);
+            return at >= 0 && at < a.n ? a.keys[at] : 0xffffffffu;
+        };
+        uint32_t keys = keys_at(p0);
+        const uint32_t before = __builtin_amdgcn_readlane(keys, 0);
+        uint32_t now = __builtin_amdgcn_readlane(keys, 1), after = now;
+        bool head = now == before;               // the token came from the chunk before
+        float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        for (int64_t p = p0; p < p1; p += U) {
+            if (p > p0) keys = keys_at(p);
+            const uint32_t rows = a.rows[min(p + static_cast<int>(threadIdx.x), p1 - 1)];
+            const int m = static_cast<int>(min(p1 - p, int64_t(U)));
+            u32x4a w[U][DY16 ? 1 : 2];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t row = __builtin_amdgcn_readlane(rows, u);
+                fetch8<DY16>(dy + row * a.width * S, mine, a.width, w[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t key = __builtin_amdgcn_readlane(keys, u + 1);
+                if (u >= m || key >= a.vocab) continue;   // (no token of the table: the last keys)
+                if (key != now) {
+                    if (head && on) store_row8<false>(a.head + c * a.width, e, a.width, acc);
+                    if (!head && on) store_sum<T16>(a, now, e, acc);
+                    head = false;
+                    now = key;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
+                }
+                float v[8];
+                settle8<DY16>(w[u], mine, a.width, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += v[j];
+            }
+            after = __builtin_amdgcn_readlane(keys, m + 1);
+        }
+        if (now >= a.vocab || !on) continue;
+        // a token that fills the chunk from the one before on is a head, whether it goes on or not
+        if (head) store_row8<false>(a.head + c * a.width, e, a.width, acc);
+        else if (now == after) store_row8<false>(a.tail + c * a.width, e, a.width, acc);
+        else store_sum<T16>(a, now, e, acc);
+    }
+}
+
+// Tokens that go over the ends of chunks: by the wave of the chunk in which they begin.
+template <bool T16>
+__global__ __launch_bounds__(64) void k_embed_spans(const EmbedSum a, int64_t slabs)
+{
+    constexpr int U = 16;
+    const int64_t all = a.chunks * slabs;
     for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
         const int64_t c = i / slabs, e = (i % slabs) * 512 + 8 * threadIdx.x;
-        const uint32_t key = a.keys[c * a.chunk];
-        if (key >= a.vocab || key != a.keys[(c + 1) * a.chunk - 1] || e >= width) continue;
-        float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        add_rows<DY16, DY16 ? 16 : 8>(a, width, c * a.chunk, (c + 1) * a.chunk, e, acc);
-        store_row8<false>(a.partial + c * width, e, width, acc);
-    }
-}
-
-// The first sorted position in [lo, n) whose key is not below `key`; all lanes together.
-__device__ __forceinline__ int64_t lower_bound(const uint32_t* keys, int64_t lo, int64_t n,
-                                               uint32_t key, int lane)
-{
-    int64_t hi = n;              // in [lo, hi]
-    while (lo < hi) {
-        const int64_t step = (hi - lo + 63) / 64;
-        const int64_t i = lo + (lane + 1) * step - 1;   // the last of the lane's step
-        const bool under = i < hi && keys[i] < key;
-        const int64_t whole = __popcll(__ballot(under)); // steps that lie below altogether
-        lo += whole * step;
-        hi = min(hi, lo + step - 1);
-        if (step == 1) break;
-    }
-    return lo;
-}
-
-// A workgroup writes `per` rows of the table: `lanes` lanes a row, so that wide rows are shared by
-// its waves and narrow ones lie side by side in one.
-template <bool DY16, bool T16>
-__global__ __launch_bounds__(256) void k_embed_sum(const EmbedSum a)
-{
-    const int lane = threadIdx.x & 63;
-    const int sub = threadIdx.x / a.lanes, along = threadIdx.x % a.lanes;
-    const int together = 256 / a.lanes;
-    // the rows of this wave: the (first + k)-th of `together`, k < mine
-    const int first_sub = __builtin_amdgcn_readfirstlane(sub);
-    const int mine = a.lanes >= 64 ? 1 : 64 / a.lanes;
-    constexpr int TS = T16 ? 2 : 4;
-    const int64_t width = by_lane(a.width);
-    const int64_t groups = (a.vocab + a.per - 1) / a.per;
-    for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
-        const int64_t v0 = g * a.per, v1 = min(a.vocab, v0 + a.per);
-        int64_t at = lower_bound(a.keys, 0, a.n, static_cast<uint32_t>(v0), lane);
-        auto window = [&]() { return at + lane < a.n ? a.keys[at + lane] : 0xffffffffu; };
-        uint32_t keys = window();                    // 64 of them, one a lane, from `at` on
-        auto bound = [&](int64_t v) {                // the first position of a key >= v > v0
-            int64_t end = at + __popcll(__ballot(keys < static_cast<uint32_t>(v)));
-            if (end == at + 64) {                    // further than the window
-                end = at = lower_bound(a.keys, end, a.n, static_cast<uint32_t>(v), lane);
-                keys = window();
-            }
-            return end;
-        };
-        for (int64_t v = v0; v < v1; v += together) {
-            int64_t first = 0, last = 0;             // of the lane's row
-            const int64_t w = v + first_sub;
-            if (w < v1) {
-                int64_t pos = bound(w);
-                for (int k = 0; k < mine && w + k < v1; ++k) {
-                    const int64_t end = bound(w + k + 1);
-                    if (first_sub + k == sub) {
-                        first = pos;
-                        last = end;
-                    }
-                    pos = end;
-                }
-            }
-            if (v + sub >= v1) continue;
-            char* to = static_cast<char*>(a.dtable) + (v + sub) * width * TS;
-            for (int64_t e = 8 * along; e < width; e += 8 * a.lanes) {
-                float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-                if (first < last) {
-                    const int64_t c0 = (first + a.chunk - 1) / a.chunk, c1 = last / a.chunk;
-                    const bool chunks = c0 < c1;
-                    add_rows<DY16, 8>(a, width, first, chunks ? c0 * a.chunk : last, e, acc);
-                    if (chunks) {
-                        add_chunks(a, width, c0, c1, e, acc);
-                        add_rows<DY16, 8>(a, width, c1 * a.chunk, last, e, acc);
-                    }
+        const int64_t mine = min(e, (a.width - 1) / 8 * 8);
+        const int64_t p0 = c * a.chunk, p1 = p0 + a.chunk;
+        if (p1 >= a.n) continue;
+        const uint32_t key = a.keys[p1 - 1];
+        if (key >= a.vocab || key != a.keys[p1]) continue;
+        if (p0 > 0 && a.keys[p0 - 1] == key) continue;      // it began before
+        float acc[8];
+        load_row8<false>(a.tail + c * a.width, mine, a.width, acc);
+        // the chunks that begin with it, as far as 64 of them at a time
+        for (int64_t d = c + 1;;) {
+            const int64_t at = d + static_cast<int>(threadIdx.x);
+            const uint64_t other = ~__ballot(at < a.chunks && a.keys[at * a.chunk] == key);
+            const int64_t end = other ? d + __ffsll(static_cast<unsigned long long>(other)) - 1
+                                      : d + 64;
+            for (; d < end; d += U) {
+                u32x4a w[U][2];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[j] *= a.scale;
+                for (int u = 0; u < U; ++u)
+                    fetch8<false>(a.head + min(d + u, end - 1) * a.width, mine, a.width, w[u]);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (d + u >= end) continue;
+                    float v[8];
+                    settle8<false>(w[u], mine, a.width, v);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[j] += v[j];
                 }
-                store_row8<T16>(to, e, width, acc);
             }
+            d = end;
+            if (other) break;
         }
+        if (e < a.width) store_sum<T16>(a, key, e, acc);
     }
 }
 
@@ -310,27 +305,35 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
                                  hipStream_t stream)
 {
     const SortPlan plan = sort_plan(a.vocab);
-    SortPass s{};
-    s.n = a.n;
-    s.vocab = static_cast<uint32_t>(a.vocab);
+    const int64_t bytes = a.vocab * a.width * (table_bf16 ? 2 : 4);
+    // The zeros are shared by the sort's launches. One workgroup on each CU writes them, so that the
+    // sort's have the other half of it.
+    const int passes = a.n > 0 ? plan.passes : 1;
+    constexpr int kThreads = 64 * kSortWaves;
     int out = 0;
-    if (a.n > 0) {
-        for (int p = 0, shift = 0; p < plan.passes; shift += plan.bits[p], ++p) {
-            s.tokens = a.tokens;
-            if (p > 0) s.tokens.p = nullptr;
-            s.keys = a.keys[out];
-            s.rows = a.rows[out];
-            out ^= 1;
-            s.keys_out = a.keys[out];
-            s.rows_out = a.rows[out];
-            s.shift = shift;
-            s.bits = plan.bits[p];
-            // the last digit ends with the largest key's
-            const int64_t digits = p + 1 < plan.passes ? int64_t(1) << s.bits : (a.vocab >> shift) + 1;
-            hipLaunchKernelGGL(k_sort_pass, dim3(static_cast<unsigned>(digits)),
-                               dim3(64 * kSortWaves), 0, stream, s);
-        }
+    for (int p = 0, shift = 0; p < passes; shift += plan.bits[p], ++p) {
+        SortPass s{};
+        s.zeros.table = static_cast<char*>(a.dtable);
+        s.zeros.from = bytes * p / passes / 16 * 16;
+        s.zeros.to = p + 1 < passes ? bytes * (p + 1) / passes / 16 * 16 : bytes;
+        s.zeros.groups = capped((s.zeros.to - s.zeros.from + 16 * kThreads - 1) / (16 * kThreads), 256);
+        s.n = a.n;
+        s.vocab = static_cast<uint32_t>(a.vocab);
+        s.tokens = a.tokens;
+        if (p > 0) s.tokens.p = nullptr;
+        s.keys = a.keys[out];
+        s.rows = a.rows[out];
+        out ^= 1;
+        s.keys_out = a.keys[out];
+        s.rows_out = a.rows[out];
+        s.shift = shift;
+        s.bits = plan.bits[p];
+        // the last digit ends with the largest key's
+        const uint32_t digits = a.n == 0 ? 0 : p + 1 < passes
+            ? 1u << s.bits : static_cast<uint32_t>(a.vocab >> shift) + 1;
+        hipLaunchKernelGGL(k_sort_pass, dim3(s.zeros.groups + digits), dim3(kThreads), 0, stream, s);
     }
+    if (a.n == 0) return hipGetLastError();
     EmbedSum m{};
     m.keys = a.keys[out];
     m.rows = a.rows[out];
@@ -339,24 +342,22 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
     m.vocab = a.vocab;
     m.width = a.width;
     m.chunk = embed_chunk(a.n);
-    m.partial = a.partial;
+    m.chunks = embed_chunks(a.n);
+    m.head = a.partial;
+    m.tail = a.partial + m.chunks * a.width;
     m.scale = a.scale;
     m.dtable = a.dtable;
-    m.lanes = row_lanes(a.width);
-    m.per = 8 * (256 / m.lanes);
-    if (a.n >= m.chunk) {
-        const int64_t slabs = (a.width + 511) / 512;
-        const dim3 grid(capped(a.n / m.chunk * slabs, 1 << 24));
-        if (dy_bf16) hipLaunchKernelGGL(k_embed_chunks<true>, grid, dim3(64), 0, stream, m, slabs);
-        else hipLaunchKernelGGL(k_embed_chunks<false>, grid, dim3(64), 0, stream, m, slabs);
+    const int64_t slabs = (a.width + 511) / 512;
+    const dim3 grid(capped(m.chunks * slabs, 1 << 24));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64), 0, stream, m, slabs); };
+    if (dy_bf16 && table_bf16) go(k_embed_chunks<true, true>);
+    else if (dy_bf16) go(k_embed_chunks<true, false>);
+    else if (table_bf16) go(k_embed_chunks<false, true>);
+    else go(k_embed_chunks<false, false>);
+    if (m.chunks > 1) {
+        if (table_bf16) go(k_embed_spans<true>);
+        else go(k_embed_spans<false>);
     }
-    const int64_t groups = (a.vocab + m.per - 1) / m.per;
-    const dim3 grid(capped(groups, 1 << 22));
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, m); };
-    if (dy_bf16 && table_bf16) go(k_embed_sum<true, true>);
-    else if (dy_bf16) go(k_embed_sum<true, false>);
-    else if (table_bf16) go(k_embed_sum<false, true>);
-    else go(k_embed_sum<false, false>);
     return hipGetLastError();
 }
 

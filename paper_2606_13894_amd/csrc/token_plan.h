@@ -29,8 +29,9 @@ inline SortPlan sort_plan(int64_t most)
     return s;
 }
 
-// Sorted positions are summed in aligned chunks where one token fills a whole chunk.
-inline int64_t embed_chunk(int64_t n) { return n <= 65536 ? 32 : 256; }
+// Sorted positions are summed in chunks.
+inline int64_t embed_chunk(int64_t n) { return n <= 65536 ? 16 : 256; }
+inline int64_t embed_chunks(int64_t n) { return ffn_ceil(n, embed_chunk(n)); }
 
 struct EmbedSpace {
     int64_t keys[2], rows[2], partial, bytes = 0;
@@ -47,7 +48,7 @@ inline EmbedSpace embed_space(int64_t n, int64_t width)
         s.keys[i] = take(4 * n);
         s.rows[i] = take(4 * n);
     }
-    s.partial = take(4 * (n / embed_chunk(n)) * width);
+    s.partial = take(8 * embed_chunks(n) * width);
     return s;
 }
 
