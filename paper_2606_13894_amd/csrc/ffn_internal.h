@@ -128,8 +128,10 @@ struct FfnTokens {
     int32_t act;
     uint16_t* o;
     int64_t ldo;
+    HeadRows head;               // launch_head_tokens alone, which writes no o
 };
 hipError_t launch_ffn_tokens(const FfnTokens& g, hipStream_t stream);
+hipError_t launch_head_tokens(const FfnTokens& g, hipStream_t stream);
 
 struct FfnPad {
     const uint16_t* src;

@@ -16,6 +16,7 @@
 // caches, so they are plain. A is rounded to bfloat16 as in ffn_gemm.hip.
 #include "act8_device.h"
 #include "ffn_internal.h"
+#include "token_device.h"
 
 namespace gefen {
 namespace {
@@ -29,16 +30,13 @@ __device__ __forceinline__ bf16x8 row_piece(const uint16_t* __restrict__ row, in
     return __builtin_bit_cast(bf16x8, load_vector<2>(row, k, n));
 }
 
-template <bool DUAL, int R, int W>
-__global__ __launch_bounds__(64 * W) void k_ffn_tokens(const FfnTokens g)
+// The wave's share of the sums of R rows of the weights from n0 on.
+template <int NM, int R, int W>
+__device__ __forceinline__ void sum_rows(const FfnTokens& g, int64_t n0, int wave, int lane,
+                                         f32x4 (&acc)[NM])
 {
-    constexpr int NM = DUAL ? 2 : 1;
     constexpr int D = R == 8 ? 64 : 32;      // k of a step
-    __shared__ f32x4 sums[W][NM][64];
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int q = lane >> 4, l16 = lane & 15;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * R;
     const int K = static_cast<int>(g.K);
     const int64_t row = min(n0 + l16 % R, g.N - 1);     // what is summed past N is not stored
     const int token = l16 % R, k0 = (R == 8 ? 4 * (l16 & 8) : 0) + 8 * q;
@@ -50,10 +48,9 @@ __global__ __launch_bounds__(64 * W) void k_ffn_tokens(const FfnTokens g)
     const int steps = (K + D - 1) / D;
     const int from = static_cast<int>(int64_t(steps) * wave / W);
     const int to = static_cast<int>(int64_t(steps) * (wave + 1) / W);
-    f32x4 acc[NM];
 #pragma unroll
     for (int m = 0; m < NM; ++m) acc[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int U = W == 16 && DUAL ? 4 : 8;          // steps whose loads go out together
+    constexpr int U = W == 16 && NM == 2 ? 4 : 8;       // steps whose loads go out together
     for (int s = from; s < to; s += U) {
         bf16x8 wv[U][NM], xv[U];
 #pragma unroll
@@ -70,21 +67,45 @@ __global__ __launch_bounds__(64 * W) void k_ffn_tokens(const FfnTokens g)
             for (int m = 0; m < NM; ++m)
                 acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[i][m], xv[i], acc[m], 0, 0, 0);
     }
+}
+
+// Lane l of the waves' sums holds elements n = 4 (l / 16) + 0..3 of token l % 16; with R = 8 the other
+// half of the sum of element n of token t is element 8 + n of token 8 + t, 40 lanes on.
+template <int R>
+__device__ __forceinline__ bool holds_sums(const FfnTokens& g, int lane)
+{
+    return (lane & 15) % R < g.tokens && !(R == 8 && (lane >= 32 || (lane & 8)));
+}
+template <int R, int W, int NM>
+__device__ __forceinline__ f32x4 all_waves(const f32x4 (&sums)[W][NM][64], int m, int lane)
+{
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int w = 0; w < W; ++w) {
+        v += sums[w][m][lane];
+        if (R == 8) v += sums[w][m][(lane + 40) & 63];
+    }
+    return v;
+}
+
+template <bool DUAL, int R, int W>
+__global__ __launch_bounds__(64 * W) void k_ffn_tokens(const FfnTokens g)
+{
+    constexpr int NM = DUAL ? 2 : 1;
+    __shared__ f32x4 sums[W][NM][64];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int q = lane >> 4, token = (lane & 15) % R;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * R;
+    f32x4 acc[NM];
+    sum_rows<NM, R, W>(g, n0, wave, lane, acc);
 #pragma unroll
     for (int m = 0; m < NM; ++m) sums[wave][m][lane] = acc[m];
     __syncthreads();
-    // Lane l holds elements n = 4 (l / 16) + 0..3 of token l % 16; with R = 8 the other half of
-    // the sum of element n of token t is element 8 + n of token 8 + t, 40 lanes on.
-    if (threadIdx.x >= 64 || token >= g.tokens || (R == 8 && (q >= 2 || l16 >= 8))) return;
+    if (threadIdx.x >= 64 || !holds_sums<R>(g, lane)) return;
     f32x4 v[NM];
 #pragma unroll
-    for (int m = 0; m < NM; ++m) {
-        v[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int w = 0; w < W; ++w) {
-            v[m] += sums[w][m][lane];
-            if (R == 8) v[m] += sums[w][m][lane + 40];
-        }
-    }
+    for (int m = 0; m < NM; ++m) v[m] = all_waves<R, W, NM>(sums, m, lane);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float r = v[0][i];
@@ -96,6 +117,56 @@ __global__ __launch_bounds__(64 * W) void k_ffn_tokens(const FfnTokens g)
         const int64_t n = n0 + 4 * q + i;
         if (n < g.N) g.o[token * g.ldo + n] = bf16_bits(r);
     }
+}
+
+// The output head's scores of a few tokens: each token's statistics over the workgroup's R rows of the
+// weight (ffn_internal.h), [token][3][workgroup]. One token, 128256 x 2048: 82 us (525 MB, 6.4 TB/s),
+// and 10 for the join of 16032 workgroups' statistics, which one workgroup reads at the rate of its CU
+// alone. More rows to a workgroup leave less to join and cost more: three times R one after the other
+// 90 + 7.5 us, two or four groups of waves with R each 98 + 7 and 110 + 6.5.
+template <int R, int W>
+__global__ __launch_bounds__(64 * W) void k_head_tokens(const FfnTokens g)
+{
+    __shared__ f32x4 sums[W][1][64];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int q = lane >> 4, token = (lane & 15) % R;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * R;
+    f32x4 acc[1];
+    sum_rows<1, R, W>(g, n0, wave, lane, acc);
+    sums[wave][0][lane] = acc[0];
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    const bool on = holds_sums<R>(g, lane);
+    const f32x4 v = all_waves<R, W, 1>(sums, 0, lane);
+    float z[4], m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        z[i] = on && n0 + 4 * q + i < g.N ? v[i] : -INFINITY;
+        m = fmaxf(m, z[i]);
+    }
+    // a token's four lanes (two, with R = 8) join; the others hold -inf
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const ScoreBase base = score_base(m);
+    float s = 0.0f, t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) score_add(z[i], base, s, t);
+    s += __shfl_xor(s, 16);
+    t += __shfl_xor(t, 16);
+    s += __shfl_xor(s, 32);
+    t += __shfl_xor(t, 32);
+    if (!on) return;
+    if (q == 0) {
+        float* __restrict__ o = g.head.stats + (int64_t(token) * 3 * gridDim.x + blockIdx.x);
+        o[0] = m;
+        o[gridDim.x] = s;
+        o[2 * int64_t(gridDim.x)] = t;
+    }
+    const int64_t at = token_at(g.head.tokens, g.head.wide, token) - n0 - 4 * q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (at == i && n0 + 4 * q + i < g.N) g.head.taken[token] = v[i];
 }
 
 template <bool DUAL, int R>
@@ -112,6 +183,20 @@ hipError_t launch_waves(const FfnTokens& g, hipStream_t stream)
     return hipGetLastError();
 }
 
+template <int R>
+hipError_t launch_head(const FfnTokens& g, hipStream_t stream)
+{
+    const int waves = ffn_token_waves(g.N, g.K, R);
+    const dim3 grid(static_cast<unsigned>(ffn_ceil(g.N, R)));
+    if (waves == 4)
+        hipLaunchKernelGGL((k_head_tokens<R, 4>), grid, dim3(256), 0, stream, g);
+    else if (waves == 8)
+        hipLaunchKernelGGL((k_head_tokens<R, 8>), grid, dim3(512), 0, stream, g);
+    else
+        hipLaunchKernelGGL((k_head_tokens<R, 16>), grid, dim3(1024), 0, stream, g);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_ffn_tokens(const FfnTokens& g, hipStream_t stream)
@@ -120,6 +205,12 @@ hipError_t launch_ffn_tokens(const FfnTokens& g, hipStream_t stream)
     if (ffn_token_rows(g.tokens) == 8)
         return g.w[1] ? launch_waves<true, 8>(g, stream) : launch_waves<false, 8>(g, stream);
     return g.w[1] ? launch_waves<true, 16>(g, stream) : launch_waves<false, 16>(g, stream);
+}
+
+hipError_t launch_head_tokens(const FfnTokens& g, hipStream_t stream)
+{
+    if (g.tokens < 1 || g.tokens > kFfnFewTokens) return hipErrorInvalidValue;
+    return ffn_token_rows(g.tokens) == 8 ? launch_head<8>(g, stream) : launch_head<16>(g, stream);
 }
 
 }  // namespace gefen

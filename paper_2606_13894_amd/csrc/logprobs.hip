@@ -7,11 +7,11 @@
 // rows are few, workgroups that share a row are joined in a fixed order.
 //
 // Best alternatives, by value and among equals by the lower index: a lane also keeps where its
-// largest score first stood. Its k lanes with the largest ones hold k scores at least as large as
-// the k-th of them, so only their vectors, a k-th of a row by the number of lanes, are read again, and the
-// few scores that reach that one are ranked by counting. (They go to a list in LDS; where it does
-// not hold them, the k best are taken one by one.) A score and its place are one 64-bit key, the
-// place inverted, so that no two are equal and no order of arrival counts.
+// largest score first stood. The lanes are 64 groups, and the k-th largest of the groups' largest scores
+// is reached by k scores at least: only the vectors of lanes that reach it are read again, and
+// the few scores that do are ranked by counting. (They go to a list in LDS; where it does not hold
+// them, the k best are taken one by one.) A score and its place are one 64-bit key, the place
+// inverted, so that no two are equal and no order of arrival counts.
 //
 // Gradients: dz_j = g ([j = token] - p_j) - h p_j (log p_j + H), p_j = exp(z_j - lse), elementwise.
 #include "token_internal.h"
@@ -23,8 +23,6 @@
 namespace gefen {
 namespace {
 
-constexpr int L = kScoreThreads;
-constexpr int kWaves = L / 64;
 constexpr int kList = 1024;              // keys of a row that LDS holds beside the lanes'
 
 // Scores order as these do; -0 is 0.
@@ -67,25 +65,48 @@ struct Vec {
     }
 };
 
+// The sums of the lanes that are FROM apart: the largest m first, so that each lane moves its sums to
+// that base once.
+template <int FROM = 1>
 __device__ __forceinline__ ScoreSum wave_join(ScoreSum a)
 {
+    float m = a.m;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        ScoreSum b;
-        b.m = __shfl_xor(a.m, d);
-        b.s = __shfl_xor(a.s, d);
-        b.t = __shfl_xor(a.t, d);
-        a = score_join(a, b);
+    for (int d = FROM; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    score_rebase(a.m, score_base(m), a.s, a.t);
+    a.m = m;
+#pragma unroll
+    for (int d = FROM; d < 64; d *= 2) {
+        a.s += __shfl_xor(a.s, d);
+        a.t += __shfl_xor(a.t, d);
     }
     return a;
 }
 
+// Several of a lane's, in order, the same way.
+template <int U>
+__device__ __forceinline__ void join_all(ScoreSum& a, ScoreSum (&v)[U])
+{
+    float m = a.m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = fmaxf(m, v[u].m);
+    const ScoreBase base = score_base(m);
+    score_rebase(a.m, base, a.s, a.t);
+    a.m = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        score_rebase(v[u].m, base, v[u].s, v[u].t);
+        a.s += v[u].s;
+        a.t += v[u].t;
+    }
+}
+
+template <int L>
 struct ListSpace {
-    uint64_t lane_keys[L];
+    uint64_t groups[64];
     uint64_t list[kList];
-    uint64_t best[kWaves];
-    uint64_t least;
-    int lanes[kScoreMaxTop];
+    uint64_t best[L / 64];
+    int lanes[L];
     int found, count;
 };
 
@@ -98,17 +119,14 @@ __device__ __forceinline__ int count_above(const uint64_t* keys, int n, uint64_t
     return above;
 }
 
-// A bound that exactly k of the distinct keys that the lanes of a wave hold reach, bit by bit
-// from the top; 0 where they are fewer than k (keys of 0 are none).
-template <int M>
-__device__ __forceinline__ uint64_t least_of_top(const uint64_t (&key)[M], int k)
+// A bound that exactly k of the distinct keys that a wave's lanes hold reach, bit by bit from the
+// top; 0 where they are fewer than k (keys of 0 are none).
+__device__ __forceinline__ uint64_t least_of_top(uint64_t key, int k)
 {
     uint64_t least = 0;
     for (int bit = 63; bit >= 0; --bit) {
         const uint64_t with = least | (uint64_t(1) << bit);
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < M; ++i) n += __popcll(__ballot(key[i] >= with));
+        const int n = __popcll(__ballot(key >= with));
         if (n >= k) least = with;
         if (n == k) break;
     }
@@ -117,26 +135,25 @@ __device__ __forceinline__ uint64_t least_of_top(const uint64_t (&key)[M], int k
 
 // The k largest keys of vectors v0 .. v1 - 1 of a row, in order, to out; 0 where there are fewer.
 // `key`: of the lane's largest score, its place that vector's number; 0 where it has read none.
-template <bool BF16>
+template <bool BF16, int L>
 __device__ void select_top(const void* row, int n, int v0, int v1, int k, uint64_t key,
-                           ListSpace& s, uint64_t* __restrict__ out)
+                           ListSpace<L>& s, uint64_t* __restrict__ out)
 {
-    constexpr int N = Vec<BF16>::N;
+    constexpr int N = Vec<BF16>::N, kWaves = L / 64;
     const int tid = threadIdx.x;
     n = by_lane(n);
-    s.lane_keys[tid] = key;
+    constexpr int kGroup = L / 64;
+    uint64_t group = key;
+#pragma unroll
+    for (int d = 1; d < kGroup; d *= 2) {
+        const uint64_t other = __shfl_xor(static_cast<unsigned long long>(group), d);
+        group = other > group ? other : group;
+    }
+    if (tid % kGroup == 0) s.groups[tid / kGroup] = group;
     if (tid == 0) s.found = s.count = 0;
     __syncthreads();
-    if (tid < 64) {
-        uint64_t some[kWaves];
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) some[w] = s.lane_keys[64 * w + tid];
-        const uint64_t least = least_of_top(some, k);
-        if (tid == 0) s.least = least;
-    }
-    __syncthreads();
-    const uint64_t least = s.least;
-    if (key && key >= least) s.lanes[atomicAdd(&s.found, 1)] = tid;   // k of them at most
+    const uint64_t least = least_of_top(s.groups[tid & 63], k);
+    if (key && key >= least) s.lanes[atomicAdd(&s.found, 1)] = tid;
     __syncthreads();
     const int per = (v1 - v0 + L - 1) / L;
     for (int i = tid; i < s.found * per; i += L) {
@@ -216,13 +233,13 @@ __device__ __forceinline__ float score_at(const void* z, int64_t i)
     else return static_cast<const float*>(z)[i];
 }
 
-template <bool BF16, bool TOP>
+template <bool BF16, bool TOP, int L>
 __global__ __launch_bounds__(L) void k_scores(const ScoreArgs a)
 {
     using V = Vec<BF16>;
-    constexpr int N = V::N, U = 4, S = BF16 ? 2 : 4;
+    constexpr int N = V::N, U = 4, S = BF16 ? 2 : 4, kWaves = L / 64;
     __shared__ ScoreSum sums[kWaves];
-    __shared__ typename std::conditional<TOP, ListSpace, int>::type list;
+    __shared__ typename std::conditional<TOP, ListSpace<L>, int>::type list;
     __shared__ uint64_t best[TOP ? kScoreMaxTop : 1];
     const int tid = threadIdx.x;
     const int vocab = static_cast<int>(a.vocab);
@@ -309,13 +326,12 @@ __global__ __launch_bounds__(L) void k_scores(const ScoreArgs a)
         c = wave_join(c);
         if ((tid & 63) == 0) sums[tid >> 6] = c;
         __syncthreads();
-        c = sums[0];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) c = score_join(c, sums[w]);
+        c = tid % 64 < kWaves ? sums[tid % 64] : ScoreSum{-INFINITY, 0.0f, 0.0f};
+        c = wave_join(c);
         if constexpr (TOP) {
             // (a NaN as the largest of a vector ends in a row whose alternatives are not given)
             const uint64_t key = place >= 0 ? score_key(top, place) : 0;
-            select_top<BF16>(row, vocab, v0, v1, a.top, key, list, best);
+            select_top<BF16, L>(row, vocab, v0, v1, a.top, key, list, best);
             if (tid < a.top) {
                 if (one) write_top(a, r, c, tid, best[tid]);
                 else a.keys[item * a.top + tid] = best[tid];
@@ -360,7 +376,7 @@ __global__ __launch_bounds__(64) void k_scores_join(const ScoreArgs a)
             for (int i = lane; i < n; i += 64) keys[i] = a.keys[r * n + i];
             __syncthreads();
             // no key below the k-th largest of the parts' largest ones is among the k largest
-            const uint64_t first[1] = {lane < parts ? keys[lane * a.top] : 0};
+            const uint64_t first = lane < parts ? keys[lane * a.top] : 0;
             const uint64_t least = max(least_of_top(first, a.top), uint64_t(1));
             int count = 0;
             for (int i = 0; i < n; i += 64) {
@@ -413,38 +429,40 @@ __global__ __launch_bounds__(256) void k_score_grad(const ScoreGradArgs a, int64
 }
 
 // ---------------------------------------------------------------- output head
-// A workgroup joins 16 rows, 64 lanes to a row by the slots, four of a lane's on their way at once.
-constexpr int kJoinRows = 16, kJoinWays = 64;
-
-__global__ __launch_bounds__(kJoinRows * kJoinWays) void k_head_join(const HeadJoinArgs a)
+// A workgroup joins R rows, 1024 / R lanes to a row by the slots, U of a lane's on their way at once.
+// R = 1: statistics that lie by rows.
+template <int R, int U>
+__global__ __launch_bounds__(1024) void k_head_join(const HeadJoinArgs a)
 {
-    __shared__ ScoreSum sums[kJoinWays][kJoinRows];
-    const int in = threadIdx.x % kJoinRows, way = threadIdx.x / kJoinRows;
-    const int64_t r = int64_t(blockIdx.x) * kJoinRows + in;
+    constexpr int kWays = 1024 / R, kWaves = 16;
+    __shared__ ScoreSum sums[kWaves][R];
+    const int in = threadIdx.x % R, way = threadIdx.x / R, wave = threadIdx.x >> 6;
+    const int64_t r = int64_t(blockIdx.x) * R + in;
+    const int64_t row = min(r, a.rows - 1);
     ScoreSum c = {-INFINITY, 0.0f, 0.0f};
-    if (r < a.rows)
-        for (int64_t s = way; s < a.slots; s += 4 * kJoinWays) {
-            ScoreSum v[4];
+    for (int64_t s = 0; s < a.slots; s += U * kWays) {
+        ScoreSum v[U];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int64_t at = min(s + u * kJoinWays, a.slots - 1);
-                const float* p = a.stats + at * 3 * a.rows + r;
-                v[u] = ScoreSum{p[0], p[a.rows], p[2 * a.rows]};
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (s + u * kJoinWays < a.slots) c = score_join(c, v[u]);
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = min(s + u * kWays + way, a.slots - 1);
+            const float* p = a.stats + (R == 1 ? 3 * row * a.slots + at : 3 * at * a.rows + row);
+            const int64_t next = R == 1 ? a.slots : a.rows;
+            v[u] = ScoreSum{p[0], p[next], p[2 * next]};
         }
-    sums[way][in] = c;
 #pragma unroll
-    for (int half = kJoinWays / 2; half > 0; half /= 2) {
-        __syncthreads();
-        if (way < half) {
-            c = score_join(c, sums[way + half][in]);
-            sums[way][in] = c;
-        }
+        for (int u = 0; u < U; ++u)
+            if (s + u * kWays + way >= a.slots) v[u] = ScoreSum{-INFINITY, 0.0f, 0.0f};
+        join_all(c, v);
     }
-    if (way > 0 || r >= a.rows) return;
+    c = wave_join<R>(c);
+    if ((threadIdx.x & 63) < R) sums[wave][in] = c;
+    __syncthreads();
+    if (threadIdx.x >= R || r >= a.rows) return;
+    ScoreSum v[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) v[w] = sums[w][in];
+    c = ScoreSum{-INFINITY, 0.0f, 0.0f};
+    join_all(c, v);
     const int64_t token = token_at(a.tokens.p, a.tokens.wide, r);
     const float taken = token >= 0 && token < a.vocab ? a.taken[r] : 0.0f;
     const ScoreRow o = score_row(c, token, a.vocab, taken);
@@ -460,11 +478,17 @@ hipError_t launch_scores(const ScoreArgs& a, bool bf16, hipStream_t stream)
     if (a.rows == 0) return hipSuccess;
     const int64_t items = a.rows * a.plan.parts;
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>(items, 1 << 20)));
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(L), 0, stream, a); };
-    if (bf16 && a.top) go(k_scores<true, true>);
-    else if (bf16) go(k_scores<true, false>);
-    else if (a.top) go(k_scores<false, true>);
-    else go(k_scores<false, false>);
+    auto go = [&](auto few, auto many) {
+        if (a.plan.threads == kScoreThreads)
+            hipLaunchKernelGGL(many, grid, dim3(kScoreThreads), 0, stream, a);
+        else
+            hipLaunchKernelGGL(few, grid, dim3(kScoreFewThreads), 0, stream, a);
+    };
+    constexpr int F = kScoreFewThreads, M = kScoreThreads;
+    if (bf16 && a.top) go(k_scores<true, true, F>, k_scores<true, true, M>);
+    else if (bf16) go(k_scores<true, false, F>, k_scores<true, false, M>);
+    else if (a.top) go(k_scores<false, true, F>, k_scores<false, true, M>);
+    else go(k_scores<false, false, F>, k_scores<false, false, M>);
     if (a.plan.parts > 1) {
         const dim3 rows(static_cast<unsigned>(std::min<int64_t>(a.rows, 1 << 20)));
         if (bf16) hipLaunchKernelGGL(k_scores_join<true>, rows, dim3(64), 0, stream, a);
@@ -485,10 +509,13 @@ hipError_t launch_score_grad(const ScoreGradArgs& a, bool bf16, hipStream_t stre
 
 hipError_t launch_head_join(const HeadJoinArgs& a, hipStream_t stream)
 {
-    const int64_t groups = (a.rows + kJoinRows - 1) / kJoinRows;
-    if (groups == 0) return hipSuccess;
-    hipLaunchKernelGGL(k_head_join, dim3(static_cast<unsigned>(groups)), dim3(kJoinRows * kJoinWays),
-                       0, stream, a);
+    if (a.rows == 0) return hipSuccess;
+    if (a.by_rows)
+        hipLaunchKernelGGL((k_head_join<1, 16>), dim3(static_cast<unsigned>(a.rows)), dim3(1024), 0,
+                           stream, a);
+    else
+        hipLaunchKernelGGL((k_head_join<16, 4>), dim3(static_cast<unsigned>((a.rows + 15) / 16)),
+                           dim3(1024), 0, stream, a);
     return hipGetLastError();
 }
 

@@ -266,26 +266,42 @@ int gefen_head_logprobs(const uint16_t* x, const uint16_t* weight, const void* t
     const bool copy = K % 8 || !aligned16(x) || !aligned16(weight);
     const HeadSpace s = head_space(T, K, V, false, copy);
     if ((rc = check_space(workspace, workspace_bytes, s.bytes))) return rc;
+    HeadRows rows{};
+    rows.tokens = tokens;
+    rows.wide = token_bytes == 8;
+    rows.stats = at<float>(workspace, s.stats);
+    rows.taken = at<float>(workspace, s.taken);
+    HeadJoinArgs j{};
+    j.stats = rows.stats;
+    j.by_rows = head_few(T, copy);
+    j.taken = rows.taken;
+    j.tokens = Tokens{tokens, token_bytes == 8};
+    j.rows = T;
+    j.vocab = V;
+    j.slots = s.slots;
+    j.logprob = logprob;
+    j.entropy = entropy;
+    j.lse = lse;
+    if (head_few(T, copy)) {
+        FfnTokens t{};
+        t.x = x;
+        t.ldx = K;
+        t.w[0] = weight;
+        t.tokens = T;
+        t.N = V;
+        t.K = K;
+        t.head = rows;
+        GEFEN_HIP(launch_head_tokens(t, stream));
+        GEFEN_HIP(launch_head_join(j, stream));
+        return GEFEN_OK;
+    }
     FfnPads pads{};
     FfnGemm z = product(kHeadStats, s.score, T, V, K, workspace, -1);
     z.a[0] = operand(x, T, K, copy, workspace, s.x, pads);
     z.b[0] = operand(weight, V, K, copy, workspace, s.w, pads);
     z.lda = z.ldb = ffn_up8(K);
-    z.head.tokens = tokens;
-    z.head.wide = token_bytes == 8;
-    z.head.stats = at<float>(workspace, s.stats);
-    z.head.taken = at<float>(workspace, s.taken);
+    z.head = rows;
     if ((rc = check_launch(z))) return rc;
-    HeadJoinArgs j{};
-    j.stats = z.head.stats;
-    j.taken = z.head.taken;
-    j.tokens = Tokens{tokens, token_bytes == 8};
-    j.rows = T;
-    j.vocab = V;
-    j.slots = head_slots(s.score.tile, V);
-    j.logprob = logprob;
-    j.entropy = entropy;
-    j.lse = lse;
     GEFEN_HIP(launch_ffn_pads(pads, stream));
     GEFEN_HIP(launch_ffn_parts(z, stream));
     GEFEN_HIP(launch_head_join(j, stream));
@@ -316,8 +332,6 @@ int gefen_head_logprobs_backward(const uint16_t* x, const uint16_t* weight, cons
     FfnPads pads{};
     const uint16_t* xp = operand(x, T, K, copy, workspace, s.x, pads);
     const uint16_t* wp = operand(weight, V, K, copy, workspace, s.w, pads);
-    const int64_t parts_x = s.chunks > 1 ? 4 * T * K * s.dx.splits
-                                         : ffn_partial_bytes(s.dx, T, K, 1);
 
     // Over the vocabulary from entry `first` on: the scores again and their gradients, and the two
     // products that read them. dx is summed over the ranges in float32.
@@ -330,6 +344,7 @@ int gefen_head_logprobs_backward(const uint16_t* x, const uint16_t* weight, cons
             z.b[0] = wp + first * K8;
             z.lda = z.ldb = K8;
             z.o[0] = at<uint16_t>(workspace, s.dz);
+            z.o[1] = s.exact ? z.o[0] + T * s.ldz : nullptr;
             z.ldo = s.ldz;
             z.head.tokens = tokens;
             z.head.wide = token_bytes == 8;
@@ -339,7 +354,8 @@ int gefen_head_logprobs_backward(const uint16_t* x, const uint16_t* weight, cons
             z.head.dlogprob = dlogprob;
             z.head.dentropy = dentropy;
 
-            FfnGemm gx = product(kFfnPlain, s.dx, T, K, C, workspace, s.partial);   // dz W
+            FfnGemm gx = product(kFfnPlain, s.dx, s.exact ? 2 * T : T, K, C, workspace,
+                                 s.partial);                                    // dz W
             gx.stages = static_cast<int32_t>(ffn_ceil(C, kFfnDepth));
             gx.b_rows_k = true;
             gx.a[0] = z.o[0];
@@ -348,24 +364,29 @@ int gefen_head_logprobs_backward(const uint16_t* x, const uint16_t* weight, cons
             gx.ldb = K8;
             gx.o[0] = dx;
             gx.ldo = K;
-            if (s.chunks > 1) gx.partial = at<float>(workspace, s.partial);
+            if (s.planes_x) gx.partial = at<float>(workspace, s.partial);
             gx.add = first > 0;
+            FfnGemm sum = gx;                     // both halves of dz are rows of gx
+            sum.M = T;
+            sum.splits = static_cast<int32_t>(s.planes_x);
 
-            FfnGemm gw = product(kFfnPlain, s.dw, C, K, T, workspace, s.partial + parts_x);
-            gw.a[0] = z.o[0];                                                       // dz^T x
+            FfnGemm gw = product(kFfnPlain, s.dw, C, K, T, workspace, s.partial + s.partial_w);
+            gw.a[0] = z.o[0];                                                   // dz^T x
+            gw.a[1] = z.o[1];
             gw.lda = s.ldz;
-            gw.b[0] = xp;
+            gw.b[0] = gw.b[1] = xp;
+            gw.segments = s.exact ? 2 : 1;
             gw.ldb = K8;
             gw.o[0] = dweight + first * K;
             gw.ldo = K;
             if (pass == 0) {
-                if ((rc = check_launch(z)) || (rc = check_launch(gx)) || (rc = check_launch(gw)))
+                if ((rc = check_launch(z)) || (rc = check_launch(gx)) || (rc = check_launch(sum)) || (rc = check_launch(gw)))
                     return rc;
                 continue;
             }
             GEFEN_HIP(launch_ffn_parts(z, stream));
             GEFEN_HIP(launch_ffn_parts(gx, stream));
-            if (first + C == V) GEFEN_HIP(launch_ffn_join(gx, stream));
+            if (first + C == V) GEFEN_HIP(launch_ffn_join(sum, stream));
             GEFEN_HIP(launch_ffn_weight_grad(gw, stream));
         }
     }

@@ -83,9 +83,11 @@ struct ScoreGradArgs {
 };
 hipError_t launch_score_grad(const ScoreGradArgs& a, bool bf16, hipStream_t stream);
 
-// The head's rows from the statistics of its tiles (HeadRows::stats, `slots` of them).
+// The head's rows from the statistics of its tiles or workgroups: `slots` of them, each three numbers
+// (HeadRows::stats), which lie [slots][3][rows], or by rows: [rows][3][slots].
 struct HeadJoinArgs {
     const float* stats;
+    bool by_rows;
     const float* taken;
     Tokens tokens;
     int64_t rows, vocab, slots;

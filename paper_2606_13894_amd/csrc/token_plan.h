@@ -55,19 +55,23 @@ inline EmbedSpace embed_space(int64_t n, int64_t width)
 // ---------------------------------------------------------------- log probabilities
 constexpr int64_t kScoreMaxTop = 32;
 constexpr int64_t kScoreMaxParts = 64;
-constexpr int kScoreThreads = 256;
+constexpr int kScoreThreads = 256, kScoreFewThreads = 1024;
+constexpr int64_t kScorePart = 2048;      // 16-byte vectors, at least: 32 KiB of a row
 
 // A row is taken by `parts` workgroups, each `per` vectors of 16 bytes of it.
 struct ScorePlan {
     int64_t parts = 1;
     int64_t per = 0;
+    int threads = kScoreThreads;
 };
 inline ScorePlan score_plan(int64_t rows, int64_t vocab, bool bf16)
 {
     const int64_t vectors = ffn_ceil(vocab, bf16 ? 8 : 4);
     ScorePlan p;
-    const int64_t most = std::min(kScoreMaxParts, ffn_ceil(vectors, 2 * kScoreThreads));
-    p.parts = std::max<int64_t>(1, std::min(most, ffn_ceil(1024, std::max<int64_t>(rows, 1))));
+    // few rows are cut into parts, and taken by workgroups of 1024 threads
+    if (rows <= 512) p.threads = kScoreFewThreads;
+    const int64_t most = std::min(kScoreMaxParts, ffn_ceil(vectors, kScorePart));
+    p.parts = std::max<int64_t>(1, std::min(most, 256 / std::max<int64_t>(rows, 1)));
     p.per = ffn_ceil(vectors, p.parts);
     p.parts = ffn_ceil(vectors, p.per);
     return p;
@@ -98,13 +102,24 @@ inline int64_t head_slots(int32_t tile, int64_t vocab)
 // (or 256 columns), and of rows whose tiles stay within 32-bit offsets.
 constexpr int64_t kHeadGradBytes = int64_t(1) << 30;
 
+// Up to this many tokens the scores' gradients are two bfloat16 numbers each, the rounded one and what
+// rounding left of it, and the products that read them take both.
+constexpr int64_t kHeadExactTokens = 256;
+
+// Whether the forward pass takes the few-token kernel.
+inline bool head_few(int64_t T, bool copy) { return T <= 8 || (copy && T <= kFfnFewTokens); }
+
 struct HeadSpace {
     int64_t x = -1, w = -1;            // padded copies
     int64_t stats = -1, taken = -1;    // forward
+    int64_t slots = 0;
     int64_t dz = -1, partial = -1;     // backward
     int64_t bytes = 0;
     int64_t columns = 0, chunks = 1;   // of the vocabulary, in the backward pass
     int64_t ldz = 0;
+    bool exact = false;
+    int64_t planes_x = 0;              // float32 sums of dx
+    int64_t partial_w = 0;             // where dweight's parts begin behind them
     FfnTile score, dx, dw;
 };
 
@@ -118,6 +133,12 @@ inline HeadSpace head_space(int64_t T, int64_t K, int64_t V, bool backward, bool
         return at;
     };
     const int64_t K8 = ffn_up8(K);
+    if (!backward && head_few(T, copy)) {   // a slot for each workgroup of the few-token kernel
+        s.slots = ffn_ceil(V, ffn_token_rows(T));
+        s.stats = take(12 * T * s.slots);
+        s.taken = take(4 * T);
+        return s;
+    }
     if (copy) {
         s.x = take(2 * T * K8);
         s.w = take(2 * V * K8);
@@ -125,7 +146,8 @@ inline HeadSpace head_space(int64_t T, int64_t K, int64_t V, bool backward, bool
     if (!backward) {
         const FfnResult z = {T, V, 1};
         s.score = ffn_choose(&z, 1, K, 1, false, false, kFfnActivate);
-        s.stats = take(12 * T * head_slots(s.score.tile, V));
+        s.slots = head_slots(s.score.tile, V);
+        s.stats = take(12 * T * s.slots);
         s.taken = take(4 * T);
         return s;
     }
@@ -137,17 +159,17 @@ inline HeadSpace head_space(int64_t T, int64_t K, int64_t V, bool backward, bool
         s.chunks = ffn_ceil(V, s.columns);
     }
     s.ldz = ffn_up8(s.columns);
-    s.dz = take(2 * T * s.ldz);
-    const FfnResult z = {T, s.columns, 1}, dx = {T, K, 1}, dw = {s.columns, K, 1};
+    s.exact = T <= kHeadExactTokens;
+    const int halves = s.exact ? 2 : 1;
+    s.dz = take(2 * halves * T * s.ldz);
+    const FfnResult z = {T, s.columns, 1}, dx = {halves * T, K, 1}, dw = {s.columns, K, 1};
     s.score = ffn_choose(&z, 1, K, 1, false, false, kFfnActivate);
     s.dx = ffn_choose(&dx, 1, s.columns, 1, false, true, kFfnStore);
-    s.dw = ffn_choose(&dw, 1, T, 1, false, true, kFfnStore);
-    // the sums over the ranges are kept in float32; dx's and dw's parts are not there at once but
-    // where there are ranges
-    const int64_t parts_x = s.chunks > 1 ? 4 * T * K * s.dx.splits
-                                         : ffn_partial_bytes(s.dx, T, K, 1);
-    const int64_t parts_w = ffn_partial_bytes(s.dw, s.columns, K, 1);
-    const int64_t partial = parts_x + parts_w;
+    s.dw = ffn_choose(&dw, 1, T, halves, false, true, kFfnStore);
+    // dx of the halves, and of ranges, is summed in float32
+    s.planes_x = s.chunks > 1 || s.exact || s.dx.splits > 1 ? halves * s.dx.splits : 0;
+    s.partial_w = 4 * T * K * s.planes_x;
+    const int64_t partial = s.partial_w + ffn_partial_bytes(s.dw, s.columns, K, 1);
     if (partial) s.partial = take(partial);
     return s;
 }

@@ -277,7 +277,7 @@ def _check_rows(r, want, top=0):
 @pytest.mark.parametrize("rows,vocab,top", [
     (1, 1, 1), (1, 7, 7), (2, 8, 3), (3, 33, 32), (5, 100, 0), (1, 5000, 20), (7, 2048, 5),
     (1, 128_256, 20), (3, 128_256, 32), (1500, 1003, 4), (1100, 50257, 1), (64, 50257, 8),
-    (2000, 64, 32), (0, 9, 2)])
+    (2000, 64, 32), (0, 9, 2), (2, 1_000_003, 20), (600, 270_000, 3)])
 def test_token_logprobs(dev, rows, vocab, top, dtype):
     z = _randn(dev, rows, vocab, seed=1).mul_(3).to(DTYPES[dtype])
     t = _randint(dev, -1, vocab + 1, rows, seed=2)

@@ -88,14 +88,14 @@ def test_token_logprobs_refusals(lib):
     _said(lib, space(0, 1, 10, 11, n), -1, "top")
     _said(lib, space(0, 1, 100, 33, n), -1, "top")
     _said(lib, space(0, 1, 100, 5, None), -1, "NULL")
-    assert space(0, 1, 100_000, 5, n) == 0 and n.value > 0
+    assert space(0, 1, 1_000_000, 5, n) == 0 and n.value > 0
 
-    def call(z=P, ld=100_000, d=0, rows=1, vocab=100_000, t=P, tb=8, top=5, lp=P, e=P, l=P, b=P,
+    def call(z=P, ld=1_000_000, d=0, rows=1, vocab=1_000_000, t=P, tb=8, top=5, lp=P, e=P, l=P, b=P,
              w=P, ws=P, nb=n.value):
         return lib.gefen_token_logprobs(z, ld, d, rows, vocab, t, tb, top, lp, e, l, b, w, ws, nb,
                                         None)
     _said(lib, call(d=3), -2, "dtype")
-    _said(lib, call(ld=99_999), -1, "overlap")
+    _said(lib, call(ld=999_999), -1, "overlap")
     _said(lib, call(rows=1 << 30), -1, "2^40")
     _said(lib, call(tb=3), -1, "token_bytes")
     _said(lib, call(top=-1), -1, "top")
