@@ -106,6 +106,7 @@ struct ListSpace {
     uint64_t groups[64];
     uint64_t list[kList];
     uint64_t best[L / 64];
+    uint64_t least;
     int lanes[L];
     int found, count;
 };
@@ -119,7 +120,7 @@ __device__ __forceinline__ int count_above(const uint64_t* keys, int n, uint64_t
     return above;
 }
 
-// A bound that exactly k of the distinct keys that a wave's lanes hold reach, bit by bit from the
+// A bound that k of the distinct keys that a wave's lanes hold reach, and few more, bit by bit from the
 // top; 0 where they are fewer than k (keys of 0 are none).
 __device__ __forceinline__ uint64_t least_of_top(uint64_t key, int k)
 {
@@ -127,8 +128,10 @@ __device__ __forceinline__ uint64_t least_of_top(uint64_t key, int k)
     for (int bit = 63; bit >= 0; --bit) {
         const uint64_t with = least | (uint64_t(1) << bit);
         const int n = __popcll(__ballot(key >= with));
-        if (n >= k) least = with;
-        if (n == k) break;
+        if (n >= k) {
+            least = with;
+            if (n <= k + k / 2 + 2) break;
+        }
     }
     return least;
 }
@@ -152,7 +155,12 @@ __device__ void select_top(const void* row, int n, int v0, int v1, int k, uint64
     if (tid % kGroup == 0) s.groups[tid / kGroup] = group;
     if (tid == 0) s.found = s.count = 0;
     __syncthreads();
-    const uint64_t least = least_of_top(s.groups[tid & 63], k);
+    if (tid < 64) {
+        const uint64_t of_groups = least_of_top(s.groups[tid], k);
+        if (tid == 0) s.least = of_groups;
+    }
+    __syncthreads();
+    const uint64_t least = s.least;
     if (key && key >= least) s.lanes[atomicAdd(&s.found, 1)] = tid;
     __syncthreads();
     const int per = (v1 - v0 + L - 1) / L;

@@ -273,7 +273,7 @@ int gefen_head_logprobs(const uint16_t* x, const uint16_t* weight, const void* t
     rows.taken = at<float>(workspace, s.taken);
     HeadJoinArgs j{};
     j.stats = rows.stats;
-    j.by_rows = head_few(T, copy);
+    j.by_rows = head_few(T, K, V, copy);
     j.taken = rows.taken;
     j.tokens = Tokens{tokens, token_bytes == 8};
     j.rows = T;
@@ -282,7 +282,7 @@ int gefen_head_logprobs(const uint16_t* x, const uint16_t* weight, const void* t
     j.logprob = logprob;
     j.entropy = entropy;
     j.lse = lse;
-    if (head_few(T, copy)) {
+    if (head_few(T, K, V, copy)) {
         FfnTokens t{};
         t.x = x;
         t.ldx = K;

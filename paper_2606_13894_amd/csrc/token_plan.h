@@ -56,7 +56,7 @@ inline EmbedSpace embed_space(int64_t n, int64_t width)
 constexpr int64_t kScoreMaxTop = 32;
 constexpr int64_t kScoreMaxParts = 64;
 constexpr int kScoreThreads = 256, kScoreFewThreads = 1024;
-constexpr int64_t kScorePart = 2048;      // 16-byte vectors, at least: 32 KiB of a row
+constexpr int64_t kScorePart = 1 << 15;   // 16-byte vectors: 512 KiB of a row
 
 // A row is taken by `parts` workgroups, each `per` vectors of 16 bytes of it.
 struct ScorePlan {
@@ -68,10 +68,12 @@ inline ScorePlan score_plan(int64_t rows, int64_t vocab, bool bf16)
 {
     const int64_t vectors = ffn_ceil(vocab, bf16 ? 8 : 4);
     ScorePlan p;
-    // few rows are cut into parts, and taken by workgroups of 1024 threads
+    // Few rows are taken by workgroups of 1024 threads each, and cut into parts only where they are
+    // longer than vocabularies are: one row of 128256 takes 15 us so, and 17 + 8 us by 8 or 31
+    // parts and a second launch that joins them.
     if (rows <= 512) p.threads = kScoreFewThreads;
     const int64_t most = std::min(kScoreMaxParts, ffn_ceil(vectors, kScorePart));
-    p.parts = std::max<int64_t>(1, std::min(most, 256 / std::max<int64_t>(rows, 1)));
+    p.parts = std::max<int64_t>(1, std::min(most, 1024 / std::max<int64_t>(rows, 1)));
     p.per = ffn_ceil(vectors, p.parts);
     p.parts = ffn_ceil(vectors, p.per);
     return p;
@@ -106,8 +108,17 @@ constexpr int64_t kHeadGradBytes = int64_t(1) << 30;
 // rounding left of it, and the products that read them take both.
 constexpr int64_t kHeadExactTokens = 256;
 
-// Whether the forward pass takes the few-token kernel.
-inline bool head_few(int64_t T, bool copy) { return T <= 8 || (copy && T <= kFfnFewTokens); }
+// Whether the forward pass takes the few-token kernel, which reads the weight as it lies. Measured, it
+// against the tiles: 1 token, 128256 x 2048, 94 us and 113; 4 tokens 104 and 113, 8 tokens 129
+// and 113 (each wave reads all tokens); 4 tokens, 128256 x 1024, 57 and 54; 1 token, 50257 x 768, 26
+// and 23 (a wave's share of a short row is too little). Where the tiles need a copy of the weight: 16
+// tokens, 128256 x 1001, 129 and 157; 50257 x 769, 2 tokens 51 and 53, 8 tokens 72 and 54; 16 tokens,
+// 1003 x 509, 19 and 22.
+inline bool head_few(int64_t T, int64_t K, int64_t V, bool copy)
+{
+    if (!copy) return T <= 4 && K >= 1024;
+    return T <= 2 || (T <= kFfnFewTokens && (K >= 896 || V * K < (1 << 24)));
+}
 
 struct HeadSpace {
     int64_t x = -1, w = -1;            // padded copies
@@ -133,7 +144,7 @@ inline HeadSpace head_space(int64_t T, int64_t K, int64_t V, bool backward, bool
         return at;
     };
     const int64_t K8 = ffn_up8(K);
-    if (!backward && head_few(T, copy)) {   // a slot for each workgroup of the few-token kernel
+    if (!backward && head_few(T, K, V, copy)) {   // a slot for each workgroup of the few-token kernel
         s.slots = ffn_ceil(V, ffn_token_rows(T));
         s.stats = take(12 * T * s.slots);
         s.taken = take(4 * T);
