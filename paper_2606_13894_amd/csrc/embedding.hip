@@ -54,7 +54,10 @@ __global__ __launch_bounds__(256) void k_embedding(const EmbedArgs a, int lanes)
 }
 
 // ---------------------------------------------------------------- zeros
-// Bytes [from, to) of the table, by `groups` workgroups of T threads.
+// Bytes [from, to) of the table, by `groups` workgroups of T threads. One workgroup of 1024 on each CU
+// leaves room for the sort's; with two the sort waits (262 MB and a pass of 8192 tokens 51 us, not
+// 47). Past the caches (not temporal), so that the sums behind them find their rows there: 2 us more
+// a launch here, 8 fewer there. The address is a multiple of 16 for every table that is.
 struct Zeros {
     char* table;
     int64_t from, to;
@@ -66,7 +69,12 @@ __device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t group)
     const u32x4a none = {0u, 0u, 0u, 0u};
     const int64_t step = int64_t(z.groups) * T * 16;
     int64_t at = z.from + (int64_t(group) * T + threadIdx.x) * 16;
-    for (; at + 16 <= z.to; at += step) store16(z.table + at, none);
+    if (reinterpret_cast<uintptr_t>(z.table) % 16 == 0) {
+        for (; at + 16 <= z.to; at += step)
+            __builtin_nontemporal_store(none, reinterpret_cast<u32x4a*>(z.table + at));
+    } else {
+        for (; at + 16 <= z.to; at += step) store16(z.table + at, none);
+    }
     for (; at < z.to; at += 2) *reinterpret_cast<uint16_t*>(z.table + at) = 0;
 }
 
@@ -201,6 +209,7 @@ __global__ __launch_bounds__(64) void k_embed_chunks(const EmbedSum a, int64_t s
         uint32_t keys = keys_at(p0);
         const uint32_t before = __builtin_amdgcn_readlane(keys, 0);
         uint32_t now = __builtin_amdgcn_readlane(keys, 1), after = now;
+        if (now >= a.vocab) continue;            // from here on no token of the table
         bool head = now == before;               // the token came from the chunk before
         float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
         for (int64_t p = p0; p < p1; p += U) {
@@ -216,7 +225,7 @@ __global__ __launch_bounds__(64) void k_embed_chunks(const EmbedSum a, int64_t s
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const uint32_t key = __builtin_amdgcn_readlane(keys, u + 1);
-                if (u >= m || key >= a.vocab) continue;   // (no token of the table: the last keys)
+                if (u >= m || key >= a.vocab) continue;
                 if (key != now) {
                     if (head && on) store_row8<false>(a.head + c * a.width, e, a.width, acc);
                     if (!head && on) store_sum<T16>(a, now, e, acc);
@@ -232,7 +241,7 @@ __global__ __launch_bounds__(64) void k_embed_chunks(const EmbedSum a, int64_t s
             }
             after = __builtin_amdgcn_readlane(keys, m + 1);
         }
-        if (now >= a.vocab || !on) continue;
+        if (!on) continue;
         // a token that fills the chunk from the one before on is a head, whether it goes on or not
         if (head) store_row8<false>(a.head + c * a.width, e, a.width, acc);
         else if (now == after) store_row8<false>(a.tail + c * a.width, e, a.width, acc);
@@ -240,46 +249,63 @@ __global__ __launch_bounds__(64) void k_embed_chunks(const EmbedSum a, int64_t s
     }
 }
 
-// Tokens that go over the ends of chunks: by the wave of the chunk in which they begin.
+// Tokens that go over the ends of chunks: by the workgroup of the chunk in which they begin, whose
+// four waves take a quarter of the other chunks each.
 template <bool T16>
-__global__ __launch_bounds__(64) void k_embed_spans(const EmbedSum a, int64_t slabs)
+__global__ __launch_bounds__(256) void k_embed_spans(const EmbedSum a, int64_t slabs)
 {
     constexpr int U = 16;
+    __shared__ float parts[3][8][64];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t all = a.chunks * slabs;
     for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
-        const int64_t c = i / slabs, e = (i % slabs) * 512 + 8 * threadIdx.x;
+        const int64_t c = i / slabs, e = (i % slabs) * 512 + 8 * lane;
         const int64_t mine = min(e, (a.width - 1) / 8 * 8);
         const int64_t p0 = c * a.chunk, p1 = p0 + a.chunk;
         if (p1 >= a.n) continue;
         const uint32_t key = a.keys[p1 - 1];
         if (key >= a.vocab || key != a.keys[p1]) continue;
         if (p0 > 0 && a.keys[p0 - 1] == key) continue;      // it began before
-        float acc[8];
-        load_row8<false>(a.tail + c * a.width, mine, a.width, acc);
-        // the chunks that begin with it, as far as 64 of them at a time
-        for (int64_t d = c + 1;;) {
-            const int64_t at = d + static_cast<int>(threadIdx.x);
-            const uint64_t other = ~__ballot(at < a.chunks && a.keys[at * a.chunk] == key);
-            const int64_t end = other ? d + __ffsll(static_cast<unsigned long long>(other)) - 1
-                                      : d + 64;
-            for (; d < end; d += U) {
-                u32x4a w[U][2];
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    fetch8<false>(a.head + min(d + u, end - 1) * a.width, mine, a.width, w[u]);
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (d + u >= end) continue;
-                    float v[8];
-                    settle8<false>(w[u], mine, a.width, v);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[j] += v[j];
-                }
-            }
-            d = end;
-            if (other) break;
+        // chunks c + 1 .. end - 1 begin with it: 64 steps of what is left at a time
+        int64_t end = c + 1, hi = a.chunks;
+        while (end < hi) {
+            const int64_t step = (hi - end + 63) / 64, at = end + (lane + 1) * step - 1;
+            const int64_t whole = __popcll(__ballot(at < hi && a.keys[at * a.chunk] == key));
+            end += whole * step;
+            hi = min(hi, end + step - 1);
+            if (step == 1) break;
         }
-        if (e < a.width) store_sum<T16>(a, key, e, acc);
+        const int64_t d0 = c + 1 + (end - c - 1) * wave / 4, d1 = c + 1 + (end - c - 1) * (wave + 1) / 4;
+        float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (wave == 0) load_row8<false>(a.tail + c * a.width, mine, a.width, acc);
+        for (int64_t d = d0; d < d1; d += U) {
+            u32x4a w[U][2];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                fetch8<false>(a.head + min(d + u, d1 - 1) * a.width, mine, a.width, w[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (d + u >= d1) continue;
+                float v[8];
+                settle8<false>(w[u], mine, a.width, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += v[j];
+            }
+        }
+        if (wave > 0) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) parts[wave - 1][j][lane] = acc[j];
+        }
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int w = 0; w < 3; ++w)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += parts[w][j][lane];
+            if (e < a.width) store_sum<T16>(a, key, e, acc);
+        }
+        __syncthreads();
     }
 }
 
@@ -348,15 +374,17 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
     m.scale = a.scale;
     m.dtable = a.dtable;
     const int64_t slabs = (a.width + 511) / 512;
-    const dim3 grid(capped(m.chunks * slabs, 1 << 24));
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64), 0, stream, m, slabs); };
-    if (dy_bf16 && table_bf16) go(k_embed_chunks<true, true>);
-    else if (dy_bf16) go(k_embed_chunks<true, false>);
-    else if (table_bf16) go(k_embed_chunks<false, true>);
-    else go(k_embed_chunks<false, false>);
+    const dim3 grid(capped(m.chunks * slabs, 1 << 23));
+    auto go = [&](auto kernel, int threads) {
+        hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, m, slabs);
+    };
+    if (dy_bf16 && table_bf16) go(k_embed_chunks<true, true>, 64);
+    else if (dy_bf16) go(k_embed_chunks<true, false>, 64);
+    else if (table_bf16) go(k_embed_chunks<false, true>, 64);
+    else go(k_embed_chunks<false, false>, 64);
     if (m.chunks > 1) {
-        if (table_bf16) go(k_embed_spans<true>);
-        else go(k_embed_spans<false>);
+        if (table_bf16) go(k_embed_spans<true>, 256);
+        else go(k_embed_spans<false>, 256);
     }
     return hipGetLastError();
 }

@@ -770,8 +770,19 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
     };
     // A wave's share of each row's statistics: over its columns c < N the largest score m, the sum
     // of exp(z - m) and that of (z - m) exp(z - m); and the score of the row's token.
+    // The head's epilogues: the column of the token of each of the lane's rows among the product's, -1
+    // where it is none of them.
+    auto head_column = [&](int64_t token) {
+        const int64_t at = token - g.head.first;
+        return token >= 0 && at >= 0 && at < g.N ? static_cast<int>(at) : -1;
+    };
     auto head_stats = [&](auto whole) {
         constexpr bool FULL = decltype(whole)::value;
+        int column[MI];
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)   // all rows' loads go out together
+            column[mi] = head_column(token_at(g.head.tokens, g.head.wide,
+                                              min(row0 + (wm * MI + mi) * 16 + l16, g.M - 1)));
         const int64_t first = col0 + wn * 64;
         const int64_t slot = PHASES ? 2 * int64_t(w.tn) + wn : w.tn;
 #pragma unroll
@@ -821,9 +832,8 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
                 o[g.M] = s;
                 o[2 * g.M] = t;
             }
-            const int64_t at = token_at(g.head.tokens, g.head.wide, row) - g.head.first;
-            const int64_t in = at - first;
-            if (at < g.N && in >= 0 && in < H + 64 && (in & (H - 1)) < 64) {
+            const int64_t in = column[mi] - first;
+            if (in >= 0 && in < H + 64 && (in & (H - 1)) < 64) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -840,15 +850,25 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
     // 0.0017. With o[1] what the rounding left goes there, and the products take both: 0.0017.
     auto head_grad = [&](auto whole) {
         constexpr bool FULL = decltype(whole)::value;
+        // -p (g + h (log p + H)) of a row as -p (a d + b), p = 2^d, d = z log2 e - l
+        struct {
+            float l, a, b, g;
+            int column;
+        } rows[MI];
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {   // all rows' loads go out together
+            const int64_t row = min(row0 + (wm * MI + mi) * 16 + l16, g.M - 1);
+            const int64_t token = token_at(g.head.tokens, g.head.wide, row);
+            const ScoreGrad r = score_grad_row(token, g.head.vocab, row, g.head.lse,
+                                               g.head.entropy, g.head.dlogprob, g.head.dentropy);
+            rows[mi] = {r.lse * kLog2E, r.h * kLn2, fmaf(r.h, r.entropy, r.g), r.g,
+                        head_column(token)};
+        }
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
             const int64_t row = row0 + (wm * MI + mi) * 16 + l16;
             const bool on = FULL || row < g.M;
-            ScoreGrad r = {0.0f, 0.0f, 0.0f, 0.0f, -1};
-            if (on)
-                r = score_grad_row(g.head.tokens, g.head.wide, row, g.head.lse, g.head.entropy,
-                                   g.head.dlogprob, g.head.dentropy);
-            const int64_t at = r.token - g.head.first;
+            const auto& r = rows[mi];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t c = col0 + h * H + wn * 64 + 16 * q;
@@ -856,8 +876,16 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
                 to_run(acc[mi][h], v);   // all four lanes of the row take part
                 if (!FULL && (!on || c >= g.ldo)) continue;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    v[i] = score_gradient(v[i], r, r.token >= 0 && at == c + i);
+                for (int i = 0; i < 16; ++i) {
+                    const float d = fmaf(v[i], kLog2E, -r.l);
+                    v[i] = -__builtin_amdgcn_exp2f(d) * fmaf(r.a, fmaxf(d, -1e4f), r.b);
+                }
+                const int in = r.column - static_cast<int>(c);
+                if (in >= 0 && in < 16) {     // the row's token is one of the run
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (i == in) v[i] += r.g;
+                }
                 if (!FULL && c + 16 > g.N) {   // columns from N to ldo are read as zeros
 #pragma unroll
                     for (int i = 0; i < 16; ++i)

@@ -69,6 +69,7 @@ struct HeadRows {
     const void* tokens;          // of the rows
     bool wide;                   // 64-bit ones
     int64_t first;               // the vocabulary entry of column 0
+    int64_t vocab;               // of all
     float* stats;                // [head_slots][3][M]
     float* taken;                // [M]: the tokens' scores
     const float* lse;

@@ -412,8 +412,9 @@ __global__ __launch_bounds__(256) void k_score_grad(const ScoreGradArgs a, int64
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t r = item / segments;
         const int64_t e0 = (item % segments) * (256 * 8 * U) + 8 * threadIdx.x;
-        const ScoreGrad g = score_grad_row(a.tokens.p, a.tokens.wide, r, a.lse, a.entropy,
-                                           a.dlogprob, a.dentropy);
+        const int64_t token = token_at(a.tokens.p, a.tokens.wide, r);
+        const ScoreGrad g = score_grad_row(token, a.vocab, r, a.lse, a.entropy, a.dlogprob,
+                                           a.dentropy);
         const char* z = static_cast<const char*>(a.z) + r * a.ld * S;
         char* dz = static_cast<char*>(a.dz) + r * a.ldd * S;
         u32x4a w[U][BF16 ? 1 : 2];
@@ -430,7 +431,7 @@ __global__ __launch_bounds__(256) void k_score_grad(const ScoreGradArgs a, int64
             settle8<BF16>(w[u], e, a.vocab, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                v[j] = score_gradient(v[j], g, g.token >= 0 && g.token == e + j);
+                v[j] = score_gradient(v[j], g, token == e + j);
             store_row8<BF16>(dz, e, a.vocab, v);
         }
     }

@@ -269,6 +269,7 @@ int gefen_head_logprobs(const uint16_t* x, const uint16_t* weight, const void* t
     HeadRows rows{};
     rows.tokens = tokens;
     rows.wide = token_bytes == 8;
+    rows.vocab = V;
     rows.stats = at<float>(workspace, s.stats);
     rows.taken = at<float>(workspace, s.taken);
     HeadJoinArgs j{};
@@ -349,6 +350,7 @@ int gefen_head_logprobs_backward(const uint16_t* x, const uint16_t* weight, cons
             z.head.tokens = tokens;
             z.head.wide = token_bytes == 8;
             z.head.first = first;
+            z.head.vocab = V;
             z.head.lse = lse;
             z.head.entropy = entropy;
             z.head.dlogprob = dlogprob;

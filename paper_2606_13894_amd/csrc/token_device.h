@@ -139,18 +139,17 @@ __device__ __forceinline__ ScoreRow score_row(const ScoreSum& a, int64_t token, 
 // nothing left (lse -inf) has none.
 struct ScoreGrad {
     float lse, entropy, g, h;
-    int64_t token;
 };
-__device__ __forceinline__ ScoreGrad score_grad_row(const void* tokens, bool wide, int64_t row,
+__device__ __forceinline__ ScoreGrad score_grad_row(int64_t token, int64_t vocab, int64_t row,
                                                     const float* lse, const float* entropy,
                                                     const float* dlogprob, const float* dentropy)
 {
     ScoreGrad r;
-    r.token = token_at(tokens, wide, row);
     r.lse = lse[row];
     r.entropy = entropy[row];
-    r.g = r.token >= 0 ? dlogprob[row] : 0.0f;
+    r.g = dlogprob[row];
     r.h = dentropy ? dentropy[row] : 0.0f;
+    if (token < 0 || token >= vocab) r.g = 0.0f;
     if (r.lse == -INFINITY) {
         r.lse = INFINITY;      // p = 0 throughout
         r.g = r.h = 0.0f;

@@ -373,7 +373,7 @@ def _score_gradient64(z, t, lse, H, g, h):
     V = z.shape[1]
     empty = (lse == -math.inf)[:, None]
     on = (t >= 0) & (t < V)
-    g = torch.where(t >= 0, g, 0.0)[:, None]
+    g = torch.where(on, g, 0.0)[:, None]
     d = torch.where(empty, -math.inf, z - torch.where(lse == -math.inf, 0.0, lse)[:, None])
     p = d.exp()
     inner = torch.where(p > 0, d + H[:, None], 0.0)
@@ -489,7 +489,7 @@ def _check_head_gradients(x, w, t, g, h, r, dx, dw):
 def test_head_logprobs_backward(dev, n, width, vocab):
     x = _randn(dev, n, width, seed=1, dtype=BF16)
     w = _randn(dev, vocab, width, seed=2).mul_(2 * width ** -0.5).to(BF16)
-    t = _randint(dev, -1, vocab, n, seed=3)
+    t = _randint(dev, -1, vocab + 1, n, seed=3)
     g, h = _randn(dev, n, seed=4), _randn(dev, n, seed=5)
     r = gf.head_logprobs(x, w, t)
     for ent in (h, None):
