@@ -422,10 +422,13 @@ class FeedForward(torch.nn.Module):
     activations below about 6 width inner / (width + 2 inner) tokens; the casts take 53 us at 2048
     and 8192, and are not done again in the backward pass). Where no gradient is wanted nothing is kept, and
     few tokens take the kernels for them. A program that serves casts the weights once and calls
-    :func:`rms_norm` and :func:`gated_ffn` itself."""
+    :func:`rms_norm` and :func:`gated_ffn` itself.
+
+    ``dropout``: in training y goes through a :class:`Dropout` of that p and ``seed``, whose mask is not
+    kept either (a pass over y forward, and one over its gradient)."""
 
     def __init__(self, width: int, inner: int, activation: str = "silu", eps: float = 1e-6,
-                 device=None):
+                 device=None, dropout: float = 0.0, seed: int = 0):
         super().__init__()
         if activation not in ACTIVATIONS:
             raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
@@ -437,12 +440,18 @@ class FeedForward(torch.nn.Module):
 
         self.w_gate, self.w_up = weight(inner, width), weight(inner, width)
         self.w_down = weight(width, inner)
+        self.drop = None
+        if dropout:
+            from .language import Dropout   # which imports this module
+            self.drop = Dropout(dropout, seed, device)
 
     def forward(self, x, residual=None):
         bf16 = torch.bfloat16
         weights = self.w_gate.to(bf16), self.w_up.to(bf16), self.w_down.to(bf16)
         if _tracked(x, residual, self.norm, *weights):
-            return _Block.apply(x, residual, self.norm, *weights, self.eps, self.activation)
-        n = rms_norm(x, self.norm, residual, self.eps)
-        y = gated_ffn(n.y, *weights, self.activation)
-        return y, (n.h if residual is not None else x.view_as(x))
+            y, h = _Block.apply(x, residual, self.norm, *weights, self.eps, self.activation)
+        else:
+            n = rms_norm(x, self.norm, residual, self.eps)
+            y = gated_ffn(n.y, *weights, self.activation)
+            h = n.h if residual is not None else x.view_as(x)
+        return (y if self.drop is None else self.drop(y)), h

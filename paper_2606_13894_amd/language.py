@@ -20,6 +20,7 @@ where an argument of a plain call wants a gradient, a gradient through its resul
 from __future__ import annotations
 
 import ctypes
+import operator
 from typing import NamedTuple, Optional
 
 import torch
@@ -145,14 +146,14 @@ def dropout(x, p: float, seed, offset: int = 0, residual=None, stream=None):
         seed = ff._operand(seed, "seed", dev, torch.int64, (2,))
         sp = seed.data_ptr()
     else:
-        number = seed & 0xFFFFFFFFFFFFFFFF
+        number = operator.index(seed) & 0xFFFFFFFFFFFFFFFF
     if residual is not None:
         residual = ff._operand(residual, "residual", dev, x.dtype, x.shape)
         rp = residual.data_ptr()
     y = torch.empty_like(x)
     ff._call(ff._library().gefen_dropout(
-        x.data_ptr(), rp, d, x.numel(), p, number, offset & 0xFFFFFFFFFFFFFFFF, sp, y.data_ptr(),
-        ff._raw_stream(dev)))
+        x.data_ptr(), rp, d, x.numel(), p, number, operator.index(offset) & 0xFFFFFFFFFFFFFFFF, sp,
+        y.data_ptr(), ff._raw_stream(dev)))
     if ff._tracked(x, residual):
         ff._no_graph(_NO_GRADIENT.format("dropout", "Dropout"), y)
     return y
@@ -167,10 +168,12 @@ class _Drop(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
-        with torch.no_grad():
-            dx = dropout(dy, ctx.p, ctx.saved_tensors[0])
-        if torch.is_grad_enabled():   # create_graph
-            ff._no_graph("Dropout has no second derivative", dx)
+        dx = None
+        if ctx.needs_input_grad[0]:
+            with torch.no_grad():
+                dx = dropout(dy, ctx.p, ctx.saved_tensors[0])
+            if torch.is_grad_enabled():   # create_graph
+                ff._no_graph("Dropout has no second derivative", dx)
         return dx, dy if ctx.residual else None, None, None
 
 
@@ -234,6 +237,8 @@ def token_logprobs(logits, tokens, top: int = 0, stream=None):
     rows, vocab = z.shape
     shape = logits.shape[:-1]
     tokens, size = _tokens(tokens, dev, shape)
+    if not 0 <= top <= min(32, vocab):
+        raise ValueError(f"top must be in [0, {min(32, vocab)}]")
     f32 = torch.float32
     logprob, entropy, lse = (z.new_empty(shape, dtype=f32) for _ in range(3))
     best = where = bp = wp = None
@@ -263,7 +268,8 @@ def _upstream(dlogprob, dentropy, dev, shape):
 def token_logprobs_backward(dlogprob, logits, tokens, lse, entropy, dentropy=None, out=None,
                             stream=None):
     """The gradient of :func:`token_logprobs`'s logits from those of logprob and entropy. ``out``
-    takes it (contiguous, or rows evenly apart); it may be ``logits`` itself."""
+    takes it (contiguous, or rows evenly apart, no gradient wanted of it); it may be ``logits``
+    itself."""
     if stream is not None:
         return ff._on(stream, token_logprobs_backward, dlogprob, logits, tokens, lse, entropy,
                       dentropy, out)
@@ -284,9 +290,12 @@ def token_logprobs_backward(dlogprob, logits, tokens, lse, entropy, dentropy=Non
         if not isinstance(out, torch.Tensor) or out.dtype is not logits.dtype or \
                 out.shape != logits.shape:
             raise ValueError(f"out must be {logits.dtype} of shape {tuple(logits.shape)}")
+        if out.requires_grad:
+            raise ValueError("out is written in place and must not want a gradient")
         to, ldd = _score_rows(out, "out", dev)
         if to.data_ptr() != out.data_ptr():
             raise ValueError("out must have its rows evenly apart")
+        torch.autograd.graph.increment_version(out)   # what was saved of it is gone
     ff._call(ff._library().gefen_token_logprobs_backward(
         z.data_ptr(), ld, d, rows, vocab, tokens.data_ptr(), size, lse.data_ptr(),
         entropy.data_ptr(), gp, hp, to.data_ptr(), ldd, ff._raw_stream(dev)))
@@ -296,7 +305,7 @@ def token_logprobs_backward(dlogprob, logits, tokens, lse, entropy, dentropy=Non
 
 
 def _of_logprob(g, like):
-    """A gradient that autograd gives as None, or in pieces, as the calls take it."""
+    """The log probabilities' gradient, zeros where none of them was used."""
     return torch.zeros_like(like) if g is None else g
 
 
