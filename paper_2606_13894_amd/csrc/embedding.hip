@@ -11,9 +11,11 @@
 // token: the whole table is set to zero by workgroups beside those of the sort, which wait for
 // memory most of their time.
 //
-// Sort: by digits of up to nine bits from the lowest; one workgroup for each value of the digit
-// reads all the tokens, counts those with a smaller digit, which is where its own begin, and those
-// of each of its waves, and writes its own in order. No workgroup waits for another.
+// Sort: by digits of up to nine bits from the lowest, no workgroup waiting for another. Up to
+// kSortFew tokens one launch a digit: a workgroup for each of its values reads all the tokens, counts
+// those with a smaller one, which is where its own begin, and those of each of its waves, and
+// writes its own in order. More take three: counts of each value in blocks of 4096 tokens, their sums
+// over the blocks, and the tokens to their places.
 #include "token_internal.h"
 
 #include "token_device.h"
@@ -88,6 +90,10 @@ struct SortPass {
     int64_t n;
     uint32_t vocab;              // the key of a token outside 0 .. vocab - 1
     int shift, bits;
+    uint32_t digits;             // the digit's values
+    uint32_t* counts;            // [digits][blocks], then their sums over the blocks before
+    uint32_t* totals;            // [digits]
+    int64_t blocks;
     Zeros zeros;                 // the first workgroups write them
 };
 
@@ -160,6 +166,134 @@ __global__ __launch_bounds__(64 * kSortWaves, 8) void k_sort_pass(const SortPass
             }
             at += __popcll(hits);
         }
+    }
+}
+
+constexpr int kSortThreads = 64 * kSortWaves;
+constexpr int kSortEach = kSortBlock / kSortThreads;   // keys of a lane
+static_assert(kSortEach * kSortThreads == kSortBlock && (1 << kSortBits) <= kSortThreads, "a block");
+
+__global__ __launch_bounds__(kSortThreads) void k_sort_count(const SortPass a)
+{
+    __shared__ uint32_t counts[1 << kSortBits];
+    if (blockIdx.x < a.zeros.groups) {
+        write_zeros<kSortThreads>(a.zeros, blockIdx.x);
+        return;
+    }
+    const int64_t block = blockIdx.x - a.zeros.groups;
+    const uint32_t tid = threadIdx.x;
+    if (tid < a.digits) counts[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kSortEach; ++u) {
+        const int64_t i = block * kSortBlock + u * kSortThreads + tid;
+        if (i < a.n) atomicAdd(&counts[(sort_key(a, i) >> a.shift) & ((1u << a.bits) - 1)], 1u);
+    }
+    __syncthreads();
+    if (tid < a.digits) a.counts[tid * a.blocks + block] = counts[tid];
+}
+
+// The inclusive sum over a wave's lanes.
+__device__ __forceinline__ uint32_t wave_sum_upto(uint32_t v, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t from = __shfl_up(v, d);
+        if (lane >= d) v += from;
+    }
+    return v;
+}
+
+// A digit value's counts to their sums over the blocks before.
+__global__ __launch_bounds__(256) void k_sort_scan(const SortPass a)
+{
+    __shared__ uint32_t of_wave[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t* __restrict__ counts = a.counts + int64_t(blockIdx.x) * a.blocks;
+    uint32_t before = 0;
+    for (int64_t b = 0; b < a.blocks; b += 256) {
+        const int64_t i = b + threadIdx.x;
+        const uint32_t v = i < a.blocks ? counts[i] : 0;
+        const uint32_t upto = wave_sum_upto(v, lane);
+        if (lane == 63) of_wave[wave] = upto;
+        __syncthreads();
+        uint32_t start = before;
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) start += of_wave[w];
+            before += of_wave[w];
+        }
+        if (i < a.blocks) counts[i] = start + upto - v;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) a.totals[blockIdx.x] = before;
+}
+
+__global__ __launch_bounds__(kSortThreads) void k_sort_place(const SortPass a)
+{
+    __shared__ uint32_t of_waves[kSortWaves][1 << kSortBits];
+    __shared__ uint32_t place[1 << kSortBits];       // of the block's first key of each value
+    __shared__ uint32_t upto_wave[kSortWaves];
+    if (blockIdx.x < a.zeros.groups) {
+        write_zeros<kSortThreads>(a.zeros, blockIdx.x);
+        return;
+    }
+    const int64_t block = blockIdx.x - a.zeros.groups;
+    const uint32_t tid = threadIdx.x;
+    const int lane = tid & 63, wave = tid >> 6;
+    const uint32_t total = tid < a.digits ? a.totals[tid] : 0;
+    const uint32_t upto = wave_sum_upto(total, lane);
+    if (lane == 63) upto_wave[wave] = upto;
+    for (uint32_t d = lane; d < a.digits; d += 64) of_waves[wave][d] = 0;
+    __syncthreads();
+    if (tid < a.digits) {
+        uint32_t start = upto - total;
+        for (int w = 0; w < wave; ++w) start += upto_wave[w];
+        place[tid] = start + a.counts[tid * a.blocks + block];
+    }
+    // a wave's keys in order, 64 at a time: a key's rank among those of its value in the wave
+    volatile uint32_t* mine = of_waves[wave];
+    const int64_t first = block * kSortBlock + int64_t(wave) * (64 * kSortEach);
+    uint32_t key[kSortEach], digit[kSortEach], rank[kSortEach];
+#pragma unroll
+    for (int u = 0; u < kSortEach; ++u) {
+        const int64_t i = first + 64 * u + lane;
+        key[u] = i < a.n ? sort_key(a, i) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kSortEach; ++u) {
+        const bool in = first + 64 * u + lane < a.n;
+        digit[u] = (key[u] >> a.shift) & ((1u << a.bits) - 1);
+        uint64_t same = __ballot(in);
+        for (int b = 0; b < a.bits; ++b) {
+            const bool set = digit[u] >> b & 1;
+            const uint64_t sets = __ballot(set);
+            same &= set ? sets : ~sets;
+        }
+        const uint64_t lower = same & ((uint64_t(1) << lane) - 1);
+        rank[u] = 0;
+        if (in) {
+            const uint32_t before = mine[digit[u]];
+            rank[u] = before + __popcll(lower);
+            if (lower == 0) mine[digit[u]] = before + __popcll(same);
+        }
+    }
+    __syncthreads();
+    if (tid < a.digits) {
+        uint32_t start = place[tid];
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t n = of_waves[w][tid];
+            of_waves[w][tid] = start;
+            start += n;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kSortEach; ++u) {
+        const int64_t i = first + 64 * u + lane;
+        if (i >= a.n) continue;
+        const uint32_t o = of_waves[wave][digit[u]] + rank[u];
+        a.keys_out[o] = key[u];
+        a.rows_out[o] = a.tokens.p ? static_cast<uint32_t>(i) : a.rows[i];
     }
 }
 
@@ -335,14 +469,20 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
     // The zeros are shared by the sort's launches. One workgroup on each CU writes them, so that the
     // sort's have the other half of it.
     const int passes = a.n > 0 ? plan.passes : 1;
-    constexpr int kThreads = 64 * kSortWaves;
-    int out = 0;
+    const bool blocks = a.n > kSortFew;
+    const int shares = blocks ? 2 * passes : passes;
+    int out = 0, share = 0;
+    auto zeros = [&]() {
+        Zeros z;
+        z.table = static_cast<char*>(a.dtable);
+        z.from = bytes * share / shares / 16 * 16;
+        ++share;
+        z.to = share < shares ? bytes * share / shares / 16 * 16 : bytes;
+        z.groups = capped((z.to - z.from + 16 * kSortThreads - 1) / (16 * kSortThreads), 256);
+        return z;
+    };
     for (int p = 0, shift = 0; p < passes; shift += plan.bits[p], ++p) {
         SortPass s{};
-        s.zeros.table = static_cast<char*>(a.dtable);
-        s.zeros.from = bytes * p / passes / 16 * 16;
-        s.zeros.to = p + 1 < passes ? bytes * (p + 1) / passes / 16 * 16 : bytes;
-        s.zeros.groups = capped((s.zeros.to - s.zeros.from + 16 * kThreads - 1) / (16 * kThreads), 256);
         s.n = a.n;
         s.vocab = static_cast<uint32_t>(a.vocab);
         s.tokens = a.tokens;
@@ -355,9 +495,24 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
         s.shift = shift;
         s.bits = plan.bits[p];
         // the last digit ends with the largest key's
-        const uint32_t digits = a.n == 0 ? 0 : p + 1 < passes
+        s.digits = a.n == 0 ? 0 : p + 1 < passes
             ? 1u << s.bits : static_cast<uint32_t>(a.vocab >> shift) + 1;
-        hipLaunchKernelGGL(k_sort_pass, dim3(s.zeros.groups + digits), dim3(kThreads), 0, stream, s);
+        s.zeros = zeros();
+        if (!blocks) {
+            hipLaunchKernelGGL(k_sort_pass, dim3(s.zeros.groups + s.digits), dim3(kSortThreads), 0,
+                               stream, s);
+            continue;
+        }
+        s.counts = a.counts;
+        s.blocks = sort_blocks(a.n);
+        s.totals = a.counts + s.blocks * (1 << kSortBits);
+        const auto grid = [&]() {
+            return dim3(s.zeros.groups + static_cast<unsigned>(s.blocks));
+        };
+        hipLaunchKernelGGL(k_sort_count, grid(), dim3(kSortThreads), 0, stream, s);
+        hipLaunchKernelGGL(k_sort_scan, dim3(s.digits), dim3(256), 0, stream, s);
+        s.zeros = zeros();
+        hipLaunchKernelGGL(k_sort_place, grid(), dim3(kSortThreads), 0, stream, s);
     }
     if (a.n == 0) return hipGetLastError();
     EmbedSum m{};

@@ -35,7 +35,8 @@ int check_table(int64_t n, int64_t vocab, int64_t width)
 
 int check_scale(double scale)
 {
-    if (!std::isfinite(scale)) return fail(GEFEN_EINVAL, "scale must be finite");
+    if (!std::isfinite(static_cast<float>(scale)))
+        return fail(GEFEN_EINVAL, "scale must be finite in float32");
     return GEFEN_OK;
 }
 
@@ -122,6 +123,7 @@ int gefen_embedding_backward(const void* dy, int32_t dtype, const void* tokens,
             a.keys[i] = at<uint32_t>(workspace, s.keys[i]);
             a.rows[i] = at<uint32_t>(workspace, s.rows[i]);
         }
+        a.counts = at<uint32_t>(workspace, s.counts);
         a.partial = at<float>(workspace, s.partial);
     }
     a.tokens = Tokens{tokens, token_bytes == 8};

@@ -33,6 +33,7 @@ struct EmbedGradArgs {
     void* dtable;
     uint32_t* keys[2];       // n each: the tokens, sorted in turns
     uint32_t* rows[2];       // n each: where they stood
+    uint32_t* counts;        // the sort's by blocks (embed_space)
     float* partial;          // 2 embed_chunks(n) rows of `width`
 };
 hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool table_bf16,

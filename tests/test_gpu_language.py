@@ -102,7 +102,9 @@ def _table_gradient(dy, t, vocab, scale):
 @pytest.mark.parametrize("n,vocab,width", [
     (0, 7, 8), (1, 1, 1), (1, 5000, 64), (31, 3, 5), (32, 1, 8), (33, 1, 9), (64, 511, 512),
     (100, 512, 513), (500, 2, 64), (1000, 513, 100), (1000, 40, 2048), (5000, 1000, 72),
-    (777, 50257, 768), (3000, 300_001, 8), (20000, 17, 33), (65_537, 100, 16)])
+    (777, 50257, 768), (3000, 300_001, 8), (20000, 17, 33), (65_537, 100, 16),
+    (20_480, 700, 8), (20_481, 700, 8), (24_576, 50257, 24), (70_001, 300_001, 9),
+    (300_000, 5, 16), (1_100_000, 3000, 3)])
 def test_embedding_backward(dev, n, vocab, width, dtype, out):
     dy = _randn(dev, n, width, seed=1, dtype=DTYPES[dtype])
     # as text has them: few tokens often

@@ -35,7 +35,7 @@ def test_embedding_refusals(lib):
     _said(lib, call(width=(1 << 20) + 1), -1, "width")
     _said(lib, call(vocab=1 << 24, width=1 << 20), -1, "2^40")
     _said(lib, call(n=1 << 24, width=1 << 20), -1, "2^40")
-    for s in (float("nan"), float("inf")):
+    for s in (float("nan"), float("inf"), 1e39):
         _said(lib, call(scale=s), -1, "scale")
     for name in ("t", "w", "y"):
         _said(lib, call(**{name: None}), -1, "NULL")

@@ -44,6 +44,8 @@ static void check_embed(int64_t n, int64_t width)
         need(s.rows[i] >= s.keys[i] + 4 * n && s.rows[i] % 16 == 0, "rows", n, width, i);
         at = s.rows[i] + 4 * n;
     }
+    need(s.counts >= at && s.counts % 16 == 0, "counts", n, width, 0);
+    if (n > kSortFew) at = s.counts + 4 * (sort_blocks(n) + 1) * (1 << kSortBits);
     need(s.partial >= at && s.partial % 16 == 0, "partial", n, width, 0);
     need(s.bytes >= s.partial + 8 * chunks * width, "bytes", n, width, s.bytes);
 }
