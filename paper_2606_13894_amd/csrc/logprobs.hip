@@ -7,7 +7,7 @@
 // rows are few, workgroups that share a row are joined in a fixed order.
 //
 // Best alternatives, by value and among equals by the lower index: a lane also keeps where its
-// largest score first stood. The lanes are 64 groups, and the k-th largest of the groups' largest scores
+// largest score first stood. The lanes are 64 groups (of lanes 64 apart), and the k-th largest of the groups' largest scores
 // is reached by k scores at least: only the vectors of lanes that reach it are read again, and
 // the few scores that do are ranked by counting. (They go to a list in LDS; where it does not hold
 // them, the k best are taken one by one.) A score and its place are one 64-bit key, the place
@@ -103,7 +103,7 @@ __device__ __forceinline__ void join_all(ScoreSum& a, ScoreSum (&v)[U])
 
 template <int L>
 struct ListSpace {
-    uint64_t groups[64];
+    unsigned long long groups[64];     // 0, as the counts, before the row
     uint64_t list[kList];
     uint64_t best[L / 64];
     uint64_t least;
@@ -145,15 +145,7 @@ __device__ void select_top(const void* row, int n, int v0, int v1, int k, uint64
     constexpr int N = Vec<BF16>::N, kWaves = L / 64;
     const int tid = threadIdx.x;
     n = by_lane(n);
-    constexpr int kGroup = L / 64;
-    uint64_t group = key;
-#pragma unroll
-    for (int d = 1; d < kGroup; d *= 2) {
-        const uint64_t other = __shfl_xor(static_cast<unsigned long long>(group), d);
-        group = other > group ? other : group;
-    }
-    if (tid % kGroup == 0) s.groups[tid / kGroup] = group;
-    if (tid == 0) s.found = s.count = 0;
+    if (key) atomicMax(&s.groups[tid & 63], static_cast<unsigned long long>(key));
     __syncthreads();
     if (tid < 64) {
         const uint64_t of_groups = least_of_top(s.groups[tid], k);
@@ -264,6 +256,10 @@ __global__ __launch_bounds__(L) void k_scores(const ScoreArgs a)
         if (one && tid == 0) {
             token = token_at(a.tokens.p, a.tokens.wide, r);
             if (token >= 0 && token < vocab) taken = score_at<BF16>(row, token);
+        }
+        if constexpr (TOP) {
+            if (tid < 64) list.groups[tid] = 0;
+            if (tid == 0) list.found = list.count = 0;
         }
         ScoreSum c = {-INFINITY, 0.0f, 0.0f};
         float top = -INFINITY;

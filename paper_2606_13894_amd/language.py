@@ -45,10 +45,20 @@ def _table_size(vocab, width):
 
 
 def _space(query, like, *sizes):
-    """The workspace that `query` asks for, and its size."""
+    """The workspace that `query` asks for, its address and its size."""
     n = ctypes.c_int64()
     ff._call(query(*sizes, n))
-    return like.new_empty(n.value, dtype=torch.uint8), n.value
+    n = n.value
+    if not n:
+        return None, None, 0
+    ws = like.new_empty(n, dtype=torch.uint8)
+    return ws, ws.data_ptr(), n
+
+
+def _row_results(tokens):
+    """Three float32 outputs, one number per token each."""
+    a = torch.empty_like(tokens, dtype=torch.float32)
+    return a, torch.empty_like(a), torch.empty_like(a)
 
 
 # ------------------------------------------------------------------ embedding
@@ -90,10 +100,10 @@ def embedding_backward(dy, tokens, vocab: int, scale: float = 1.0, dtype=torch.f
     _table_size(vocab, width)
     out = dy.new_empty((vocab, width), dtype=dtype)
     lib = ff._library()
-    ws, n = _space(lib.gefen_embedding_backward_workspace, dy, tokens.numel(), vocab, width)
+    ws, wp, n = _space(lib.gefen_embedding_backward_workspace, dy, tokens.numel(), vocab, width)
     ff._call(lib.gefen_embedding_backward(
         dy.data_ptr(), d, tokens.data_ptr(), size, tokens.numel(), vocab, width, scale,
-        out.data_ptr(), ff._dtype(out, "dtable"), ws.data_ptr(), n, ff._raw_stream(dev)))
+        out.data_ptr(), ff._dtype(out, "dtable"), wp, n, ff._raw_stream(dev)))
     if ff._tracked(dy):
         ff._no_graph(ff._BACKWARD_ONLY.format("embedding_backward"), out)
     return out
@@ -216,6 +226,8 @@ def _score_rows(z, what, dev):
         ff._operand(z, what, dev)
     if not z.dim() or not z.shape[-1]:
         raise ValueError(f"{what} must have rows of at least one element")
+    if z.dim() == 2 and z.is_contiguous():
+        return z, z.shape[1]
     rows = z.reshape(-1, z.shape[-1]) if z.numel() else z.new_empty((0, z.shape[-1]))
     if rows.shape[0] == 1 and rows.stride(1) == 1:
         return rows, rows.shape[1]
@@ -239,18 +251,17 @@ def token_logprobs(logits, tokens, top: int = 0, stream=None):
     tokens, size = _tokens(tokens, dev, shape)
     if not 0 <= top <= min(32, vocab):
         raise ValueError(f"top must be in [0, {min(32, vocab)}]")
-    f32 = torch.float32
-    logprob, entropy, lse = (z.new_empty(shape, dtype=f32) for _ in range(3))
-    best = where = bp = wp = None
+    logprob, entropy, lse = _row_results(tokens)
+    best = where = bp = kp = None
     if top:
-        best = z.new_empty((*shape, top), dtype=f32)
-        where = z.new_empty((*shape, top), dtype=torch.int64)
-        bp, wp = best.data_ptr(), where.data_ptr()
+        best = lse.new_empty((*shape, top))
+        where = tokens.new_empty((*shape, top), dtype=torch.int64)
+        bp, kp = best.data_ptr(), where.data_ptr()
     lib = ff._library()
-    ws, n = _space(lib.gefen_token_logprobs_workspace, z, d, rows, vocab, top)
+    ws, wp, n = _space(lib.gefen_token_logprobs_workspace, z, d, rows, vocab, top)
     ff._call(lib.gefen_token_logprobs(
         z.data_ptr(), ld, d, rows, vocab, tokens.data_ptr(), size, top, logprob.data_ptr(),
-        entropy.data_ptr(), lse.data_ptr(), bp, wp, ws.data_ptr(), n, ff._raw_stream(dev)))
+        entropy.data_ptr(), lse.data_ptr(), bp, kp, wp, n, ff._raw_stream(dev)))
     if ff._tracked(logits):
         ff._no_graph(_NO_GRADIENT.format("token_logprobs", "LogProbs"), logprob, entropy, lse,
                      *((best,) if top else ()))
@@ -284,7 +295,7 @@ def token_logprobs_backward(dlogprob, logits, tokens, lse, entropy, dentropy=Non
     entropy = ff._operand(entropy, "entropy", dev, f32, shape)
     g, h, gp, hp = _upstream(dlogprob, dentropy, dev, shape)
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        out = torch.empty_like(z) if z is logits else logits.new_empty(logits.shape)
         to, ldd = out, vocab
     else:
         if not isinstance(out, torch.Tensor) or out.dtype is not logits.dtype or \
@@ -369,12 +380,11 @@ def head_logprobs(x, weight, tokens, stream=None):
     wants = ff._tracked(x, weight)
     dev, x, weight, tokens, size, n, width, vocab = _head_operands(x, weight, tokens)
     lib = ff._library()
-    logprob, entropy, lse = (x.new_empty(x.shape[:-1], dtype=torch.float32) for _ in range(3))
-    ws, nb = _head_space(lib, x, weight, n, width, vocab, 0)
+    logprob, entropy, lse = _row_results(tokens)
+    ws, wp, nb = _head_space(lib, x, weight, n, width, vocab, 0)
     ff._call(lib.gefen_head_logprobs(
         x.data_ptr(), weight.data_ptr(), tokens.data_ptr(), size, n, width, vocab,
-        logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), ws.data_ptr(), nb,
-        ff._raw_stream(dev)))
+        logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), wp, nb, ff._raw_stream(dev)))
     if wants:
         ff._no_graph(_NO_GRADIENT.format("head_logprobs", "Head"), logprob, entropy, lse)
     return HeadLogProbs(logprob, entropy, lse)
@@ -395,11 +405,10 @@ def head_logprobs_backward(dlogprob, x, weight, tokens, lse, entropy, dentropy=N
     g, h, gp, hp = _upstream(dlogprob, dentropy, dev, shape)
     lib = ff._library()
     dx, dw = torch.empty_like(x), torch.empty_like(weight)
-    ws, nb = _head_space(lib, x, weight, n, width, vocab, ff._BACKWARD)
+    ws, wp, nb = _head_space(lib, x, weight, n, width, vocab, ff._BACKWARD)
     ff._call(lib.gefen_head_logprobs_backward(
         x.data_ptr(), weight.data_ptr(), tokens.data_ptr(), size, n, width, vocab, lse.data_ptr(),
-        entropy.data_ptr(), gp, hp, dx.data_ptr(), dw.data_ptr(), ws.data_ptr(), nb,
-        ff._raw_stream(dev)))
+        entropy.data_ptr(), gp, hp, dx.data_ptr(), dw.data_ptr(), wp, nb, ff._raw_stream(dev)))
     if wants:
         ff._no_graph(ff._BACKWARD_ONLY.format("head_logprobs_backward"), dx, dw)
     return dx, dw
