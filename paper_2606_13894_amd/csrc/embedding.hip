@@ -16,6 +16,9 @@
 // those with a smaller one, which is where its own begin, and those of each of its waves, and
 // writes its own in order. More take three: counts of each value in blocks of 4096 tokens, their sums
 // over the blocks, and the tokens to their places.
+//
+// Up to kSortRank tokens two launches do it all: each token's place is the number of those before it,
+// counted one by one, and a workgroup for each token that is the first of its run adds the run up.
 #include "token_internal.h"
 
 #include "token_device.h"
@@ -167,6 +170,38 @@ __global__ __launch_bounds__(64 * kSortWaves, 8) void k_sort_pass(const SortPass
             at += __popcll(hits);
         }
     }
+}
+
+// The place of each of 64 tokens: the number of smaller ones, and of equal ones that stand before it.
+// A lane has a token, and each wave the others to compare it with, 64 in its lanes at a time.
+__global__ __launch_bounds__(64 * kSortWaves) void k_sort_rank(const SortPass a)
+{
+    __shared__ uint32_t counts[kSortWaves][64];
+    if (blockIdx.x < a.zeros.groups) {
+        write_zeros<64 * kSortWaves>(a.zeros, blockIdx.x);
+        return;
+    }
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = static_cast<int>(a.n);
+    const int i = (blockIdx.x - a.zeros.groups) * 64 + lane;
+    const uint32_t key = i < n ? sort_key(a, i) : 0;
+    const int to = n * (wave + 1) / kSortWaves;
+    uint32_t less = 0;
+    for (int j = n * wave / kSortWaves; j < to; j += 64) {
+        const uint32_t other = j + lane < to ? sort_key(a, j + lane) : 0xffffffffu;
+        const int m = min(64, to - j);
+        for (int k = 0; k < m; ++k) {
+            const uint32_t o = __builtin_amdgcn_readlane(other, k);
+            less += o < key + (j + k < i);
+        }
+    }
+    counts[wave][lane] = less;
+    __syncthreads();
+    if (wave > 0 || i >= n) return;
+    for (int w = 1; w < kSortWaves; ++w) less += counts[w][lane];
+    a.keys_out[less] = key;
+    a.rows_out[less] = static_cast<uint32_t>(i);
 }
 
 constexpr int kSortThreads = 64 * kSortWaves;
@@ -443,6 +478,75 @@ __global__ __launch_bounds__(256) void k_embed_spans(const EmbedSum a, int64_t s
     }
 }
 
+// Few tokens: a workgroup for each sorted position and 512 columns, which has something to do where a
+// token begins. Its waves share runs of more than kAlone.
+template <bool DY16, bool T16>
+__global__ __launch_bounds__(256) void k_embed_runs(const EmbedSum a, int64_t slabs)
+{
+    constexpr int U = 16, kAlone = 16, S = DY16 ? 2 : 4;
+    __shared__ float parts[3][8][64];
+    const char* dy = static_cast<const char*>(a.dy);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = static_cast<int>(a.n);
+    const int first = static_cast<int>(blockIdx.x / slabs);
+    const int64_t e = (blockIdx.x % slabs) * 512 + 8 * lane;
+    const int64_t mine = min(e, (a.width - 1) / 8 * 8);
+    // the keys from the one before on, 64 of them, and the end of the run
+    const int at = first - 1 + lane;
+    const uint32_t keys = at >= 0 && at < n ? a.keys[at] : 0xffffffffu;
+    const uint32_t key = __builtin_amdgcn_readlane(keys, 1);
+    if (key >= a.vocab || static_cast<uint32_t>(__builtin_amdgcn_readlane(keys, 0)) == key) return;
+    const uint64_t others = ~__ballot(keys == key) >> 2;    // from the second of the run on
+    int end = first + 63;
+    if (others) {
+        end = first + __ffsll(static_cast<unsigned long long>(others));
+    } else {                                                // longer than that: 64 probes at a time
+        int hi = n;
+        while (end < hi) {
+            const int step = (hi - end + 63) / 64, p = end + (lane + 1) * step - 1;
+            end += __popcll(__ballot(p < hi && a.keys[p] == key)) * step;
+            hi = min(hi, end + step - 1);
+            if (step == 1) break;
+        }
+    }
+    const int m = end - first;
+    if (m <= kAlone && wave > 0) return;
+    const int p0 = m <= kAlone ? first : first + m * wave / 4;
+    const int p1 = m <= kAlone ? end : first + m * (wave + 1) / 4;
+    float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    for (int p = p0; p < p1; p += U) {
+        const uint32_t rows = a.rows[min(p + lane, p1 - 1)];
+        u32x4a w[U][DY16 ? 1 : 2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u < p1)
+                fetch8<DY16>(dy + int64_t(__builtin_amdgcn_readlane(rows, u)) * a.width * S, mine,
+                             a.width, w[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p + u >= p1) continue;
+            float v[8];
+            settle8<DY16>(w[u], mine, a.width, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] += v[j];
+        }
+    }
+    if (m > kAlone) {
+        if (wave > 0) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) parts[wave - 1][j][lane] = acc[j];
+        }
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int w = 0; w < 3; ++w)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] += parts[w][j][lane];
+    }
+    if (e < a.width) store_sum<T16>(a, key, e, acc);
+}
+
 inline unsigned capped(int64_t groups, int64_t most) { return static_cast<unsigned>(groups < most ? groups : most); }
 
 }  // namespace
@@ -468,7 +572,8 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
     const int64_t bytes = a.vocab * a.width * (table_bf16 ? 2 : 4);
     // The zeros are shared by the sort's launches. One workgroup on each CU writes them, so that the
     // sort's have the other half of it.
-    const int passes = a.n > 0 ? plan.passes : 1;
+    const bool rank = a.n <= kSortRank;
+    const int passes = rank ? 1 : plan.passes;
     const bool blocks = a.n > kSortFew;
     const int shares = blocks ? 2 * passes : passes;
     int out = 0, share = 0;
@@ -495,9 +600,15 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
         s.shift = shift;
         s.bits = plan.bits[p];
         // the last digit ends with the largest key's
-        s.digits = a.n == 0 ? 0 : p + 1 < passes
+        s.digits = p + 1 < passes
             ? 1u << s.bits : static_cast<uint32_t>(a.vocab >> shift) + 1;
         s.zeros = zeros();
+        if (rank) {
+            const unsigned groups = static_cast<unsigned>((a.n + 63) / 64);
+            hipLaunchKernelGGL(k_sort_rank, dim3(s.zeros.groups + groups), dim3(64 * kSortWaves), 0,
+                               stream, s);
+            continue;
+        }
         if (!blocks) {
             hipLaunchKernelGGL(k_sort_pass, dim3(s.zeros.groups + s.digits), dim3(kSortThreads), 0,
                                stream, s);
@@ -529,6 +640,15 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
     m.scale = a.scale;
     m.dtable = a.dtable;
     const int64_t slabs = (a.width + 511) / 512;
+    if (rank) {
+        const dim3 each(static_cast<unsigned>(a.n * slabs));
+        auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, each, dim3(256), 0, stream, m, slabs); };
+        if (dy_bf16 && table_bf16) run(k_embed_runs<true, true>);
+        else if (dy_bf16) run(k_embed_runs<true, false>);
+        else if (table_bf16) run(k_embed_runs<false, true>);
+        else run(k_embed_runs<false, false>);
+        return hipGetLastError();
+    }
     const dim3 grid(capped(m.chunks * slabs, 1 << 23));
     auto go = [&](auto kernel, int threads) {
         hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, m, slabs);
@@ -537,10 +657,8 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
     else if (dy_bf16) go(k_embed_chunks<true, false>, 64);
     else if (table_bf16) go(k_embed_chunks<false, true>, 64);
     else go(k_embed_chunks<false, false>, 64);
-    if (m.chunks > 1) {
-        if (table_bf16) go(k_embed_spans<true>, 256);
-        else go(k_embed_spans<false>, 256);
-    }
+    if (table_bf16) go(k_embed_spans<true>, 256);
+    else go(k_embed_spans<false>, 256);
     return hipGetLastError();
 }
 

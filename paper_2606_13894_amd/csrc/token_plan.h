@@ -29,6 +29,11 @@ inline SortPlan sort_plan(int64_t most)
     return s;
 }
 
+// Up to kSortRank tokens are sorted by counting, and each token's run is added up by one workgroup: the
+// gradient of 1024 tokens takes 13 us so and 22 by digits and chunks (1000 x 64), 24 and 32 (50257 x
+// 768); of 2048 21 and 22, and where all of them are one token 81 and 24 (1024: 43).
+constexpr int64_t kSortRank = 1024;
+
 // More tokens than kSortFew are sorted by blocks: the gradient of 16384 takes 48 us by one launch a
 // digit and 51 by blocks (128256 x 64), of 65536 114 and 63, of 2^22 7.5 ms and 0.54.
 constexpr int64_t kSortFew = 20480;
@@ -56,7 +61,7 @@ inline EmbedSpace embed_space(int64_t n, int64_t width)
         s.rows[i] = take(4 * n);
     }
     s.counts = take(n > kSortFew ? 4 * (sort_blocks(n) + 1) * (1 << kSortBits) : 0);
-    s.partial = take(8 * embed_chunks(n) * width);
+    s.partial = take(n > kSortRank ? 8 * embed_chunks(n) * width : 0);
     return s;
 }
 

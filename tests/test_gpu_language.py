@@ -103,6 +103,7 @@ def _table_gradient(dy, t, vocab, scale):
     (0, 7, 8), (1, 1, 1), (1, 5000, 64), (31, 3, 5), (32, 1, 8), (33, 1, 9), (64, 511, 512),
     (100, 512, 513), (500, 2, 64), (1000, 513, 100), (1000, 40, 2048), (5000, 1000, 72),
     (777, 50257, 768), (3000, 300_001, 8), (20000, 17, 33), (65_537, 100, 16),
+    (1024, 3, 24), (1025, 3, 24), (1024, 70_000, 520), (900, 1, 600), (2500, 128_256, 40),
     (20_480, 700, 8), (20_481, 700, 8), (24_576, 50257, 24), (70_001, 300_001, 9),
     (300_000, 5, 16), (1_100_000, 3000, 3)])
 def test_embedding_backward(dev, n, vocab, width, dtype, out):
@@ -120,15 +121,20 @@ def test_embedding_backward(dev, n, vocab, width, dtype, out):
     assert torch.equal(again, g)
 
 
-@pytest.mark.parametrize("kind", ["one", "ordered", "turned", "none", "past", "last", "runs"])
-def test_embedding_backward_orders(dev, kind):
-    n, vocab, width = 4100, 3000, 136
+@pytest.mark.parametrize("n", [1000, 4100])
+@pytest.mark.parametrize("kind", ["one", "ordered", "turned", "none", "past", "last", "runs",
+                                  "around 63"])
+def test_embedding_backward_orders(dev, kind, n):
+    vocab, width = 3000, 136
     dy = _randn(dev, n, width, seed=1, dtype=BF16)
     i = torch.arange(n, device=dev)
     t = {"one": torch.full_like(i, 1234), "ordered": i.clamp(max=vocab - 1),
          "turned": (n - 1 - i).clamp(max=vocab - 1), "none": torch.full_like(i, -5),
          "past": torch.full_like(i, vocab), "last": torch.full_like(i, vocab - 1),
-         "runs": (i // 47) * 31 % vocab}[kind]
+         "runs": (i // 47) * 31 % vocab,
+         # runs of 61 to 67 tokens, as long as the 64 keys that a wave sees and a little more
+         "around 63": torch.repeat_interleave(
+             torch.arange(70, device=dev), 61 + torch.arange(70, device=dev) % 7)[:n] * 40}[kind]
     g = gf.embedding_backward(dy, t, vocab)
     want, size, count = _table_gradient(dy, t, vocab, 1.0)
     _within(g, want, (count + 2) * UNIT * size, kind)

@@ -45,7 +45,7 @@ def test_embedding_refusals(lib):
 def test_embedding_backward_refusals(lib):
     n = ctypes.c_int64()
     space = lib.gefen_embedding_backward_workspace
-    assert space(100, 50, 64, n) == 0 and n.value >= 4 * 4 * 100 + 4 * 3 * 64
+    assert space(100, 50, 64, n) == 0 and n.value >= 4 * 4 * 100
     _said(lib, space(100, 50, 64, None), -1, "NULL")
     _said(lib, space(-1, 50, 64, n), -1, "tokens")
     _said(lib, space(100, 0, 64, n), -1, "vocab")

@@ -47,7 +47,7 @@ static void check_embed(int64_t n, int64_t width)
     need(s.counts >= at && s.counts % 16 == 0, "counts", n, width, 0);
     if (n > kSortFew) at = s.counts + 4 * (sort_blocks(n) + 1) * (1 << kSortBits);
     need(s.partial >= at && s.partial % 16 == 0, "partial", n, width, 0);
-    need(s.bytes >= s.partial + 8 * chunks * width, "bytes", n, width, s.bytes);
+    need(s.bytes >= s.partial + (n > kSortRank ? 8 * chunks * width : 0), "bytes", n, width, s.bytes);
 }
 
 static void check_scores(int64_t rows, int64_t vocab, bool bf16, int64_t top)
@@ -124,7 +124,7 @@ int main()
         check_scores(log_int(1, 1 << 20), log_int(1, int64_t(1) << 24), i & 1, i % 33);
         check_head(log_int(1, 1 << 20), log_int(1, 1 << 14), log_int(1, int64_t(1) << 24), i & 1);
     }
-    for (int64_t n : {1, 15, 16, 17, 65535, 65536, 65537}) check_embed(n, 8);
+    for (int64_t n : {1, 15, 16, 17, 1024, 1025, 20480, 20481, 65535, 65536, 65537}) check_embed(n, 8);
     for (int64_t V : {1, 255, 256, 257, 1 << 20, (1 << 20) + 1, 1 << 24})
         for (int64_t T : {1, 256, 257, 1 << 24}) check_head(T, 1, V, true);
     std::printf("ok\n");
