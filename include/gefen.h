@@ -574,9 +574,9 @@ int gefen_token_logprobs_backward(const void* logits, int64_t ld, int32_t dtype,
  * formed tile by tile in float32, not rounded, and never stored.
  *  x  n x width;  weight  vocab x width, bfloat16 (uint16 bit patterns).
  *  workspace  gefen_head_logprobs_workspace(...) bytes: flags as for gefen_gated_ffn_workspace. It
- *          holds the tiles' statistics (backward: the scores' gradients of a range of the vocabulary in
- *          bfloat16, at most 2^30 bytes or 256 columns, and float32 sums of products that are
- *          split), and a copy of matrices whose rows are no multiple of 8 elements long.
+ *          holds the tiles' statistics (backward: the scores' gradients of a range of the vocabulary,
+ *          at most 2^30 bytes or 256 columns, and float32 sums of products that are split or go over
+ *          ranges), and a copy of matrices whose rows are no multiple of 8 elements long.
  * Errors: EINVAL, EHIP. */
 int gefen_head_logprobs_workspace(int64_t tokens, int64_t width, int64_t vocab, int32_t flags,
                                   int64_t* bytes);
@@ -586,7 +586,8 @@ int gefen_head_logprobs(const uint16_t* x, const uint16_t* weight, const void* t
                         int64_t workspace_bytes, void* stream);
 
 /* gefen_head_logprobs_backward -- the scores again, their gradients dz as in
- * gefen_token_logprobs_backward, rounded to bfloat16 for the products that read them, and
+ * gefen_token_logprobs_backward, for the products that read them rounded to bfloat16 (up to 256
+ * tokens as the sum of two such numbers, which holds 16 bits of them), and
  *   dx = dz weight;  dweight = dz^T x
  * with float32 accumulation, each rounded once.
  *  dx  n x width;  dweight  vocab x width. dentropy may be NULL.

@@ -7,13 +7,18 @@
 // rows are few, workgroups that share a row are joined in a fixed order.
 //
 // Best alternatives, by value and among equals by the lower index: a lane also keeps where its
-// largest score first stood. The lanes are 64 groups (of lanes 64 apart), and the k-th largest of the groups' largest scores
-// is reached by k scores at least: only the vectors of lanes that reach it are read again, and
-// the few scores that do are ranked by counting. (They go to a list in LDS; where it does not hold
-// them, the k best are taken one by one.) A score and its place are one 64-bit key, the place
-// inverted, so that no two are equal and no order of arrival counts.
+// largest score first stood. The lanes are 64 groups (of lanes 64 apart), and the k-th largest of the
+// groups' largest scores is reached by k scores at least: only the vectors of lanes that reach it are
+// read again, and the few scores that do are ranked by counting. (They go to a list in LDS; where it
+// does not hold them, the k best are taken one by one.) A score and its place are one 64-bit key, the
+// place inverted, so that no two are equal and no order of arrival counts.
 //
-// Gradients: dz_j = g ([j = token] - p_j) - h p_j (log p_j + H), p_j = exp(z_j - lse), elementwise.
+// Many rows are bound by memory: 2048 of 128256 bfloat16 with 5 alternatives 106 us (525 MB, 5.0 TB/s);
+// 1023 of 50257 float32 38 us (206 MB, 5.5 TB/s). One row is bound by its CU's arithmetic: 128256 with
+// 20 alternatives 15.5 us.
+//
+// Gradients: dz_j = g ([j = token] - p_j) - h p_j (log p_j + H), p_j = exp(z_j - lse), elementwise:
+// 1023 of 50257 float32 68 to 71 us (411 MB, 5.8 to 6.0 TB/s).
 #include "token_internal.h"
 
 #include "token_device.h"
@@ -438,7 +443,8 @@ __global__ __launch_bounds__(256) void k_score_grad(const ScoreGradArgs a, int64
 
 // ---------------------------------------------------------------- output head
 // A workgroup joins R rows, 1024 / R lanes to a row by the slots, U of a lane's on their way at once.
-// R = 1: statistics that lie by rows.
+// R = 1: statistics that lie by rows. 8192 rows of 1002 slots 35 us (99 MB, 2.8 TB/s), one row of 16032
+// slots 6.5.
 template <int R, int U>
 __global__ __launch_bounds__(1024) void k_head_join(const HeadJoinArgs a)
 {

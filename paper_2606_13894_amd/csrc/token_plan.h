@@ -82,8 +82,10 @@ inline ScorePlan score_plan(int64_t rows, int64_t vocab, bool bf16)
     const int64_t vectors = ffn_ceil(vocab, bf16 ? 8 : 4);
     ScorePlan p;
     // Few rows are taken by workgroups of 1024 threads each, and cut into parts only where they are
-    // longer than vocabularies are: one row of 128256 takes 15 us so, and 17 + 8 us by 8 or 31
-    // parts and a second launch that joins them.
+    // longer than vocabularies are. In a graph one row of 128256 takes 12.0 us so, 15.6 with 5
+    // and 16.7 with 20 alternatives; two parts and the second launch that joins them 10.6, 17.7 and
+    // 19.2, eight parts of 256 threads 7.6, 11.9 and 25.1. But a call takes the host 14 us, and the
+    // workspace and second launch 4 more.
     if (rows <= 512) p.threads = kScoreFewThreads;
     const int64_t most = std::min(kScoreMaxParts, ffn_ceil(vectors, kScorePart));
     p.parts = std::max<int64_t>(1, std::min(most, 1024 / std::max<int64_t>(rows, 1)));
@@ -118,11 +120,14 @@ inline int64_t head_slots(int32_t tile, int64_t vocab)
 constexpr int64_t kHeadGradBytes = int64_t(1) << 30;
 
 // Up to this many tokens the scores' gradients are two bfloat16 numbers each, the rounded one and what
-// rounding left of it, and the products that read them take both.
+// rounding left of it, and the products that read them take both: an output then lies 0.0017 of its norm
+// from the formula, as its own rounding alone leaves it, and not 0.0024. The backward pass of 256
+// tokens, bound by the weight's bytes more than by the products, takes 741 us so (128256 x 2048) and that
+// of 257 688; 50257 x 768 158 and 129. At 8192 tokens it would cost two thirds more.
 constexpr int64_t kHeadExactTokens = 256;
 
 // Whether the forward pass takes the few-token kernel, which reads the weight as it lies. Measured, it
-// against the tiles: 1 token, 128256 x 2048, 94 us and 113; 4 tokens 104 and 113, 8 tokens 129
+// (when its join took 10 us, not 6.5) against the tiles: 1 token, 128256 x 2048, 94 us and 113; 4 tokens 104 and 113, 8 tokens 129
 // and 113 (each wave reads all tokens); 4 tokens, 128256 x 1024, 57 and 54; 1 token, 50257 x 768, 26
 // and 23 (a wave's share of a short row is too little). Where the tiles need a copy of the weight: 16
 // tokens, 128256 x 1001, 129 and 157; 50257 x 769, 2 tokens 51 and 53, 8 tokens 72 and 54; 16 tokens,

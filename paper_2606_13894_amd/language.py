@@ -191,7 +191,9 @@ class Dropout(torch.nn.Module):
     """``y = drop(x, residual)`` in training: :func:`dropout` with the next offset each time. The
     buffer ``state`` (seed, next offset) lies on the device, so that a captured training step
     drops other elements in each replay, and a saved state resumes. Modules of one model take
-    different seeds. Evaluation, and p = 0, give x (plus residual)."""
+    different seeds. Evaluation, and p = 0, give x (plus residual). A forward pass must not be run a
+    second time in the place of saved activations (``torch.utils.checkpoint``): it would take the next
+    offset, and drop other elements."""
 
     def __init__(self, p: float = 0.1, seed: int = 0, device=None):
         super().__init__()
