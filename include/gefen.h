@@ -590,7 +590,8 @@ int gefen_head_logprobs(const uint16_t* x, const uint16_t* weight, const void* t
  * tokens as the sum of two such numbers, which holds 16 bits of them), and
  *   dx = dz weight;  dweight = dz^T x
  * with float32 accumulation, each rounded once.
- *  dx  n x width;  dweight  vocab x width. dentropy may be NULL.
+ *  dx  n x width;  dweight  vocab x width; one of them may be NULL: it is not computed.
+ *  dentropy  may be NULL (0).
  * Errors: EINVAL, EHIP. */
 int gefen_head_logprobs_backward(const uint16_t* x, const uint16_t* weight, const void* tokens,
                                  int32_t token_bytes, int64_t n, int64_t width, int64_t vocab,

@@ -320,13 +320,12 @@ int gefen_head_logprobs_backward(const uint16_t* x, const uint16_t* weight, cons
     int rc;
     const int64_t T = n, K = width, V = vocab;
     if ((rc = check_head(T, K, V)) || (rc = check_tokens(T, token_bytes))) return rc;
-    if (!dweight) return fail(GEFEN_EINVAL, "NULL argument");
     hipStream_t stream = as_stream(stream_);
     if (!T) {
-        GEFEN_HIP(launch_zero_bf16(dweight, V * K, stream));
+        if (dweight) GEFEN_HIP(launch_zero_bf16(dweight, V * K, stream));
         return GEFEN_OK;
     }
-    if (!x || !weight || !tokens || !lse || !entropy || !dlogprob || !dx)
+    if (!x || !weight || !tokens || !lse || !entropy || !dlogprob || (!dx && !dweight))
         return fail(GEFEN_EINVAL, "NULL argument");
     const bool copy = K % 8 || !aligned16(x) || !aligned16(weight);
     const HeadSpace s = head_space(T, K, V, true, copy);
@@ -381,7 +380,7 @@ int gefen_head_logprobs_backward(const uint16_t* x, const uint16_t* weight, cons
             gw.b[0] = gw.b[1] = xp;
             gw.segments = s.exact ? 2 : 1;
             gw.ldb = K8;
-            gw.o[0] = dweight + first * K;
+            gw.o[0] = dweight ? dweight + first * K : nullptr;
             gw.ldo = K;
             if (pass == 0) {
                 if ((rc = check_launch(z)) || (rc = check_launch(gx)) || (rc = check_launch(sum)) || (rc = check_launch(gw)))
@@ -389,9 +388,9 @@ int gefen_head_logprobs_backward(const uint16_t* x, const uint16_t* weight, cons
                 continue;
             }
             GEFEN_HIP(launch_ffn_parts(z, stream));
-            GEFEN_HIP(launch_ffn_parts(gx, stream));
-            if (first + C == V) GEFEN_HIP(launch_ffn_join(sum, stream));
-            GEFEN_HIP(launch_ffn_weight_grad(gw, stream));
+            if (dx) GEFEN_HIP(launch_ffn_parts(gx, stream));
+            if (dx && first + C == V) GEFEN_HIP(launch_ffn_join(sum, stream));
+            if (dweight) GEFEN_HIP(launch_ffn_weight_grad(gw, stream));
         }
     }
     return GEFEN_OK;

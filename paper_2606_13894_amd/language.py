@@ -193,7 +193,8 @@ class Dropout(torch.nn.Module):
     drops other elements in each replay, and a saved state resumes. Modules of one model take
     different seeds. Evaluation, and p = 0, give x (plus residual). A forward pass must not be run a
     second time in the place of saved activations (``torch.utils.checkpoint``): it would take the next
-    offset, and drop other elements."""
+    offset, and drop other elements. (Where a wrapper makes the buffers of all ranks those of rank 0,
+    all of them drop the same elements.)"""
 
     def __init__(self, p: float = 0.1, seed: int = 0, device=None):
         super().__init__()
@@ -393,12 +394,15 @@ def head_logprobs(x, weight, tokens, stream=None):
 
 
 def head_logprobs_backward(dlogprob, x, weight, tokens, lse, entropy, dentropy=None,
-                           stream=None):
-    """(dx, dweight) of :func:`head_logprobs`, bfloat16, from the gradients of logprob and entropy.
-    The scores are formed again, for a range of the vocabulary at a time."""
+                           x_grad: bool = True, weight_grad: bool = True, stream=None):
+    """(dx, dweight) of :func:`head_logprobs`, bfloat16, from the gradients of logprob and entropy;
+    None in the place of one that is not asked for. The scores are formed again, for a range of the
+    vocabulary at a time."""
     if stream is not None:
         return ff._on(stream, head_logprobs_backward, dlogprob, x, weight, tokens, lse, entropy,
-                      dentropy)
+                      dentropy, x_grad, weight_grad)
+    if not x_grad and not weight_grad:
+        raise ValueError("neither gradient is asked for")
     wants = ff._tracked(dlogprob, dentropy, x, weight)
     dev, x, weight, tokens, size, n, width, vocab = _head_operands(x, weight, tokens)
     shape = x.shape[:-1]
@@ -406,13 +410,16 @@ def head_logprobs_backward(dlogprob, x, weight, tokens, lse, entropy, dentropy=N
     entropy = ff._operand(entropy, "entropy", dev, torch.float32, shape)
     g, h, gp, hp = _upstream(dlogprob, dentropy, dev, shape)
     lib = ff._library()
-    dx, dw = torch.empty_like(x), torch.empty_like(weight)
+    dx = torch.empty_like(x) if x_grad else None
+    dw = torch.empty_like(weight) if weight_grad else None
     ws, wp, nb = _head_space(lib, x, weight, n, width, vocab, ff._BACKWARD)
     ff._call(lib.gefen_head_logprobs_backward(
         x.data_ptr(), weight.data_ptr(), tokens.data_ptr(), size, n, width, vocab, lse.data_ptr(),
-        entropy.data_ptr(), gp, hp, dx.data_ptr(), dw.data_ptr(), wp, nb, ff._raw_stream(dev)))
+        entropy.data_ptr(), gp, hp, dx.data_ptr() if x_grad else None,
+        dw.data_ptr() if weight_grad else None, wp, nb, ff._raw_stream(dev)))
     if wants:
-        ff._no_graph(ff._BACKWARD_ONLY.format("head_logprobs_backward"), dx, dw)
+        ff._no_graph(ff._BACKWARD_ONLY.format("head_logprobs_backward"),
+                     *(g for g in (dx, dw) if g is not None))
     return dx, dw
 
 
@@ -429,9 +436,10 @@ class _HeadScores(torch.autograd.Function):
         x, weight, tokens, lse, entropy = ctx.saved_tensors
         with torch.no_grad():
             dx, dw = head_logprobs_backward(_of_logprob(dlogprob, lse), x, weight, tokens, lse,
-                                            entropy, dentropy)
+                                            entropy, dentropy, *ctx.needs_input_grad[:2])
         if torch.is_grad_enabled():   # create_graph
-            ff._no_graph("Head has no second derivative", dx, dw)
+            ff._no_graph("Head has no second derivative",
+                         *(g for g in (dx, dw) if g is not None))
         return dx, dw, None
 
 

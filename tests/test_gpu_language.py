@@ -508,6 +508,35 @@ def test_head_logprobs_backward(dev, n, width, vocab):
     assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
 
 
+@pytest.mark.parametrize("n,width,vocab", [(3, 64, 1000), (64, 509, 1003), (300, 72, 700),
+                                           (4500, 64, 140_001)])
+def test_head_backward_of_one_gradient(dev, n, width, vocab):
+    """One gradient without the other has the bits that both have, through the call and where the
+    module's weight, or its input, is frozen."""
+    x = _randn(dev, n, width, seed=1, dtype=BF16)
+    w = _randn(dev, vocab, width, seed=2).mul_(2 * width ** -0.5).to(BF16)
+    t = _randint(dev, -1, vocab, n, seed=3)
+    g, h = _randn(dev, n, seed=4), _randn(dev, n, seed=5)
+    r = gf.head_logprobs(x, w, t)
+    arguments = (g, x, w, t, r.lse, r.entropy, h)
+    dx, dw = gf.head_logprobs_backward(*arguments)
+    a, none = gf.head_logprobs_backward(*arguments, weight_grad=False)
+    assert none is None and torch.equal(a, dx)
+    none, b = gf.head_logprobs_backward(*arguments, x_grad=False)
+    assert none is None and torch.equal(b, dw)
+    with pytest.raises(ValueError, match="neither"):
+        gf.head_logprobs_backward(*arguments, x_grad=False, weight_grad=False)
+    for of_x in (True, False):
+        head = gf.Head(width, vocab, weight=torch.nn.Parameter(w.float(), requires_grad=not of_x))
+        leaf = x.clone().requires_grad_(of_x)
+        logprob, entropy = head(leaf, t)
+        torch.autograd.backward((logprob, entropy), (g, h))
+        if of_x:
+            assert torch.equal(leaf.grad, dx) and head.weight.grad is None
+        else:
+            assert torch.equal(head.weight.grad, dw.float()) and leaf.grad is None
+
+
 @pytest.mark.parametrize("n,width,vocab", [(4500, 64, 140_001), (40_000, 40, 30_000)])
 def test_head_backward_by_ranges(dev, n, width, vocab):
     """More gradients of scores than are held at once: ranges of the vocabulary, dx summed over

@@ -146,5 +146,7 @@ def test_head_refusals(lib):
                                                 ws, nb, None)
     _said(lib, back(tb=0), -1, "token_bytes")
     _said(lib, back(nb=back_bytes - 1), -1, "workspace")
-    for name in ("x", "w", "t", "l", "e", "g", "dx", "dw"):
+    for name in ("x", "w", "t", "l", "e", "g"):
         _said(lib, back(**{name: None}), -1, "NULL")
+    _said(lib, back(dx=None, dw=None), -1, "NULL")
+    assert back(rows=0, x=None, dx=None, dw=None) == 0
