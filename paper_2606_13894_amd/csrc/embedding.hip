@@ -10,9 +10,9 @@
 // of its part, and a second launch adds such parts in order: a token that stands often, as some
 // always do, is shared by as many waves as it fills chunks. Most rows of a table are asked for by no
 // token: the whole table is set to zero by workgroups beside those of the sort, which wait for
-// memory most of their time. Bound by those zeros: of 8192 tokens, 128256 x 2048 bfloat16, the two
-// launches of the sort take 53 + 50 us with 263 MB of zeros each (5.1 TB/s), the chunks 13, the ends of
-// chunks 8.
+// memory most of their time, and what of a long table these have no time for by a launch of its own.
+// Bound by those zeros: of 8192 tokens, 128256 x 2048 bfloat16, the two launches of the sort take 15 and
+// 11 us with 42 MB of zeros each, the other 441 MB 66 (6.6 TB/s), the chunks 13 and the ends of chunks 8.
 //
 // Sort: by digits of up to nine bits from the lowest, no workgroup waiting for another. Up to
 // kSortFew tokens one launch a digit: a workgroup for each of its values reads all the tokens, counts
@@ -22,7 +22,7 @@
 //
 // Up to kSortRank tokens two launches do it all: each token's place is the number of those before it,
 // counted one by one, and a workgroup for each token that is the first of its run adds the run up. 1023
-// tokens, 50257 x 768 float32: 32.7 us with the zeros (154 MB, 4.7 TB/s) and 5.2.
+// tokens, 50257 x 768 float32: 13 us with 42 MB of zeros, 18 for the other 112, and 5.
 #include "token_internal.h"
 
 #include "token_device.h"
@@ -86,6 +86,13 @@ __device__ __forceinline__ void write_zeros(const Zeros& z, uint32_t group)
     }
     for (; at < z.to; at += 2) *reinterpret_cast<uint16_t*>(z.table + at) = 0;
 }
+
+// The rest of a long table, 16 bytes a thread: 6.8 TB/s, where those beside the sort reach 5.1. So each
+// launch of the sort takes as much as it has time for: a gradient of 128256 x 2048 bfloat16 takes 124.8 us
+// with all zeros beside the sort of 8192 tokens, 115.9 with 10 MiB at each launch, 113.7 with 40 and
+// 116.1 with 80. (Two vectors a thread 122.4.) Twice that much is left to them before a launch more pays.
+constexpr int64_t kZerosBeside = int64_t(40) << 20;
+__global__ __launch_bounds__(256) void k_zeros(const Zeros z) { write_zeros<256>(z, blockIdx.x); }
 
 // ---------------------------------------------------------------- sort
 struct SortPass {
@@ -574,19 +581,20 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
 {
     const SortPlan plan = sort_plan(a.vocab);
     const int64_t bytes = a.vocab * a.width * (table_bf16 ? 2 : 4);
-    // The zeros are shared by the sort's launches. One workgroup on each CU writes them, so that the
-    // sort's have the other half of it.
+    // The zeros are shared by the sort's launches, as far as these have time. One workgroup on each CU
+    // writes them, so that the sort's have the other half of it.
     const bool rank = a.n <= kSortRank;
     const int passes = rank ? 1 : plan.passes;
     const bool blocks = a.n > kSortFew;
     const int shares = blocks ? 2 * passes : passes;
+    const int64_t beside = bytes > 2 * shares * kZerosBeside ? shares * kZerosBeside : bytes;
     int out = 0, share = 0;
     auto zeros = [&]() {
         Zeros z;
         z.table = static_cast<char*>(a.dtable);
-        z.from = bytes * share / shares / 16 * 16;
+        z.from = beside * share / shares / 16 * 16;
         ++share;
-        z.to = share < shares ? bytes * share / shares / 16 * 16 : bytes;
+        z.to = share < shares ? beside * share / shares / 16 * 16 : beside;
         z.groups = capped((z.to - z.from + 16 * kSortThreads - 1) / (16 * kSortThreads), 256);
         return z;
     };
@@ -628,6 +636,11 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, bool dy_bf16, bool tabl
         hipLaunchKernelGGL(k_sort_scan, dim3(s.digits), dim3(256), 0, stream, s);
         s.zeros = zeros();
         hipLaunchKernelGGL(k_sort_place, grid(), dim3(kSortThreads), 0, stream, s);
+    }
+    if (beside < bytes) {
+        Zeros z{static_cast<char*>(a.dtable), beside, bytes, 0};
+        z.groups = capped((bytes - beside + 16 * 256 - 1) / (16 * 256), 1 << 23);
+        hipLaunchKernelGGL(k_zeros, dim3(z.groups), dim3(256), 0, stream, z);
     }
     if (a.n == 0) return hipGetLastError();
     EmbedSum m{};

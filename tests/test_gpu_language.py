@@ -140,6 +140,28 @@ def test_embedding_backward_orders(dev, kind, n):
     _within(g, want, (count + 2) * UNIT * size, kind)
 
 
+@pytest.mark.parametrize("n,vocab,width,out", [
+    (0, 50_000, 1001, "f32"), (5, 50_000, 1001, "f32"), (1024, 160_001, 517, "bf16"),
+    (2000, 160_001, 1037, "bf16"), (21_000, 200_000, 1201, "bf16")])
+def test_embedding_backward_of_a_table_with_zeros_apart(dev, n, vocab, width, out):
+    """Tables whose zeros take a launch beside the sort's: every row that no token asks for is 0
+    whatever was there, also in the last rows and bytes."""
+    dtype = DTYPES[out]
+    was = torch.full((vocab, width), float("nan"), dtype=dtype, device=dev)
+    del was                                       # the memory that the gradient gets
+    dy = _randn(dev, n, width, seed=1, dtype=BF16)
+    t = _randint(dev, 0, vocab, n, seed=2)
+    if n > 3:
+        t[1], t[2], t[3] = vocab - 1, 0, vocab - 1
+    g = gf.embedding_backward(dy, t, vocab, dtype=dtype)
+    used, at = torch.unique(t, return_inverse=True)
+    want, size, count = _table_gradient(dy, at, len(used), 1.0)
+    _within(g[used], want, (count + 1) * UNIT * size + HALF[dtype] * (want.abs() + UNIT * size),
+            "dtable")
+    g[used] = 0
+    assert not g.any()
+
+
 def test_embedding_backward_sums_in_order(dev):
     """Few rows of a token are added one by one in increasing position, whatever stands between."""
     dy = _randn(dev, 300, 40, seed=1)
