@@ -127,15 +127,18 @@ constexpr int64_t kHeadGradBytes = int64_t(1) << 30;
 constexpr int64_t kHeadExactTokens = 256;
 
 // Whether the forward pass takes the few-token kernel, which reads the weight as it lies. Measured, it
-// (when its join took 10 us, not 6.5) against the tiles: 1 token, 128256 x 2048, 94 us and 113; 4 tokens 104 and 113, 8 tokens 129
-// and 113 (each wave reads all tokens); 4 tokens, 128256 x 1024, 57 and 54; 1 token, 50257 x 768, 26
-// and 23 (a wave's share of a short row is too little). Where the tiles need a copy of the weight: 16
-// tokens, 128256 x 1001, 129 and 157; 50257 x 769, 2 tokens 51 and 53, 8 tokens 72 and 54; 16 tokens,
-// 1003 x 509, 19 and 22.
+// against the tiles, in a graph and on weights that change from call to call (each wave reads all tokens,
+// so that more of them take longer): 1 token, 128256 x 2048 92 us and 110; 2 tokens, 50257 x 1280 29 and
+// 32, 128256 x 1024 50 and 54, 50257 x 768 25 and 23 (a wave's share of a short row is too little); 4
+// tokens, 128256 x 2048 102 and 109, 200064 x 1536 123 and 119; 8 tokens, 16384 x 8192 70 and 79, 32000 x
+// 4096 69 and 62. Where the tiles need a copy of the weight: 2 tokens, 128256 x 401 61 and 68, 200000 x
+// 201 82 and 62; 4 tokens, 50257 x 769 57 and 53; 16 tokens, 128256 x 1001 137 and 156, 1003 x 509 11 and
+// 15.
 inline bool head_few(int64_t T, int64_t K, int64_t V, bool copy)
 {
-    if (!copy) return T <= 4 && K >= 1024;
-    return T <= 2 || (T <= kFfnFewTokens && (K >= 896 || V * K < (1 << 24)));
+    if (!copy) return T <= 8 && K >= (T <= 2 ? 1024 : T <= 4 ? 2048 : 8192);
+    if (T <= 2 && K >= 256) return true;
+    return T <= kFfnFewTokens && (K >= 896 || V * K < (1 << 24));
 }
 
 struct HeadSpace {

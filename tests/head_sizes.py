@@ -11,5 +11,5 @@ SIZES = [
     (103, 1197, 20836), (184, 3584, 5424), (970, 4342, 1661), (11, 2297, 2), (9, 1551, 5),
     (1875, 4518, 1), (3841, 1586, 2), (5069, 1419, 67), (88, 1728, 3484), (3386, 4424, 66),
     (68, 3808, 16042), (278, 4005, 10569), (6388, 760, 4068), (5077, 784, 7845),
-    (4, 1024, 9001), (3, 8, 1_100_000),
+    (4, 1024, 9001), (3, 8, 1_100_000), (8, 8192, 777), (4, 2048, 5001),
 ]
