@@ -132,7 +132,7 @@ struct FfnTokens {
     HeadRows head;               // launch_head_tokens alone, which writes no o
 };
 hipError_t launch_ffn_tokens(const FfnTokens& g, hipStream_t stream);
-hipError_t launch_head_tokens(const FfnTokens& g, hipStream_t stream);
+hipError_t launch_head_tokens(const FfnTokens& g, int groups, hipStream_t stream);
 
 struct FfnPad {
     const uint16_t* src;

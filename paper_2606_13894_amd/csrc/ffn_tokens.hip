@@ -124,49 +124,60 @@ __global__ __launch_bounds__(64 * W) void k_ffn_tokens(const FfnTokens g)
 // and 6.5 for the join of 16032 workgroups' statistics, which one workgroup reads at the rate of its CU
 // alone. More rows to a workgroup leave less to join and cost more: three times R one after the other
 // 90 us, two or four groups of waves with R each 98 and 110.
-template <int R, int W>
-__global__ __launch_bounds__(64 * W) void k_head_tokens(const FfnTokens g)
+//
+// Short rows: G groups of R, of W = 1 wave each, which has no one to wait for, and one slot for them all.
+// Four waves to R rows are bound by the dispatch of so many workgroups there (16032 take 47 us): one token,
+// 128256 x 256 23 us in all, and 47 so; 200000 x 768 58 (5.4 TB/s) and 74.
+template <int R, int W, int G>
+__global__ __launch_bounds__(64 * W * G) void k_head_tokens(const FfnTokens g)
 {
-    __shared__ f32x4 sums[W][1][64];
+    static_assert(W == 1 || G == 1, "groups are of one wave");
+    __shared__ f32x4 sums[G][W][1][64];
+    __shared__ ScoreSum stats[G][R];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = G > 1 ? wave : 0, in = G > 1 ? 0 : wave;
     const int q = lane >> 4, token = (lane & 15) % R;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * R;
+    const int64_t n0 = (static_cast<int64_t>(blockIdx.x) * G + group) * R;
     f32x4 acc[1];
-    sum_rows<1, R, W>(g, n0, wave, lane, acc);
-    sums[wave][0][lane] = acc[0];
+    sum_rows<1, R, W>(g, n0, in, lane, acc);
+    sums[group][in][0][lane] = acc[0];
     __syncthreads();
-    if (threadIdx.x >= 64) return;
-    const bool on = holds_sums<R>(g, lane);
-    const f32x4 v = all_waves<R, W, 1>(sums, 0, lane);
-    float z[4], m = -INFINITY;
+    if (in == 0) {
+        const bool on = holds_sums<R>(g, lane);
+        const f32x4 v = all_waves<R, W, 1>(sums[group], 0, lane);
+        float z[4], m = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        z[i] = on && n0 + 4 * q + i < g.N ? v[i] : -INFINITY;
-        m = fmaxf(m, z[i]);
+        for (int i = 0; i < 4; ++i) {
+            z[i] = on && n0 + 4 * q + i < g.N ? v[i] : -INFINITY;
+            m = fmaxf(m, z[i]);
+        }
+        // a token's four lanes (two, with R = 8) join; the others hold -inf
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const ScoreBase base = score_base(m);
+        float s = 0.0f, t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) score_add(z[i], base, s, t);
+        s += __shfl_xor(s, 16);
+        t += __shfl_xor(t, 16);
+        s += __shfl_xor(s, 32);
+        t += __shfl_xor(t, 32);
+        if (on && q == 0) stats[group][token] = ScoreSum{m, s, t};
+        const int64_t at = token_at(g.head.tokens, g.head.wide, on ? token : 0) - n0 - 4 * q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (on && at == i && n0 + 4 * q + i < g.N) g.head.taken[token] = v[i];
     }
-    // a token's four lanes (two, with R = 8) join; the others hold -inf
-    m = fmaxf(m, __shfl_xor(m, 16));
-    m = fmaxf(m, __shfl_xor(m, 32));
-    const ScoreBase base = score_base(m);
-    float s = 0.0f, t = 0.0f;
+    if (G > 1) __syncthreads();
+    if (threadIdx.x >= g.tokens) return;
+    ScoreSum c = stats[0][threadIdx.x];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) score_add(z[i], base, s, t);
-    s += __shfl_xor(s, 16);
-    t += __shfl_xor(t, 16);
-    s += __shfl_xor(s, 32);
-    t += __shfl_xor(t, 32);
-    if (!on) return;
-    if (q == 0) {
-        float* __restrict__ o = g.head.stats + (int64_t(token) * 3 * gridDim.x + blockIdx.x);
-        o[0] = m;
-        o[gridDim.x] = s;
-        o[2 * int64_t(gridDim.x)] = t;
-    }
-    const int64_t at = token_at(g.head.tokens, g.head.wide, token) - n0 - 4 * q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (at == i && n0 + 4 * q + i < g.N) g.head.taken[token] = v[i];
+    for (int i = 1; i < G; ++i) c = score_join(c, stats[i][threadIdx.x]);
+    float* __restrict__ o = g.head.stats + (int64_t(threadIdx.x) * 3 * gridDim.x + blockIdx.x);
+    o[0] = c.m;
+    o[gridDim.x] = c.s;
+    o[2 * int64_t(gridDim.x)] = c.t;
 }
 
 template <bool DUAL, int R>
@@ -184,16 +195,20 @@ hipError_t launch_waves(const FfnTokens& g, hipStream_t stream)
 }
 
 template <int R>
-hipError_t launch_head(const FfnTokens& g, hipStream_t stream)
+hipError_t launch_head(const FfnTokens& g, int groups, hipStream_t stream)
 {
     const int waves = ffn_token_waves(g.N, g.K, R);
-    const dim3 grid(static_cast<unsigned>(ffn_ceil(g.N, R)));
-    if (waves == 4)
-        hipLaunchKernelGGL((k_head_tokens<R, 4>), grid, dim3(256), 0, stream, g);
+    const dim3 grid(static_cast<unsigned>(ffn_ceil(g.N, R * groups)));
+    if (groups == 4)
+        hipLaunchKernelGGL((k_head_tokens<R, 1, 4>), grid, dim3(256), 0, stream, g);
+    else if (groups != 1)
+        return hipErrorInvalidValue;
+    else if (waves == 4)
+        hipLaunchKernelGGL((k_head_tokens<R, 4, 1>), grid, dim3(256), 0, stream, g);
     else if (waves == 8)
-        hipLaunchKernelGGL((k_head_tokens<R, 8>), grid, dim3(512), 0, stream, g);
+        hipLaunchKernelGGL((k_head_tokens<R, 8, 1>), grid, dim3(512), 0, stream, g);
     else
-        hipLaunchKernelGGL((k_head_tokens<R, 16>), grid, dim3(1024), 0, stream, g);
+        hipLaunchKernelGGL((k_head_tokens<R, 16, 1>), grid, dim3(1024), 0, stream, g);
     return hipGetLastError();
 }
 
@@ -207,10 +222,11 @@ hipError_t launch_ffn_tokens(const FfnTokens& g, hipStream_t stream)
     return g.w[1] ? launch_waves<true, 16>(g, stream) : launch_waves<false, 16>(g, stream);
 }
 
-hipError_t launch_head_tokens(const FfnTokens& g, hipStream_t stream)
+hipError_t launch_head_tokens(const FfnTokens& g, int groups, hipStream_t stream)
 {
     if (g.tokens < 1 || g.tokens > kFfnFewTokens) return hipErrorInvalidValue;
-    return ffn_token_rows(g.tokens) == 8 ? launch_head<8>(g, stream) : launch_head<16>(g, stream);
+    return ffn_token_rows(g.tokens) == 8 ? launch_head<8>(g, groups, stream)
+                                         : launch_head<16>(g, groups, stream);
 }
 
 }  // namespace gefen

@@ -294,7 +294,7 @@ int gefen_head_logprobs(const uint16_t* x, const uint16_t* weight, const void* t
         t.N = V;
         t.K = K;
         t.head = rows;
-        GEFEN_HIP(launch_head_tokens(t, stream));
+        GEFEN_HIP(launch_head_tokens(t, head_groups(K, V), stream));
         GEFEN_HIP(launch_head_join(j, stream));
         return GEFEN_OK;
     }

@@ -129,17 +129,24 @@ constexpr int64_t kHeadExactTokens = 256;
 // Whether the forward pass takes the few-token kernel, which reads the weight as it lies. Measured, it
 // against the tiles, in a graph and on weights that change from call to call (each wave reads all tokens,
 // so that more of them take longer): 1 token, 128256 x 2048 92 us and 110; 2 tokens, 50257 x 1280 29 and
-// 32, 128256 x 1024 50 and 54, 50257 x 768 25 and 23 (a wave's share of a short row is too little); 4
-// tokens, 128256 x 2048 102 and 109, 200064 x 1536 123 and 119; 8 tokens, 16384 x 8192 70 and 79, 32000 x
-// 4096 69 and 62. Where the tiles need a copy of the weight: 2 tokens, 128256 x 401 61 and 68, 200000 x
-// 201 82 and 62; 4 tokens, 50257 x 769 57 and 53; 16 tokens, 128256 x 1001 137 and 156, 1003 x 509 11 and
-// 15.
+// 32; 4 tokens, 128256 x 2048 102 and 109, 200064 x 1536 123 and 119; 8 tokens, 16384 x 8192 70 and 79,
+// 32000 x 4096 69 and 62. With groups, below: 1 token, 200000 x 768 58 and 65, 50257 x 768 23 and 23.
+// Where the tiles need a copy of the weight: 1 token, 128256 x 401 41 and 68, 50257 x 769 47 and 53; 4
+// tokens, 128256 x 1601 249 and 250; 8 tokens, 128256 x 1601 320 and 252; 16 tokens, 128256 x 1001 137 and
+// 156, 128256 x 401 61 and 69, 1003 x 509 11 and 15. Rows that begin near a multiple of 512 bytes apart are
+// slower than others: 8 tokens, 50257 x 513 54 and 41, 50257 x 601 40 and 45.
 inline bool head_few(int64_t T, int64_t K, int64_t V, bool copy)
 {
-    if (!copy) return T <= 8 && K >= (T <= 2 ? 1024 : T <= 4 ? 2048 : 8192);
-    if (T <= 2 && K >= 256) return true;
-    return T <= kFfnFewTokens && (K >= 896 || V * K < (1 << 24));
+    if (!copy && K < 1024) return T <= 2 && V >= 65536;
+    if (!copy) return T <= (K < 2048 ? 2 : K < 8192 ? 4 : 8);
+    if (T <= 2 || V * K < (1 << 24)) return T <= kFfnFewTokens;
+    return T <= (K < 1024 ? kFfnFewTokens : 4) && (2 * K + 16) % 512 >= 32;
 }
+
+// Groups of rows, of a wave each, to a workgroup of that kernel, where four waves to a group of rows are
+// too little work: 1 token, 200000 x 768 58 us and 74, 128256 x 401 41 and 59, 128256 x 1024 50 and 51, x
+// 1280 63 and 59; 1003 x 509, which has too few of them, 10.9 and 10.4.
+inline int head_groups(int64_t K, int64_t V) { return K < 1024 && V >= 16384 ? 4 : 1; }
 
 struct HeadSpace {
     int64_t x = -1, w = -1;            // padded copies
@@ -166,7 +173,7 @@ inline HeadSpace head_space(int64_t T, int64_t K, int64_t V, bool backward, bool
     };
     const int64_t K8 = ffn_up8(K);
     if (!backward && head_few(T, K, V, copy)) {   // a slot for each workgroup of the few-token kernel
-        s.slots = ffn_ceil(V, ffn_token_rows(T));
+        s.slots = ffn_ceil(V, ffn_token_rows(T) * head_groups(K, V));
         s.stats = take(12 * T * s.slots);
         s.taken = take(4 * T);
         return s;

@@ -1,5 +1,5 @@
 // What the plan makes of the output head's sizes given as arguments (tokens width vocabulary ...): one
-// line per product, "kind tile splits stages", "few rows waves" where the few-token kernel scores
+// line per product, "kind tile splits stages", "few rows waves" (of a group of rows) where the few-token kernel scores
 // them, and "ranges n" for the ranges of the backward pass.
 #include "token_plan.h"
 
@@ -22,7 +22,8 @@ int main(int argc, char** argv)
         const HeadSpace b = head_space(T, K, V, true, copy);
         if (head_few(T, K, V, copy)) {
             const int rows = ffn_token_rows(T);
-            std::printf("few %d %d\n", rows, ffn_token_waves(V, K, rows));
+            std::printf("few %d %d\n", rows,
+                        head_groups(K, V) > 1 ? 1 : ffn_token_waves(V, K, rows));
         } else {
             tile("scores", head_space(T, K, V, false, copy).score);
         }

@@ -38,5 +38,5 @@ def test_products_are_covered(seen):
 
 def test_few_tokens_and_ranges_are_covered(seen):
     few = {(int(v[1]), int(v[2])) for v in seen if v[0] == "few"}
-    assert few == {(rows, waves) for rows in (8, 16) for waves in (4, 8, 16)}
+    assert few == {(rows, waves) for rows in (8, 16) for waves in (1, 4, 8, 16)}
     assert {min(int(v[1]), 2) for v in seen if v[0] == "ranges"} == {1, 2}

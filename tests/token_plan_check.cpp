@@ -81,6 +81,9 @@ static void check_head(int64_t T, int64_t K, int64_t V, bool copy)
     if (!few) {
         need(copy == (f.x >= 0) && copy == (f.w >= 0), "copies", T, K, V);
         need(f.slots == head_slots(f.score.tile, V) && f.score.splits == 1, "slots", T, K, V);
+    } else {
+        const int64_t rows = ffn_token_rows(T) * head_groups(K, V);
+        need(f.slots * rows >= V && (f.slots - 1) * rows < V, "slots", T, K, V);
     }
     take(f.x, 2 * T * K8);
     take(f.w, 2 * V * K8);
