@@ -82,10 +82,10 @@ inline ScorePlan score_plan(int64_t rows, int64_t vocab, bool bf16)
     const int64_t vectors = ffn_ceil(vocab, bf16 ? 8 : 4);
     ScorePlan p;
     // Few rows are taken by workgroups of 1024 threads each, and cut into parts only where they are
-    // longer than vocabularies are. In a graph one row of 128256 takes 12.0 us so, 15.6 with 5
-    // and 16.7 with 20 alternatives; two parts and the second launch that joins them 10.6, 17.7 and
-    // 19.2, eight parts of 256 threads 7.6, 11.9 and 25.1. But a call takes the host 14 us, and the
-    // workspace and second launch 4 more.
+    // longer than vocabularies are. In a graph one row of 128256 takes 12.0 us so, 15.8 with 5
+    // and 16.4 with 20 alternatives; two parts and the second launch that joins them 10.6, 14.5 and
+    // 16.3, eight parts of 256 threads 7.6, 11.9 and 15.3. But a call takes the host 11 to 14 us, and
+    // the workspace and second launch 4 more.
     if (rows <= 512) p.threads = kScoreFewThreads;
     const int64_t most = std::min(kScoreMaxParts, ffn_ceil(vectors, kScorePart));
     p.parts = std::max<int64_t>(1, std::min(most, 1024 / std::max<int64_t>(rows, 1)));
