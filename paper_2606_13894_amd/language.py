@@ -16,6 +16,10 @@ device tensors; one below 0 stands for none (padding, a position without a loss)
 vocabulary's size on makes NaN of what it asks for. As in ``feed_forward.py`` tensors may have any
 leading dimensions, calls are asynchronous on ``stream`` (the current torch stream by default), and
 where an argument of a plain call wants a gradient, a gradient through its results is an error.
+
+Calls and modules can be captured into graphs, backward passes too (``torch.autograd.grad``, or
+``backward`` after a warm-up on a side stream). As with any module, no eager result that still holds
+its autograd graph over the same parameters may be kept while a backward pass is captured.
 """
 from __future__ import annotations
 
