@@ -774,6 +774,43 @@ def test_captured_training_step(dev):
             assert torch.equal(a, b), k
 
 
+def test_captured_accumulation(dev):
+    """The same with ``backward``, which adds to the parameters' gradients: two passes in a graph."""
+    torch.manual_seed(0)
+    vocab, width, n = 300, 64, 50
+    emb = gf.Embedding(vocab, width, device=dev)
+    drop = gf.Dropout(0.2, seed=5, device=dev)
+    head = gf.Head(width, vocab, weight=emb.table, device=dev)
+    t, nxt = _randint(dev, -1, vocab, n, seed=1), _randint(dev, -1, vocab, n, seed=2)
+
+    def step():
+        emb.table.grad = None
+        for _ in range(2):
+            (-head(drop(emb(t)), nxt)[0].mean()).backward()
+
+    side = torch.cuda.Stream(dev)
+    side.wait_stream(torch.cuda.current_stream(dev))
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            step()
+    torch.cuda.current_stream(dev).wait_stream(side)
+    torch.cuda.synchronize()
+    emb.table.grad = None
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    captured = emb.table.grad
+    for k in range(3):
+        t.copy_(_randint(dev, -1, vocab, n, seed=10 + k))
+        at = drop.state.clone()
+        graph.replay()
+        got = captured.clone()
+        drop.state.copy_(at)
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, emb.table.grad), k
+
+
 def test_two_graphs_of_calls(dev):
     """Two captured graphs of the plain calls with workspaces from one pool, replayed in turns."""
     w = _randn(dev, 3000, 256, seed=1).to(BF16)
