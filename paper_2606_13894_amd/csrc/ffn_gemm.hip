@@ -814,7 +814,7 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
             m = fmaxf(m, __shfl_xor(m, 32));
             const ScoreBase base = score_base(m);
             float s = 0.0f, t = 0.0f;
-            if (__all(!base.huge && low > -kScoreHuge)) {
+            if (__all(!base.far && low > kScoreLow)) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll

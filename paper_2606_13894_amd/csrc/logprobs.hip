@@ -312,7 +312,7 @@ __global__ __launch_bounds__(L) void k_scores(const ScoreArgs a)
             c.m = fmaxf(old, m);
             const ScoreBase base = score_base(c.m);
             score_rebase(old, base, c.s, c.t);
-            if (__all(!base.huge && low > -kScoreHuge)) {
+            if (__all(!base.far && low > kScoreLow)) {
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll

@@ -33,29 +33,31 @@ __device__ __forceinline__ int by_lane(int n)
 // Over a set of scores z with m the largest: s = sum 2^d and t = sum d 2^d, d = z log2 e - B, where
 // the base B is m log2 e as rounded to float32. One multiply-add forms d from the exact product; that
 // B is rounded does not matter, since whatever is made of s and t takes the same B.
-// From 2^126 on in magnitude, where z log2 e may overflow, d = (z - m) log2 e instead. Where no score
+// From |m| = 2^20 on d = (z - m) log2 e instead, whose base is m log2 e itself: below, B is off by 1/16 at
+// most; with m it would grow until 2^d overflows, or is 0, for every score (from 2^31 on). Where no score
 // is above -inf, B is 0: no difference of infinities is formed and each term is 0. In t, d is held at
 // -1e4, far below where 2^d is 0, so that -inf adds 0. A NaN or +inf among the scores makes s NaN
 // (inf - inf), and nothing that follows takes that away.
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kScoreHuge = 8.507059173023462e37f;   // 2^126
+constexpr float kScoreFar = 1048576.0f;               // 2^20
+constexpr float kScoreLow = -8.507059173023462e37f;   // -2^126: above it z log2 e does not overflow
 
 struct ScoreBase {
     float m, b;
-    bool huge;
+    bool far;
 };
 __device__ __forceinline__ ScoreBase score_base(float m)
 {
     ScoreBase r;
     r.m = m == -INFINITY ? 0.0f : m;
     r.b = r.m * kLog2E;
-    r.huge = fabsf(r.m) >= kScoreHuge;
+    r.far = fabsf(r.m) >= kScoreFar;
     return r;
 }
 __device__ __forceinline__ float score_far(float z, const ScoreBase& r)
 {
-    return r.huge ? (z - r.m) * kLog2E : fmaf(z, kLog2E, -r.b);
+    return r.far ? (z - r.m) * kLog2E : fmaf(z, kLog2E, -r.b);
 }
 
 // One score, whatever it and the base are.
@@ -66,7 +68,7 @@ __device__ __forceinline__ void score_add(float z, const ScoreBase& r, float& s,
     s += e;
     t = fmaf(e, fmaxf(d, -1e4f), t);
 }
-// One whose base is not huge, above -2^126.
+// One above kScoreLow, whose base is not far.
 __device__ __forceinline__ void score_add_plain(float z, float b, float& s, float& t)
 {
     const float d = fmaf(z, kLog2E, -b);
@@ -83,7 +85,11 @@ struct ScoreSum {
 __device__ __forceinline__ void score_rebase(float old, const ScoreBase& to, float& s, float& t)
 {
     const ScoreBase from = score_base(old);
-    const float gap = to.huge || from.huge ? (from.m - to.m) * kLog2E : from.b - to.b;
+    float gap = from.b - to.b;              // of the bases themselves, whichever kind they are
+    if (__any(from.far || to.far)) {
+        if (from.far) gap = to.far ? (from.m - to.m) * kLog2E : fmaf(from.m, kLog2E, -to.b);
+        else if (to.far) gap = -fmaf(to.m, kLog2E, -from.b);
+    }
     const float d = old == -INFINITY ? -1e4f : fmaxf(gap, -1e4f);   // (nothing was summed yet)
     const float e = __builtin_amdgcn_exp2f(d);
     t = e * fmaf(s, d, t);
@@ -124,7 +130,7 @@ __device__ __forceinline__ ScoreRow score_row(const ScoreSum& a, int64_t token, 
     } else {
         const ScoreBase base = score_base(a.m);
         const float l = log2f(a.s);
-        r.lse = fmaf(kLn2, base.huge ? l : l - fmaf(a.m, kLog2E, -base.b), a.m);
+        r.lse = fmaf(kLn2, base.far ? l : l - fmaf(a.m, kLog2E, -base.b), a.m);
         r.entropy = fmaxf(kLn2 * (l - a.t / a.s), 0.0f);
         r.logprob = score_logprob(taken, base, l);
     }

@@ -1,0 +1,85 @@
+"""Scores far from zero, as a finite mask over a whole row leaves them, against float64 formulas.
+
+Bounds are those of ``test_gpu_language.py``: they grow with a score's distance d from the row's largest
+one, not with the score itself, but for lse, which is rounded to float32. Where d is far above the sum's
+logarithm, a log probability has up to four roundings of it (the difference, the products with log2 e and
+ln 2, the logarithm's subtraction) and the two constants' own, 0.3 of one in all: 4.3 units of d, of which
+those bounds have 3."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_language import (BF16, DTYPES, F32, F64, UNIT, _check_rows, _randint,  # noqa: F401
+                               _rows64, _within, dev)
+
+pytestmark = pytest.mark.gpu
+
+gf = pytest.importorskip("paper_2606_13894_amd")
+
+LEVELS = [3e4, 1e5, 2.0 ** 20 - 1, 2.0 ** 20, 1.3e6, 1e8, 1e9, 3e9, 1e10, 7e14, 1e20, 1e30, 8e37, 9e37,
+          3e38]
+
+
+def _rows(z, t):
+    want = _rows64(z, t)
+    more = 2 * UNIT * torch.nan_to_num(want["d"].abs(), posinf=0.0)
+    want["b_lp"] = want["b_lp"] + more
+    want["b_logprob"] = want["b_logprob"] + more.gather(1, t.clamp(min=0)[:, None])[:, 0]
+    return want
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab", [(30, 777), (30, 50257), (600, 1003), (60, 300_001)])
+def test_rows_at_one_level(dev, rows, vocab, dtype):  # noqa: F811
+    """A row whose scores are all masked by the same finite number, or lie a few steps of its type
+    around it: what counts is their differences."""
+    dt = DTYPES[dtype]
+    z = torch.empty(rows, vocab, dtype=dt, device=dev)
+    step = _randint(dev, 0, 4, vocab, seed=1)
+    for r in range(rows):
+        v = torch.tensor(LEVELS[r // 2 % len(LEVELS)] * (-1) ** r, dtype=dt)
+        levels = [v]
+        for _ in range(3):                       # the next numbers of the type
+            levels.append(torch.nextafter(levels[-1], torch.zeros_like(v)))
+        z[r] = torch.stack(levels).to(dev)[step] if r % 4 < 2 else v
+    t = _randint(dev, 0, vocab, rows, seed=2)
+    want = _rows(z, t)
+    for top in (0, 4):
+        _check_rows(gf.token_logprobs(z, t, top=top), want, top)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("rows,vocab", [(3, 4000), (700, 4000), (2, 400_000)])
+def test_levels_among_lanes(dev, rows, vocab, sign, dtype):  # noqa: F811
+    """Scores around 2^20, on both sides of which the sums take different forms, so that lanes, waves and
+    parts of a row differ in theirs; and rows whose scores grow or fall along the row."""
+    z = sign * (2.0 ** 20 + torch.randint(-6, 7, (rows, vocab), device=dev,
+                                          generator=torch.Generator(dev).manual_seed(1)).to(F32))
+    z = z.to(DTYPES[dtype])
+    ramp = torch.linspace(-2e6, 2e6, vocab, device=dev).to(DTYPES[dtype])
+    z[0], z[1] = ramp, ramp.flip(0)
+    t = _randint(dev, 0, vocab, rows, seed=2)
+    t[:2] = torch.tensor([vocab - 1, 5], device=dev)
+    _check_rows(gf.token_logprobs(z, t, top=3), _rows(z, t), 3)
+
+
+@pytest.mark.parametrize("n,vocab,width", [(1, 1003, 64), (9, 1003, 64), (16, 999, 61), (64, 1000, 128),
+                                           (1, 70_000, 64), (300, 4097, 256), (1000, 6000, 64)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_head_at_one_level(dev, n, vocab, width, sign):  # noqa: F811
+    """Every score is the same number of about 10^13 (exactly: 1.25 times a power of two times the width), or, in
+    odd rows, 2^-20 of it."""
+    x = torch.full((n, width), sign * 1.25 * 2.0 ** 18, dtype=BF16, device=dev)
+    x[1::2] = sign * 1.25 * 2.0 ** -2
+    w = torch.full((vocab, width), 2.0 ** 19, dtype=BF16, device=dev)
+    t = _randint(dev, 0, vocab, n, seed=1)
+    r = gf.head_logprobs(x, w, t)
+    size = torch.where(torch.arange(n, device=dev) % 2 == 0, 1.25 * 2.0 ** 37, 1.25 * 2.0 ** 17).to(F64)
+    lse = sign * width * size + math.log(vocab)
+    log = torch.full((n,), math.log(vocab), dtype=F64, device=dev)
+    bound = (vocab / 256 + 64 + 16) * UNIT * (1 + log)
+    _within(r.logprob, -log, bound, "logprob")
+    _within(r.entropy, log, bound, "entropy")
+    _within(r.lse, lse, bound + UNIT * lse.abs(), "lse")
