@@ -108,10 +108,14 @@ __device__ __forceinline__ ScoreSum score_join(ScoreSum a, ScoreSum b)
     return r;
 }
 
-// log2 p of a score from the row's sums and log2 s; lse = m + ln 2 (log2 s + (B - m log2 e)).
+// log p of a score from the row's sums and log2 s; lse = m + ln 2 (log2 s + (B - m log2 e)). Of a finite
+// score far below m the product with log2 e overflows (m = 0: from -2.36e38 down, the type's lowest value
+// among them), where log p itself does not.
 __device__ __forceinline__ float score_logprob(float z, const ScoreBase& base, float log2s)
 {
-    return kLn2 * (score_far(z, base) - log2s);
+    const float d = score_far(z, base);
+    if (d == -INFINITY && z > -INFINITY) return fmaf(-kLn2, log2s, z - base.m);
+    return kLn2 * (d - log2s);
 }
 
 // A row's results. `taken`: its token's score.

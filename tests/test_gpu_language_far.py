@@ -83,3 +83,48 @@ def test_head_at_one_level(dev, n, vocab, width, sign):  # noqa: F811
     _within(r.logprob, -log, bound, "logprob")
     _within(r.entropy, log, bound, "entropy")
     _within(r.lse, lse, bound + UNIT * lse.abs(), "lse")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab", [(6, 40), (6, 50257), (700, 1003), (6, 600_001)])
+def test_the_lowest_number_among_others(dev, rows, vocab, dtype):  # noqa: F811
+    """Rows of ordinary scores, some masked by the type's lowest number (or a little less): the log
+    probability of a masked token is z - lse, not -inf, also among the alternatives where fewer scores
+    than these are left. (Rows 2 and 3: among scores of 10^38, below which it may pass the type's range.)"""
+    dt = DTYPES[dtype]
+    low = torch.finfo(dt).min
+    z = torch.randn(rows, vocab, generator=torch.Generator(dev).manual_seed(1), device=dev).to(dt)
+    gone = torch.rand(rows, vocab, generator=torch.Generator(dev).manual_seed(2), device=dev) < 0.5
+    z[gone] = low
+    z[1] = low
+    z[1, :3] = torch.tensor([1.0, -2.0, 0.5], dtype=dt)          # three left
+    z[2] = -2e38
+    z[2, 7] = 1e38
+    z[3] = low
+    z[3, 7] = 3e38
+    z[4] = -2.5e38
+    z[4, ::2] = low
+    z[4, 9] = -1e6
+    t = _randint(dev, 0, vocab, rows, seed=3)
+    t[:6] = torch.tensor([gone[0].nonzero()[0, 0].item(), 20, 8, 8, 10, -1], device=dev)
+    want = _rows(z, t)
+    assert torch.isfinite(want["logprob"][[0, 1, 2, 4]]).all()
+    for top in (0, 6, 32):
+        _check_rows(gf.token_logprobs(z, t, top=top), want, top)
+
+
+@pytest.mark.parametrize("n,vocab,width", [(1, 1003, 64), (9, 1003, 64), (16, 999, 61), (64, 1000, 128),
+                                           (1, 70_000, 64), (300, 4097, 256)])
+def test_head_of_a_score_far_below(dev, n, vocab, width):  # noqa: F811
+    """Every second weight row gives scores of -3 * 2^126 (two terms, exactly), the others 0."""
+    x = torch.zeros(n, width, dtype=BF16, device=dev)
+    x[:, :2] = 2.0 ** 63
+    w = torch.zeros(vocab, width, dtype=BF16, device=dev)
+    w[1::2, :2] = -1.5 * 2.0 ** 63
+    t = torch.ones(n, dtype=torch.int64, device=dev)
+    t[1::2] = 2
+    r = gf.head_logprobs(x, w, t)
+    lse = math.log((vocab + 1) // 2)
+    want = torch.where(t == 1, -3.0 * 2.0 ** 126, 0.0).to(F64) - lse
+    bound = (vocab / 256 + 64 + 16) * UNIT * (1 + lse)
+    _within(r.logprob, want, bound + 2 * UNIT * want.abs(), "logprob")
