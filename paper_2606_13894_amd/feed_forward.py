@@ -428,7 +428,7 @@ class FeedForward(torch.nn.Module):
     kept either (a pass over y forward, and one over its gradient)."""
 
     def __init__(self, width: int, inner: int, activation: str = "silu", eps: float = 1e-6,
-                 device=None, dropout: float = 0.0, seed: int = 0):
+                 device=None, dropout: float = 0.0, seed: Optional[int] = None):
         super().__init__()
         if activation not in ACTIVATIONS:
             raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")

@@ -194,22 +194,41 @@ class _Drop(torch.autograd.Function):
 class Dropout(torch.nn.Module):
     """``y = drop(x, residual)`` in training: :func:`dropout` with the next offset each time. The
     buffer ``state`` (seed, next offset) lies on the device, so that a captured training step
-    drops other elements in each replay, and a saved state resumes. Modules of one model take
-    different seeds. Evaluation, and p = 0, give x (plus residual). A forward pass must not be run a
-    second time in the place of saved activations (``torch.utils.checkpoint``): it would take the next
-    offset, and drop other elements. (Where a wrapper makes the buffers of all ranks those of rank 0,
-    all of them drop the same elements.)"""
+    drops other elements in each replay, and a saved state resumes. Without ``seed`` the first training
+    pass draws one from torch's host generator where the state is new (two zeros), so that the modules of a
+    model drop different elements, and the same ones in each run after ``torch.manual_seed``; copies
+    of a module that has run drop what it drops. Evaluation, and p = 0, give x (plus residual). A
+    forward pass must not be run a second time in the place of saved activations
+    (``torch.utils.checkpoint``): it would take the next offset, and drop other elements. (Where a
+    wrapper makes the buffers of all ranks those of rank 0, all of them drop the same elements.)"""
 
-    def __init__(self, p: float = 0.1, seed: int = 0, device=None):
+    _draw = False       # whether the next training pass draws the seed
+
+    def __init__(self, p: float = 0.1, seed: Optional[int] = None, device=None):
         super().__init__()
         if not 0.0 <= p <= 1.0:
             raise ValueError("p must be in [0, 1]")
         self.p = p
-        self.register_buffer("state", torch.tensor([seed, 0], dtype=torch.int64, device=device))
+        self._draw = self._draws = seed is None
+        self.register_buffer("state", torch.tensor([seed or 0, 0], dtype=torch.int64,
+                                                   device=device))
+
+    def _load_from_state_dict(self, *args):
+        super()._load_from_state_dict(*args)
+        self._draw = self.__dict__.get("_draws", False)
+
+    def _draw_seed(self):
+        # decided on the device: a state that was loaded, or has moved on between replays, stays
+        seed = torch.randint(1, 2 ** 63 - 1, (), device="cpu").item()
+        self.state[:1].masked_fill_((self.state[:1] == 0) & (self.state[1:] == 0), seed)
+        # (what was captured has not run yet)
+        self._draw = self.state.device.type == "cuda" and torch.cuda.is_current_stream_capturing()
 
     def forward(self, x, residual=None):
         if not self.training or self.p == 0.0:
             return x if residual is None else x + residual
+        if self._draw:
+            self._draw_seed()
         state = self.state.clone()
         self.state[1:].add_(1)
         return _Drop.apply(x, residual, self.p, state)
