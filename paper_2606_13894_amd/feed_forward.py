@@ -425,7 +425,8 @@ class FeedForward(torch.nn.Module):
     :func:`rms_norm` and :func:`gated_ffn` itself.
 
     ``dropout``: in training y goes through a :class:`Dropout` of that p and ``seed``, whose mask is not
-    kept either (a pass over y forward, and one over its gradient)."""
+    kept either (a pass over y forward, and one over its gradient), and which cannot be recomputed within
+    a backward pass (``torch.utils.checkpoint``): that is an error."""
 
     def __init__(self, width: int, inner: int, activation: str = "silu", eps: float = 1e-6,
                  device=None, dropout: float = 0.0, seed: Optional[int] = None):

@@ -198,9 +198,10 @@ class Dropout(torch.nn.Module):
     pass draws one from torch's host generator where the state is new (two zeros), so that the modules of a
     model drop different elements, and the same ones in each run after ``torch.manual_seed``; copies
     of a module that has run drop what it drops. Evaluation, and p = 0, give x (plus residual). A
-    forward pass must not be run a second time in the place of saved activations
-    (``torch.utils.checkpoint``): it would take the next offset, and drop other elements. (Where a
-    wrapper makes the buffers of all ranks those of rank 0, all of them drop the same elements.)"""
+    training pass that is run again within a backward pass, in the place of saved activations
+    (``torch.utils.checkpoint``), is an error: it would take the next offset, and drop other elements
+    than the first time. (Where a wrapper makes the buffers of all ranks those of rank 0, all of them drop
+    the same elements.)"""
 
     _draw = False       # whether the next training pass draws the seed
 
@@ -227,6 +228,9 @@ class Dropout(torch.nn.Module):
     def forward(self, x, residual=None):
         if not self.training or self.p == 0.0:
             return x if residual is None else x + residual
+        if torch._C._current_graph_task_id() != -1:
+            raise RuntimeError("Dropout is run again within a backward pass: it would drop other "
+                               "elements than the first time (leave it out of what is recomputed)")
         if self._draw:
             self._draw_seed()
         state = self.state.clone()

@@ -51,3 +51,26 @@ def test_first_pass_in_a_graph(dev):  # noqa: F811
         drop.load_state_dict({"state": torch.tensor([77, 5])})
         graph.replay()
         assert torch.equal(y, gf.dropout(x, 0.25, 77, 5)) and drop.state.tolist() == [77, 6]
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_recomputed_blocks(dev, reentrant):  # noqa: F811
+    """Activations that are computed again: an error with dropout, the same gradients without."""
+    from torch.utils.checkpoint import checkpoint
+    torch.manual_seed(3)
+    block = gf.FeedForward(64, 128, device=dev)
+    x = _randn(dev, 20, 64, seed=1, dtype=BF16).requires_grad_()
+    up = _randn(dev, 20, 64, seed=2, dtype=BF16)
+    inputs = [x, *block.parameters()]
+    for v in inputs:
+        v.grad = None
+    torch.autograd.backward(block(x)[0], up)
+    want = [v.grad.clone() for v in inputs]
+    for v in inputs:
+        v.grad = None
+    torch.autograd.backward(checkpoint(block, x, use_reentrant=reentrant)[0], up)
+    assert all(torch.equal(v.grad, w) for v, w in zip(inputs, want))
+    dropping = gf.FeedForward(64, 128, device=dev, dropout=0.1)
+    y, _ = checkpoint(dropping, x, use_reentrant=reentrant)
+    with pytest.raises(RuntimeError, match="run again within a backward pass"):
+        torch.autograd.backward(y, up)

@@ -73,3 +73,24 @@ def test_evaluation_draws_nothing():
     for drop in (gf.Dropout(0.0), gf.Dropout(0.3).eval()):
         assert drop(x) is x
     assert torch.equal(torch.get_rng_state(), before)
+
+
+@pytest.mark.parametrize("reentrant", [False, True])
+def test_recomputed_passes_are_errors(calls, reentrant):  # noqa: F811
+    """A second forward pass in the backward pass would drop other elements."""
+    from torch.utils.checkpoint import checkpoint
+    drop = _host(gf.Dropout(0.1, seed=3))
+    x = torch.ones(4, dtype=torch.bfloat16).as_subclass(_On0).requires_grad_()
+
+    def block(v):
+        v = drop(v)
+        return v * v
+
+    y = checkpoint(block, x, use_reentrant=reentrant, preserve_rng_state=False)
+    assert drop.state.tolist() == [3, 1]
+    with pytest.raises(RuntimeError, match="run again within a backward pass"):
+        y.sum().backward()
+    assert drop.state.tolist() == [3, 1]
+    drop.eval()
+    checkpoint(block, x, use_reentrant=reentrant, preserve_rng_state=False).sum().backward()
+    assert torch.equal(x.grad, torch.full_like(x, 2.0))
