@@ -446,6 +446,11 @@ class FeedForward(torch.nn.Module):
             from .language import Dropout   # which imports this module
             self.drop = Dropout(dropout, seed, device)
 
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        if "drop" not in self._modules:     # a module that was pickled before it could have one
+            self.__dict__.setdefault("drop", None)
+
     def forward(self, x, residual=None):
         bf16 = torch.bfloat16
         weights = self.w_gate.to(bf16), self.w_up.to(bf16), self.w_down.to(bf16)

@@ -1,5 +1,6 @@
 """``Dropout``'s numbers without a device (the stand-ins of ``test_language_calls_cpu.py``)."""
 import copy
+import pickle
 
 import pytest
 import torch
@@ -94,3 +95,14 @@ def test_recomputed_passes_are_errors(calls, reentrant):  # noqa: F811
     drop.eval()
     checkpoint(block, x, use_reentrant=reentrant, preserve_rng_state=False).sum().backward()
     assert torch.equal(x.grad, torch.full_like(x, 2.0))
+
+
+def test_blocks_pickled_without_dropout():
+    """Whole blocks that were saved before they had dropout load and run; others keep theirs."""
+    block = gf.FeedForward(8, 8)
+    del block.drop
+    assert pickle.loads(pickle.dumps(block)).drop is None
+    assert pickle.loads(pickle.dumps(gf.FeedForward(8, 8))).drop is None
+    assert copy.deepcopy(block).drop is None
+    dropping = pickle.loads(pickle.dumps(gf.FeedForward(8, 8, dropout=0.2, seed=4)))
+    assert dropping.drop.p == 0.2 and dropping.drop.state.tolist() == [4, 0]
