@@ -561,7 +561,10 @@ int gefen_token_logprobs(const void* logits, int64_t ld, int32_t dtype, int64_t 
 /* gefen_token_logprobs_backward -- with g = dlogprob (0 for a token outside the vocabulary) and
  * h = dentropy of a row, and lse and entropy from the forward pass:
  *   dlogits_j = g ([j = token] - p_j) - h p_j (log p_j + entropy)
- * 0 where p_j is 0 and in a row with nothing left.
+ * 0 where p_j is 0 and in a row with nothing left. p_j is exp(logits_j - lse) with lse as it is given: that
+ * it is rounded to float32 moves p_j by up to |lse| 2^-24 of it. (Of a row that a finite number far
+ * from 0 masks throughout, where nothing of log vocab is left in lse, p_j is 1: mask such rows by -inf, or
+ * give them no gradients.)
  *  dentropy  device float[rows], or NULL (0).
  *  dlogits   rows x vocab of dtype, rows ldd elements apart; may be logits itself (ldd = ld).
  * Errors: EINVAL, EDTYPE, EHIP. */
@@ -589,7 +592,8 @@ int gefen_head_logprobs(const uint16_t* x, const uint16_t* weight, const void* t
  * gefen_token_logprobs_backward, for the products that read them rounded to bfloat16 (up to 256
  * tokens as the sum of two such numbers, which holds 16 bits of them), and
  *   dx = dz weight;  dweight = dz^T x
- * with float32 accumulation, each rounded once.
+ * with float32 accumulation, each rounded once. (Where |lse| is large, its rounding and that of the
+ * product with log2 e move p_j by up to |lse| 2^-23 of it.)
  *  dx  n x width;  dweight  vocab x width; one of them may be NULL: it is not computed.
  *  dentropy  may be NULL (0).
  * Errors: EINVAL, EHIP. */

@@ -63,7 +63,7 @@ hipError_t launch_rms_norm_grad(const NormGradArgs& a, bool bf16, hipStream_t st
 enum : int32_t { kActSilu = 0, kActGelu = 1 };
 enum : int32_t { kFfnGateUp = 0, kFfnPlain = 1, kFfnGateGrad = 2, kHeadStats = 3, kHeadGrad = 4 };
 
-// The output head's products: what their epilogues read and write beside the sums (token_internal.h
+// The output head's products: what their epilogues read and write beside the sums (token_device.h
 // gives the formulas).
 struct HeadRows {
     const void* tokens;          // of the rows

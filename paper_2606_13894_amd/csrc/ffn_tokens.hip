@@ -120,8 +120,8 @@ __global__ __launch_bounds__(64 * W) void k_ffn_tokens(const FfnTokens g)
 }
 
 // The output head's scores of a few tokens: each token's statistics over the workgroup's R rows of the
-// weight (ffn_internal.h), [token][3][workgroup]. One token, 128256 x 2048: 82 us (525 MB, 6.4 TB/s),
-// and 6.5 for the join of 16032 workgroups' statistics, which one workgroup reads at the rate of its CU
+// weight (ffn_internal.h), [token][3][workgroup]. One token, 128256 x 2048: 83 us (525 MB, 6.3 TB/s),
+// and 7.8 for the join of 16032 workgroups' statistics, which one workgroup reads at the rate of its CU
 // alone. More rows to a workgroup leave less to join and cost more: three times R one after the other
 // 90 us, two or four groups of waves with R each 98 and 110.
 //

@@ -443,8 +443,8 @@ __global__ __launch_bounds__(256) void k_score_grad(const ScoreGradArgs a, int64
 
 // ---------------------------------------------------------------- output head
 // A workgroup joins R rows, 1024 / R lanes to a row by the slots, U of a lane's on their way at once.
-// R = 1: statistics that lie by rows. 8192 rows of 1002 slots 35 us (99 MB, 2.8 TB/s), one row of 16032
-// slots 6.5.
+// R = 1: statistics that lie by rows. 8192 rows of 1002 slots 36 us (99 MB, 2.8 TB/s), one row of 16032
+// slots 7.8.
 template <int R, int U>
 __global__ __launch_bounds__(1024) void k_head_join(const HeadJoinArgs a)
 {

@@ -82,10 +82,14 @@ inline ScorePlan score_plan(int64_t rows, int64_t vocab, bool bf16)
     const int64_t vectors = ffn_ceil(vocab, bf16 ? 8 : 4);
     ScorePlan p;
     // Few rows are taken by workgroups of 1024 threads each, and cut into parts only where they are
-    // longer than vocabularies are. In a graph one row of 128256 takes 12.0 us so, 15.8 with 5
-    // and 16.4 with 20 alternatives; two parts and the second launch that joins them 10.6, 14.5 and
-    // 16.3, eight parts of 256 threads 7.6, 11.9 and 15.3. But a call takes the host 11 to 14 us, and
-    // the workspace and second launch 4 more.
+    // longer than vocabularies are. Rows of 128256 in a graph, microseconds so, and in eight parts (four of
+    // 128 rows) of 256 threads with the second launch that joins them:
+    //   rows                  1           8           32          128
+    //   no alternatives   12.2  7.5   12.5  8.8   12.7  9.6   14.2 14.6
+    //   5                 15.8 11.8   16.4 13.5   16.6 14.2   18.2 19.3
+    //   20                16.4 15.5   17.1 17.3   17.3 18.1   19.1 23.2
+    // But a plain call, which the host bounds, takes 12 to 19 us so, and 15 to 23 with the workspace and
+    // second launch.
     if (rows <= 512) p.threads = kScoreFewThreads;
     const int64_t most = std::min(kScoreMaxParts, ffn_ceil(vectors, kScorePart));
     p.parts = std::max<int64_t>(1, std::min(most, 1024 / std::max<int64_t>(rows, 1)));

