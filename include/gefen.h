@@ -562,9 +562,9 @@ int gefen_token_logprobs(const void* logits, int64_t ld, int32_t dtype, int64_t 
  * h = dentropy of a row, and lse and entropy from the forward pass:
  *   dlogits_j = g ([j = token] - p_j) - h p_j (log p_j + entropy)
  * 0 where p_j is 0 and in a row with nothing left. p_j is exp(logits_j - lse) with lse as it is given: that
- * it is rounded to float32 moves p_j by up to |lse| 2^-24 of it. (Of a row that a finite number far
- * from 0 masks throughout, where nothing of log vocab is left in lse, p_j is 1: mask such rows by -inf, or
- * give them no gradients.)
+ * it is rounded to float32 moves p_j by up to |lse| 2^-24 of it, and of a row that a finite number far from
+ * 0 masks throughout, where nothing of log vocab is left in lse, p_j is 1. The split forms below do without
+ * that.
  *  dentropy  device float[rows], or NULL (0).
  *  dlogits   rows x vocab of dtype, rows ldd elements apart; may be logits itself (ldd = ld).
  * Errors: EINVAL, EDTYPE, EHIP. */
@@ -572,6 +572,22 @@ int gefen_token_logprobs_backward(const void* logits, int64_t ld, int32_t dtype,
                                   int64_t vocab, const void* tokens, int32_t token_bytes,
                                   const float* lse, const float* entropy, const float* dlogprob,
                                   const float* dentropy, void* dlogits, int64_t ldd, void* stream);
+
+/* gefen_token_logprobs_split, gefen_token_logprobs_backward_split -- the same with lse as the sum of two
+ * numbers: lse_rest is what rounding left of it (device float[rows]), and p_j = exp(logits_j - lse - lse_rest)
+ * is off by units of its own and of |log p_j| only, whatever lse is.
+ * Errors: as above. */
+int gefen_token_logprobs_split(const void* logits, int64_t ld, int32_t dtype, int64_t rows,
+                               int64_t vocab, const void* tokens, int32_t token_bytes, int32_t top,
+                               float* logprob, float* entropy, float* lse, float* lse_rest,
+                               float* top_logprobs, int64_t* top_tokens, void* workspace,
+                               int64_t workspace_bytes, void* stream);
+int gefen_token_logprobs_backward_split(const void* logits, int64_t ld, int32_t dtype,
+                                        int64_t rows, int64_t vocab, const void* tokens,
+                                        int32_t token_bytes, const float* lse,
+                                        const float* lse_rest, const float* entropy,
+                                        const float* dlogprob, const float* dentropy,
+                                        void* dlogits, int64_t ldd, void* stream);
 
 /* gefen_head_logprobs -- the same logprob, entropy and lse of the scores z = x weight^T, which are
  * formed tile by tile in float32, not rounded, and never stored.

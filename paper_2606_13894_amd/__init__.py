@@ -49,7 +49,8 @@ SYMBOLS = [
     "gefen_gated_ffn", "gefen_gated_ffn_backward", "gefen_gated_ffn_workspace",
     "gefen_embedding", "gefen_embedding_backward", "gefen_embedding_backward_workspace",
     "gefen_dropout", "gefen_token_logprobs", "gefen_token_logprobs_workspace",
-    "gefen_token_logprobs_backward", "gefen_head_logprobs", "gefen_head_logprobs_workspace",
+    "gefen_token_logprobs_backward", "gefen_token_logprobs_split",
+    "gefen_token_logprobs_backward_split", "gefen_head_logprobs", "gefen_head_logprobs_workspace",
     "gefen_head_logprobs_backward",
 ]
 
@@ -133,6 +134,10 @@ def load_library(path: str = LIB_PATH):
                                                                                             vp]
     lib.gefen_token_logprobs_backward.argtypes = [vp, i64, i32, i64, i64, vp, i32] + [vp] * 5 + [
         i64, vp]
+    lib.gefen_token_logprobs_split.argtypes = [vp, i64, i32, i64, i64, vp, i32, i32] + [vp] * 7 + [
+        i64, vp]
+    lib.gefen_token_logprobs_backward_split.argtypes = [vp, i64, i32, i64, i64, vp, i32] + [
+        vp] * 6 + [i64, vp]
     lib.gefen_head_logprobs_workspace.argtypes = [i64, i64, i64, i32, P(i64)]
     lib.gefen_head_logprobs.argtypes = [vp, vp, vp, i32, i64, i64, i64] + [vp] * 4 + [i64, vp]
     lib.gefen_head_logprobs_backward.argtypes = [vp, vp, vp, i32, i64, i64, i64] + [vp] * 7 + [

@@ -868,7 +868,7 @@ __global__ __launch_bounds__(Shape<SIZE>::kThreads, 2) void k_ffn_gemm(const Ffn
         for (int mi = 0; mi < MI; ++mi) {   // all rows' loads go out together
             const int64_t row = min(row0 + (wm * MI + mi) * 16 + l16, g.M - 1);
             const int64_t token = token_at(g.head.tokens, g.head.wide, row);
-            const ScoreGrad r = score_grad_row(token, g.head.vocab, row, g.head.lse,
+            const ScoreGrad r = score_grad_row(token, g.head.vocab, row, g.head.lse, nullptr,
                                                g.head.entropy, g.head.dlogprob, g.head.dentropy);
             rows[mi] = {r.lse * kLog2E, r.h * kLn2, fmaf(r.h, r.entropy, r.g), r.g,
                         head_column(token)};

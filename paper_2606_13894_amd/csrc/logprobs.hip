@@ -230,6 +230,7 @@ __device__ __forceinline__ void write_row(const ScoreArgs& a, int64_t row, const
     a.logprob[row] = r.logprob;
     a.entropy[row] = r.entropy;
     a.lse[row] = r.lse;
+    if (a.rest) a.rest[row] = r.rest;
 }
 
 template <bool BF16>
@@ -417,8 +418,8 @@ __global__ __launch_bounds__(256) void k_score_grad(const ScoreGradArgs a, int64
         const int64_t r = item / segments;
         const int64_t e0 = (item % segments) * (256 * 8 * U) + 8 * threadIdx.x;
         const int64_t token = token_at(a.tokens.p, a.tokens.wide, r);
-        const ScoreGrad g = score_grad_row(token, a.vocab, r, a.lse, a.entropy, a.dlogprob,
-                                           a.dentropy);
+        const ScoreGrad g = score_grad_row(token, a.vocab, r, a.lse, a.rest, a.entropy,
+                                           a.dlogprob, a.dentropy);
         const char* z = static_cast<const char*>(a.z) + r * a.ld * S;
         char* dz = static_cast<char*>(a.dz) + r * a.ldd * S;
         u32x4a w[U][BF16 ? 1 : 2];

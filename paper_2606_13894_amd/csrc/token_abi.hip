@@ -67,6 +67,73 @@ int check_head(int64_t tokens, int64_t width, int64_t vocab)
     return GEFEN_OK;
 }
 
+int scores(const void* logits, int64_t ld, int32_t dtype, int64_t rows, int64_t vocab,
+           const void* tokens, int32_t token_bytes, int32_t top, float* logprob, float* entropy,
+           float* lse, float* rest, float* top_logprobs, int64_t* top_tokens, void* workspace,
+           int64_t workspace_bytes, void* stream)
+{
+    int rc;
+    if ((rc = check_dtype(dtype)) || (rc = check_scores(rows, vocab, ld)) ||
+        (rc = check_tokens(0, token_bytes)) || (rc = check_top(top, vocab)))
+        return rc;
+    if (!rows) return GEFEN_OK;
+    if (!logits || !tokens || !logprob || !entropy || !lse || (top && (!top_logprobs || !top_tokens)))
+        return fail(GEFEN_EINVAL, "NULL argument");
+    ScoreArgs a{};
+    a.plan = score_plan(rows, vocab, dtype == GEFEN_BF16);
+    const ScoreSpace s = score_space(a.plan, rows, top);
+    if ((rc = check_space(workspace, workspace_bytes, s.bytes))) return rc;
+    a.z = logits;
+    a.ld = ld;
+    a.tokens = Tokens{tokens, token_bytes == 8};
+    a.rows = rows;
+    a.vocab = vocab;
+    a.top = top;
+    a.logprob = logprob;
+    a.entropy = entropy;
+    a.lse = lse;
+    a.rest = rest;
+    a.top_logprob = top_logprobs;
+    a.top_token = top_tokens;
+    if (s.bytes) {
+        a.keys = at<uint64_t>(workspace, s.keys);
+        a.stats = at<float>(workspace, s.stats);
+    }
+    GEFEN_HIP(launch_scores(a, dtype == GEFEN_BF16, as_stream(stream)));
+    return GEFEN_OK;
+}
+
+int scores_backward(const void* logits, int64_t ld, int32_t dtype, int64_t rows, int64_t vocab,
+                    const void* tokens, int32_t token_bytes, const float* lse, const float* rest,
+                    const float* entropy, const float* dlogprob, const float* dentropy,
+                    void* dlogits, int64_t ldd, void* stream)
+{
+    int rc;
+    if ((rc = check_dtype(dtype)) || (rc = check_scores(rows, vocab, ld)) ||
+        (rc = check_scores(rows, vocab, ldd)) || (rc = check_tokens(0, token_bytes)))
+        return rc;
+    if (!rows) return GEFEN_OK;
+    if (!logits || !tokens || !lse || !entropy || !dlogprob || !dlogits)
+        return fail(GEFEN_EINVAL, "NULL argument");
+    if (logits == dlogits && ld != ldd)
+        return fail(GEFEN_EINVAL, "dlogits in the place of logits has its rows as far apart");
+    ScoreGradArgs a{};
+    a.z = logits;
+    a.ld = ld;
+    a.tokens = Tokens{tokens, token_bytes == 8};
+    a.rows = rows;
+    a.vocab = vocab;
+    a.lse = lse;
+    a.rest = rest;
+    a.entropy = entropy;
+    a.dlogprob = dlogprob;
+    a.dentropy = dentropy;
+    a.dz = dlogits;
+    a.ldd = ldd;
+    GEFEN_HIP(launch_score_grad(a, dtype == GEFEN_BF16, as_stream(stream)));
+    return GEFEN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -179,34 +246,19 @@ int gefen_token_logprobs(const void* logits, int64_t ld, int32_t dtype, int64_t 
                          int64_t* top_tokens, void* workspace, int64_t workspace_bytes,
                          void* stream)
 {
-    int rc;
-    if ((rc = check_dtype(dtype)) || (rc = check_scores(rows, vocab, ld)) ||
-        (rc = check_tokens(0, token_bytes)) || (rc = check_top(top, vocab)))
-        return rc;
-    if (!rows) return GEFEN_OK;
-    if (!logits || !tokens || !logprob || !entropy || !lse || (top && (!top_logprobs || !top_tokens)))
-        return fail(GEFEN_EINVAL, "NULL argument");
-    ScoreArgs a{};
-    a.plan = score_plan(rows, vocab, dtype == GEFEN_BF16);
-    const ScoreSpace s = score_space(a.plan, rows, top);
-    if ((rc = check_space(workspace, workspace_bytes, s.bytes))) return rc;
-    a.z = logits;
-    a.ld = ld;
-    a.tokens = Tokens{tokens, token_bytes == 8};
-    a.rows = rows;
-    a.vocab = vocab;
-    a.top = top;
-    a.logprob = logprob;
-    a.entropy = entropy;
-    a.lse = lse;
-    a.top_logprob = top_logprobs;
-    a.top_token = top_tokens;
-    if (s.bytes) {
-        a.keys = at<uint64_t>(workspace, s.keys);
-        a.stats = at<float>(workspace, s.stats);
-    }
-    GEFEN_HIP(launch_scores(a, dtype == GEFEN_BF16, as_stream(stream)));
-    return GEFEN_OK;
+    return scores(logits, ld, dtype, rows, vocab, tokens, token_bytes, top, logprob, entropy, lse,
+                  nullptr, top_logprobs, top_tokens, workspace, workspace_bytes, stream);
+}
+
+int gefen_token_logprobs_split(const void* logits, int64_t ld, int32_t dtype, int64_t rows,
+                               int64_t vocab, const void* tokens, int32_t token_bytes, int32_t top,
+                               float* logprob, float* entropy, float* lse, float* lse_rest,
+                               float* top_logprobs, int64_t* top_tokens, void* workspace,
+                               int64_t workspace_bytes, void* stream)
+{
+    if (rows > 0 && !lse_rest) return fail(GEFEN_EINVAL, "NULL argument");
+    return scores(logits, ld, dtype, rows, vocab, tokens, token_bytes, top, logprob, entropy, lse,
+                  lse_rest, top_logprobs, top_tokens, workspace, workspace_bytes, stream);
 }
 
 int gefen_token_logprobs_backward(const void* logits, int64_t ld, int32_t dtype, int64_t rows,
@@ -214,29 +266,20 @@ int gefen_token_logprobs_backward(const void* logits, int64_t ld, int32_t dtype,
                                   const float* lse, const float* entropy, const float* dlogprob,
                                   const float* dentropy, void* dlogits, int64_t ldd, void* stream)
 {
-    int rc;
-    if ((rc = check_dtype(dtype)) || (rc = check_scores(rows, vocab, ld)) ||
-        (rc = check_scores(rows, vocab, ldd)) || (rc = check_tokens(0, token_bytes)))
-        return rc;
-    if (!rows) return GEFEN_OK;
-    if (!logits || !tokens || !lse || !entropy || !dlogprob || !dlogits)
-        return fail(GEFEN_EINVAL, "NULL argument");
-    if (logits == dlogits && ld != ldd)
-        return fail(GEFEN_EINVAL, "dlogits in the place of logits has its rows as far apart");
-    ScoreGradArgs a{};
-    a.z = logits;
-    a.ld = ld;
-    a.tokens = Tokens{tokens, token_bytes == 8};
-    a.rows = rows;
-    a.vocab = vocab;
-    a.lse = lse;
-    a.entropy = entropy;
-    a.dlogprob = dlogprob;
-    a.dentropy = dentropy;
-    a.dz = dlogits;
-    a.ldd = ldd;
-    GEFEN_HIP(launch_score_grad(a, dtype == GEFEN_BF16, as_stream(stream)));
-    return GEFEN_OK;
+    return scores_backward(logits, ld, dtype, rows, vocab, tokens, token_bytes, lse, nullptr,
+                           entropy, dlogprob, dentropy, dlogits, ldd, stream);
+}
+
+int gefen_token_logprobs_backward_split(const void* logits, int64_t ld, int32_t dtype,
+                                        int64_t rows, int64_t vocab, const void* tokens,
+                                        int32_t token_bytes, const float* lse,
+                                        const float* lse_rest, const float* entropy,
+                                        const float* dlogprob, const float* dentropy,
+                                        void* dlogits, int64_t ldd, void* stream)
+{
+    if (rows > 0 && !lse_rest) return fail(GEFEN_EINVAL, "NULL argument");
+    return scores_backward(logits, ld, dtype, rows, vocab, tokens, token_bytes, lse, lse_rest,
+                           entropy, dlogprob, dentropy, dlogits, ldd, stream);
 }
 
 int gefen_head_logprobs_workspace(int64_t tokens, int64_t width, int64_t vocab, int32_t flags,

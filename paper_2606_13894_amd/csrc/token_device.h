@@ -118,14 +118,15 @@ __device__ __forceinline__ float score_logprob(float z, const ScoreBase& base, f
     return kLn2 * (d - log2s);
 }
 
-// A row's results. `taken`: its token's score.
+// A row's results. `taken`: its token's score; `rest`: what rounding left of lse.
 struct ScoreRow {
-    float lse, entropy, logprob;
+    float lse, rest, entropy, logprob;
 };
 __device__ __forceinline__ ScoreRow score_row(const ScoreSum& a, int64_t token, int64_t vocab,
                                               float taken)
 {
     ScoreRow r;
+    r.rest = 0.0f;
     if (a.s != a.s) {                       // NaN
         r.lse = r.entropy = r.logprob = a.s;
     } else if (a.m == -INFINITY) {          // nothing left in the row
@@ -134,7 +135,10 @@ __device__ __forceinline__ ScoreRow score_row(const ScoreSum& a, int64_t token, 
     } else {
         const ScoreBase base = score_base(a.m);
         const float l = log2f(a.s);
-        r.lse = fmaf(kLn2, base.far ? l : l - fmaf(a.m, kLog2E, -base.b), a.m);
+        const float over = base.far ? l : l - fmaf(a.m, kLog2E, -base.b);   // of m
+        r.lse = fmaf(kLn2, over, a.m);
+        const float x = kLn2 * over;
+        r.rest = fabsf(a.m) >= fabsf(x) ? (a.m - r.lse) + x : (x - r.lse) + a.m;
         r.entropy = fmaxf(kLn2 * (l - a.t / a.s), 0.0f);
         r.logprob = score_logprob(taken, base, l);
     }
@@ -146,29 +150,32 @@ __device__ __forceinline__ ScoreRow score_row(const ScoreSum& a, int64_t token, 
 // ---------------------------------------------------------------- gradients of scores
 //   dz_j = g ([j = token] - p_j) - h p_j (log p_j + H),  p_j = exp(z_j - lse)
 // with g the gradient of the token's log probability and h that of the entropy H. A row with
-// nothing left (lse -inf) has none.
+// nothing left (lse -inf) has none. lse may be the sum of two numbers: that it is rounded to one moves p_j by
+// |lse| 2^-24 of it, and of a row that a finite number far from 0 masks throughout leaves p_j = 1.
 struct ScoreGrad {
-    float lse, entropy, g, h;
+    float lse, rest, entropy, g, h;
 };
 __device__ __forceinline__ ScoreGrad score_grad_row(int64_t token, int64_t vocab, int64_t row,
-                                                    const float* lse, const float* entropy,
-                                                    const float* dlogprob, const float* dentropy)
+                                                    const float* lse, const float* rest,
+                                                    const float* entropy, const float* dlogprob,
+                                                    const float* dentropy)
 {
     ScoreGrad r;
     r.lse = lse[row];
+    r.rest = rest ? rest[row] : 0.0f;
     r.entropy = entropy[row];
     r.g = dlogprob[row];
     r.h = dentropy ? dentropy[row] : 0.0f;
     if (token < 0 || token >= vocab) r.g = 0.0f;
     if (r.lse == -INFINITY) {
         r.lse = INFINITY;      // p = 0 throughout
-        r.g = r.h = 0.0f;
+        r.rest = r.g = r.h = 0.0f;
     }
     return r;
 }
 __device__ __forceinline__ float score_gradient(float z, const ScoreGrad& r, bool taken)
 {
-    const float d = z - r.lse;
+    const float d = (z - r.lse) - r.rest;
     const float p = __builtin_amdgcn_exp2f(d * kLog2E);
     const float dz = -p * fmaf(r.h, fmaxf(d, -1e4f) + r.entropy, r.g);
     return taken ? dz + r.g : dz;

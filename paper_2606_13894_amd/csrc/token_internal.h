@@ -63,6 +63,7 @@ struct ScoreArgs {
     float* logprob;
     float* entropy;
     float* lse;
+    float* rest;             // what rounding left of lse; or null
     float* top_logprob;      // rows x top
     int64_t* top_token;
     float* stats;            // rows x parts x 3, where there are parts
@@ -76,6 +77,7 @@ struct ScoreGradArgs {
     Tokens tokens;
     int64_t rows, vocab;
     const float* lse;
+    const float* rest;       // or null (0)
     const float* entropy;
     const float* dlogprob;
     const float* dentropy;   // or null

@@ -273,6 +273,11 @@ def token_logprobs(logits, tokens, top: int = 0, stream=None):
     (``padded[..., :vocab]``)."""
     if stream is not None:
         return ff._on(stream, token_logprobs, logits, tokens, top)
+    return _token_logprobs(logits, tokens, top, False)[0]
+
+
+def _token_logprobs(logits, tokens, top, split):
+    """The results, and with ``split`` what rounding left of lse."""
     dev = ff._device(logits, "logits")
     d = ff._dtype(logits, "logits")
     z, ld = _score_rows(logits, "logits", dev)
@@ -289,13 +294,16 @@ def token_logprobs(logits, tokens, top: int = 0, stream=None):
         bp, kp = best.data_ptr(), where.data_ptr()
     lib = ff._library()
     ws, wp, n = _space(lib.gefen_token_logprobs_workspace, z, d, rows, vocab, top)
-    ff._call(lib.gefen_token_logprobs(
+    rest = torch.empty_like(lse) if split else None
+    entry, more = (lib.gefen_token_logprobs_split, (rest.data_ptr(),)) if split else (
+        lib.gefen_token_logprobs, ())
+    ff._call(entry(
         z.data_ptr(), ld, d, rows, vocab, tokens.data_ptr(), size, top, logprob.data_ptr(),
-        entropy.data_ptr(), lse.data_ptr(), bp, kp, wp, n, ff._raw_stream(dev)))
+        entropy.data_ptr(), lse.data_ptr(), *more, bp, kp, wp, n, ff._raw_stream(dev)))
     if ff._tracked(logits):
         ff._no_graph(_NO_GRADIENT.format("token_logprobs", "LogProbs"), logprob, entropy, lse,
                      *((best,) if top else ()))
-    return TokenLogProbs(logprob, entropy, lse, best, where)
+    return TokenLogProbs(logprob, entropy, lse, best, where), rest
 
 
 def _upstream(dlogprob, dentropy, dev, shape):
@@ -310,11 +318,16 @@ def token_logprobs_backward(dlogprob, logits, tokens, lse, entropy, dentropy=Non
                             stream=None):
     """The gradient of :func:`token_logprobs`'s logits from those of logprob and entropy. ``out``
     takes it (contiguous, or rows evenly apart, no gradient wanted of it); it may be ``logits``
-    itself. The probabilities are exp(logits - lse), off by |lse| 2^-24 of them: a row that is masked
-    throughout is to be so by -inf, which gives it no gradient, not by a finite number far from 0."""
+    itself. The probabilities are exp(logits - lse), off by |lse| 2^-24 of them, since lse is rounded: rows
+    far from 0, as a finite mask over all of one leaves it, are for :class:`LogProbs`, which keeps what
+    rounding left of lse."""
     if stream is not None:
         return ff._on(stream, token_logprobs_backward, dlogprob, logits, tokens, lse, entropy,
                       dentropy, out)
+    return _token_logprobs_backward(dlogprob, logits, tokens, lse, None, entropy, dentropy, out)
+
+
+def _token_logprobs_backward(dlogprob, logits, tokens, lse, rest, entropy, dentropy, out):
     dev = ff._device(logits, "logits")
     d = ff._dtype(logits, "logits")
     z, ld = _score_rows(logits, "logits", dev)
@@ -338,8 +351,11 @@ def token_logprobs_backward(dlogprob, logits, tokens, lse, entropy, dentropy=Non
         if to.data_ptr() != out.data_ptr():
             raise ValueError("out must have its rows evenly apart")
         torch.autograd.graph.increment_version(out)   # what was saved of it is gone
-    ff._call(ff._library().gefen_token_logprobs_backward(
-        z.data_ptr(), ld, d, rows, vocab, tokens.data_ptr(), size, lse.data_ptr(),
+    lib = ff._library()
+    entry, more = (lib.gefen_token_logprobs_backward, ()) if rest is None else (
+        lib.gefen_token_logprobs_backward_split, (rest.data_ptr(),))
+    ff._call(entry(
+        z.data_ptr(), ld, d, rows, vocab, tokens.data_ptr(), size, lse.data_ptr(), *more,
         entropy.data_ptr(), gp, hp, to.data_ptr(), ldd, ff._raw_stream(dev)))
     if ff._tracked(dlogprob, dentropy, logits):
         ff._no_graph(ff._BACKWARD_ONLY.format("token_logprobs_backward"), out)
@@ -354,25 +370,24 @@ def _of_logprob(g, like):
 class _Scores(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tokens):
-        r = token_logprobs(logits, tokens)
-        ctx.save_for_backward(logits, tokens, r.lse, r.entropy)
+        r, rest = _token_logprobs(logits, tokens, 0, True)
+        ctx.save_for_backward(logits, tokens, r.lse, rest, r.entropy)
         ctx.set_materialize_grads(False)
         return r.logprob, r.entropy
 
     @staticmethod
     def backward(ctx, dlogprob, dentropy):
-        logits, tokens, lse, entropy = ctx.saved_tensors
+        logits, tokens, lse, rest, entropy = ctx.saved_tensors
         with torch.no_grad():
-            dz = token_logprobs_backward(_of_logprob(dlogprob, lse), logits, tokens, lse, entropy,
-                                         dentropy)
+            dz = _token_logprobs_backward(_of_logprob(dlogprob, lse), logits, tokens, lse, rest,
+                                          entropy, dentropy, None)
         if torch.is_grad_enabled():   # create_graph
             ff._no_graph("LogProbs has no second derivative", dz)
         return dz, None
 
 
 class LogProbs(torch.nn.Module):
-    """``logprob, entropy = scores(logits, tokens)`` of :func:`token_logprobs`, under autograd (and
-    with the gradients of :func:`token_logprobs_backward`, for scores of no great size)."""
+    """``logprob, entropy = scores(logits, tokens)`` of :func:`token_logprobs`, under autograd."""
 
     def forward(self, logits, tokens):
         return _Scores.apply(logits, tokens)

@@ -10,8 +10,8 @@ import math
 import pytest
 import torch
 
-from test_gpu_language import (BF16, DTYPES, F32, F64, UNIT, _check_rows, _randint,  # noqa: F401
-                               _rows64, _within, dev)
+from test_gpu_language import (BF16, DTYPES, F32, F64, HALF, UNIT, _check_rows,  # noqa: F401
+                               _randint, _rows64, _within, dev)
 
 pytestmark = pytest.mark.gpu
 
@@ -128,3 +128,89 @@ def test_head_of_a_score_far_below(dev, n, vocab, width):  # noqa: F811
     want = torch.where(t == 1, -3.0 * 2.0 ** 126, 0.0).to(F64) - lse
     bound = (vocab / 256 + 64 + 16) * UNIT * (1 + lse)
     _within(r.logprob, want, bound + 2 * UNIT * want.abs(), "logprob")
+
+
+def _gradient(z, t, g, h):
+    """The float64 gradient of the scores, from the scores alone, and its bound before the output's
+    rounding. p is off by what its exponent is off by, (4 |log p| + 8) units (as in the sums) and the logarithm
+    of the sum's bound, which the entropy's holds; values below 2^-126 may be flushed before their factor."""
+    w = _rows64(z, t)
+    V = z.shape[1]
+    g, h, H, err = (v.to(F64)[:, None] for v in (g, h, w["H"], w["b_H"]))
+    on = ((t >= 0) & (t < V))[:, None]
+    g = torch.where(on, g, 0.0)
+    lp = torch.where(w["p"] > 0, w["lp"], 0.0)
+    hit = torch.zeros_like(w["p"]).scatter_(1, t.clamp(0, V - 1)[:, None], 1.0) * on
+    inner = lp + H
+    want = hit * g - w["p"] * (g + h * inner)
+    size = g.abs() + h.abs() * inner.abs()
+    bound = w["p"] * (size * ((4 * lp.abs() + 16) * UNIT + err)
+                      + h.abs() * (2 * err + 4 * UNIT * (lp.abs() + H.abs())))
+    return want, bound + hit * 2 * UNIT * g.abs() + 2.0 ** -126 * (1 + g.abs() + 120 * h.abs())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab", [(40, 7), (40, 1003), (40, 50257), (40, 300_001)])
+def test_gradients_of_the_module(dev, rows, vocab, dtype):  # noqa: F811
+    """Rows at one level, some of their scores a few steps of the type lower, the lowest number among
+    others, large scores, ordinary ones and empty rows: the gradients are the formula's, whatever lse is."""
+    dt = DTYPES[dtype]
+    gen = torch.Generator(dev).manual_seed(1)
+    z = torch.randn(rows, vocab, generator=gen, device=dev)
+    z[35:39] *= torch.tensor([1e2, 1e4, 1e6, 1e9], device=dev)[:, None]
+    z = z.to(dt)
+    step = _randint(dev, 0, 3, vocab, seed=1)
+    for r in range(30):
+        v = torch.tensor(LEVELS[r // 2] * (-1) ** r, dtype=dt)
+        levels = [v]
+        for _ in range(2):
+            levels.append(torch.nextafter(levels[-1], torch.zeros_like(v)))
+        z[r] = torch.stack(levels).to(dev)[step] if r % 4 < 2 else v
+    z[30] = torch.finfo(dt).min
+    z[31, ::2] = torch.finfo(dt).min
+    z[32, 1::2] = -1e9
+    z[33] = -math.inf
+    t = _randint(dev, -1, vocab + 1, rows, seed=2)
+    g, h = (torch.randn(rows, generator=gen, device=dev) for _ in range(2))
+    leaf = z.clone().requires_grad_()
+    logprob, entropy = gf.LogProbs()(leaf, t)
+    torch.autograd.backward((logprob, entropy), (g, h))
+    want, bound = _gradient(z, t, g, h)
+    want[33], bound[33] = 0.0, 0.0
+    _within(leaf.grad, want, bound + HALF[dt] * want.abs(), "dlogits")
+    plain = gf.token_logprobs(z, t)
+    assert torch.equal(torch.nan_to_num(logprob), torch.nan_to_num(plain.logprob))
+    assert torch.equal(entropy, plain.entropy)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab,top", [(3, 9, 4), (700, 1003, 0), (2, 600_001, 20)])
+def test_lse_in_two_numbers(dev, rows, vocab, top, dtype):  # noqa: F811
+    """Their sum is closer to lse than one number can be; the other results are those of the plain entry."""
+    from test_gpu_language_written import CODE, Filled, _call
+    dt = DTYPES[dtype]
+    lib = gf.load_library()
+    z = (torch.randn(rows, vocab, generator=torch.Generator(dev).manual_seed(1), device=dev)
+         * 3 + 1000).to(dt)
+    z[0] = -3e4
+    z[1] = -math.inf
+    z[2 % rows, 5] = math.nan if rows > 2 else 1.0
+    t = _randint(dev, -1, vocab + 1, rows, seed=2)
+    out = [Filled(dev, (rows,), F32) for _ in range(4)]
+    best = [Filled(dev, (rows, top), d) for d in (F32, torch.int64)]
+    _call(dev, lib, lib.gefen_token_logprobs_split,
+          lambda b: lib.gefen_token_logprobs_workspace(CODE[dt], rows, vocab, top, b),
+          z.data_ptr(), vocab, CODE[dt], rows, vocab, t.data_ptr(), 8, top, *(o.p for o in out),
+          *(o.p for o in best))
+    logprob, entropy, lse, rest = (o.check() for o in out)
+    r = gf.token_logprobs(z, t, top=top)
+    for got, want in ((logprob, r.logprob), (entropy, r.entropy), (lse, r.lse),
+                      (best[0].check(), r.top_logprobs), (best[1].check(), r.top_tokens)):
+        if want is not None:
+            assert torch.equal(torch.nan_to_num(got, nan=9.0), torch.nan_to_num(want, nan=9.0))
+    want = _rows64(z, t)
+    fine = torch.isfinite(r.lse)
+    assert (rest[~fine] == 0).all() and fine.any() and not fine.all()
+    # b_H holds the logarithm's bound; the sum of the two is off by that alone
+    both = (lse.to(F64) + rest.to(F64))[fine]
+    assert ((both - want["lse"][fine]).abs() <= want["b_H"][fine] + 2.0 ** -40).all()
